@@ -89,7 +89,8 @@ typedef enum {
     MERIT_OP_BILATERAL = 12
 } merit_op;
 
-typedef enum { MERIT_U8 = 0, MERIT_F16 = 1, MERIT_F32 = 2 } merit_dtype;
+/* (MERIT_BF16: the operators along a sequence of tokens, merit_tokens.h; no transform here takes it) */
+typedef enum { MERIT_U8 = 0, MERIT_F16 = 1, MERIT_F32 = 2, MERIT_BF16 = 3 } merit_dtype;
 
 /* What an out-of-range coordinate x yields. */
 typedef enum {

@@ -18,6 +18,12 @@ import threading
 import warnings
 
 from . import build as _build
+from . import tokens
+from .tokens import (  # noqa: F401  (the operators along a sequence of tokens)
+    MERIT_ACT_NONE, MERIT_ACT_RELU, MERIT_ACT_SILU, MERIT_BF16, MERIT_CONV_MAX_TAPS, MERIT_PASS_BACKWARD,
+    MERIT_PASS_FORWARD, MERIT_PASS_STEP, MERIT_SCAN_MAX_STATES, MERIT_SCAN_TILE, TokenPlan, merit_causal_conv,
+    merit_causal_conv_backward, merit_causal_conv_step, merit_group_norm, merit_group_norm_backward,
+    merit_plan_causal_conv, merit_plan_group_norm, merit_plan_scan, merit_scan, merit_scan_backward, merit_scan_step)
 
 MERIT_MAX_INDEX = 12
 MERIT_MAX_DIMS = 6
@@ -127,6 +133,7 @@ def lib():
                  "merit_sad_search", "merit_plan_packed_weights_bytes", "merit_conv2d_pack_weights",
                  "merit_conv2d_packed", "merit_conv2d_packed_noalloc"):
         getattr(L, name).restype = c_int
+    tokens._declare(L)
     L.merit_status_string.argtypes = [c_int]
     L.merit_status_string.restype = ctypes.c_char_p
     _lib = L

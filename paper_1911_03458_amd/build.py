@@ -14,10 +14,14 @@ LIB_PATH = os.path.join(_HERE, "libmerit.so")
 CALLS_SRC = os.path.join(CSRC, "torch_calls.cpp")
 CALLS_PATH = os.path.join(_HERE, "_torch_calls.so")      # a Python module over libmerit.so and PyTorch
 
-SOURCES = ["merit_plan.cpp", "pool2d.hip", "sad_search.hip", "conv2d.hip", "conv2d_chws.hip", "conv2d_px.hip", "conv2d_split.hip", "maxpool_f16.hip", "generic.hip", "corr.hip", "dwconv.hip", "sepfilter.hip", "bilateral.hip", "probe.hip"]
+SOURCES = ["merit_plan.cpp", "pool2d.hip", "sad_search.hip", "conv2d.hip", "conv2d_chws.hip", "conv2d_px.hip", "conv2d_split.hip", "maxpool_f16.hip", "generic.hip", "corr.hip", "dwconv.hip", "sepfilter.hip", "bilateral.hip", "probe.hip",
+           "token_plan.cpp", "groupnorm.hip", "causal_conv.hip", "scan.hip", "scan_backward.hip"]
 HEADERS = [os.path.join(CSRC, "merit_internal.h"), os.path.join(ROOT, "include", "merit.h"),
-           os.path.join(ROOT, "include", "merit_probe.h")]
-CALLS_DEPS = [CALLS_SRC, os.path.join(ROOT, "include", "merit.h")]
+           os.path.join(ROOT, "include", "merit_probe.h"), os.path.join(ROOT, "include", "merit_tokens.h"),
+           os.path.join(CSRC, "tokens.h"), os.path.join(CSRC, "scan.h")]
+TOKEN_CALLS_SRC = os.path.join(CSRC, "token_calls.cpp")
+CALLS_DEPS = [CALLS_SRC, TOKEN_CALLS_SRC, os.path.join(ROOT, "include", "merit.h"),
+              os.path.join(ROOT, "include", "merit_tokens.h")]
 
 
 def hipcc_path() -> str:
@@ -71,7 +75,7 @@ def calls_are_stale() -> bool:
 
 
 def build_torch_calls(force: bool = True) -> str:
-    """Compile csrc/torch_calls.cpp (host code, no kernels) against PyTorch and the built library."""
+    """Compile csrc/torch_calls.cpp and csrc/token_calls.cpp (host code, no kernels) against PyTorch and the built library."""
     if not force and not calls_are_stale():
         return CALLS_PATH
     import sysconfig
@@ -84,7 +88,7 @@ def build_torch_calls(force: bool = True) -> str:
     tmp = CALLS_PATH + ".%d.tmp" % os.getpid()      # (never a half-written module in the way of another process)
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
-           '-DMERIT_TORCH="%s"' % torch.__version__, CALLS_SRC, "-o", tmp,
+           '-DMERIT_TORCH="%s"' % torch.__version__, CALLS_SRC, TOKEN_CALLS_SRC, "-o", tmp,
            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
     cmd += ["-isystem" + d for d in ext.include_paths() + [os.path.join(rocm, "include")]]
     cmd += ["-L" + _HERE, "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN"] + ["-L" + d for d in libs]

@@ -1,0 +1,659 @@
+// Group norm with an activation, channels last, forward and backward:
+//     y = act((x - mean) rstd w + b)      mean, var over the S positions x Cg channels of a group
+//     du = dy act'(u),  g = du w,  xh = (x - mean) rstd
+//     dx = rstd (g - mean(g) - xh mean(g xh)),   dw = sum du xh,   db = sum du
+// Bound by memory: 2 (forward) or 3 (backward) passes of the tensor over HBM where it is read once.
+//
+// Two forms.
+//  - one row a group (S = 1, a token's heads): a group is a run of channels of one row.  A run of lanes, a wavefront or a
+//    workgroup holds it in registers, so x is read once.  A wavefront keeps its columns and walks down the rows, which
+//    keeps weights and the parameter gradients' sums in registers.
+//  - chunks (any S): workgroups reduce row chunks to partial statistics, a second launch joins them and applies.
+// Variances are sums of squared distances from a mean that is known by then (of the row, or of the batch of values in
+// registers, batches joined by their counts): a mean far from zero costs no digits.
+#include "tokens.h"
+
+namespace merit {
+
+namespace {
+
+constexpr int NT = 256;
+
+// ---------------------------------------------------------------------------
+// one row a group
+// ---------------------------------------------------------------------------
+// Where a thread's channels are: unit j of U begins at channel c0 + j * step * V
+struct RowPlace {
+    int group, first, step, cu;
+    bool active;
+    int64_t row0, rstep;
+};
+__device__ __forceinline__ RowPlace row_place(int G, int cu, int lg, int wpg)
+{
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    RowPlace q;
+    q.cu = cu;
+    if (wpg == 1) {
+        q.group = (int)blockIdx.x * (64 / lg) + lane / lg;
+        q.first = lane & (lg - 1);
+        q.step = lg;
+        q.row0 = (int64_t)blockIdx.y * 4 + wave;
+        q.rstep = (int64_t)gridDim.y * 4;
+    } else {
+        q.group = (int)blockIdx.x;
+        q.first = tid;
+        q.step = NT;
+        q.row0 = blockIdx.y;
+        q.rstep = gridDim.y;
+    }
+    q.active = q.group < G;
+    return q;
+}
+
+// the sum over a group's lanes; `slot`: four floats of LDS, not those of the sum before it
+__device__ __forceinline__ float sum_group(float v, int lg, int wpg, float *slot)
+{
+    v = sum_lanes(v, lg);
+    if (wpg == 1) return v;
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (slot[0] + slot[1]) + (slot[2] + slot[3]);
+}
+
+template <typename T, int V, int U>
+__global__ __launch_bounds__(NT) void merit_norm_rows(NormParams p, int cu, int lg, int wpg)
+{
+    __shared__ float slots[2][4];
+    const RowPlace q = row_place(p.G, cu, lg, wpg);
+    const float inv = 1.0f / (float)p.Cg;
+    float w[U][V], b[U][V];
+    bool ok[U];
+    int c[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+        const int u = q.first + j * q.step;
+        ok[j] = q.active && u < q.cu;
+        c[j] = q.group * p.Cg + u * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[j][i] = ok[j] ? load_param<T>(p.w, c[j] + i, 1.0f) : 0.0f;
+            b[j][i] = ok[j] ? load_param<T>(p.b, c[j] + i, 0.0f) : 0.0f;
+        }
+    }
+    vec_t<T, V> next[U] = {};
+    if (q.row0 < p.N) {
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (ok[j]) next[j] = load_vec<T, V>(p.x.data, q.row0 * p.x.s0 + c[j]);
+    }
+    for (int64_t r = q.row0; r < p.N; r += q.rstep) {
+        vec_t<T, V> now[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) now[j] = next[j];
+        if (r + q.rstep < p.N) {
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                if (ok[j]) next[j] = load_vec<T, V>(p.x.data, (r + q.rstep) * p.x.s0 + c[j]);
+        }
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s += ok[j] ? at<T, V>(now[j], i) : 0.0f;
+        const float mean = sum_group(s, lg, wpg, slots[0]) * inv;
+        float m2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = ok[j] ? at<T, V>(now[j], i) - mean : 0.0f;
+                m2 = fmaf(d, d, m2);
+            }
+        const float rstd = __builtin_amdgcn_rsqf(sum_group(m2, lg, wpg, slots[1]) * inv + p.eps);
+        if (q.active && q.first == 0) {
+            if (p.mean) p.mean[r * p.G + q.group] = mean;
+            if (p.rstd) p.rstd[r * p.G + q.group] = rstd;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (!ok[j]) continue;
+            vec_t<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                put<T, V>(o, i, apply_act(fmaf((at<T, V>(now[j], i) - mean) * rstd, w[j][i], b[j][i]), p.act));
+            store_vec<T, V>(p.y.data, r * p.y.s0 + c[j], o);
+        }
+    }
+}
+
+template <typename T, int V, int U>
+__global__ __launch_bounds__(NT) void merit_norm_rows_backward(NormParams p, int cu, int lg, int wpg)
+{
+    __shared__ float slots[2][2][4];
+    __shared__ float red[4][64][V];
+    const RowPlace q = row_place(p.G, cu, lg, wpg);
+    const float inv = 1.0f / (float)p.Cg;
+    float w[U][V], b[U][V], s1[U][V], s2[U][V];
+    bool ok[U];
+    int c[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+        const int u = q.first + j * q.step;
+        ok[j] = q.active && u < q.cu;
+        c[j] = q.group * p.Cg + u * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[j][i] = ok[j] ? load_param<T>(p.w, c[j] + i, 1.0f) : 0.0f;
+            b[j][i] = ok[j] ? load_param<T>(p.b, c[j] + i, 0.0f) : 0.0f;
+            s1[j][i] = s2[j][i] = 0.0f;
+        }
+    }
+    for (int64_t r = q.row0; r < p.N; r += q.rstep) {
+        const float mean = q.active ? p.mean[r * p.G + q.group] : 0.0f;
+        const float rstd = q.active ? p.rstd[r * p.G + q.group] : 0.0f;
+        vec_t<T, V> xv[U], dv[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (ok[j]) {
+                xv[j] = load_vec<T, V>(p.x.data, r * p.x.s0 + c[j]);
+                dv[j] = load_vec<T, V>(p.dy.data, r * p.dy.s0 + c[j]);
+            }
+        float m1 = 0.0f, m2 = 0.0f;
+        float xh[U][V], g[U][V];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (!ok[j]) continue;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                xh[j][i] = (at<T, V>(xv[j], i) - mean) * rstd;
+                const float du = at<T, V>(dv[j], i) * act_slope(fmaf(xh[j][i], w[j][i], b[j][i]), p.act);
+                s1[j][i] += du;
+                s2[j][i] = fmaf(du, xh[j][i], s2[j][i]);
+                g[j][i] = du * w[j][i];
+                m1 += g[j][i];
+                m2 = fmaf(g[j][i], xh[j][i], m2);
+            }
+        }
+        m1 = sum_lanes(m1, lg);
+        m2 = sum_lanes(m2, lg);
+        if (wpg != 1) {
+            float(*slot)[4] = slots[((r - q.row0) / q.rstep) & 1];      // (the sums before these may still be read)
+            if ((threadIdx.x & 63) == 0) slot[0][threadIdx.x >> 6] = m1, slot[1][threadIdx.x >> 6] = m2;
+            __syncthreads();
+            m1 = (slot[0][0] + slot[0][1]) + (slot[0][2] + slot[0][3]);
+            m2 = (slot[1][0] + slot[1][1]) + (slot[1][2] + slot[1][3]);
+        }
+        m1 *= inv;
+        m2 *= inv;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (!ok[j]) continue;
+            vec_t<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) put<T, V>(o, i, rstd * (g[j][i] - m1 - xh[j][i] * m2));
+            store_vec<T, V>(p.dx.data, r * p.dx.s0 + c[j], o);
+        }
+    }
+    if (!p.dw && !p.db) return;
+    float *out = p.part + (int64_t)blockIdx.y * 2 * p.C;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (wpg == 1) {         // the four wavefronts have the same columns
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < V; ++i) red[wave][lane][i] = k ? s2[j][i] : s1[j][i];
+                __syncthreads();
+                if (wave == 0 && ok[j])
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        out[k * p.C + c[j] + i] = (red[0][lane][i] + red[1][lane][i]) + (red[2][lane][i] + red[3][lane][i]);
+            } else if (ok[j]) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) out[k * p.C + c[j] + i] = k ? s2[j][i] : s1[j][i];
+            }
+        }
+}
+
+// ---------------------------------------------------------------------------
+// chunks
+// ---------------------------------------------------------------------------
+// A workgroup has a row chunk of the columns of a tile: `groups` whole groups, or a piece of one that is wider than the
+// workgroup.  Thread (row ty of rw, column tx of cols) keeps its column.
+struct Tile {
+    int g0, groups;        // first group, groups
+    int piece, pieces;
+    int cw, cols;          // columns of a group (of its piece), of the tile
+    int rw, tx, ty;
+    bool in;               // the thread has a column
+    int c;                 // its first channel
+    int64_t n, chunk, r0, r1;
+};
+template <int V> __device__ __forceinline__ Tile tile_of(const NormParams &p)
+{
+    const int cu = p.Cg / V;
+    Tile t;
+    // workgroups: column tiles of a chunk, chunks of an image, images (one number: an extent of the launch holds 65535 only)
+    const uint32_t row = blockIdx.x / (uint32_t)p.ctiles;
+    const int ct = (int)(blockIdx.x - row * (uint32_t)p.ctiles);
+    const uint32_t n = row / (uint32_t)p.chunks;
+    t.n = n;
+    t.chunk = row - n * (uint32_t)p.chunks;
+    t.pieces = (cu + NT - 1) / NT;
+    if (t.pieces > 1) {
+        t.g0 = ct / t.pieces;
+        t.groups = 1;
+        t.piece = ct - t.g0 * t.pieces;
+        t.cw = min(NT, cu - t.piece * NT);
+    } else {
+        const int gt = min(p.G, NT / cu);
+        t.g0 = ct * gt;
+        t.groups = min(gt, p.G - t.g0);
+        t.piece = 0;
+        t.cw = cu;
+    }
+    t.cols = t.groups * t.cw;
+    t.rw = NT / t.cols;
+    t.ty = (int)threadIdx.x / t.cols;
+    t.tx = (int)threadIdx.x - t.ty * t.cols;
+    t.in = t.ty < t.rw;
+    t.c = t.g0 * p.Cg + (t.piece * NT + t.tx) * V;
+    t.r0 = t.chunk * p.chunk_rows;
+    t.r1 = min(t.r0 + p.chunk_rows, p.S);
+    return t;
+}
+
+// (n, mean, m2) of two sets of values -> of both
+__device__ __forceinline__ void join(float &n, float &mean, float &m2, float nb, float mb, float m2b)
+{
+    const float sum = n + nb, part = nb / sum, d = mb - mean;
+    mean = fmaf(d, part, mean);
+    m2 += m2b + d * d * n * part;
+    n = sum;
+}
+
+// A value of the group, which the chunks' means are taken from: next to a mean that is far from zero their distances keep
+// all digits
+template <typename T> __device__ __forceinline__ float shift_of(const NormParams &p, int64_t n, int g)
+{
+    return (float)static_cast<const T *>(p.x.data)[n * p.x.s0 + (int64_t)g * p.Cg];
+}
+
+template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_stats(NormParams p)
+{
+    __shared__ float sn[NT], sm[NT], sq[NT];
+    const Tile t = tile_of<V>(p);
+    const int64_t n = t.n, base = n * p.x.s0 + t.c;
+    constexpr int RB = 4;                   // rows in flight
+    float cnt = 0.0f, mean = 0.0f, m2 = 0.0f;
+    if (t.in && t.r0 < t.r1) {
+        const float k0 = shift_of<T>(p, n, t.g0 + t.tx / t.cw);
+        int64_t r = t.r0 + t.ty;
+        for (; r + (RB - 1) * t.rw < t.r1; r += RB * t.rw) {
+            vec_t<T, V> v[RB];
+#pragma unroll
+            for (int k = 0; k < RB; ++k) v[k] = load_vec<T, V>(p.x.data, base + (r + k * t.rw) * p.x.s1);
+            float s = 0.0f, q = 0.0f;
+#pragma unroll
+            for (int k = 0; k < RB; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s += at<T, V>(v[k], i) - k0;
+            s *= 1.0f / (RB * V);
+#pragma unroll
+            for (int k = 0; k < RB; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = (at<T, V>(v[k], i) - k0) - s;
+                    q = fmaf(d, d, q);
+                }
+            join(cnt, mean, m2, (float)(RB * V), s, q);
+        }
+        for (; r < t.r1; r += t.rw) {
+            const vec_t<T, V> v = load_vec<T, V>(p.x.data, base + r * p.x.s1);
+            float s = 0.0f, q = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) s += at<T, V>(v, i) - k0;
+            s *= 1.0f / V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = (at<T, V>(v, i) - k0) - s;
+                q = fmaf(d, d, q);
+            }
+            join(cnt, mean, m2, (float)V, s, q);
+        }
+    }
+    sn[threadIdx.x] = cnt;
+    sm[threadIdx.x] = mean;
+    sq[threadIdx.x] = m2;
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int g = wave; g < t.groups; g += NT / 64) {
+        float a = 0.0f, b = 0.0f;
+        for (int e = lane; e < t.rw * t.cw; e += 64) {
+            const int row = e / t.cw, k = row * t.cols + g * t.cw + (e - row * t.cw);
+            a += sn[k];
+            b = fmaf(sn[k], sm[k], b);
+        }
+        a = sum_lanes(a, 64);
+        b = sum_lanes(b, 64);
+        b = a > 0.0f ? b / a : 0.0f;
+        float q = 0.0f;
+        for (int e = lane; e < t.rw * t.cw; e += 64) {
+            const int row = e / t.cw, k = row * t.cols + g * t.cw + (e - row * t.cw);
+            const float d = sm[k] - b;
+            q += fmaf(sn[k] * d, d, sq[k]);
+        }
+        q = sum_lanes(q, 64);
+        if (lane == 0) {
+            const int64_t parts = p.chunks * t.pieces;
+            float *o = p.part + 2 * ((n * p.G + t.g0 + g) * parts + t.chunk * t.pieces + t.piece);
+            o[0] = b;
+            o[1] = q;
+            // (kept for the second launch: its first workgroups may write over x)
+            if (p.S > 0 && t.chunk == 0 && t.piece == 0) p.part[2 * p.N * p.G * parts + n * p.G + t.g0 + g] = shift_of<T>(p, n, t.g0 + g);
+        }
+    }
+}
+
+// values of partial k of a group
+template <int V> __device__ __forceinline__ float part_count(const NormParams &p, const Tile &t, int64_t k)
+{
+    const int64_t chunk = k / t.pieces;
+    const int piece = (int)(k - chunk * t.pieces), cu = p.Cg / V;
+    const int64_t rows = min(p.chunk_rows, p.S - chunk * p.chunk_rows);
+    return (float)rows * (float)((t.pieces > 1 ? min(NT, cu - piece * NT) : cu) * V);
+}
+
+template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_apply(NormParams p)
+{
+    __shared__ float stat[NT][2];
+    const Tile t = tile_of<V>(p);
+    const int64_t n = t.n, parts = p.chunks * t.pieces;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int g = wave; g < t.groups; g += NT / 64) {
+        const float *in = p.part + 2 * (n * p.G + t.g0 + g) * parts;
+        float a = 0.0f, b = 0.0f;
+        for (int64_t k = lane; k < parts; k += 64) {
+            const float cnt = part_count<V>(p, t, k);
+            a += cnt;
+            b = fmaf(cnt, in[2 * k], b);
+        }
+        a = sum_lanes(a, 64);
+        b = sum_lanes(b, 64);
+        const float off = a > 0.0f ? b / a : 0.0f;
+        float q = 0.0f;
+        for (int64_t k = lane; k < parts; k += 64) {
+            const float d = in[2 * k] - off;
+            q += fmaf(part_count<V>(p, t, k) * d, d, in[2 * k + 1]);
+        }
+        q = sum_lanes(q, 64);
+        const float mean = a > 0.0f ? p.part[2 * p.N * p.G * parts + n * p.G + t.g0 + g] + off : 0.0f;
+        const float rstd = __builtin_amdgcn_rsqf((a > 0.0f ? q / a : 0.0f) + p.eps);
+        if (lane == 0) {
+            stat[g][0] = mean;
+            stat[g][1] = rstd;
+            if (t.chunk == 0 && t.piece == 0) {
+                if (p.mean) p.mean[n * p.G + t.g0 + g] = mean;
+                if (p.rstd) p.rstd[n * p.G + t.g0 + g] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    if (!t.in) return;
+    const float mean = stat[t.tx / t.cw][0], rstd = stat[t.tx / t.cw][1];
+    float w[V], b[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        w[i] = load_param<T>(p.w, t.c + i, 1.0f);
+        b[i] = load_param<T>(p.b, t.c + i, 0.0f);
+    }
+    const int64_t xb = n * p.x.s0 + t.c, yb = n * p.y.s0 + t.c;
+#pragma unroll 4
+    for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.rw) {
+        const vec_t<T, V> v = load_vec<T, V>(p.x.data, xb + r * p.x.s1);
+        vec_t<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) put<T, V>(o, i, apply_act(fmaf((at<T, V>(v, i) - mean) * rstd, w[i], b[i]), p.act));
+        store_vec<T, V>(p.y.data, yb + r * p.y.s1, o);
+    }
+}
+
+// per channel sum du, sum du xh; per group their sums with the weights
+template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_sums(NormParams p)
+{
+    __shared__ float red[2][NT][V];
+    const Tile t = tile_of<V>(p);
+    const int64_t n = t.n;
+    float w[V], b[V], s1[V], s2[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s1[i] = s2[i] = 0.0f;
+    if (t.in) {
+        const int g = t.g0 + t.tx / t.cw;
+        const float mean = p.mean[n * p.G + g], rstd = p.rstd[n * p.G + g];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[i] = load_param<T>(p.w, t.c + i, 1.0f);
+            b[i] = load_param<T>(p.b, t.c + i, 0.0f);
+        }
+        const int64_t xb = n * p.x.s0 + t.c, db = n * p.dy.s0 + t.c;
+#pragma unroll 4
+        for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.rw) {
+            const vec_t<T, V> xv = load_vec<T, V>(p.x.data, xb + r * p.x.s1), dv = load_vec<T, V>(p.dy.data, db + r * p.dy.s1);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float xh = (at<T, V>(xv, i) - mean) * rstd;
+                const float du = at<T, V>(dv, i) * act_slope(fmaf(xh, w[i], b[i]), p.act);
+                s1[i] += du;
+                s2[i] = fmaf(du, xh, s2[i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        red[0][threadIdx.x][i] = s1[i];
+        red[1][threadIdx.x][i] = s2[i];
+    }
+    __syncthreads();
+    float g1 = 0.0f, g2 = 0.0f;
+    if (t.ty == 0) {
+        float *out = p.part + (n * p.chunks + t.chunk) * 2 * p.C;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float a = s1[i], q = s2[i];
+            for (int k = 1; k < t.rw; ++k) {
+                a += red[0][k * t.cols + t.tx][i];
+                q += red[1][k * t.cols + t.tx][i];
+            }
+            out[t.c + i] = a;
+            out[p.C + t.c + i] = q;
+            g1 = fmaf(w[i], a, g1);
+            g2 = fmaf(w[i], q, g2);
+        }
+    }
+    __syncthreads();
+    if (t.ty == 0) {
+        red[0][t.tx][0] = g1;
+        red[1][t.tx][0] = g2;
+    }
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    float *groups = p.part + p.N * p.chunks * 2 * p.C;
+    for (int g = wave; g < t.groups; g += NT / 64) {
+        float a = 0.0f, q = 0.0f;
+        for (int e = lane; e < t.cw; e += 64) {
+            a += red[0][g * t.cw + e][0];
+            q += red[1][g * t.cw + e][0];
+        }
+        a = sum_lanes(a, 64);
+        q = sum_lanes(q, 64);
+        if (lane == 0) {
+            float *o = groups + 2 * ((n * p.G + t.g0 + g) * p.chunks * t.pieces + t.chunk * t.pieces + t.piece);
+            o[0] = a;
+            o[1] = q;
+        }
+    }
+}
+
+template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_apply_backward(NormParams p)
+{
+    __shared__ float stat[NT][2];
+    const Tile t = tile_of<V>(p);
+    const int64_t n = t.n, parts = p.chunks * t.pieces;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const float inv = 1.0f / ((float)p.S * (float)p.Cg);
+    const float *groups = p.part + p.N * p.chunks * 2 * p.C;
+    for (int g = wave; g < t.groups; g += NT / 64) {
+        const float *in = groups + 2 * (n * p.G + t.g0 + g) * parts;
+        float a = 0.0f, q = 0.0f;
+        for (int64_t k = lane; k < parts; k += 64) {
+            a += in[2 * k];
+            q += in[2 * k + 1];
+        }
+        a = sum_lanes(a, 64);
+        q = sum_lanes(q, 64);
+        if (lane == 0) {
+            stat[g][0] = a * inv;
+            stat[g][1] = q * inv;
+        }
+    }
+    __syncthreads();
+    if (!t.in) return;
+    const int gl = t.tx / t.cw, g = t.g0 + gl;
+    const float m1 = stat[gl][0], m2 = stat[gl][1], mean = p.mean[n * p.G + g], rstd = p.rstd[n * p.G + g];
+    float w[V], b[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        w[i] = load_param<T>(p.w, t.c + i, 1.0f);
+        b[i] = load_param<T>(p.b, t.c + i, 0.0f);
+    }
+    const int64_t xb = n * p.x.s0 + t.c, db = n * p.dy.s0 + t.c, ob = n * p.dx.s0 + t.c;
+#pragma unroll 4
+    for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.rw) {
+        const vec_t<T, V> xv = load_vec<T, V>(p.x.data, xb + r * p.x.s1), dv = load_vec<T, V>(p.dy.data, db + r * p.dy.s1);
+        vec_t<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float xh = (at<T, V>(xv, i) - mean) * rstd;
+            const float g1 = at<T, V>(dv, i) * act_slope(fmaf(xh, w[i], b[i]), p.act) * w[i];
+            put<T, V>(o, i, rstd * (g1 - m1 - xh * m2));
+        }
+        store_vec<T, V>(p.dx.data, ob + r * p.dx.s1, o);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// sums over workgroups' partial results
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(1024) void merit_reduce_rows(ReduceParams p)
+{
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t j = (int64_t)blockIdx.x * 64 + lane;
+    int k = 0;
+    while (k < p.nseg - 1 && j >= p.seg[k].len) j -= p.seg[k].len, ++k;
+    const bool in = j < p.seg[k].len && p.seg[k].out;
+    float s = 0.0f;
+    if (in) {
+        const float *col = p.in + p.seg[k].at + j;
+#pragma unroll 8
+        for (int64_t r = wave; r < p.rows; r += 16) s += col[r * p.pitch];
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && in) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += red[i][lane];
+        p.seg[k].out[j] = s;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+struct RowsForm {
+    int cu, lg, wpg, U;
+};
+RowsForm norm_rows_form(const NormParams &p)
+{
+    RowsForm f;
+    f.cu = p.Cg / p.vec;
+    f.wpg = f.cu > 256 ? 4 : 1;
+    f.lg = 1;
+    while (f.lg < 64 && f.lg < f.cu) f.lg *= 2;
+    const int per = (f.cu + f.lg * f.wpg - 1) / (f.lg * f.wpg);
+    f.U = per <= 1 ? 1 : per <= 2 ? 2 : 4;
+        return f;
+}
+
+template <typename T, int V> hipError_t norm_forward(const NormParams &p, hipStream_t s)
+{
+    if (p.rows_form) {
+        const RowsForm f = norm_rows_form(p);
+        const dim3 grid(p.ctiles, (unsigned)p.chunks);
+        if (f.U == 1) merit_norm_rows<T, V, 1><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
+        else if (f.U == 2) merit_norm_rows<T, V, 2><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
+        else merit_norm_rows<T, V, 4><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
+        return hipGetLastError();
+    }
+    const unsigned grid = (unsigned)(p.N * p.chunks * p.ctiles);
+    merit_norm_stats<T, V><<<grid, NT, 0, s>>>(p);
+    merit_norm_apply<T, V><<<grid, NT, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T, int V> hipError_t norm_backward(const NormParams &p, hipStream_t s)
+{
+    int64_t rows;
+    if (p.rows_form) {
+        const RowsForm f = norm_rows_form(p);
+        const dim3 grid(p.ctiles, (unsigned)p.chunks);
+        if (f.U == 1) merit_norm_rows_backward<T, V, 1><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
+        else if (f.U == 2) merit_norm_rows_backward<T, V, 2><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
+        else merit_norm_rows_backward<T, V, 4><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
+        rows = p.chunks;
+    } else {
+        const unsigned grid = (unsigned)(p.N * p.chunks * p.ctiles);
+        merit_norm_sums<T, V><<<grid, NT, 0, s>>>(p);
+        merit_norm_apply_backward<T, V><<<grid, NT, 0, s>>>(p);
+        rows = p.N * p.chunks;
+    }
+    if (p.dw || p.db) {
+        ReduceParams r = {};
+        r.in = p.part;
+        r.rows = rows;
+        r.pitch = 2ll * p.C;
+        r.nseg = 2;
+        r.seg[0] = {p.db, 0, p.C};
+        r.seg[1] = {p.dw, p.C, p.C};
+        return launch_reduce_rows(r, s);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_reduce_rows(const ReduceParams &p, hipStream_t s)
+{
+    int64_t cols = 0;
+    for (int k = 0; k < p.nseg; ++k) cols += p.seg[k].len;
+    merit_reduce_rows<<<(unsigned)((cols + 63) / 64), 1024, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm(const NormParams &p, int type, hipStream_t s)
+{
+    if (type == MERIT_F32) return p.vec == 4 ? norm_forward<float, 4>(p, s) : norm_forward<float, 1>(p, s);
+    if (type == MERIT_F16) return p.vec == 8 ? norm_forward<f16_t, 8>(p, s) : norm_forward<f16_t, 1>(p, s);
+    return p.vec == 8 ? norm_forward<bf16_t, 8>(p, s) : norm_forward<bf16_t, 1>(p, s);
+}
+
+hipError_t launch_norm_backward(const NormParams &p, int type, hipStream_t s)
+{
+    if (type == MERIT_F32) return p.vec == 4 ? norm_backward<float, 4>(p, s) : norm_backward<float, 1>(p, s);
+    if (type == MERIT_F16) return p.vec == 8 ? norm_backward<f16_t, 8>(p, s) : norm_backward<f16_t, 1>(p, s);
+    return p.vec == 8 ? norm_backward<bf16_t, 8>(p, s) : norm_backward<bf16_t, 1>(p, s);
+}
+
+}  // namespace merit

@@ -1,0 +1,278 @@
+// Selective state space scan, backward.  With dy' = dy silu(z) and a_t = exp(s_t A):
+//     l_t = C_t dy'_t + a_{t+1} l_{t+1}                    the adjoint of h_t, from the last token to the first
+//     dB_t[n] = sum_d l_t s x,    dC_t[n] = sum_d dy'_t h_t        (sums over the channels of a group)
+//     u = sum_n l_t B_t,  q[n] = l_t a_t h_{t-1},  ds = u x + sum_n q A,  dx = u s + skip dy'
+//     ddt = ds sigmoid(dt + dt_bias),  dA[n] = sum_{b,t} q s,  dz = dy (C_t h_t + skip x) silu'(z)
+// Tiles of 16 tokens from the last to the first; a tile starts from the state that the forward pass kept before it, so the
+// states of its tokens are computed once more and stay in registers with their decays.  dB and dC are sums over
+// channels, which are lanes: the 16 tokens' values of a state are added across lanes so that every halving of the lanes
+// halves the values too (15 exchanges for 16 sums of 16 lanes), then wavefronts through LDS, then workgroups through
+// memory in a second launch, in a fixed order.
+#include "scan.h"
+
+namespace merit {
+
+using namespace scan;
+
+namespace {
+
+// lanes whose bit BIT is 0: the sum of `lo` over the two lanes that differ in it; the others: the sum of `hi`
+template <int BIT> __device__ __forceinline__ float halve(float lo, float hi)
+{
+    if constexpr (BIT >= 4) {
+        typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+        u32x2 r;
+        const unsigned a = __builtin_bit_cast(unsigned, lo), b = __builtin_bit_cast(unsigned, hi);
+        if constexpr (BIT == 5) r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
+        else r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a, b, false, false));
+        const unsigned u = r.x, v = r.y;        // (as values: a bit cast of a vector's element takes its first)
+        return __builtin_bit_cast(float, u) + __builtin_bit_cast(float, v);
+    } else {
+        static_assert(BIT == 2 || BIT == 3, "");
+        const int a = __builtin_bit_cast(int, lo), b = __builtin_bit_cast(int, hi);
+        int o;
+        if constexpr (BIT == 3) {       // row_ror:8 into the lower, then the upper eight lanes of sixteen
+            o = __builtin_amdgcn_update_dpp(0, a, 0x128, 0xF, 0x3, false);
+            o = __builtin_amdgcn_update_dpp(o, b, 0x128, 0xF, 0xC, false);
+        } else {                        // row_ror:12 into the even quads, row_ror:4 into the odd ones
+            o = __builtin_amdgcn_update_dpp(0, a, 0x12C, 0xF, 0x5, false);
+            o = __builtin_amdgcn_update_dpp(o, b, 0x124, 0xF, 0xA, false);
+        }
+        return ((threadIdx.x >> BIT) & 1 ? hi : lo) + __builtin_bit_cast(float, o);
+    }
+}
+
+// v[t], t < 16, summed over the lanes of a wavefront that have the same state (all but the lowest log2 LPC lane bits);
+// the lane keeps the sums of KEEP tokens, from first_token() on
+template <int LPC> struct Sums {
+    static constexpr int CW = 64 / LPC;                    // channels of a wavefront
+    static constexpr int KEEP = CW >= TT ? 1 : TT / CW;
+    static __device__ __forceinline__ int first_token()
+    {
+        const int lane = threadIdx.x & 63;                 // bits 5, 4, ... of the lane are bits 3, 2, ... of the token
+        return ((lane >> 2) & 15) & ~(KEEP - 1);
+    }
+    static __device__ __forceinline__ void over_channels(float (&v)[TT])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = halve<5>(v[i], v[i + 8]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = halve<4>(v[i], v[i + 4]);
+        if constexpr (LPC <= 8) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v[i] = halve<3>(v[i], v[i + 2]);
+        }
+        if constexpr (LPC <= 4) v[0] = halve<2>(v[0], v[1]);
+        if constexpr (LPC <= 2) v[0] += lane_xor<1>(v[0]);
+        if constexpr (LPC <= 1) v[0] += lane_xor<0>(v[0]);
+    }
+    // of the lanes that hold the same sum, the one that writes it
+    static __device__ __forceinline__ bool writes() { return LPC >= 4 || (threadIdx.x & (3 & ~(LPC - 1))) == 0; }
+};
+
+template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_back(ScanParams p)
+{
+    using S = Shape<SPL, LPC>;
+    using Q = Sums<LPC>;
+    __shared__ __align__(16) float bl[TT * S::NP], cl[TT * S::NP];
+    __shared__ __align__(16) float red[NT / 64][TT * 2 * S::NP];
+    const Where w = where<LPC>(p, p.chunks);
+    const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
+    float A[SPL], dA[SPL], carry[SPL];
+    bool ok[SPL];
+    const int64_t hat = (w.b * p.D + w.d) * p.N + n0;
+#pragma unroll
+    for (int s = 0; s < SPL; ++s) {
+        ok[s] = w.in && (!PAD || n0 + s < p.N);
+        A[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] : 0.0f;
+        dA[s] = 0.0f;
+        carry[s] = ok[s] && p.dh_last ? p.dh_last[hat + s] : 0.0f;     // a_{t+1} l_{t+1}
+    }
+    const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
+    float dskip = 0.0f, dbias = 0.0f;
+    const int64_t tend = min(w.tile1, (w.n + TT - 1) / TT);
+    // behind the sequence's end every gradient is 0
+    for (int64_t t = max(max(tend, w.tile0) * TT, (int64_t)0) + w.lane; w.in && t < min(w.tile1 * TT, p.L); t += LPC) {
+        store_el(p.dx.data, p.type, w.b * p.dx.s0 + t * p.dx.s1 + w.d, 0.0f);
+        store_el(p.ddt.data, p.type, w.b * p.ddt.s0 + t * p.ddt.s1 + w.d, 0.0f);
+        if (p.z.data) store_el(p.dz.data, p.type, w.b * p.dz.s0 + t * p.dz.s1 + w.d, 0.0f);
+    }
+    float *bc = p.part_bc + ((int64_t)(w.g * p.ctiles + w.ct) * p.B + w.b) * p.L * 2 * p.N;
+    for (int64_t e = max(tend, w.tile0) * TT * 2 * p.N + threadIdx.x; e < min(w.tile1 * TT, p.L) * 2 * p.N; e += NT) bc[e] = 0.0f;
+
+    for (int64_t tile = tend - 1; tile >= w.tile0; --tile) {
+        float x[S::TPL], raw[S::TPL], z[S::TPL], dy[S::TPL], dyo[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL], in_[S::TPL], da_[S::TPL];
+        {
+            float br[S::EB], cr[S::EB];
+            load_states<SPL, LPC>(p.Bm, p, w, tile, br);
+            load_states<SPL, LPC>(p.Cm, p, w, tile, cr);
+            load_rows<SPL, LPC>(p.x, p.type, w, tile, x);
+            load_rows<SPL, LPC>(p.dt, p.type, w, tile, raw);
+            load_rows<SPL, LPC>(p.dy, p.type, w, tile, dyo);
+            if (p.z.data) load_rows<SPL, LPC>(p.z, p.type, w, tile, z);
+            __syncthreads();            // (the tile before is done with bl and cl)
+            stage_states<SPL, LPC>(bl, br);
+            stage_states<SPL, LPC>(cl, cr);
+            __syncthreads();
+        }
+        float hs[SPL], h[TT][SPL], a[TT][SPL];
+        const float *kept = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N + n0;
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) hs[s] = ok[s] ? kept[s] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::TPL; ++i) {
+            const bool in = tile * TT + i * LPC + w.lane < w.n;
+            raw[i] += bias;
+            dt[i] = in ? (p.softplus ? softplusf(raw[i]) : raw[i]) : 0.0f;
+            dx[i] = dt[i] * x[i];
+            dy[i] = p.z.data ? dyo[i] * siluf(z[i]) : dyo[i];
+            y[i] = in_[i] = da_[i] = 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const float dtv = from_lane<LPC>(dt[t / LPC], t % LPC), dxv = from_lane<LPC>(dx[t / LPC], t % LPC);
+            float Bv[SPL], Cv[SPL], acc = 0.0f;
+            read_states<SPL>(bl + t * S::NP + n0, Bv);
+            read_states<SPL>(cl + t * S::NP + n0, Cv);
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) {
+                a[t][s] = __builtin_amdgcn_exp2f(dtv * (A[s] * LOG2E));
+                h[t][s] = fmaf(a[t][s], t ? h[t ? t - 1 : 0][s] : hs[s], dxv * Bv[s]);
+                if (PAD && !ok[s]) h[t][s] = 0.0f;
+                acc = fmaf(h[t][s], Cv[s], acc);
+            }
+            if (p.z.data) {
+                acc = sum_channel<LPC>(acc);
+                if (LPC == 1 || w.lane == t % LPC) y[t / LPC] = acc;
+            }
+        }
+#pragma unroll
+        for (int t = TT - 1; t >= 0; --t) {
+            const float dtv = from_lane<LPC>(dt[t / LPC], t % LPC), dxv = from_lane<LPC>(dx[t / LPC], t % LPC);
+            const float dyv = from_lane<LPC>(dy[t / LPC], t % LPC);
+            float Bv[SPL], Cv[SPL], u = 0.0f, v = 0.0f;
+            read_states<SPL>(bl + t * S::NP + n0, Bv);
+            read_states<SPL>(cl + t * S::NP + n0, Cv);
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) {
+                float l = fmaf(Cv[s], dyv, carry[s]);
+                if (PAD && !ok[s]) l = 0.0f;
+                u = fmaf(l, Bv[s], u);
+                carry[s] = a[t][s] * l;
+                const float q = carry[s] * (t ? h[t ? t - 1 : 0][s] : hs[s]);
+                v = fmaf(q, A[s], v);
+                dA[s] = fmaf(q, dtv, dA[s]);
+                a[t][s] = l * dxv;                  // now dB's and dC's terms
+                h[t][s] *= dyv;
+            }
+            u = sum_channel<LPC>(u);
+            v = sum_channel<LPC>(v);
+            if (LPC == 1 || w.lane == t % LPC) in_[t / LPC] = u, da_[t / LPC] = v;
+        }
+#pragma unroll
+        for (int i = 0; i < S::TPL; ++i) {
+            const int64_t t = tile * TT + i * LPC + w.lane;
+            const bool in = w.in && t < w.n;
+            float ds = fmaf(in_[i], x[i], da_[i]);
+            if (p.softplus) ds *= sigmoidf(raw[i]);
+            if (in) {
+                dskip = fmaf(dy[i], x[i], dskip);
+                dbias += ds;
+            }
+            if (w.in && t < p.L) {
+                store_el(p.dx.data, p.type, w.b * p.dx.s0 + t * p.dx.s1 + w.d, in ? (p.skip ? fmaf(in_[i], dt[i], skip * dy[i]) : in_[i] * dt[i]) : 0.0f);
+                store_el(p.ddt.data, p.type, w.b * p.ddt.s0 + t * p.ddt.s1 + w.d, in ? ds : 0.0f);
+                if (p.z.data)
+                    store_el(p.dz.data, p.type, w.b * p.dz.s0 + t * p.dz.s1 + w.d,
+                             in ? dyo[i] * (p.skip ? fmaf(skip, x[i], y[i]) : y[i]) * act_slope(z[i], MERIT_ACT_SILU) : 0.0f);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) {
+            float vb[TT], vc[TT];
+#pragma unroll
+            for (int t = 0; t < TT; ++t) vb[t] = a[t][s], vc[t] = h[t][s];
+            Q::over_channels(vb);
+            Q::over_channels(vc);
+            if (Q::writes()) {
+#pragma unroll
+                for (int k = 0; k < Q::KEEP; ++k) {
+                    float *o = red[wave] + (Q::first_token() + k) * 2 * S::NP + n0 + s;
+                    o[0] = vb[k];
+                    o[S::NP] = vc[k];
+                }
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < TT * 2 * S::NP; e += NT) {
+            const int n = e % S::NP, k = e / S::NP;         // k = 2 t + (0: dB, 1: dC)
+            const int64_t t = tile * TT + k / 2;
+            const float v = (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]);
+            if (n < p.N && t < p.L) bc[(t * 2 + (k & 1)) * p.N + n] = t < w.n ? v : 0.0f;
+        }
+    }
+    if (p.dh0 && w.chunk == 0) {
+#pragma unroll
+        for (int s = 0; s < SPL; ++s)
+            if (ok[s]) p.dh0[hat + s] = carry[s];
+    }
+    float *part = p.part_a + (w.b * p.chunks + w.chunk) * ((int64_t)p.D * p.N + 2 * p.D);
+#pragma unroll
+    for (int s = 0; s < SPL; ++s)
+        if (ok[s]) part[(int64_t)w.d * p.N + n0 + s] = dA[s];
+    dskip = sum_channel<LPC>(dskip);
+    dbias = sum_channel<LPC>(dbias);
+    if (w.in && w.lane == 0) {
+        part[(int64_t)p.D * p.N + w.d] = dskip;
+        part[(int64_t)p.D * p.N + p.D + w.d] = dbias;
+    }
+}
+
+// dB, dC: the sums over a group's channel tiles, rounded once
+__global__ __launch_bounds__(NT) void merit_scan_sum_bc(ScanParams p)
+{
+    const int64_t id = (int64_t)blockIdx.x * NT + threadIdx.x, per = (int64_t)p.B * p.L * 2 * p.N;
+    const int g = (int)(id / per);
+    if (g >= p.G) return;
+    const int64_t e = id - g * per, row = e / (2 * p.N), b = row / p.L, t = row - b * p.L;
+    const int k = (int)(e - row * 2 * p.N), n = k < p.N ? k : k - p.N;
+    const float *in = p.part_bc + (int64_t)g * p.ctiles * per + e;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < p.ctiles; ++i) s += in[i * per];
+    const Rows &o = k < p.N ? p.dB : p.dC;
+    store_el(o.data, p.type, b * o.s0 + t * o.s1 + (int64_t)g * p.N + n, s);
+}
+
+struct Backward {
+    const ScanParams &p;
+    hipStream_t s;
+    template <int SPL, int LPC, bool PAD> hipError_t run()
+    {
+        merit_scan_back<SPL, LPC, PAD><<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, 0, s>>>(p);
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+hipError_t launch_scan_backward(const ScanParams &p, hipStream_t s)
+{
+    if (p.B > 0) {
+        const hipError_t e = by_states(p.N, Backward{p, s});
+        if (e != hipSuccess) return e;
+        const int64_t count = (int64_t)p.G * p.B * p.L * 2 * p.N;
+        if (count) merit_scan_sum_bc<<<(unsigned)((count + NT - 1) / NT), NT, 0, s>>>(p);
+    }
+    ReduceParams r = {};
+    r.in = p.part_a;
+    r.rows = p.B * p.chunks;
+    r.pitch = (int64_t)p.D * p.N + 2 * p.D;
+    r.nseg = 3;
+    r.seg[0] = {p.dA, 0, (int64_t)p.D * p.N};
+    r.seg[1] = {p.dskip, (int64_t)p.D * p.N, p.D};
+    r.seg[2] = {p.ddt_bias, (int64_t)p.D * p.N + p.D, p.D};
+    return launch_reduce_rows(r, s);
+}
+
+}  // namespace merit

@@ -169,6 +169,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, method
 
 }  // namespace
 
+bool merit_add_token_calls(PyObject *module);      // token_calls.cpp
+
 PyMODINIT_FUNC PyInit__torch_calls() {
   PyObject *m = PyModule_Create(&module), *ops = m ? PyDict_New() : nullptr;
   bool ok = ops != nullptr;
@@ -177,7 +179,7 @@ PyMODINIT_FUNC PyInit__torch_calls() {
     ok = v && PyDict_SetItemString(ops, o.name, v) == 0;
     Py_XDECREF(v);
   }
-  ok = ok && PyObject_SetAttrString(m, "OPS", ops) == 0 && PyModule_AddStringConstant(m, "TORCH", MERIT_TORCH) == 0;
+  ok = ok && PyObject_SetAttrString(m, "OPS", ops) == 0 && PyModule_AddStringConstant(m, "TORCH", MERIT_TORCH) == 0 && merit_add_token_calls(m);
   Py_XDECREF(ops);
   if (!ok) Py_CLEAR(m);
   return m;
