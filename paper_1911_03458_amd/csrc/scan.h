@@ -16,11 +16,13 @@ template <int SPL, int LPC> struct Shape {
 };
 
 struct Where {
-    int64_t b, n;          // sequence, its tokens
+    int64_t b;             // sequence
+    int n;                 // its tokens
     int chunk, g, ct;
-    int d, lane;           // channel, the lane's number among its channel's
+    int d, lane;           // channel (of a lane that has none: the group's last), the lane's number among its channel's
     bool in;               // the channel is there
-    int64_t tile0, tile1;  // tiles of the chunk
+    int tile0, tile1;      // tiles of the chunk
+    int tend;              // the first of them that has no token of the sequence
 };
 template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, int chunks)
 {
@@ -35,62 +37,77 @@ template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, i
     const int cl = w.ct * (NT / LPC) + (int)threadIdx.x / LPC;
     w.lane = (int)threadIdx.x & (LPC - 1);
     w.in = cl < p.Dg;
-    w.d = w.g * p.Dg + cl;
-    w.n = p.lens ? min((int64_t)max(p.lens[w.b], 0), p.L) : p.L;
-    w.tile0 = w.chunk * p.chunk_tiles;
-    w.tile1 = min(w.tile0 + p.chunk_tiles, p.tiles);
+    w.d = w.g * p.Dg + min(cl, p.Dg - 1);
+    w.n = p.lens ? min(max(p.lens[w.b], 0), (int)p.L) : (int)p.L;
+    w.tile0 = w.chunk * (int)p.chunk_tiles;
+    w.tile1 = min(w.tile0 + (int)p.chunk_tiles, (int)p.tiles);
+    w.tend = min(w.tile1, (w.n + TT - 1) / TT);
     return w;
 }
 
-// The tokens of tile `tile` that belong to the lane, 0 behind the sequence's end
-template <typename T, int SPL, int LPC>
-__device__ __forceinline__ void load_rows_t(const Rows &r, const Where &w, int64_t tile, float (&v)[Shape<SPL, LPC>::TPL])
+// Loads go out without a branch and stay raw (a 16-bit element in the low half) until their values are wanted, a tile later:
+// a guarded load would be waited for where the guard ends.  Tokens behind the end, channels and states that are not there
+// read the last one that is, and are replaced by zeros when the values are made.  Not called for a sequence of no tokens.
+template <int COUNT, typename F>
+__device__ __forceinline__ void load_raw(const void *base, int type, uint32_t (&v)[COUNT], F &&at)
 {
-    const T *base = static_cast<const T *>(r.data) + w.b * r.s0 + w.d;
+    if (type == MERIT_F32) {
 #pragma unroll
-    for (int i = 0; i < Shape<SPL, LPC>::TPL; ++i) {
-        const int64_t t = tile * TT + i * LPC + w.lane;
-        v[i] = w.in && t < w.n ? (float)base[t * r.s1] : 0.0f;
+        for (int i = 0; i < COUNT; ++i) v[i] = static_cast<const uint32_t *>(base)[at(i)];
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = static_cast<const uint16_t *>(base)[at(i)];
     }
 }
-template <int SPL, int LPC>
-__device__ __forceinline__ void load_rows(const Rows &r, int type, const Where &w, int64_t tile, float (&v)[Shape<SPL, LPC>::TPL])
+template <int COUNT> __device__ __forceinline__ void values(const uint32_t (&raw)[COUNT], int type, float (&v)[COUNT])
 {
-    if (type == MERIT_BF16) load_rows_t<bf16_t, SPL, LPC>(r, w, tile, v);
-    else if (type == MERIT_F16) load_rows_t<f16_t, SPL, LPC>(r, w, tile, v);
-    else load_rows_t<float, SPL, LPC>(r, w, tile, v);
+    if (type == MERIT_BF16) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = __builtin_bit_cast(float, raw[i] << 16);
+    } else if (type == MERIT_F16) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = (float)__builtin_bit_cast(f16_t, (uint16_t)raw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = __builtin_bit_cast(float, raw[i]);
+    }
 }
 
-// The thread's elements of B or C of a tile, 0 behind the end and behind N
-template <typename T, int SPL, int LPC>
-__device__ __forceinline__ void load_states_t(const Rows &r, const ScanParams &p, const Where &w, int64_t tile,
-                                              float (&v)[Shape<SPL, LPC>::EB])
+// the lane's tokens of a tile, in the channel
+template <int SPL, int LPC>
+__device__ __forceinline__ void load_rows(const Rows &r, int type, const Where &w, int tile, uint32_t (&v)[Shape<SPL, LPC>::TPL])
+{
+    load_raw(r.data, type, v, [&](int i) { return w.b * r.s0 + min(tile * TT + i * LPC + w.lane, w.n - 1) * r.s1 + w.d; });
+}
+// the thread's elements of B or C of a tile
+template <int SPL, int LPC>
+__device__ __forceinline__ void load_states(const Rows &r, const ScanParams &p, const Where &w, int tile, uint32_t (&v)[Shape<SPL, LPC>::EB])
 {
     constexpr int NP = Shape<SPL, LPC>::NP;
-    const T *base = static_cast<const T *>(r.data) + w.b * r.s0 + (int64_t)w.g * p.N;
-#pragma unroll
-    for (int i = 0; i < Shape<SPL, LPC>::EB; ++i) {
-        const int e = i * NT + (int)threadIdx.x, n = e % NP;
-        const int64_t t = tile * TT + e / NP;
-        v[i] = e < TT * NP && n < p.N && t < w.n ? (float)base[t * r.s1 + n] : 0.0f;
-    }
+    load_raw(r.data, p.type, v, [&](int i) {
+        const int e = (i * NT + (int)threadIdx.x) & (TT * NP - 1), n = e % NP;
+        return w.b * r.s0 + min(tile * TT + e / NP, w.n - 1) * r.s1 + w.g * p.N + min(n, p.N - 1);
+    });
 }
 template <int SPL, int LPC>
-__device__ __forceinline__ void load_states(const Rows &r, const ScanParams &p, const Where &w, int64_t tile,
-                                            float (&v)[Shape<SPL, LPC>::EB])
+__device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, const Where &w, int tile, const uint32_t (&raw)[Shape<SPL, LPC>::EB])
 {
-    if (p.type == MERIT_BF16) load_states_t<bf16_t, SPL, LPC>(r, p, w, tile, v);
-    else if (p.type == MERIT_F16) load_states_t<f16_t, SPL, LPC>(r, p, w, tile, v);
-    else load_states_t<float, SPL, LPC>(r, p, w, tile, v);
-}
-template <int SPL, int LPC>
-__device__ __forceinline__ void stage_states(float *lds, const float (&v)[Shape<SPL, LPC>::EB])
-{
+    constexpr int NP = Shape<SPL, LPC>::NP;
+    float v[Shape<SPL, LPC>::EB];
+    values(raw, p.type, v);
 #pragma unroll
     for (int i = 0; i < Shape<SPL, LPC>::EB; ++i) {
         const int e = i * NT + (int)threadIdx.x;
-        if (e < TT * Shape<SPL, LPC>::NP) lds[e] = v[i];
+        if (e < TT * NP) lds[e] = e % NP < p.N && tile * TT + e / NP < w.n ? v[i] : 0.0f;
     }
+}
+
+// A barrier for LDS alone: loads from memory stay in flight across it
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 __device__ __forceinline__ void store_el(void *base, int type, int64_t at, float v)

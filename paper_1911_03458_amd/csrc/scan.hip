@@ -32,33 +32,33 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
         h[s] = ok[s] && p.h0 ? p.h0[hat + s] : 0.0f;
     }
     const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
-    const int64_t tend = min(w.tile1, (w.n + TT - 1) / TT);
-
-    float xr[S::TPL], dr[S::TPL], zr[S::TPL] = {}, br[S::EB], cr[S::EB];
-    auto fetch = [&](int64_t tile) {
+    uint32_t xr[S::TPL], dr[S::TPL], zr[S::TPL] = {}, br[S::EB], cr[S::EB];
+    auto fetch = [&](int tile) {
         load_rows<SPL, LPC>(p.x, p.type, w, tile, xr);
         load_rows<SPL, LPC>(p.dt, p.type, w, tile, dr);
         if (p.z.data) load_rows<SPL, LPC>(p.z, p.type, w, tile, zr);
         load_states<SPL, LPC>(p.Bm, p, w, tile, br);
         load_states<SPL, LPC>(p.Cm, p, w, tile, cr);
     };
-    if (w.tile0 < tend) fetch(w.tile0);
-    for (int64_t tile = w.tile0; tile < tend; ++tile) {
+    if (w.tile0 < w.tend) fetch(w.tile0);
+    for (int tile = w.tile0; tile < w.tend; ++tile) {
         float *bt = bl[tile & 1], *ct = cl[tile & 1];
-        stage_states<SPL, LPC>(bt, br);
-        stage_states<SPL, LPC>(ct, cr);
+        stage_states<SPL, LPC>(bt, p, w, tile, br);
+        stage_states<SPL, LPC>(ct, p, w, tile, cr);
         float x[S::TPL], z[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL];
+        values(xr, p.type, x);
+        values(zr, p.type, z);
+        values(dr, p.type, dt);
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
             const bool in = tile * TT + i * LPC + w.lane < w.n;
-            x[i] = xr[i], z[i] = zr[i];
-            const float v = dr[i] + bias;
+            const float v = dt[i] + bias;
             dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
-            dx[i] = dt[i] * x[i];
+            dx[i] = in ? dt[i] * x[i] : 0.0f;
             y[i] = 0.0f;
         }
-        if (tile + 1 < tend) fetch(tile + 1);
-        __syncthreads();
+        fetch(min(tile + 1, w.tend - 1));
+        lds_barrier();
         if (p.states && w.in) {
             float *o = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N + n0;
 #pragma unroll
@@ -83,7 +83,7 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
         if (w.in) {
 #pragma unroll
             for (int i = 0; i < S::TPL; ++i) {
-                const int64_t t = tile * TT + i * LPC + w.lane;
+                const int t = tile * TT + i * LPC + w.lane;
                 float v = p.skip ? fmaf(skip, x[i], y[i]) : y[i];         // (absent: not 0 times an infinite x)
                 if (p.z.data) v *= siluf(z[i]);
                 if (t < p.L) store_el(p.y.data, p.type, w.b * p.y.s0 + t * p.y.s1 + w.d, t < w.n ? v : 0.0f);
@@ -91,7 +91,7 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
         }
     }
     if (!w.in) return;
-    for (int64_t t = max(tend, w.tile0) * TT + w.lane; t < min(w.tile1 * TT, p.L); t += LPC)
+    for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; t < min((int64_t)w.tile1 * TT, p.L); t += LPC)
         store_el(p.y.data, p.type, w.b * p.y.s0 + t * p.y.s1 + w.d, 0.0f);
     if (p.h_last && w.chunk == p.chunks - 1) {
 #pragma unroll

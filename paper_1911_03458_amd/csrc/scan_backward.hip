@@ -90,44 +90,52 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
     }
     const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
     float dskip = 0.0f, dbias = 0.0f;
-    const int64_t tend = min(w.tile1, (w.n + TT - 1) / TT);
     // behind the sequence's end every gradient is 0
-    for (int64_t t = max(max(tend, w.tile0) * TT, (int64_t)0) + w.lane; w.in && t < min(w.tile1 * TT, p.L); t += LPC) {
+    for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; w.in && t < min((int64_t)w.tile1 * TT, p.L); t += LPC) {
         store_el(p.dx.data, p.type, w.b * p.dx.s0 + t * p.dx.s1 + w.d, 0.0f);
         store_el(p.ddt.data, p.type, w.b * p.ddt.s0 + t * p.ddt.s1 + w.d, 0.0f);
         if (p.z.data) store_el(p.dz.data, p.type, w.b * p.dz.s0 + t * p.dz.s1 + w.d, 0.0f);
     }
     float *bc = p.part_bc + ((int64_t)(w.g * p.ctiles + w.ct) * p.B + w.b) * p.L * 2 * p.N;
-    for (int64_t e = max(tend, w.tile0) * TT * 2 * p.N + threadIdx.x; e < min(w.tile1 * TT, p.L) * 2 * p.N; e += NT) bc[e] = 0.0f;
+    for (int64_t e = (int64_t)max(w.tend, w.tile0) * TT * 2 * p.N + threadIdx.x; e < min((int64_t)w.tile1 * TT, p.L) * 2 * p.N; e += NT) bc[e] = 0.0f;
 
-    for (int64_t tile = tend - 1; tile >= w.tile0; --tile) {
-        float x[S::TPL], raw[S::TPL], z[S::TPL], dy[S::TPL], dyo[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL], in_[S::TPL], da_[S::TPL];
-        {
-            float br[S::EB], cr[S::EB];
-            load_states<SPL, LPC>(p.Bm, p, w, tile, br);
-            load_states<SPL, LPC>(p.Cm, p, w, tile, cr);
-            load_rows<SPL, LPC>(p.x, p.type, w, tile, x);
-            load_rows<SPL, LPC>(p.dt, p.type, w, tile, raw);
-            load_rows<SPL, LPC>(p.dy, p.type, w, tile, dyo);
-            if (p.z.data) load_rows<SPL, LPC>(p.z, p.type, w, tile, z);
-            __syncthreads();            // (the tile before is done with bl and cl)
-            stage_states<SPL, LPC>(bl, br);
-            stage_states<SPL, LPC>(cl, cr);
-            __syncthreads();
-        }
-        float hs[SPL], h[TT][SPL], a[TT][SPL];
-        const float *kept = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N + n0;
+    uint32_t xr[S::TPL], dr[S::TPL], yr[S::TPL], zr[S::TPL] = {}, br[S::EB], cr[S::EB];
+    float hr[SPL];
+    auto fetch = [&](int tile) {
+        load_rows<SPL, LPC>(p.x, p.type, w, tile, xr);
+        load_rows<SPL, LPC>(p.dt, p.type, w, tile, dr);
+        load_rows<SPL, LPC>(p.dy, p.type, w, tile, yr);
+        if (p.z.data) load_rows<SPL, LPC>(p.z, p.type, w, tile, zr);
+        load_states<SPL, LPC>(p.Bm, p, w, tile, br);
+        load_states<SPL, LPC>(p.Cm, p, w, tile, cr);
+        const float *kept = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N;
 #pragma unroll
-        for (int s = 0; s < SPL; ++s) hs[s] = ok[s] ? kept[s] : 0.0f;
+        for (int s = 0; s < SPL; ++s) hr[s] = kept[PAD ? min(n0 + s, p.N - 1) : n0 + s];
+    };
+    if (w.tile0 < w.tend) fetch(w.tend - 1);
+    for (int tile = w.tend - 1; tile >= w.tile0; --tile) {
+        float x[S::TPL], raw[S::TPL], z[S::TPL], dy[S::TPL], dyo[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL], in_[S::TPL], da_[S::TPL];
+        values(xr, p.type, x);
+        values(dr, p.type, raw);
+        values(yr, p.type, dyo);
+        values(zr, p.type, z);
+        lds_barrier();              // (the tile before is done with bl and cl)
+        stage_states<SPL, LPC>(bl, p, w, tile, br);
+        stage_states<SPL, LPC>(cl, p, w, tile, cr);
+        float hs[SPL], h[TT][SPL], a[TT][SPL];
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) hs[s] = ok[s] ? hr[s] : 0.0f;
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
-            const bool in = tile * TT + i * LPC + w.lane < w.n;
+            const bool in = w.in && tile * TT + i * LPC + w.lane < w.n;
             raw[i] += bias;
             dt[i] = in ? (p.softplus ? softplusf(raw[i]) : raw[i]) : 0.0f;
-            dx[i] = dt[i] * x[i];
-            dy[i] = p.z.data ? dyo[i] * siluf(z[i]) : dyo[i];
+            dx[i] = in ? dt[i] * x[i] : 0.0f;
+            dy[i] = in ? (p.z.data ? dyo[i] * siluf(z[i]) : dyo[i]) : 0.0f;
             y[i] = in_[i] = da_[i] = 0.0f;
         }
+        fetch(max(tile - 1, w.tile0));
+        lds_barrier();
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             const float dtv = from_lane<LPC>(dt[t / LPC], t % LPC), dxv = from_lane<LPC>(dx[t / LPC], t % LPC);
@@ -171,7 +179,7 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
         }
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
-            const int64_t t = tile * TT + i * LPC + w.lane;
+            const int t = tile * TT + i * LPC + w.lane;
             const bool in = w.in && t < w.n;
             float ds = fmaf(in_[i], x[i], da_[i]);
             if (p.softplus) ds *= sigmoidf(raw[i]);
@@ -203,7 +211,7 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
                 }
             }
         }
-        __syncthreads();
+        lds_barrier();
         for (int e = threadIdx.x; e < TT * 2 * S::NP; e += NT) {
             const int n = e % S::NP, k = e / S::NP;         // k = 2 t + (0: dB, 1: dC)
             const int64_t t = tile * TT + k / 2;
