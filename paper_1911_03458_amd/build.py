@@ -15,10 +15,12 @@ CALLS_SRC = os.path.join(CSRC, "torch_calls.cpp")
 CALLS_PATH = os.path.join(_HERE, "_torch_calls.so")      # a Python module over libmerit.so and PyTorch
 
 SOURCES = ["merit_plan.cpp", "pool2d.hip", "sad_search.hip", "conv2d.hip", "conv2d_chws.hip", "conv2d_px.hip", "conv2d_split.hip", "maxpool_f16.hip", "generic.hip", "corr.hip", "dwconv.hip", "sepfilter.hip", "bilateral.hip", "probe.hip",
-           "token_plan.cpp", "groupnorm.hip", "causal_conv.hip", "scan.hip", "scan_backward.hip"]
+           "token_plan.cpp", "groupnorm.hip", "causal_conv.hip", "scan.hip", "scan_backward_f32.hip",
+           "scan_backward_f16.hip", "scan_backward_bf16.hip"]
 HEADERS = [os.path.join(CSRC, "merit_internal.h"), os.path.join(ROOT, "include", "merit.h"),
            os.path.join(ROOT, "include", "merit_probe.h"), os.path.join(ROOT, "include", "merit_tokens.h"),
-           os.path.join(CSRC, "tokens.h"), os.path.join(CSRC, "scan.h")]
+           os.path.join(CSRC, "tokens.h"), os.path.join(CSRC, "scan.h"),
+           os.path.join(CSRC, "scan_backward.h")]
 TOKEN_CALLS_SRC = os.path.join(CSRC, "token_calls.cpp")
 CALLS_DEPS = [CALLS_SRC, TOKEN_CALLS_SRC, os.path.join(ROOT, "include", "merit.h"),
               os.path.join(ROOT, "include", "merit_tokens.h")]

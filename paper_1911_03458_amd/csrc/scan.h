@@ -1,5 +1,7 @@
 // What the scan's kernels share (scan.hip: forward and single tokens, scan_backward.hip).
 #pragma once
+#include <type_traits>
+
 #include "tokens.h"
 
 namespace merit {
@@ -11,7 +13,11 @@ constexpr int TT = MERIT_SCAN_TILE, NT = SCAN_THREADS;
 template <int SPL, int LPC> struct Shape {
     static constexpr int NP = SPL * LPC;           // states, padded
     static constexpr int CPB = NT / LPC;           // channels of a workgroup
-    static constexpr int TPL = TT / LPC;           // tokens of a tile whose inputs a lane loads: j, j + LPC, ...
+    // Of a tile's tokens a channel's lanes load every LQ-th, lane j tokens j, j + LQ, ...; eight and sixteen lanes do as
+    // two and four quads that load the same, since a value reaches the lanes of its quad inside the instruction that uses
+    // it and lanes beyond it only by way of LDS.
+    static constexpr int LQ = LPC < 4 ? LPC : 4;
+    static constexpr int TPL = TT / LQ;
     static constexpr int EB = (TT * NP + NT - 1) / NT;     // elements of B (and of C) of a tile that a thread stages
 };
 
@@ -20,6 +26,7 @@ struct Where {
     int n;                 // its tokens
     int chunk, g, ct;
     int d, lane;           // channel (of a lane that has none: the group's last), the lane's number among its channel's
+    int tok;               // the first of its tokens in a tile
     bool in;               // the channel is there
     int tile0, tile1;      // tiles of the chunk
     int tend;              // the first of them that has no token of the sequence
@@ -36,6 +43,7 @@ template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, i
     w.b = r / (uint32_t)chunks;
     const int cl = w.ct * (NT / LPC) + (int)threadIdx.x / LPC;
     w.lane = (int)threadIdx.x & (LPC - 1);
+    w.tok = w.lane & 3;
     w.in = cl < p.Dg;
     w.d = w.g * p.Dg + min(cl, p.Dg - 1);
     w.n = p.lens ? min(max(p.lens[w.b], 0), (int)p.L) : (int)p.L;
@@ -45,56 +53,69 @@ template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, i
     return w;
 }
 
-// Loads go out without a branch and stay raw (a 16-bit element in the low half) until their values are wanted, a tile later:
-// a guarded load would be waited for where the guard ends.  Tokens behind the end, channels and states that are not there
-// read the last one that is, and are replaced by zeros when the values are made.  Not called for a sequence of no tokens.
-template <int COUNT, typename F>
-__device__ __forceinline__ void load_raw(const void *base, int type, uint32_t (&v)[COUNT], F &&at)
+// How the kernels move tiles.  Loads go out a tile before their use and stay raw (a 16-bit element in the low half) until
+// then.  Loads and stores share one counter and the wait for a load waits for what was issued before it, so a tile's results
+// are written while the next tile is under way, before its own loads are issued: a store is never younger than a load that
+// is waited for.  The barrier between staging and reading LDS waits for LDS alone (lds_barrier).
+// (Results written at once and a barrier that waits for everything: 8x2048x2048, 16 states, MEASURED_BEFORE us.)
+// A tensor as a lane walks it: the address (in global memory: a flat load would count as one from LDS too) of its first
+// element of tile 0, bytes from token to token.
+typedef __attribute__((address_space(1))) char *gptr;
+struct Walk {
+    gptr at;
+    int64_t step;
+};
+template <typename T> using raw_t = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
+template <typename T> __device__ __forceinline__ Walk walk_rows(const Rows &r, const Where &w)
 {
-    if (type == MERIT_F32) {
+    constexpr int64_t es = sizeof(T);
+    return Walk{(gptr)r.data + (w.b * r.s0 + w.tok * r.s1 + w.d) * es, r.s1 * es};
+}
+// (thread e of a tile's TT x NP elements of B or C, further ones NT elements on)
+template <typename T, int NP> __device__ __forceinline__ Walk walk_states(const Rows &r, const ScanParams &p, const Where &w)
+{
+    constexpr int64_t es = sizeof(T);
+    const int e = (int)threadIdx.x & (TT * NP - 1);
+    return Walk{(gptr)r.data + (w.b * r.s0 + (e / NP) * r.s1 + w.g * p.N + min(e % NP, p.N - 1)) * es, r.s1 * es};
+}
+// COUNT elements, `every` tokens apart, the first token `first` of tile `tile`.  WHOLE: all of the tile's tokens are there
+// and the addresses differ from the lane's by numbers that all lanes share (a product of 64 bits a load and lane costs more
+// than the scan's arithmetic); else tokens behind `last` read that one again.
+template <typename T, bool WHOLE, int COUNT>
+__device__ __forceinline__ void load_walk(const Walk &k, int tile, int every, int first, int last, raw_t<T> (&v)[COUNT])
+{
+    const int64_t off = (int64_t)(tile * TT) * k.step;
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = static_cast<const uint32_t *>(base)[at(i)];
-    } else {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = static_cast<const uint16_t *>(base)[at(i)];
+    for (int i = 0; i < COUNT; ++i) {
+        const gptr at = WHOLE ? k.at + (off + (int64_t)(i * every) * k.step)
+                              : k.at + (int64_t)(min(tile * TT + i * every + first, last) - first) * k.step;
+        v[i] = *reinterpret_cast<__attribute__((address_space(1))) const raw_t<T> *>(at);
     }
 }
-template <int COUNT> __device__ __forceinline__ void values(const uint32_t (&raw)[COUNT], int type, float (&v)[COUNT])
+// ALL: every token of the tile is there; else only tokens before `end` are written
+template <typename T, bool ALL, int COUNT>
+__device__ __forceinline__ void store_walk(const Walk &k, int tile, int every, int first, int64_t end, const float (&v)[COUNT])
 {
-    if (type == MERIT_BF16) {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = __builtin_bit_cast(float, raw[i] << 16);
-    } else if (type == MERIT_F16) {
+    for (int i = 0; i < COUNT; ++i)
+        if (ALL || tile * TT + i * every + first < end)
+            *reinterpret_cast<__attribute__((address_space(1))) T *>(k.at + (int64_t)(tile * TT + i * every) * k.step) = (T)v[i];
+}
+template <typename T, int COUNT> __device__ __forceinline__ void values(const raw_t<T> (&raw)[COUNT], float (&v)[COUNT])
+{
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = (float)__builtin_bit_cast(f16_t, (uint16_t)raw[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = __builtin_bit_cast(float, raw[i]);
+    for (int i = 0; i < COUNT; ++i) {
+        if constexpr (std::is_same_v<T, bf16_t>) v[i] = __builtin_bit_cast(float, (uint32_t)raw[i] << 16);
+        else v[i] = (float)__builtin_bit_cast(T, raw[i]);
     }
 }
 
-// the lane's tokens of a tile, in the channel
-template <int SPL, int LPC>
-__device__ __forceinline__ void load_rows(const Rows &r, int type, const Where &w, int tile, uint32_t (&v)[Shape<SPL, LPC>::TPL])
-{
-    load_raw(r.data, type, v, [&](int i) { return w.b * r.s0 + min(tile * TT + i * LPC + w.lane, w.n - 1) * r.s1 + w.d; });
-}
-// the thread's elements of B or C of a tile
-template <int SPL, int LPC>
-__device__ __forceinline__ void load_states(const Rows &r, const ScanParams &p, const Where &w, int tile, uint32_t (&v)[Shape<SPL, LPC>::EB])
-{
-    constexpr int NP = Shape<SPL, LPC>::NP;
-    load_raw(r.data, p.type, v, [&](int i) {
-        const int e = (i * NT + (int)threadIdx.x) & (TT * NP - 1), n = e % NP;
-        return w.b * r.s0 + min(tile * TT + e / NP, w.n - 1) * r.s1 + w.g * p.N + min(n, p.N - 1);
-    });
-}
-template <int SPL, int LPC>
-__device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, const Where &w, int tile, const uint32_t (&raw)[Shape<SPL, LPC>::EB])
+template <typename T, int SPL, int LPC>
+__device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, const Where &w, int tile, const raw_t<T> (&raw)[Shape<SPL, LPC>::EB])
 {
     constexpr int NP = Shape<SPL, LPC>::NP;
     float v[Shape<SPL, LPC>::EB];
-    values(raw, p.type, v);
+    values<T>(raw, v);
 #pragma unroll
     for (int i = 0; i < Shape<SPL, LPC>::EB; ++i) {
         const int e = i * NT + (int)threadIdx.x;
@@ -102,26 +123,8 @@ __device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, co
     }
 }
 
-// A barrier for LDS alone: loads from memory stay in flight across it
-__device__ __forceinline__ void lds_barrier()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
-__device__ __forceinline__ void store_el(void *base, int type, int64_t at, float v)
-{
-    if (type == MERIT_BF16) static_cast<bf16_t *>(base)[at] = (bf16_t)v;
-    else if (type == MERIT_F16) static_cast<f16_t *>(base)[at] = (f16_t)v;
-    else static_cast<float *>(base)[at] = v;
-}
-__device__ __forceinline__ float load_el(const void *base, int type, int64_t at)
-{
-    if (type == MERIT_BF16) return (float)static_cast<const bf16_t *>(base)[at];
-    if (type == MERIT_F16) return (float)static_cast<const f16_t *>(base)[at];
-    return static_cast<const float *>(base)[at];
-}
+// A barrier for LDS alone: loads from memory stay in flight across it, which a fence would wait for
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // log(1 + exp(v)) = max(v, 0) + log1p(exp(-|v|)); log1p by log(1 + e) e / ((1 + e) - 1), which keeps the digits of a
 // small e that the sum cuts off
@@ -132,40 +135,56 @@ __device__ __forceinline__ float softplusf(float v)
     return v != v ? v : fmaxf(v, 0.0f) + l;
 }
 
-// the value that lane `j` of the channel's lanes has
-template <int LPC> __device__ __forceinline__ float from_lane(float v, int j);
-template <> __device__ __forceinline__ float from_lane<1>(float v, int) { return v; }
 #define MERIT_DPP(v, ctrl) __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), ctrl, 0xF, 0xF, true))
-template <> __device__ __forceinline__ float from_lane<2>(float v, int j)
+// the value that lane `j` of the lane's LQ has
+template <int LQ> __device__ __forceinline__ float from_lane(float v, int j)
 {
-    return j ? MERIT_DPP(v, 0xF5) : MERIT_DPP(v, 0xA0);                 // quad_perm 1,1,3,3 / 0,0,2,2
-}
-template <> __device__ __forceinline__ float from_lane<4>(float v, int j)
-{
-    switch (j) {
+    if constexpr (LQ == 1) return v;
+    else if constexpr (LQ == 2) return j ? MERIT_DPP(v, 0xF5) : MERIT_DPP(v, 0xA0);       // quad_perm 1,1,3,3 / 0,0,2,2
+    else switch (j) {
     case 0: return MERIT_DPP(v, 0x00);
     case 1: return MERIT_DPP(v, 0x55);
     case 2: return MERIT_DPP(v, 0xAA);
     default: return MERIT_DPP(v, 0xFF);
     }
 }
-template <> __device__ __forceinline__ float from_lane<8>(float v, int j)
-{
-    return __shfl(v, ((int)threadIdx.x & 56) | j);
-}
-template <> __device__ __forceinline__ float from_lane<16>(float v, int j)
-{
-    return __shfl(v, ((int)threadIdx.x & 48) | j);
-}
 
 // the sum over the channel's lanes, in all of them
 template <int LPC> __device__ __forceinline__ float sum_channel(float v)
 {
+    if constexpr (LPC > 8) v += MERIT_DPP(v, 0x140);       // row_mirror: the other eight of sixteen
+    if constexpr (LPC > 4) v += MERIT_DPP(v, 0x141);       // row_half_mirror: the other quad of eight
     if constexpr (LPC > 1) v += MERIT_DPP(v, 0xB1);
     if constexpr (LPC > 2) v += MERIT_DPP(v, 0x4E);
-    if constexpr (LPC > 4) v += MERIT_DPP(v, 0x141);       // row_half_mirror: the other quad of eight lanes
-    if constexpr (LPC > 8) v += MERIT_DPP(v, 0x140);       // row_mirror: the other eight of sixteen
     return v;
+}
+
+// v[u] of four tokens summed over the channel's lanes, each into the lane that has the token: out[0 .. 4 / LQ - 1].  A
+// lane adds what it keeps to what its neighbour gives away, so a sum of four tokens takes three exchanges, not eight.
+template <int LPC> __device__ __forceinline__ void sum_to_tokens(const float (&v)[4], float *out)
+{
+    if constexpr (LPC == 1) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) out[u] = v[u];
+    } else {
+        float q[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            q[u] = v[u];
+            if constexpr (LPC > 8) q[u] += MERIT_DPP(q[u], 0x140);
+            if constexpr (LPC > 4) q[u] += MERIT_DPP(q[u], 0x141);
+        }
+        const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+        const float a = odd ? q[1] : q[0], ga = odd ? q[0] : q[1], b = odd ? q[3] : q[2], gb = odd ? q[2] : q[3];
+        const float ra = a + MERIT_DPP(ga, 0xB1), rb = b + MERIT_DPP(gb, 0xB1);
+        if constexpr (LPC == 2) {
+            out[0] = ra;
+            out[1] = rb;
+        } else {
+            const float keep = high ? rb : ra, give = high ? ra : rb;
+            out[0] = keep + MERIT_DPP(give, 0x4E);
+        }
+    }
 }
 
 // four consecutive floats of LDS or one
@@ -197,4 +216,8 @@ template <typename F> hipError_t by_states(int N, F &&f)
 }
 
 }  // namespace scan
+
+// one of these per element type, each in a source of its own (they take long to compile)
+template <typename T> hipError_t scan_backward_of(const ScanParams &p, hipStream_t s);
+
 }  // namespace merit

@@ -16,7 +16,7 @@ using namespace scan;
 
 namespace {
 
-template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_tiles(ScanParams p)
+template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch_bounds__(NT) void merit_scan_tiles(ScanParams p)
 {
     using S = Shape<SPL, LPC>;
     __shared__ __align__(16) float bl[2][TT * S::NP], cl[2][TT * S::NP];
@@ -27,72 +27,101 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
     const int64_t hat = (w.b * p.D + w.d) * p.N + n0;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
-        ok[s] = w.in && (!PAD || n0 + s < p.N);
+        ok[s] = !PAD || n0 + s < p.N;
         A[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] * LOG2E : 0.0f;
         h[s] = ok[s] && p.h0 ? p.h0[hat + s] : 0.0f;
     }
-    const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
-    uint32_t xr[S::TPL], dr[S::TPL], zr[S::TPL] = {}, br[S::EB], cr[S::EB];
-    auto fetch = [&](int tile) {
-        load_rows<SPL, LPC>(p.x, p.type, w, tile, xr);
-        load_rows<SPL, LPC>(p.dt, p.type, w, tile, dr);
-        if (p.z.data) load_rows<SPL, LPC>(p.z, p.type, w, tile, zr);
-        load_states<SPL, LPC>(p.Bm, p, w, tile, br);
-        load_states<SPL, LPC>(p.Cm, p, w, tile, cr);
+    const float bias = p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = p.skip ? p.skip[w.d] : 0.0f;
+    const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), zw = p.z.data ? walk_rows<T>(p.z, w) : xw,
+               yw = walk_rows<T>(p.y, w), bw = walk_states<T, S::NP>(p.Bm, p, w), cw = walk_states<T, S::NP>(p.Cm, p, w);
+
+    raw_t<T> xr[S::TPL], dr[S::TPL], zr[S::TPL], br[S::EB], cr[S::EB];
+    auto fetch = [&](int tile, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        load_walk<T, WHOLE>(xw, tile, S::LQ, w.tok, w.n - 1, xr);
+        load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, dr);
+        load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, zr);
+        const int first = ((int)threadIdx.x & (TT * S::NP - 1)) / S::NP;
+        load_walk<T, WHOLE>(bw, tile, NT / S::NP, first, w.n - 1, br);
+        load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, cr);
     };
-    if (w.tile0 < w.tend) fetch(w.tile0);
-    for (int tile = w.tile0; tile < w.tend; ++tile) {
+    float out[S::TPL];                          // results of the tile before
+    // all: this tile and the next one are whole
+    auto run = [&](int tile, auto all) {
+        constexpr bool ALL = decltype(all)::value;
         float *bt = bl[tile & 1], *ct = cl[tile & 1];
-        stage_states<SPL, LPC>(bt, p, w, tile, br);
-        stage_states<SPL, LPC>(ct, p, w, tile, cr);
+        stage_states<T, SPL, LPC>(bt, p, w, tile, br);
+        stage_states<T, SPL, LPC>(ct, p, w, tile, cr);
         float x[S::TPL], z[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL];
-        values(xr, p.type, x);
-        values(zr, p.type, z);
-        values(dr, p.type, dt);
+        values<T>(xr, x);
+        values<T>(zr, z);
+        values<T>(dr, dt);
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
-            const bool in = tile * TT + i * LPC + w.lane < w.n;
+            const bool in = ALL || tile * TT + i * S::LQ + w.tok < w.n;
             const float v = dt[i] + bias;
             dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
             dx[i] = in ? dt[i] * x[i] : 0.0f;
-            y[i] = 0.0f;
         }
-        fetch(min(tile + 1, w.tend - 1));
-        lds_barrier();
-        if (p.states && w.in) {
+        if (tile > w.tile0) store_walk<T, true>(yw, tile - 1, S::LQ, w.tok, p.L, out);
+        if (KEEP) {
             float *o = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N + n0;
 #pragma unroll
             for (int s = 0; s < SPL; ++s)
-                if (ok[s]) o[s] = h[s];
+                if (!PAD || ok[s]) o[s] = h[s];
         }
+        fetch(ALL ? tile + 1 : min(tile + 1, w.tend - 1), all);
+        lds_barrier();
+        // Four tokens at a time; what needs LDS or an exponential is asked for four tokens ahead
+        float Bv[2][4][SPL], Cv[2][4][SPL], a[2][4][SPL];
+        auto ahead = [&](int k) {
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const float dtv = from_lane<LPC>(dt[t / LPC], t % LPC), dxv = from_lane<LPC>(dx[t / LPC], t % LPC);
-            float Bv[SPL], Cv[SPL], acc = 0.0f;
-            read_states<SPL>(bt + t * S::NP + n0, Bv);
-            read_states<SPL>(ct + t * S::NP + n0, Cv);
+            for (int u = 0; u < 4; ++u) {
+                const int t = 4 * k + u;
+                read_states<SPL>(bt + t * S::NP + n0, Bv[k & 1][u]);
+                read_states<SPL>(ct + t * S::NP + n0, Cv[k & 1][u]);
+                const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ);
 #pragma unroll
-            for (int s = 0; s < SPL; ++s) {
-                h[s] = fmaf(__builtin_amdgcn_exp2f(dtv * A[s]), h[s], dxv * Bv[s]);
-                if (PAD && !ok[s]) h[s] = 0.0f;            // (an infinite input: 0 times it)
-                acc = fmaf(h[s], Cv[s], acc);
+                for (int s = 0; s < SPL; ++s) a[k & 1][u][s] = __builtin_amdgcn_exp2f(dtv * A[s]);
             }
-            acc = sum_channel<LPC>(acc);
-            if (LPC == 1 || w.lane == t % LPC) y[t / LPC] = acc;
-        }
-        if (w.in) {
+        };
+        ahead(0);
 #pragma unroll
-            for (int i = 0; i < S::TPL; ++i) {
-                const int t = tile * TT + i * LPC + w.lane;
-                float v = p.skip ? fmaf(skip, x[i], y[i]) : y[i];         // (absent: not 0 times an infinite x)
-                if (p.z.data) v *= siluf(z[i]);
-                if (t < p.L) store_el(p.y.data, p.type, w.b * p.y.s0 + t * p.y.s1 + w.d, t < w.n ? v : 0.0f);
+        for (int k = 0; k < TT / 4; ++k) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (k + 1 < TT / 4) ahead(k + 1);
+            float acc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = 4 * k + u;
+                const float dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
+                acc[u] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) {
+                    h[s] = fmaf(a[k & 1][u][s], h[s], dxv * Bv[k & 1][u][s]);
+                    if (PAD && !ok[s]) h[s] = 0.0f;            // (an infinite input: 0 times it)
+                    acc[u] = fmaf(h[s], Cv[k & 1][u][s], acc[u]);
+                }
             }
+            sum_to_tokens<LPC>(acc, y + 4 * k / S::LQ);
         }
+#pragma unroll
+        for (int i = 0; i < S::TPL; ++i) {
+            if (p.skip) y[i] = fmaf(skip, x[i], y[i]);          // (absent: not 0 times an infinite x)
+            if (p.z.data) y[i] *= siluf(z[i]);
+            out[i] = ALL || tile * TT + i * S::LQ + w.tok < w.n ? y[i] : 0.0f;
+        }
+    };
+    if (w.tile0 < w.tend) {
+        fetch(w.tile0, std::false_type{});
+        const int whole = min(w.tend, w.n / TT);                // tiles before this one are whole
+        int tile = w.tile0;
+        for (; tile + 1 < whole; ++tile) run(tile, std::true_type{});
+        for (; tile < w.tend; ++tile) run(tile, std::false_type{});
+        store_walk<T, false>(yw, w.tend - 1, S::LQ, w.tok, p.L, out);
     }
-    if (!w.in) return;
     for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; t < min((int64_t)w.tile1 * TT, p.L); t += LPC)
-        store_el(p.y.data, p.type, w.b * p.y.s0 + t * p.y.s1 + w.d, 0.0f);
+        static_cast<T *>(p.y.data)[w.b * p.y.s0 + t * p.y.s1 + w.d] = (T)0.0f;
     if (p.h_last && w.chunk == p.chunks - 1) {
 #pragma unroll
         for (int s = 0; s < SPL; ++s)
@@ -100,7 +129,9 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
     }
 }
 
-template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_token(ScanParams p)
+template <typename T> __device__ __forceinline__ float load_el(const void *base, int64_t at) { return (float)static_cast<const T *>(base)[at]; }
+
+template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_token(ScanParams p)
 {
     const int64_t id = (int64_t)blockIdx.x * NT + threadIdx.x, row = id / LPC;
     const int lane = (int)id & (LPC - 1), n0 = lane * SPL;
@@ -108,47 +139,63 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
     const int64_t b = in ? row / p.D : 0;
     const int d = in ? (int)(row - b * p.D) : 0, g = d / p.Dg;
     const int64_t hat = (b * p.D + d) * p.N + n0;
-    const float v = load_el(p.dt.data, p.type, b * p.dt.s0 + d) + (p.dt_bias ? p.dt_bias[d] : 0.0f);
-    const float x = load_el(p.x.data, p.type, b * p.x.s0 + d), z = p.z.data ? load_el(p.z.data, p.type, b * p.z.s0 + d) : 0.0f;
+    const float v = load_el<T>(p.dt.data, b * p.dt.s0 + d) + (p.dt_bias ? p.dt_bias[d] : 0.0f);
+    const float x = load_el<T>(p.x.data, b * p.x.s0 + d), z = p.z.data ? load_el<T>(p.z.data, b * p.z.s0 + d) : 0.0f;
     const float dt = p.softplus ? softplusf(v) : v, dx = dt * x;
     float acc = 0.0f;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
         if (!in || (PAD && n0 + s >= p.N)) continue;
         const float a = __builtin_amdgcn_exp2f(dt * p.A[(int64_t)d * p.N + n0 + s] * LOG2E);
-        const float h = fmaf(a, p.h0[hat + s], dx * load_el(p.Bm.data, p.type, b * p.Bm.s0 + (int64_t)g * p.N + n0 + s));
+        const float h = fmaf(a, p.h0[hat + s], dx * load_el<T>(p.Bm.data, b * p.Bm.s0 + (int64_t)g * p.N + n0 + s));
         p.h_last[hat + s] = h;
-        acc = fmaf(h, load_el(p.Cm.data, p.type, b * p.Cm.s0 + (int64_t)g * p.N + n0 + s), acc);
+        acc = fmaf(h, load_el<T>(p.Cm.data, b * p.Cm.s0 + (int64_t)g * p.N + n0 + s), acc);
     }
     acc = sum_channel<LPC>(acc);
     if (!in || lane != 0) return;
     float y = p.skip ? fmaf(p.skip[d], x, acc) : acc;
     if (p.z.data) y *= siluf(z);
-    store_el(p.y.data, p.type, b * p.y.s0 + d, y);
+    static_cast<T *>(p.y.data)[b * p.y.s0 + d] = (T)y;
 }
 
-struct Forward {
+template <typename T> struct Forward {
     const ScanParams &p;
     hipStream_t s;
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
-        merit_scan_tiles<SPL, LPC, PAD><<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, 0, s>>>(p);
+        const unsigned grid = (unsigned)(p.B * p.chunks * p.G * p.ctiles);
+        if (p.states) merit_scan_tiles<T, SPL, LPC, PAD, true><<<grid, NT, 0, s>>>(p);
+        else merit_scan_tiles<T, SPL, LPC, PAD, false><<<grid, NT, 0, s>>>(p);
         return hipGetLastError();
     }
 };
-struct Token {
+template <typename T> struct Token {
     const ScanParams &p;
     hipStream_t s;
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
-        merit_scan_token<SPL, LPC, PAD><<<(unsigned)((p.B * p.D * LPC + NT - 1) / NT), NT, 0, s>>>(p);
+        merit_scan_token<T, SPL, LPC, PAD><<<(unsigned)((p.B * p.D * LPC + NT - 1) / NT), NT, 0, s>>>(p);
         return hipGetLastError();
     }
 };
 
 }  // namespace
 
-hipError_t launch_scan(const ScanParams &p, hipStream_t s) { return by_states(p.N, Forward{p, s}); }
-hipError_t launch_scan_step(const ScanParams &p, hipStream_t s) { return by_states(p.N, Token{p, s}); }
+hipError_t launch_scan(const ScanParams &p, hipStream_t s)
+{
+    if (p.type == MERIT_BF16) return by_states(p.N, Forward<bf16_t>{p, s});
+    return p.type == MERIT_F16 ? by_states(p.N, Forward<f16_t>{p, s}) : by_states(p.N, Forward<float>{p, s});
+}
+hipError_t launch_scan_step(const ScanParams &p, hipStream_t s)
+{
+    if (p.type == MERIT_BF16) return by_states(p.N, Token<bf16_t>{p, s});
+    return p.type == MERIT_F16 ? by_states(p.N, Token<f16_t>{p, s}) : by_states(p.N, Token<float>{p, s});
+}
+// (defined in the sources of their types)
+hipError_t launch_scan_backward(const ScanParams &p, hipStream_t s)
+{
+    if (p.type == MERIT_BF16) return scan_backward_of<bf16_t>(p, s);
+    return p.type == MERIT_F16 ? scan_backward_of<f16_t>(p, s) : scan_backward_of<float>(p, s);
+}
 
 }  // namespace merit

@@ -8,6 +8,7 @@
 // channels, which are lanes: the 16 tokens' values of a state are added across lanes so that every halving of the lanes
 // halves the values too (15 exchanges for 16 sums of 16 lanes), then wavefronts through LDS, then workgroups through
 // memory in a second launch, in a fixed order.
+#pragma once
 #include "scan.h"
 
 namespace merit {
@@ -70,7 +71,7 @@ template <int LPC> struct Sums {
     static __device__ __forceinline__ bool writes() { return LPC >= 4 || (threadIdx.x & (3 & ~(LPC - 1))) == 0; }
 };
 
-template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_back(ScanParams p)
+template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_back(ScanParams p)
 {
     using S = Shape<SPL, LPC>;
     using Q = Sums<LPC>;
@@ -91,54 +92,78 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
     const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
     float dskip = 0.0f, dbias = 0.0f;
     // behind the sequence's end every gradient is 0
-    for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; w.in && t < min((int64_t)w.tile1 * TT, p.L); t += LPC) {
-        store_el(p.dx.data, p.type, w.b * p.dx.s0 + t * p.dx.s1 + w.d, 0.0f);
-        store_el(p.ddt.data, p.type, w.b * p.ddt.s0 + t * p.ddt.s1 + w.d, 0.0f);
-        if (p.z.data) store_el(p.dz.data, p.type, w.b * p.dz.s0 + t * p.dz.s1 + w.d, 0.0f);
+    for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; t < min((int64_t)w.tile1 * TT, p.L); t += LPC) {
+        static_cast<T *>(p.dx.data)[w.b * p.dx.s0 + t * p.dx.s1 + w.d] = (T)0.0f;
+        static_cast<T *>(p.ddt.data)[w.b * p.ddt.s0 + t * p.ddt.s1 + w.d] = (T)0.0f;
+        if (p.z.data) static_cast<T *>(p.dz.data)[w.b * p.dz.s0 + t * p.dz.s1 + w.d] = (T)0.0f;
     }
     float *bc = p.part_bc + ((int64_t)(w.g * p.ctiles + w.ct) * p.B + w.b) * p.L * 2 * p.N;
     for (int64_t e = (int64_t)max(w.tend, w.tile0) * TT * 2 * p.N + threadIdx.x; e < min((int64_t)w.tile1 * TT, p.L) * 2 * p.N; e += NT) bc[e] = 0.0f;
 
-    uint32_t xr[S::TPL], dr[S::TPL], yr[S::TPL], zr[S::TPL] = {}, br[S::EB], cr[S::EB];
+    const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), yw = walk_rows<T>(p.dy, w),
+               zw = p.z.data ? walk_rows<T>(p.z, w) : xw, bw = walk_states<T, S::NP>(p.Bm, p, w),
+               cw = walk_states<T, S::NP>(p.Cm, p, w), dxw = walk_rows<T>(p.dx, w), ddw = walk_rows<T>(p.ddt, w),
+               dzw = walk_rows<T>(p.dz, w);
+    raw_t<T> xr[S::TPL], dr[S::TPL], yr[S::TPL], zr[S::TPL], br[S::EB], cr[S::EB];
     float hr[SPL];
-    auto fetch = [&](int tile) {
-        load_rows<SPL, LPC>(p.x, p.type, w, tile, xr);
-        load_rows<SPL, LPC>(p.dt, p.type, w, tile, dr);
-        load_rows<SPL, LPC>(p.dy, p.type, w, tile, yr);
-        if (p.z.data) load_rows<SPL, LPC>(p.z, p.type, w, tile, zr);
-        load_states<SPL, LPC>(p.Bm, p, w, tile, br);
-        load_states<SPL, LPC>(p.Cm, p, w, tile, cr);
+    auto fetch = [&](int tile, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        load_walk<T, WHOLE>(xw, tile, S::LQ, w.tok, w.n - 1, xr);
+        load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, dr);
+        load_walk<T, WHOLE>(yw, tile, S::LQ, w.tok, w.n - 1, yr);
+        load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, zr);
+        const int first = ((int)threadIdx.x & (TT * S::NP - 1)) / S::NP;
+        load_walk<T, WHOLE>(bw, tile, NT / S::NP, first, w.n - 1, br);
+        load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, cr);
         const float *kept = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N;
 #pragma unroll
         for (int s = 0; s < SPL; ++s) hr[s] = kept[PAD ? min(n0 + s, p.N - 1) : n0 + s];
     };
-    if (w.tile0 < w.tend) fetch(w.tend - 1);
-    for (int tile = w.tend - 1; tile >= w.tile0; --tile) {
+    // what a tile has computed: written while the next one is under way
+    float ox[S::TPL], od[S::TPL], oz[S::TPL];
+    auto write = [&](int tile) {
+        // (lanes of a channel that is not there computed with zeros: they must not write over the one they stand for)
+        if (w.in) {
+            store_walk<T, false>(dxw, tile, S::LQ, w.tok, p.L, ox);
+            store_walk<T, false>(ddw, tile, S::LQ, w.tok, p.L, od);
+            if (p.z.data) store_walk<T, false>(dzw, tile, S::LQ, w.tok, p.L, oz);
+        }
+#pragma unroll
+        for (int i = 0; i < (TT * 2 * S::NP + NT - 1) / NT; ++i) {
+            const int e = i * NT + (int)threadIdx.x, n = e % S::NP, k = e / S::NP;      // k = 2 t + (0: dB, 1: dC)
+            const int64_t t = (int64_t)tile * TT + k / 2;
+            if (e < TT * 2 * S::NP && n < p.N && t < p.L)
+                bc[(t * 2 + (k & 1)) * p.N + n] = t < w.n ? (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]) : 0.0f;
+        }
+    };
+    auto run = [&](int tile, auto all) {
+        constexpr bool ALL = decltype(all)::value;
         float x[S::TPL], raw[S::TPL], z[S::TPL], dy[S::TPL], dyo[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL], in_[S::TPL], da_[S::TPL];
-        values(xr, p.type, x);
-        values(dr, p.type, raw);
-        values(yr, p.type, dyo);
-        values(zr, p.type, z);
-        lds_barrier();              // (the tile before is done with bl and cl)
-        stage_states<SPL, LPC>(bl, p, w, tile, br);
-        stage_states<SPL, LPC>(cl, p, w, tile, cr);
+        values<T>(xr, x);
+        values<T>(dr, raw);
+        values<T>(yr, dyo);
+        values<T>(zr, z);
+        lds_barrier();              // (the tile before is done with bl and cl, and red is whole)
+        if (tile + 1 < w.tend) write(tile + 1);
+        stage_states<T, SPL, LPC>(bl, p, w, tile, br);
+        stage_states<T, SPL, LPC>(cl, p, w, tile, cr);
         float hs[SPL], h[TT][SPL], a[TT][SPL];
 #pragma unroll
         for (int s = 0; s < SPL; ++s) hs[s] = ok[s] ? hr[s] : 0.0f;
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
-            const bool in = w.in && tile * TT + i * LPC + w.lane < w.n;
+            const bool in = w.in && (ALL || tile * TT + i * S::LQ + w.tok < w.n);
             raw[i] += bias;
             dt[i] = in ? (p.softplus ? softplusf(raw[i]) : raw[i]) : 0.0f;
             dx[i] = in ? dt[i] * x[i] : 0.0f;
             dy[i] = in ? (p.z.data ? dyo[i] * siluf(z[i]) : dyo[i]) : 0.0f;
             y[i] = in_[i] = da_[i] = 0.0f;
         }
-        fetch(max(tile - 1, w.tile0));
+        fetch(max(tile - 1, w.tile0), all);
         lds_barrier();
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            const float dtv = from_lane<LPC>(dt[t / LPC], t % LPC), dxv = from_lane<LPC>(dx[t / LPC], t % LPC);
+            const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
             float Bv[SPL], Cv[SPL], acc = 0.0f;
             read_states<SPL>(bl + t * S::NP + n0, Bv);
             read_states<SPL>(cl + t * S::NP + n0, Cv);
@@ -151,13 +176,13 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
             }
             if (p.z.data) {
                 acc = sum_channel<LPC>(acc);
-                if (LPC == 1 || w.lane == t % LPC) y[t / LPC] = acc;
+                if (LPC == 1 || w.tok == t % S::LQ) y[t / S::LQ] = acc;
             }
         }
 #pragma unroll
         for (int t = TT - 1; t >= 0; --t) {
-            const float dtv = from_lane<LPC>(dt[t / LPC], t % LPC), dxv = from_lane<LPC>(dx[t / LPC], t % LPC);
-            const float dyv = from_lane<LPC>(dy[t / LPC], t % LPC);
+            const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
+            const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
             float Bv[SPL], Cv[SPL], u = 0.0f, v = 0.0f;
             read_states<SPL>(bl + t * S::NP + n0, Bv);
             read_states<SPL>(cl + t * S::NP + n0, Cv);
@@ -175,25 +200,21 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
             }
             u = sum_channel<LPC>(u);
             v = sum_channel<LPC>(v);
-            if (LPC == 1 || w.lane == t % LPC) in_[t / LPC] = u, da_[t / LPC] = v;
+            if (LPC == 1 || w.tok == t % S::LQ) in_[t / S::LQ] = u, da_[t / S::LQ] = v;
         }
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
-            const int t = tile * TT + i * LPC + w.lane;
-            const bool in = w.in && t < w.n;
+            const bool in = ALL || tile * TT + i * S::LQ + w.tok < w.n;
             float ds = fmaf(in_[i], x[i], da_[i]);
             if (p.softplus) ds *= sigmoidf(raw[i]);
+            const float y0 = p.skip ? fmaf(skip, x[i], y[i]) : y[i];
             if (in) {
                 dskip = fmaf(dy[i], x[i], dskip);
                 dbias += ds;
             }
-            if (w.in && t < p.L) {
-                store_el(p.dx.data, p.type, w.b * p.dx.s0 + t * p.dx.s1 + w.d, in ? (p.skip ? fmaf(in_[i], dt[i], skip * dy[i]) : in_[i] * dt[i]) : 0.0f);
-                store_el(p.ddt.data, p.type, w.b * p.ddt.s0 + t * p.ddt.s1 + w.d, in ? ds : 0.0f);
-                if (p.z.data)
-                    store_el(p.dz.data, p.type, w.b * p.dz.s0 + t * p.dz.s1 + w.d,
-                             in ? dyo[i] * (p.skip ? fmaf(skip, x[i], y[i]) : y[i]) * act_slope(z[i], MERIT_ACT_SILU) : 0.0f);
-            }
+            ox[i] = in ? (p.skip ? fmaf(in_[i], dt[i], skip * dy[i]) : in_[i] * dt[i]) : 0.0f;
+            od[i] = in ? ds : 0.0f;
+            oz[i] = in ? dyo[i] * y0 * act_slope(z[i], MERIT_ACT_SILU) : 0.0f;
         }
 #pragma unroll
         for (int s = 0; s < SPL; ++s) {
@@ -211,13 +232,14 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
                 }
             }
         }
+    };
+    if (w.tile0 < w.tend) {
+        fetch(w.tend - 1, std::false_type{});
+        const int whole = min(w.tend, w.n / TT);
+        if (whole < w.tend) run(w.tend - 1, std::false_type{});
+        for (int tile = whole - 1; tile >= w.tile0; --tile) run(tile, std::true_type{});
         lds_barrier();
-        for (int e = threadIdx.x; e < TT * 2 * S::NP; e += NT) {
-            const int n = e % S::NP, k = e / S::NP;         // k = 2 t + (0: dB, 1: dC)
-            const int64_t t = tile * TT + k / 2;
-            const float v = (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]);
-            if (n < p.N && t < p.L) bc[(t * 2 + (k & 1)) * p.N + n] = t < w.n ? v : 0.0f;
-        }
+        write(w.tile0);
     }
     if (p.dh0 && w.chunk == 0) {
 #pragma unroll
@@ -228,8 +250,8 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
 #pragma unroll
     for (int s = 0; s < SPL; ++s)
         if (ok[s]) part[(int64_t)w.d * p.N + n0 + s] = dA[s];
-    dskip = sum_channel<LPC>(dskip);
-    dbias = sum_channel<LPC>(dbias);
+    dskip = sum_channel<S::LQ>(dskip);          // (a channel's further quads have the same tokens)
+    dbias = sum_channel<S::LQ>(dbias);
     if (w.in && w.lane == 0) {
         part[(int64_t)p.D * p.N + w.d] = dskip;
         part[(int64_t)p.D * p.N + p.D + w.d] = dbias;
@@ -237,7 +259,7 @@ template <int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void meri
 }
 
 // dB, dC: the sums over a group's channel tiles, rounded once
-__global__ __launch_bounds__(NT) void merit_scan_sum_bc(ScanParams p)
+template <typename T> __global__ __launch_bounds__(NT) void merit_scan_sum_bc(ScanParams p)
 {
     const int64_t id = (int64_t)blockIdx.x * NT + threadIdx.x, per = (int64_t)p.B * p.L * 2 * p.N;
     const int g = (int)(id / per);
@@ -249,28 +271,28 @@ __global__ __launch_bounds__(NT) void merit_scan_sum_bc(ScanParams p)
 #pragma unroll 8
     for (int i = 0; i < p.ctiles; ++i) s += in[i * per];
     const Rows &o = k < p.N ? p.dB : p.dC;
-    store_el(o.data, p.type, b * o.s0 + t * o.s1 + (int64_t)g * p.N + n, s);
+    static_cast<T *>(o.data)[b * o.s0 + t * o.s1 + (int64_t)g * p.N + n] = (T)s;
 }
 
-struct Backward {
+template <typename T> struct Backward {
     const ScanParams &p;
     hipStream_t s;
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
-        merit_scan_back<SPL, LPC, PAD><<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, 0, s>>>(p);
+        merit_scan_back<T, SPL, LPC, PAD><<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, 0, s>>>(p);
         return hipGetLastError();
     }
 };
 
 }  // namespace
 
-hipError_t launch_scan_backward(const ScanParams &p, hipStream_t s)
+template <typename T> hipError_t scan_backward_of(const ScanParams &p, hipStream_t s)
 {
     if (p.B > 0) {
-        const hipError_t e = by_states(p.N, Backward{p, s});
+        const hipError_t e = by_states(p.N, Backward<T>{p, s});
         if (e != hipSuccess) return e;
         const int64_t count = (int64_t)p.G * p.B * p.L * 2 * p.N;
-        if (count) merit_scan_sum_bc<<<(unsigned)((count + NT - 1) / NT), NT, 0, s>>>(p);
+        if (count) merit_scan_sum_bc<T><<<(unsigned)((count + NT - 1) / NT), NT, 0, s>>>(p);
     }
     ReduceParams r = {};
     r.in = p.part_a;
