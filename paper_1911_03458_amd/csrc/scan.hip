@@ -35,27 +35,30 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
     const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), zw = p.z.data ? walk_rows<T>(p.z, w) : xw,
                yw = walk_rows<T>(p.y, w), bw = walk_states<T, S::NP>(p.Bm, p, w), cw = walk_states<T, S::NP>(p.Cm, p, w);
 
-    raw_t<T> xr[S::TPL], dr[S::TPL], zr[S::TPL], br[S::EB], cr[S::EB];
-    auto fetch = [&](int tile, auto whole) {
+    // Two tiles in flight: a tile's arithmetic is over before a load of it comes back
+    struct Raw {
+        raw_t<T> x[S::TPL], dt[S::TPL], z[S::TPL], b[S::EB], c[S::EB];
+    };
+    Raw even, odd;
+    auto fetch = [&](Raw &r, int tile, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
-        load_walk<T, WHOLE>(xw, tile, S::LQ, w.tok, w.n - 1, xr);
-        load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, dr);
-        load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, zr);
+        load_walk<T, WHOLE>(xw, tile, S::LQ, w.tok, w.n - 1, r.x);
+        load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, r.dt);
+        load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, r.z);
         const int first = ((int)threadIdx.x & (TT * S::NP - 1)) / S::NP;
-        load_walk<T, WHOLE>(bw, tile, NT / S::NP, first, w.n - 1, br);
-        load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, cr);
+        load_walk<T, WHOLE>(bw, tile, NT / S::NP, first, w.n - 1, r.b);
+        load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, r.c);
     };
     float out[S::TPL];                          // results of the tile before
-    // all: this tile and the next one are whole
-    auto run = [&](int tile, auto all) {
+    // all: this tile and the one after the next are whole
+    auto run = [&](Raw &r, float *bt, float *ct, int tile, auto all) {
         constexpr bool ALL = decltype(all)::value;
-        float *bt = bl[tile & 1], *ct = cl[tile & 1];
-        stage_states<T, SPL, LPC>(bt, p, w, tile, br);
-        stage_states<T, SPL, LPC>(ct, p, w, tile, cr);
+        stage_states<T, SPL, LPC>(bt, p, w, tile, r.b);
+        stage_states<T, SPL, LPC>(ct, p, w, tile, r.c);
         float x[S::TPL], z[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL];
-        values<T>(xr, x);
-        values<T>(zr, z);
-        values<T>(dr, dt);
+        values<T>(r.x, x);
+        values<T>(r.z, z);
+        values<T>(r.dt, dt);
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
             const bool in = ALL || tile * TT + i * S::LQ + w.tok < w.n;
@@ -70,7 +73,7 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
             for (int s = 0; s < SPL; ++s)
                 if (!PAD || ok[s]) o[s] = h[s];
         }
-        fetch(ALL ? tile + 1 : min(tile + 1, w.tend - 1), all);
+        fetch(r, ALL ? tile + 2 : min(tile + 2, w.tend - 1), all);
         lds_barrier();
         // Four tokens at a time; what needs LDS or an exponential is asked for four tokens ahead
         float Bv[2][4][SPL], Cv[2][4][SPL], a[2][4][SPL];
@@ -113,11 +116,18 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
         }
     };
     if (w.tile0 < w.tend) {
-        fetch(w.tile0, std::false_type{});
+        fetch(even, w.tile0, std::false_type{});
+        fetch(odd, min(w.tile0 + 1, w.tend - 1), std::false_type{});
         const int whole = min(w.tend, w.n / TT);                // tiles before this one are whole
         int tile = w.tile0;
-        for (; tile + 1 < whole; ++tile) run(tile, std::true_type{});
-        for (; tile < w.tend; ++tile) run(tile, std::false_type{});
+        for (; tile + 3 < whole; tile += 2) {
+            run(even, bl[0], cl[0], tile, std::true_type{});
+            run(odd, bl[1], cl[1], tile + 1, std::true_type{});
+        }
+        for (; tile < w.tend; tile += 2) {
+            run(even, bl[0], cl[0], tile, std::false_type{});
+            if (tile + 1 < w.tend) run(odd, bl[1], cl[1], tile + 1, std::false_type{});
+        }
         store_walk<T, false>(yw, w.tend - 1, S::LQ, w.tok, p.L, out);
     }
     for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; t < min((int64_t)w.tile1 * TT, p.L); t += LPC)
