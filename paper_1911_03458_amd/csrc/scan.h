@@ -31,7 +31,8 @@ struct Where {
     int tile0, tile1;      // tiles of the chunk
     int tend;              // the first of them that has no token of the sequence
 };
-template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, int chunks)
+// The workgroup's part: `chunks` chunks of every sequence, from `first` on
+template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, int first, int chunks)
 {
     Where w;
     uint32_t r = blockIdx.x;
@@ -39,7 +40,7 @@ template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, i
     r /= (uint32_t)p.ctiles;
     w.g = (int)(r % (uint32_t)p.G);
     r /= (uint32_t)p.G;
-    w.chunk = (int)(r % (uint32_t)chunks);
+    w.chunk = first + (int)(r % (uint32_t)chunks);
     w.b = r / (uint32_t)chunks;
     const int cl = w.ct * (NT / LPC) + (int)threadIdx.x / LPC;
     w.lane = (int)threadIdx.x & (LPC - 1);
@@ -196,6 +197,31 @@ template <int SPL> __device__ __forceinline__ void read_states(const float *at, 
     } else {
 #pragma unroll
         for (int s = 0; s < SPL; ++s) v[s] = at[s];
+    }
+}
+
+// A state (or its adjoint) through `count` chunks from `q` on: their decay, then what they add.  Four chunks' loads go out
+// together.
+template <int SPL>
+__device__ __forceinline__ void through_chunks(const ScanParams &p, const Where &w, int n0, const float (&A2)[SPL], const bool (&ok)[SPL],
+                                               float (&h)[SPL], int q, int count, int dir)
+{
+    constexpr int AT_ONCE = 4;
+    for (; count > 0; count -= AT_ONCE, q += dir * AT_ONCE) {
+        float sum[AT_ONCE], add[AT_ONCE][SPL];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int64_t at = (w.b * p.chunks + q + dir * min(k, count - 1)) * p.D + w.d;
+            sum[k] = p.chunk_dt[at];
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) add[k][s] = p.chunk_h[at * p.N + min(n0 + s, p.N - 1)];
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (k < count)
+#pragma unroll
+                for (int s = 0; s < SPL; ++s)
+                    if (ok[s]) h[s] = fmaf(__builtin_amdgcn_exp2f(sum[k] * A2[s]), h[s], add[k][s]);
     }
 }
 

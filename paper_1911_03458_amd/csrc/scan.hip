@@ -16,11 +16,16 @@ using namespace scan;
 
 namespace {
 
-template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch_bounds__(NT) void merit_scan_tiles(ScanParams p)
+// WHAT a launch leaves: the results; the results and the states before every tile; of every chunk but the last the state
+// that it adds (from a state of 0) and the sum of its steps, from which the next launch's chunks find their first states
+enum { RESULTS, KEEP_STATES, CHUNK_STATES };
+
+template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_bounds__(NT) void merit_scan_tiles(ScanParams p)
 {
     using S = Shape<SPL, LPC>;
-    __shared__ __align__(16) float bl[2][TT * S::NP], cl[2][TT * S::NP];
-    const Where w = where<LPC>(p, p.chunks);
+    constexpr bool KEEP = WHAT == KEEP_STATES, SUMS = WHAT == CHUNK_STATES;
+    __shared__ __align__(16) float bl[2][TT * S::NP], cl[SUMS ? 1 : 2][SUMS ? 4 : TT * S::NP];
+    const Where w = where<LPC>(p, 0, SUMS ? p.chunks - 1 : p.chunks);
     const int n0 = w.lane * SPL;
     float A[SPL], h[SPL];
     bool ok[SPL];
@@ -29,8 +34,10 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
     for (int s = 0; s < SPL; ++s) {
         ok[s] = !PAD || n0 + s < p.N;
         A[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] * LOG2E : 0.0f;
-        h[s] = ok[s] && p.h0 ? p.h0[hat + s] : 0.0f;
+        h[s] = !SUMS && ok[s] && p.h0 ? p.h0[hat + s] : 0.0f;
     }
+    float steps = 0.0f;
+    if (!SUMS) through_chunks<SPL>(p, w, n0, A, ok, h, 0, w.chunk, 1);
     const float bias = p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = p.skip ? p.skip[w.d] : 0.0f;
     const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), zw = p.z.data ? walk_rows<T>(p.z, w) : xw,
                yw = walk_rows<T>(p.y, w), bw = walk_states<T, S::NP>(p.Bm, p, w), cw = walk_states<T, S::NP>(p.Cm, p, w);
@@ -44,20 +51,20 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
         constexpr bool WHOLE = decltype(whole)::value;
         load_walk<T, WHOLE>(xw, tile, S::LQ, w.tok, w.n - 1, r.x);
         load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, r.dt);
-        load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, r.z);
+        if (!SUMS) load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, r.z);
         const int first = ((int)threadIdx.x & (TT * S::NP - 1)) / S::NP;
         load_walk<T, WHOLE>(bw, tile, NT / S::NP, first, w.n - 1, r.b);
-        load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, r.c);
+        if (!SUMS) load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, r.c);
     };
     float out[S::TPL];                          // results of the tile before
     // all: this tile and the one after the next are whole
     auto run = [&](Raw &r, float *bt, float *ct, int tile, auto all) {
         constexpr bool ALL = decltype(all)::value;
         stage_states<T, SPL, LPC>(bt, p, w, tile, r.b);
-        stage_states<T, SPL, LPC>(ct, p, w, tile, r.c);
+        if constexpr (!SUMS) stage_states<T, SPL, LPC>(ct, p, w, tile, r.c);
         float x[S::TPL], z[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL];
         values<T>(r.x, x);
-        values<T>(r.z, z);
+        if constexpr (!SUMS) values<T>(r.z, z);
         values<T>(r.dt, dt);
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
@@ -65,8 +72,9 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
             const float v = dt[i] + bias;
             dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
             dx[i] = in ? dt[i] * x[i] : 0.0f;
+            steps += dt[i];
         }
-        if (tile > w.tile0) store_walk<T, true>(yw, tile - 1, S::LQ, w.tok, p.L, out);
+        if (!SUMS && tile > w.tile0) store_walk<T, true>(yw, tile - 1, S::LQ, w.tok, p.L, out);
         if (KEEP) {
             float *o = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N + n0;
 #pragma unroll
@@ -82,7 +90,7 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
             for (int u = 0; u < 4; ++u) {
                 const int t = 4 * k + u;
                 read_states<SPL>(bt + t * S::NP + n0, Bv[k & 1][u]);
-                read_states<SPL>(ct + t * S::NP + n0, Cv[k & 1][u]);
+                if (!SUMS) read_states<SPL>(ct + t * S::NP + n0, Cv[k & 1][u]);
                 const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ);
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) a[k & 1][u][s] = __builtin_amdgcn_exp2f(dtv * A[s]);
@@ -103,11 +111,12 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
                 for (int s = 0; s < SPL; ++s) {
                     h[s] = fmaf(a[k & 1][u][s], h[s], dxv * Bv[k & 1][u][s]);
                     if (PAD && !ok[s]) h[s] = 0.0f;            // (an infinite input: 0 times it)
-                    acc[u] = fmaf(h[s], Cv[k & 1][u][s], acc[u]);
+                    if (!SUMS) acc[u] = fmaf(h[s], Cv[k & 1][u][s], acc[u]);
                 }
             }
-            sum_to_tokens<LPC>(acc, y + 4 * k / S::LQ);
+            if (!SUMS) sum_to_tokens<LPC>(acc, y + 4 * k / S::LQ);
         }
+        if (SUMS) return;
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
             if (p.skip) y[i] = fmaf(skip, x[i], y[i]);          // (absent: not 0 times an infinite x)
@@ -122,13 +131,22 @@ template <typename T, int SPL, int LPC, bool PAD, bool KEEP> __global__ __launch
         int tile = w.tile0;
         for (; tile + 3 < whole; tile += 2) {
             run(even, bl[0], cl[0], tile, std::true_type{});
-            run(odd, bl[1], cl[1], tile + 1, std::true_type{});
+            run(odd, bl[1], cl[SUMS ? 0 : 1], tile + 1, std::true_type{});
         }
         for (; tile < w.tend; tile += 2) {
             run(even, bl[0], cl[0], tile, std::false_type{});
-            if (tile + 1 < w.tend) run(odd, bl[1], cl[1], tile + 1, std::false_type{});
+            if (tile + 1 < w.tend) run(odd, bl[1], cl[SUMS ? 0 : 1], tile + 1, std::false_type{});
         }
-        store_walk<T, false>(yw, w.tend - 1, S::LQ, w.tok, p.L, out);
+        if (!SUMS) store_walk<T, false>(yw, w.tend - 1, S::LQ, w.tok, p.L, out);
+    }
+    if (SUMS) {
+        const int64_t at = (w.b * p.chunks + w.chunk) * p.D + w.d;
+        steps = sum_channel<S::LQ>(steps);      // (a channel's further quads have the same tokens)
+        if (w.lane == 0) p.chunk_dt[at] = steps;
+#pragma unroll
+        for (int s = 0; s < SPL; ++s)
+            if (ok[s]) p.chunk_h[at * p.N + n0 + s] = h[s];
+        return;
     }
     for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; t < min((int64_t)w.tile1 * TT, p.L); t += LPC)
         static_cast<T *>(p.y.data)[w.b * p.y.s0 + t * p.y.s1 + w.d] = (T)0.0f;
@@ -173,9 +191,10 @@ template <typename T> struct Forward {
     hipStream_t s;
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
-        const unsigned grid = (unsigned)(p.B * p.chunks * p.G * p.ctiles);
-        if (p.states) merit_scan_tiles<T, SPL, LPC, PAD, true><<<grid, NT, 0, s>>>(p);
-        else merit_scan_tiles<T, SPL, LPC, PAD, false><<<grid, NT, 0, s>>>(p);
+        const unsigned per = (unsigned)(p.B * p.G * p.ctiles);
+        if (p.chunks > 1) merit_scan_tiles<T, SPL, LPC, PAD, CHUNK_STATES><<<per * (p.chunks - 1), NT, 0, s>>>(p);
+        if (p.states) merit_scan_tiles<T, SPL, LPC, PAD, KEEP_STATES><<<per * p.chunks, NT, 0, s>>>(p);
+        else merit_scan_tiles<T, SPL, LPC, PAD, RESULTS><<<per * p.chunks, NT, 0, s>>>(p);
         return hipGetLastError();
     }
 };

@@ -77,7 +77,7 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
     using Q = Sums<LPC>;
     __shared__ __align__(16) float bl[TT * S::NP], cl[TT * S::NP];
     __shared__ __align__(16) float red[NT / 64][TT * 2 * S::NP];
-    const Where w = where<LPC>(p, p.chunks);
+    const Where w = where<LPC>(p, 0, p.chunks);
     const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
     float A[SPL], dA[SPL], carry[SPL];
     bool ok[SPL];
@@ -89,6 +89,10 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
         dA[s] = 0.0f;
         carry[s] = ok[s] && p.dh_last ? p.dh_last[hat + s] : 0.0f;     // a_{t+1} l_{t+1}
     }
+    float A2[SPL];
+#pragma unroll
+    for (int s = 0; s < SPL; ++s) A2[s] = A[s] * LOG2E;
+    through_chunks<SPL>(p, w, n0, A2, ok, carry, p.chunks - 1, p.chunks - 1 - w.chunk, -1);
     const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
     float dskip = 0.0f, dbias = 0.0f;
     // behind the sequence's end every gradient is 0
@@ -157,50 +161,66 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
             dt[i] = in ? (p.softplus ? softplusf(raw[i]) : raw[i]) : 0.0f;
             dx[i] = in ? dt[i] * x[i] : 0.0f;
             dy[i] = in ? (p.z.data ? dyo[i] * siluf(z[i]) : dyo[i]) : 0.0f;
-            y[i] = in_[i] = da_[i] = 0.0f;
         }
         fetch(max(tile - 1, w.tile0), all);
         lds_barrier();
+        // the tile's states once more, four tokens at a time, what needs LDS asked for four tokens ahead
+        float Bv[2][4][SPL], Cv[2][4][SPL];
+        auto ahead = [&](int k) {
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
-            float Bv[SPL], Cv[SPL], acc = 0.0f;
-            read_states<SPL>(bl + t * S::NP + n0, Bv);
-            read_states<SPL>(cl + t * S::NP + n0, Cv);
+            for (int u = 0; u < 4; ++u) {
+                read_states<SPL>(bl + (4 * k + u) * S::NP + n0, Bv[k & 1][u]);
+                read_states<SPL>(cl + (4 * k + u) * S::NP + n0, Cv[k & 1][u]);
+            }
+        };
+        ahead(0);
 #pragma unroll
-            for (int s = 0; s < SPL; ++s) {
-                a[t][s] = __builtin_amdgcn_exp2f(dtv * (A[s] * LOG2E));
-                h[t][s] = fmaf(a[t][s], t ? h[t ? t - 1 : 0][s] : hs[s], dxv * Bv[s]);
-                if (PAD && !ok[s]) h[t][s] = 0.0f;
-                acc = fmaf(h[t][s], Cv[s], acc);
+        for (int k = 0; k < TT / 4; ++k) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (k + 1 < TT / 4) ahead(k + 1);
+            float acc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = 4 * k + u;
+                const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
+                acc[u] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) {
+                    a[t][s] = __builtin_amdgcn_exp2f(dtv * A2[s]);
+                    h[t][s] = fmaf(a[t][s], t ? h[t ? t - 1 : 0][s] : hs[s], dxv * Bv[k & 1][u][s]);
+                    if (PAD && !ok[s]) h[t][s] = 0.0f;
+                    acc[u] = fmaf(h[t][s], Cv[k & 1][u][s], acc[u]);
+                }
             }
-            if (p.z.data) {
-                acc = sum_channel<LPC>(acc);
-                if (LPC == 1 || w.tok == t % S::LQ) y[t / S::LQ] = acc;
-            }
+            sum_to_tokens<LPC>(acc, y + 4 * k / S::LQ);
         }
+        // (the last four tokens' B and C are the first of the way back)
 #pragma unroll
-        for (int t = TT - 1; t >= 0; --t) {
-            const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
-            const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
-            float Bv[SPL], Cv[SPL], u = 0.0f, v = 0.0f;
-            read_states<SPL>(bl + t * S::NP + n0, Bv);
-            read_states<SPL>(cl + t * S::NP + n0, Cv);
+        for (int k = TT / 4 - 1; k >= 0; --k) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (k) ahead(k - 1);
+            float u4[4], v4[4];
 #pragma unroll
-            for (int s = 0; s < SPL; ++s) {
-                float l = fmaf(Cv[s], dyv, carry[s]);
-                if (PAD && !ok[s]) l = 0.0f;
-                u = fmaf(l, Bv[s], u);
-                carry[s] = a[t][s] * l;
-                const float q = carry[s] * (t ? h[t ? t - 1 : 0][s] : hs[s]);
-                v = fmaf(q, A[s], v);
-                dA[s] = fmaf(q, dtv, dA[s]);
-                a[t][s] = l * dxv;                  // now dB's and dC's terms
-                h[t][s] *= dyv;
+            for (int u = 3; u >= 0; --u) {
+                const int t = 4 * k + u;
+                const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
+                const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
+                u4[u] = v4[u] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) {
+                    float l = fmaf(Cv[k & 1][u][s], dyv, carry[s]);
+                    if (PAD && !ok[s]) l = 0.0f;
+                    u4[u] = fmaf(l, Bv[k & 1][u][s], u4[u]);
+                    carry[s] = a[t][s] * l;
+                    const float q = carry[s] * (t ? h[t ? t - 1 : 0][s] : hs[s]);
+                    v4[u] = fmaf(q, A[s], v4[u]);
+                    dA[s] = fmaf(q, dtv, dA[s]);
+                    a[t][s] = l * dxv;                  // now dB's and dC's terms
+                    h[t][s] *= dyv;
+                }
             }
-            u = sum_channel<LPC>(u);
-            v = sum_channel<LPC>(v);
-            if (LPC == 1 || w.tok == t % S::LQ) in_[t / S::LQ] = u, da_[t / S::LQ] = v;
+            sum_to_tokens<LPC>(u4, in_ + 4 * k / S::LQ);
+            sum_to_tokens<LPC>(v4, da_ + 4 * k / S::LQ);
         }
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
@@ -258,6 +278,109 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
     }
 }
 
+// Of every chunk but the first: the adjoint of the state before it that its own tokens leave, and the sum of its steps
+template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_back_chunks(ScanParams p)
+{
+    using S = Shape<SPL, LPC>;
+    __shared__ __align__(16) float cl[2][TT * S::NP];
+    const Where w = where<LPC>(p, 1, p.chunks - 1);
+    const int n0 = w.lane * SPL;
+    float A[SPL], carry[SPL], steps = 0.0f;
+    bool ok[SPL];
+#pragma unroll
+    for (int s = 0; s < SPL; ++s) {
+        ok[s] = !PAD || n0 + s < p.N;
+        A[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] * LOG2E : 0.0f;
+        carry[s] = 0.0f;
+    }
+    const float bias = p.dt_bias ? p.dt_bias[w.d] : 0.0f;
+    const Walk dw = walk_rows<T>(p.dt, w), yw = walk_rows<T>(p.dy, w), zw = p.z.data ? walk_rows<T>(p.z, w) : yw,
+               cw = walk_states<T, S::NP>(p.Cm, p, w);
+    struct Raw {
+        raw_t<T> dt[S::TPL], dy[S::TPL], z[S::TPL], c[S::EB];
+    };
+    Raw even, odd;
+    auto fetch = [&](Raw &r, int tile, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, r.dt);
+        load_walk<T, WHOLE>(yw, tile, S::LQ, w.tok, w.n - 1, r.dy);
+        load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, r.z);
+        load_walk<T, WHOLE>(cw, tile, NT / S::NP, ((int)threadIdx.x & (TT * S::NP - 1)) / S::NP, w.n - 1, r.c);
+    };
+    auto run = [&](Raw &r, float *ct, int tile, auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        stage_states<T, SPL, LPC>(ct, p, w, tile, r.c);
+        float dt[S::TPL], dy[S::TPL], z[S::TPL];
+        values<T>(r.dt, dt);
+        values<T>(r.dy, dy);
+        values<T>(r.z, z);
+#pragma unroll
+        for (int i = 0; i < S::TPL; ++i) {
+            const bool in = ALL || tile * TT + i * S::LQ + w.tok < w.n;
+            const float v = dt[i] + bias;
+            dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
+            dy[i] = in ? (p.z.data ? dy[i] * siluf(z[i]) : dy[i]) : 0.0f;
+            steps += dt[i];
+        }
+        fetch(r, max(tile - 2, w.tile0), all);
+        lds_barrier();
+        float Cv[2][4][SPL], a[2][4][SPL];
+        auto ahead = [&](int k) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = 4 * k + u;
+                read_states<SPL>(ct + t * S::NP + n0, Cv[k & 1][u]);
+                const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ);
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) a[k & 1][u][s] = __builtin_amdgcn_exp2f(dtv * A[s]);
+            }
+        };
+        ahead(TT / 4 - 1);
+#pragma unroll
+        for (int k = TT / 4 - 1; k >= 0; --k) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (k) ahead(k - 1);
+#pragma unroll
+            for (int u = 3; u >= 0; --u) {
+                const int t = 4 * k + u;
+                const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) {
+                    carry[s] = a[k & 1][u][s] * fmaf(Cv[k & 1][u][s], dyv, carry[s]);
+                    if (PAD && !ok[s]) carry[s] = 0.0f;
+                }
+            }
+        }
+    };
+    if (w.tile0 < w.tend) {
+        int tile = w.tend - 1;
+        const int whole = min(w.tend, w.n / TT);
+        fetch(even, tile, std::false_type{});
+        fetch(odd, max(tile - 1, w.tile0), std::false_type{});
+        if (tile >= whole) {                            // (the next two are fetched into the other order)
+            run(even, cl[0], tile, std::false_type{});
+            --tile;
+            for (; tile > w.tile0; tile -= 2) {
+                run(odd, cl[1], tile, std::true_type{});
+                run(even, cl[0], tile - 1, std::true_type{});
+            }
+            if (tile == w.tile0) run(odd, cl[1], tile, std::true_type{});
+        } else {
+            for (; tile > w.tile0; tile -= 2) {
+                run(even, cl[0], tile, std::true_type{});
+                run(odd, cl[1], tile - 1, std::true_type{});
+            }
+            if (tile == w.tile0) run(even, cl[0], tile, std::true_type{});
+        }
+    }
+    const int64_t at = (w.b * p.chunks + w.chunk) * p.D + w.d;
+    steps = sum_channel<S::LQ>(steps);
+    if (w.lane == 0) p.chunk_dt[at] = steps;
+#pragma unroll
+    for (int s = 0; s < SPL; ++s)
+        if (ok[s]) p.chunk_h[at * p.N + n0 + s] = carry[s];
+}
+
 // dB, dC: the sums over a group's channel tiles, rounded once
 template <typename T> __global__ __launch_bounds__(NT) void merit_scan_sum_bc(ScanParams p)
 {
@@ -279,6 +402,8 @@ template <typename T> struct Backward {
     hipStream_t s;
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
+        if (p.chunks > 1)
+            merit_scan_back_chunks<T, SPL, LPC, PAD><<<(unsigned)(p.B * (p.chunks - 1) * p.G * p.ctiles), NT, 0, s>>>(p);
         merit_scan_back<T, SPL, LPC, PAD><<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, 0, s>>>(p);
         return hipGetLastError();
     }

@@ -157,13 +157,27 @@ int64_t conv_bytes(const CconvParams &p, int type, bool backward)
 // ---- scan ----------------------------------------------------------------------------------------
 int64_t scan_part_bc(const ScanParams &p) { return (int64_t)p.G * p.ctiles * p.B * p.L * 2 * p.N; }
 int64_t scan_part_a(const ScanParams &p) { return p.B * p.chunks * ((int64_t)p.D * p.N + 2 * p.D); }
-void scan_layout(ScanParams &p)
+// A sequence runs in one piece where that gives three of four compute units a workgroup (256 workgroups, 8x2048x2048 with 16
+// states: 237 us; as two chunks 272).  On fewer workgroups its chunks run side by side, which takes a launch more and most
+// of a chunk's arithmetic twice: forward two workgroups a unit (32 sequences' parts of 8191 tokens: 169 us in 16 chunks,
+// 875 in one), backward one (its registers allow no more).  A chunk is two tiles at least, and there are at most 4 sqrt(tiles) of
+// them: the last one passes through what all others left.  Below six tiles the second launch costs more than it saves.
+int64_t scan_chunk_floats(const ScanParams &p) { return p.chunks > 1 ? p.B * p.chunks * (int64_t)p.D * (p.N + 1) : 0; }
+void scan_layout(ScanParams &p, bool backward)
 {
     const int cpb = SCAN_THREADS / scan_lpc(p.N);
     p.ctiles = (int)cdiv(p.Dg, cpb);
     p.tiles = cdiv(p.L, MERIT_SCAN_TILE);
     p.chunks = 1;
     p.chunk_tiles = p.tiles > 0 ? p.tiles : 1;
+    const int64_t blocks = p.B * p.G * p.ctiles;
+    if (blocks == 0 || blocks > 192 || p.tiles < 6) return;
+    int64_t chunks = cdiv(backward ? 256 : 512, blocks);
+    if (chunks > p.tiles / 2) chunks = p.tiles / 2;
+    while (chunks * chunks > 16 * p.tiles) --chunks;
+    if (chunks < 2) return;
+    p.chunk_tiles = cdiv(p.tiles, chunks);
+    p.chunks = (int)cdiv(p.tiles, p.chunk_tiles);
 }
 
 merit_token_plan *new_plan(int kind, int type)
@@ -252,7 +266,7 @@ merit_status merit_plan_scan(merit_dtype type, int64_t B, int64_t L, int64_t D, 
     p.B = B; p.L = L; p.D = (int)D; p.N = (int)N; p.G = (int)groups; p.Dg = (int)(D / groups);
     p.softplus = softplus != 0;
     p.type = type;
-    scan_layout(p);
+    scan_layout(p, false);
     const int64_t per = (int64_t)p.chunks * p.G * p.ctiles, lanes = (int64_t)D * scan_lpc(p.N), bc = groups * 2 * N;
     // (the last: launch_reduce_rows over A's gradient, 1024 threads for 64 sums)
     if (B > MAX_BLOCKS || D * (N + 2) > MAX_BLOCKS * 8 || B * per >= MAX_BLOCKS || cdiv(B * lanes, 256) >= MAX_BLOCKS ||
@@ -280,7 +294,11 @@ merit_status merit_token_plan_workspace(const merit_token_plan *plan, merit_pass
     const bool backward = pass == MERIT_PASS_BACKWARD;
     if (plan->kind == NORM) *bytes = norm_bytes(plan->norm, plan->type, backward);
     else if (plan->kind == CONV) *bytes = conv_bytes(plan->conv, plan->type, backward);
-    else *bytes = backward ? 4 * (scan_part_bc(plan->scan) + scan_part_a(plan->scan)) : 0;
+    else {
+        ScanParams q = plan->scan;
+        scan_layout(q, backward);
+        *bytes = 4 * (scan_chunk_floats(q) + (backward ? scan_part_bc(q) + scan_part_a(q) : 0));
+    }
     return MERIT_OK;
 }
 
@@ -300,8 +318,13 @@ merit_status merit_token_plan_kernel(const merit_token_plan *plan, merit_pass pa
     } else if (plan->kind == CONV) {
         *name = pass == MERIT_PASS_STEP ? "merit_cconv_step" : backward ? "merit_cconv_backward+merit_reduce_rows" : "merit_cconv";
     } else {
+        ScanParams q = plan->scan;
+        scan_layout(q, backward);
+        const bool split = q.chunks > 1;
         *name = pass == MERIT_PASS_STEP ? "merit_scan_token"
-                : backward              ? "merit_scan_back+merit_scan_sum_bc+merit_reduce_rows"
+                : backward              ? (split ? "merit_scan_back_chunks+merit_scan_back+merit_scan_sum_bc+merit_reduce_rows"
+                                                 : "merit_scan_back+merit_scan_sum_bc+merit_reduce_rows")
+                : split                 ? "merit_scan_tiles+merit_scan_tiles"
                                         : "merit_scan_tiles";
     }
     return MERIT_OK;
@@ -454,7 +477,7 @@ merit_status merit_causal_conv_step(const merit_token_plan *plan, const merit_ca
 }
 
 // ---- scan -----------------------------------------------------------------------------------------------
-merit_status merit_scan(const merit_token_plan *plan, const merit_scan_args *a, void *, int64_t, void *stream)
+merit_status merit_scan(const merit_token_plan *plan, const merit_scan_args *a, void *workspace, int64_t workspace_bytes, void *stream)
 {
     if (!plan || !a) return MERIT_ERR_NULL;
     if (plan->kind != SCAN) return MERIT_ERR_INVALID_ARG;
@@ -476,6 +499,11 @@ merit_status merit_scan(const merit_token_plan *plan, const merit_scan_args *a, 
     p.h_last = v.f32(a->h_last);
     p.states = v.f32(a->states);
     if (v.st != MERIT_OK) return v.st;
+    scan_layout(p, false);
+    const merit_status st = scratch(4 * scan_chunk_floats(p), workspace, workspace_bytes);
+    if (st != MERIT_OK) return st;
+    p.chunk_dt = static_cast<float *>(workspace);
+    p.chunk_h = p.chunk_dt + (p.chunks > 1 ? p.B * p.chunks * p.D : 0);
     return done(launch_scan(p, static_cast<hipStream_t>(stream)));
 }
 
@@ -509,11 +537,14 @@ merit_status merit_scan_backward(const merit_token_plan *plan, const merit_scan_
     p.ddt_bias = v.f32(a->ddt_bias);
     p.dh0 = v.f32(a->dh0);
     if (v.st != MERIT_OK) return v.st;
-    const int64_t need = 4 * (scan_part_bc(p) + scan_part_a(p));
+    scan_layout(p, true);
+    const int64_t need = 4 * (scan_part_bc(p) + scan_part_a(p) + scan_chunk_floats(p));
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
     p.part_a = static_cast<float *>(workspace);
     p.part_bc = p.part_a + scan_part_a(p);
+    p.chunk_dt = p.part_bc + scan_part_bc(p);
+    p.chunk_h = p.chunk_dt + (p.chunks > 1 ? p.B * p.chunks * p.D : 0);
     return done(launch_scan_backward(p, static_cast<hipStream_t>(stream)));
 }
 
