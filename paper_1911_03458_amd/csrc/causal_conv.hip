@@ -57,12 +57,13 @@ __device__ __forceinline__ vec_t<T, V> row_of(const CconvParams &p, const Place 
 template <typename T, int V, int K>
 __device__ __forceinline__ void load_taps(const CconvParams &p, int c, float (&w)[K][V], float (&b)[V])
 {
+    float flat[K * V];
+    load_params<T>(p.w, (int64_t)c * K, 0.0f, flat);
+    load_params<T>(p.b, c, 0.0f, b);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        b[i] = load_param<T>(p.b, c + i, 0.0f);
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int a = 0; a < K; ++a) w[a][i] = load_param<T>(p.w, (int64_t)(c + i) * K + a, 0.0f);
-    }
+        for (int a = 0; a < K; ++a) w[a][i] = flat[i * K + a];
 }
 
 template <typename T, int V, int K> __global__ __launch_bounds__(NT) void merit_cconv(CconvParams p)

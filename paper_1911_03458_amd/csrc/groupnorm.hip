@@ -74,11 +74,8 @@ __global__ __launch_bounds__(NT) void merit_norm_rows(NormParams p, int cu, int 
         const int u = q.first + j * q.step;
         ok[j] = q.active && u < q.cu;
         c[j] = q.group * p.Cg + u * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            w[j][i] = ok[j] ? load_param<T>(p.w, c[j] + i, 1.0f) : 0.0f;
-            b[j][i] = ok[j] ? load_param<T>(p.b, c[j] + i, 0.0f) : 0.0f;
-        }
+        load_params<T>(p.w, ok[j] ? c[j] : 0, 1.0f, w[j]);       // (a lane without channels: any, not used)
+        load_params<T>(p.b, ok[j] ? c[j] : 0, 0.0f, b[j]);
     }
     vec_t<T, V> next[U] = {};
     if (q.row0 < p.N) {
@@ -141,12 +138,10 @@ __global__ __launch_bounds__(NT) void merit_norm_rows_backward(NormParams p, int
         const int u = q.first + j * q.step;
         ok[j] = q.active && u < q.cu;
         c[j] = q.group * p.Cg + u * V;
+        load_params<T>(p.w, ok[j] ? c[j] : 0, 1.0f, w[j]);
+        load_params<T>(p.b, ok[j] ? c[j] : 0, 0.0f, b[j]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            w[j][i] = ok[j] ? load_param<T>(p.w, c[j] + i, 1.0f) : 0.0f;
-            b[j][i] = ok[j] ? load_param<T>(p.b, c[j] + i, 0.0f) : 0.0f;
-            s1[j][i] = s2[j][i] = 0.0f;
-        }
+        for (int i = 0; i < V; ++i) s1[j][i] = s2[j][i] = 0.0f;
     }
     for (int64_t r = q.row0; r < p.N; r += q.rstep) {
         const float mean = q.active ? p.mean[r * p.G + q.group] : 0.0f;
@@ -268,10 +263,25 @@ template <int V> __device__ __forceinline__ Tile tile_of(const NormParams &p)
 // (n, mean, m2) of two sets of values -> of both
 __device__ __forceinline__ void join(float &n, float &mean, float &m2, float nb, float mb, float m2b)
 {
-    const float sum = n + nb, part = nb / sum, d = mb - mean;
+    const float sum = n + nb, part = sum > 0.0f ? nb * __builtin_amdgcn_rcpf(sum) : 0.0f, d = mb - mean;
     mean = fmaf(d, part, mean);
     m2 += m2b + d * d * n * part;
     n = sum;
+}
+
+// over aligned runs of `lanes` (a power of two) lanes, in every one of them
+__device__ __forceinline__ void join_lanes(float &n, float &mean, float &m2, int lanes)
+{
+#define MERIT_JOIN(BIT) if (lanes > 1 << BIT) join(n, mean, m2, lane_xor<BIT>(n), lane_xor<BIT>(mean), lane_xor<BIT>(m2));
+    MERIT_JOIN(0) MERIT_JOIN(1) MERIT_JOIN(2) MERIT_JOIN(3) MERIT_JOIN(4) MERIT_JOIN(5)
+#undef MERIT_JOIN
+}
+// threads (a power of two, at most a wavefront) that a workgroup has for each of its groups
+__device__ __forceinline__ int group_lanes(int groups)
+{
+    int lanes = 64;
+    while (lanes * groups > NT) lanes /= 2;
+    return lanes;
 }
 
 // A value of the group, which the chunks' means are taken from: next to a mean that is far from zero their distances keep
@@ -290,11 +300,12 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_st
     float cnt = 0.0f, mean = 0.0f, m2 = 0.0f;
     if (t.in && t.r0 < t.r1) {
         const float k0 = shift_of<T>(p, n, t.g0 + t.tx / t.cw);
-        int64_t r = t.r0 + t.ty;
+        int64_t r = t.r0 + t.ty, at0 = base + r * p.x.s1;
+        const int64_t xs = t.rw * p.x.s1;
         for (; r + (RB - 1) * t.rw < t.r1; r += RB * t.rw) {
             vec_t<T, V> v[RB];
 #pragma unroll
-            for (int k = 0; k < RB; ++k) v[k] = load_vec<T, V>(p.x.data, base + (r + k * t.rw) * p.x.s1);
+            for (int k = 0; k < RB; ++k, at0 += xs) v[k] = load_vec<T, V>(p.x.data, at0);
             float s = 0.0f, q = 0.0f;
 #pragma unroll
             for (int k = 0; k < RB; ++k)
@@ -310,8 +321,8 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_st
                 }
             join(cnt, mean, m2, (float)(RB * V), s, q);
         }
-        for (; r < t.r1; r += t.rw) {
-            const vec_t<T, V> v = load_vec<T, V>(p.x.data, base + r * p.x.s1);
+        for (; r < t.r1; r += t.rw, at0 += xs) {
+            const vec_t<T, V> v = load_vec<T, V>(p.x.data, at0);
             float s = 0.0f, q = 0.0f;
 #pragma unroll
             for (int i = 0; i < V; ++i) s += at<T, V>(v, i) - k0;
@@ -328,42 +339,30 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_st
     sm[threadIdx.x] = mean;
     sq[threadIdx.x] = m2;
     __syncthreads();
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int g = wave; g < t.groups; g += NT / 64) {
-        float a = 0.0f, b = 0.0f;
-        for (int e = lane; e < t.rw * t.cw; e += 64) {
+    const int lanes = group_lanes(t.groups), g = (int)threadIdx.x / lanes, lane = (int)threadIdx.x & (lanes - 1);
+    cnt = mean = m2 = 0.0f;
+    if (g < t.groups)
+        for (int e = lane; e < t.rw * t.cw; e += lanes) {
             const int row = e / t.cw, k = row * t.cols + g * t.cw + (e - row * t.cw);
-            a += sn[k];
-            b = fmaf(sn[k], sm[k], b);
+            join(cnt, mean, m2, sn[k], sm[k], sq[k]);
         }
-        a = sum_lanes(a, 64);
-        b = sum_lanes(b, 64);
-        b = a > 0.0f ? b / a : 0.0f;
-        float q = 0.0f;
-        for (int e = lane; e < t.rw * t.cw; e += 64) {
-            const int row = e / t.cw, k = row * t.cols + g * t.cw + (e - row * t.cw);
-            const float d = sm[k] - b;
-            q += fmaf(sn[k] * d, d, sq[k]);
-        }
-        q = sum_lanes(q, 64);
-        if (lane == 0) {
-            const int64_t parts = p.chunks * t.pieces;
-            float *o = p.part + 2 * ((n * p.G + t.g0 + g) * parts + t.chunk * t.pieces + t.piece);
-            o[0] = b;
-            o[1] = q;
-            // (kept for the second launch: its first workgroups may write over x)
-            if (p.S > 0 && t.chunk == 0 && t.piece == 0) p.part[2 * p.N * p.G * parts + n * p.G + t.g0 + g] = shift_of<T>(p, n, t.g0 + g);
-        }
+    join_lanes(cnt, mean, m2, lanes);
+    if (g < t.groups && lane == 0) {
+        const int64_t parts = p.chunks * t.pieces;
+        float *o = p.part + 2 * ((n * p.G + t.g0 + g) * parts + t.chunk * t.pieces + t.piece);
+        o[0] = mean;
+        o[1] = m2;
+        // (kept for the second launch: its first workgroups may write over x)
+        if (p.S > 0 && t.chunk == 0 && t.piece == 0) p.part[2 * p.N * p.G * parts + n * p.G + t.g0 + g] = shift_of<T>(p, n, t.g0 + g);
     }
 }
 
 // values of partial k of a group
-template <int V> __device__ __forceinline__ float part_count(const NormParams &p, const Tile &t, int64_t k)
+template <int V> __device__ __forceinline__ float part_count(const NormParams &p, const Tile &t, int k)
 {
-    const int64_t chunk = k / t.pieces;
-    const int piece = (int)(k - chunk * t.pieces), cu = p.Cg / V;
-    const int64_t rows = min(p.chunk_rows, p.S - chunk * p.chunk_rows);
-    return (float)rows * (float)((t.pieces > 1 ? min(NT, cu - piece * NT) : cu) * V);
+    const int chunk = t.pieces == 1 ? k : k / t.pieces, cu = p.Cg / V;
+    const int cw = t.pieces == 1 ? cu : min(NT, cu - (k - chunk * t.pieces) * NT);
+    return (float)min((int)p.chunk_rows, (int)p.S - chunk * (int)p.chunk_rows) * (float)(cw * V);
 }
 
 template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_apply(NormParams p)
@@ -371,27 +370,21 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
     __shared__ float stat[NT][2];
     const Tile t = tile_of<V>(p);
     const int64_t n = t.n, parts = p.chunks * t.pieces;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int g = wave; g < t.groups; g += NT / 64) {
-        const float *in = p.part + 2 * (n * p.G + t.g0 + g) * parts;
-        float a = 0.0f, b = 0.0f;
-        for (int64_t k = lane; k < parts; k += 64) {
-            const float cnt = part_count<V>(p, t, k);
-            a += cnt;
-            b = fmaf(cnt, in[2 * k], b);
+    {
+        const int lanes = group_lanes(t.groups), g = (int)threadIdx.x / lanes, lane = (int)threadIdx.x & (lanes - 1);
+        float cnt = 0.0f, off = 0.0f, m2 = 0.0f;
+        if (g < t.groups) {
+            const float2 *in = reinterpret_cast<const float2 *>(p.part) + (n * p.G + t.g0 + g) * parts;
+#pragma unroll 4
+            for (int k = lane; k < (int)parts; k += lanes) {
+                const float2 v = in[k];
+                join(cnt, off, m2, part_count<V>(p, t, k), v.x, v.y);
+            }
         }
-        a = sum_lanes(a, 64);
-        b = sum_lanes(b, 64);
-        const float off = a > 0.0f ? b / a : 0.0f;
-        float q = 0.0f;
-        for (int64_t k = lane; k < parts; k += 64) {
-            const float d = in[2 * k] - off;
-            q += fmaf(part_count<V>(p, t, k) * d, d, in[2 * k + 1]);
-        }
-        q = sum_lanes(q, 64);
-        const float mean = a > 0.0f ? p.part[2 * p.N * p.G * parts + n * p.G + t.g0 + g] + off : 0.0f;
-        const float rstd = __builtin_amdgcn_rsqf((a > 0.0f ? q / a : 0.0f) + p.eps);
-        if (lane == 0) {
+        join_lanes(cnt, off, m2, lanes);
+        if (g < t.groups && lane == 0) {
+            const float mean = cnt > 0.0f ? p.part[2 * p.N * p.G * parts + n * p.G + t.g0 + g] + off : 0.0f;
+            const float rstd = __builtin_amdgcn_rsqf((cnt > 0.0f ? m2 / cnt : 0.0f) + p.eps);
             stat[g][0] = mean;
             stat[g][1] = rstd;
             if (t.chunk == 0 && t.piece == 0) {
@@ -404,19 +397,24 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
     if (!t.in) return;
     const float mean = stat[t.tx / t.cw][0], rstd = stat[t.tx / t.cw][1];
     float w[V], b[V];
+    load_params<T>(p.w, t.c, 1.0f, w);
+    load_params<T>(p.b, t.c, 0.0f, b);
+    const int64_t first = t.r0 + t.ty, xs = t.rw * p.x.s1, ys = t.rw * p.y.s1;
+    int64_t xa = n * p.x.s0 + first * p.x.s1 + t.c, ya = n * p.y.s0 + first * p.y.s1 + t.c;
+    constexpr int RB = 4;                   // rows in flight (y may be x: no load moves over a store by itself)
+    for (int r = (int)first; r < (int)t.r1; r += RB * t.rw) {
+        vec_t<T, V> v[RB];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        w[i] = load_param<T>(p.w, t.c + i, 1.0f);
-        b[i] = load_param<T>(p.b, t.c + i, 0.0f);
-    }
-    const int64_t xb = n * p.x.s0 + t.c, yb = n * p.y.s0 + t.c;
-#pragma unroll 4
-    for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.rw) {
-        const vec_t<T, V> v = load_vec<T, V>(p.x.data, xb + r * p.x.s1);
-        vec_t<T, V> o;
+        for (int k = 0; k < RB; ++k, xa += xs)
+            if (k == 0 || r + k * t.rw < (int)t.r1) v[k] = load_vec<T, V>(p.x.data, xa);
 #pragma unroll
-        for (int i = 0; i < V; ++i) put<T, V>(o, i, apply_act(fmaf((at<T, V>(v, i) - mean) * rstd, w[i], b[i]), p.act));
-        store_vec<T, V>(p.y.data, yb + r * p.y.s1, o);
+        for (int k = 0; k < RB; ++k, ya += ys) {
+            if (k && r + k * t.rw >= (int)t.r1) break;
+            vec_t<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) put<T, V>(o, i, apply_act(fmaf((at<T, V>(v[k], i) - mean) * rstd, w[i], b[i]), p.act));
+            store_vec<T, V>(p.y.data, ya, o);
+        }
     }
 }
 
@@ -432,15 +430,13 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_su
     if (t.in) {
         const int g = t.g0 + t.tx / t.cw;
         const float mean = p.mean[n * p.G + g], rstd = p.rstd[n * p.G + g];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            w[i] = load_param<T>(p.w, t.c + i, 1.0f);
-            b[i] = load_param<T>(p.b, t.c + i, 0.0f);
-        }
-        const int64_t xb = n * p.x.s0 + t.c, db = n * p.dy.s0 + t.c;
+        load_params<T>(p.w, t.c, 1.0f, w);
+        load_params<T>(p.b, t.c, 0.0f, b);
+        const int64_t first = t.r0 + t.ty, xs = t.rw * p.x.s1, ds = t.rw * p.dy.s1;
+        int64_t xa = n * p.x.s0 + first * p.x.s1 + t.c, da = n * p.dy.s0 + first * p.dy.s1 + t.c;
 #pragma unroll 4
-        for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.rw) {
-            const vec_t<T, V> xv = load_vec<T, V>(p.x.data, xb + r * p.x.s1), dv = load_vec<T, V>(p.dy.data, db + r * p.dy.s1);
+        for (int r = (int)first; r < (int)t.r1; r += t.rw, xa += xs, da += ds) {
+            const vec_t<T, V> xv = load_vec<T, V>(p.x.data, xa), dv = load_vec<T, V>(p.dy.data, da);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float xh = (at<T, V>(xv, i) - mean) * rstd;
@@ -456,43 +452,31 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_su
         red[1][threadIdx.x][i] = s2[i];
     }
     __syncthreads();
-    float g1 = 0.0f, g2 = 0.0f;
-    if (t.ty == 0) {
-        float *out = p.part + (n * p.chunks + t.chunk) * 2 * p.C;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float a = s1[i], q = s2[i];
-            for (int k = 1; k < t.rw; ++k) {
-                a += red[0][k * t.cols + t.tx][i];
-                q += red[1][k * t.cols + t.tx][i];
-            }
-            out[t.c + i] = a;
-            out[p.C + t.c + i] = q;
-            g1 = fmaf(w[i], a, g1);
-            g2 = fmaf(w[i], q, g2);
-        }
+    // the rows' sums, a thread for each channel and kind; they replace the first row's
+    const int per = t.cols * V;
+    float *out = p.part + (n * p.chunks + t.chunk) * 2 * p.C + t.g0 * p.Cg + t.piece * NT * V;
+    for (int m = threadIdx.x; m < 2 * per; m += NT) {
+        const int kind = m >= per, c = kind ? m - per : m;
+        float *col = &red[kind][0][0] + c, s = col[0];
+        for (int k = 1; k < t.rw; ++k) s += col[k * per];
+        col[0] = s;
+        out[kind * p.C + c] = s;
     }
     __syncthreads();
-    if (t.ty == 0) {
-        red[0][t.tx][0] = g1;
-        red[1][t.tx][0] = g2;
-    }
-    __syncthreads();
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    float *groups = p.part + p.N * p.chunks * 2 * p.C;
-    for (int g = wave; g < t.groups; g += NT / 64) {
-        float a = 0.0f, q = 0.0f;
-        for (int e = lane; e < t.cw; e += 64) {
-            a += red[0][g * t.cw + e][0];
-            q += red[1][g * t.cw + e][0];
+    const int lanes = group_lanes(t.groups), g = (int)threadIdx.x / lanes, lane = (int)threadIdx.x & (lanes - 1);
+    float a = 0.0f, q = 0.0f;
+    if (g < t.groups)
+        for (int e = lane; e < t.cw * V; e += lanes) {
+            const float wc = load_param<T>(p.w, (t.g0 + g) * p.Cg + t.piece * NT * V + e, 1.0f);
+            a = fmaf(wc, (&red[0][0][0])[g * t.cw * V + e], a);
+            q = fmaf(wc, (&red[1][0][0])[g * t.cw * V + e], q);
         }
-        a = sum_lanes(a, 64);
-        q = sum_lanes(q, 64);
-        if (lane == 0) {
-            float *o = groups + 2 * ((n * p.G + t.g0 + g) * p.chunks * t.pieces + t.chunk * t.pieces + t.piece);
-            o[0] = a;
-            o[1] = q;
-        }
+    a = sum_lanes(a, lanes);
+    q = sum_lanes(q, lanes);
+    if (g < t.groups && lane == 0) {
+        float *o = p.part + p.N * p.chunks * 2 * p.C + 2 * ((n * p.G + t.g0 + g) * p.chunks * t.pieces + t.chunk * t.pieces + t.piece);
+        o[0] = a;
+        o[1] = q;
     }
 }
 
@@ -501,19 +485,22 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
     __shared__ float stat[NT][2];
     const Tile t = tile_of<V>(p);
     const int64_t n = t.n, parts = p.chunks * t.pieces;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const float inv = 1.0f / ((float)p.S * (float)p.Cg);
-    const float *groups = p.part + p.N * p.chunks * 2 * p.C;
-    for (int g = wave; g < t.groups; g += NT / 64) {
-        const float *in = groups + 2 * (n * p.G + t.g0 + g) * parts;
+    {
+        const int lanes = group_lanes(t.groups), g = (int)threadIdx.x / lanes, lane = (int)threadIdx.x & (lanes - 1);
         float a = 0.0f, q = 0.0f;
-        for (int64_t k = lane; k < parts; k += 64) {
-            a += in[2 * k];
-            q += in[2 * k + 1];
+        if (g < t.groups) {
+            const float2 *in = reinterpret_cast<const float2 *>(p.part + p.N * p.chunks * 2 * p.C) + (n * p.G + t.g0 + g) * parts;
+#pragma unroll 4
+            for (int k = lane; k < (int)parts; k += lanes) {
+                const float2 v = in[k];
+                a += v.x;
+                q += v.y;
+            }
         }
-        a = sum_lanes(a, 64);
-        q = sum_lanes(q, 64);
-        if (lane == 0) {
+        a = sum_lanes(a, lanes);
+        q = sum_lanes(q, lanes);
+        if (g < t.groups && lane == 0) {
             stat[g][0] = a * inv;
             stat[g][1] = q * inv;
         }
@@ -523,23 +510,32 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
     const int gl = t.tx / t.cw, g = t.g0 + gl;
     const float m1 = stat[gl][0], m2 = stat[gl][1], mean = p.mean[n * p.G + g], rstd = p.rstd[n * p.G + g];
     float w[V], b[V];
+    load_params<T>(p.w, t.c, 1.0f, w);
+    load_params<T>(p.b, t.c, 0.0f, b);
+    const int64_t first = t.r0 + t.ty, xs = t.rw * p.x.s1, ds = t.rw * p.dy.s1, os = t.rw * p.dx.s1;
+    int64_t xa = n * p.x.s0 + first * p.x.s1 + t.c, da = n * p.dy.s0 + first * p.dy.s1 + t.c,
+            oa = n * p.dx.s0 + first * p.dx.s1 + t.c;
+    constexpr int RB = 4;
+    for (int r = (int)first; r < (int)t.r1; r += RB * t.rw) {
+        vec_t<T, V> xv[RB], dv[RB];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        w[i] = load_param<T>(p.w, t.c + i, 1.0f);
-        b[i] = load_param<T>(p.b, t.c + i, 0.0f);
-    }
-    const int64_t xb = n * p.x.s0 + t.c, db = n * p.dy.s0 + t.c, ob = n * p.dx.s0 + t.c;
-#pragma unroll 4
-    for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.rw) {
-        const vec_t<T, V> xv = load_vec<T, V>(p.x.data, xb + r * p.x.s1), dv = load_vec<T, V>(p.dy.data, db + r * p.dy.s1);
-        vec_t<T, V> o;
+        for (int k = 0; k < RB; ++k, xa += xs, da += ds)
+            if (k == 0 || r + k * t.rw < (int)t.r1) {
+                xv[k] = load_vec<T, V>(p.x.data, xa);
+                dv[k] = load_vec<T, V>(p.dy.data, da);
+            }
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float xh = (at<T, V>(xv, i) - mean) * rstd;
-            const float g1 = at<T, V>(dv, i) * act_slope(fmaf(xh, w[i], b[i]), p.act) * w[i];
-            put<T, V>(o, i, rstd * (g1 - m1 - xh * m2));
+        for (int k = 0; k < RB; ++k, oa += os) {
+            if (k && r + k * t.rw >= (int)t.r1) break;
+            vec_t<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float xh = (at<T, V>(xv[k], i) - mean) * rstd;
+                const float g1 = at<T, V>(dv[k], i) * act_slope(fmaf(xh, w[i], b[i]), p.act) * w[i];
+                put<T, V>(o, i, rstd * (g1 - m1 - xh * m2));
+            }
+            store_vec<T, V>(p.dx.data, oa, o);
         }
-        store_vec<T, V>(p.dx.data, ob + r * p.dx.s1, o);
     }
 }
 

@@ -11,7 +11,7 @@ using namespace merit;
 
 namespace {
 
-constexpr int64_t MAX_CHANNELS = 1 << 24, MAX_ROWS = std::numeric_limits<int32_t>::max() - 63;   // (tokens are counted in 32 bits, up to the next tile)
+constexpr int64_t MAX_CHANNELS = 1 << 24, MAX_ROWS = std::numeric_limits<int32_t>::max() - 1023;   // (rows are counted in 32 bits, past the last by up to four of a workgroup's)
 constexpr int64_t MAX_BLOCKS = 1 << 24;                 // of 256 threads: 2^32 threads a launch
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -141,10 +141,28 @@ template <typename T, int V> __device__ __forceinline__ void store_vec(void *bas
 {
     *reinterpret_cast<vec_t<T, V> *>(static_cast<T *>(base) + at) = v;
 }
+// COUNT parameters from element i on.  One branch for all of them: loads that each stand in a branch of their own are waited
+// for one by one (16 of them were half of a norm's second launch).
+template <typename T, int COUNT> __device__ __forceinline__ void load_params(Param p, int64_t i, float absent, float (&v)[COUNT])
+{
+    if (!p.data) {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) v[k] = absent;
+    } else if (p.f32) {
+        const float *q = static_cast<const float *>(p.data) + i;
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) v[k] = q[k];
+    } else {
+        const T *q = static_cast<const T *>(p.data) + i;
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) v[k] = (float)q[k];
+    }
+}
 template <typename T> __device__ __forceinline__ float load_param(Param p, int64_t i, float absent)
 {
-    if (!p.data) return absent;
-    return p.f32 ? static_cast<const float *>(p.data)[i] : (float)static_cast<const T *>(p.data)[i];
+    float v[1];
+    load_params<T>(p, i, absent, v);
+    return v[0];
 }
 
 // ---- elementary functions -----------------------------------------------------------
