@@ -17,7 +17,8 @@ struct Place {
     int64_t b, t0;
     int c;
     int64_t n;             // tokens of the sequence
-    bool in;
+    bool in;               // the strip is there
+    bool own;              // so are the channels; a lane that has none does its wavefront's last ones again (and stores the same)
     int64_t strip;
     int sub, ct, row_lanes;
     int64_t row_block;
@@ -35,11 +36,12 @@ template <int V> __device__ __forceinline__ Place place(const CconvParams &p)
     const int unit = (int)(blockIdx.x - (uint32_t)q.row_block * tiles) * q.ct + ((int)threadIdx.x & (q.ct - 1));
     q.sub = (int)threadIdx.x / q.ct;
     const int64_t s = q.row_block * q.row_lanes + q.sub;
-    q.in = unit < cu && s < p.B * p.strips;
+    q.in = s < p.B * p.strips;
+    q.own = q.in && unit < cu;
     q.b = q.in ? s / p.strips : 0;
     q.strip = s - q.b * p.strips;
     q.t0 = q.strip * p.strip;
-    q.c = unit * V;
+    q.c = min(unit, cu - 1) * V;
     q.n = p.L;
     if (p.lens && q.in) q.n = min((int64_t)max(p.lens[q.b], 0), p.L);
     return q;
@@ -66,11 +68,16 @@ __device__ __forceinline__ void load_taps(const CconvParams &p, int c, float (&w
         for (int a = 0; a < K; ++a) w[a][i] = flat[i * K + a];
 }
 
+// Strips run in batches of RB rows, two batches of loads in flight.  Loads and stores share one counter, so a load is waited
+// for alone only where it is known how many loads and stores came after it: in a wavefront whose lanes all have a whole strip
+// no load and no store stands under a condition.  Others (a sequence's end, channels that do not fill a wavefront) go row by row.
+constexpr int RB = 4;
+__device__ __forceinline__ bool whole_wavefront(bool lane_whole) { return __all(lane_whole) && __ballot(1) == ~0ull; }
+
 template <typename T, int V, int K> __global__ __launch_bounds__(NT) void merit_cconv(CconvParams p)
 {
     const Place q = place<V>(p);
     if (!q.in) return;
-    constexpr int RB = 4;
     float w[K][V], b[V], win[K][V];         // win[K-1]: the row of the current token
     load_taps<T, V, K>(p, q.c, w, b);
     const int64_t t1 = min(q.t0 + p.strip, q.n), t2 = min(q.t0 + p.strip, p.L);
@@ -83,32 +90,51 @@ template <typename T, int V, int K> __global__ __launch_bounds__(NT) void merit_
             for (int i = 0; i < V; ++i) win[j][i] = at<T, V>(v, i);
         }
     }
-    for (int64_t t = q.t0; t < t1; t += RB) {
-        vec_t<T, V> v[RB];
+    auto token = [&](const vec_t<T, V> &row) {      // one token: the window moves on, y of its last row
+        vec_t<T, V> o;
 #pragma unroll
-        for (int k = 0; k < RB; ++k)
-            if (t + k < t1) v[k] = load_vec<T, V>(p.x.data, q.b * p.x.s0 + (t + k) * p.x.s1 + q.c);
+        for (int i = 0; i < V; ++i) {
+            float u = b[i];
 #pragma unroll
-        for (int k = 0; k < RB; ++k) {
-            if (t + k >= t1) break;
-            vec_t<T, V> o;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float u = b[i];
-#pragma unroll
-                for (int a = 0; a < K - 1; ++a) {
-                    win[a][i] = win[a + 1][i];
-                    u = fmaf(w[a][i], win[a][i], u);
-                }
-                win[K - 1][i] = at<T, V>(v[k], i);
-                u = fmaf(w[K - 1][i], win[K - 1][i], u);
-                put<T, V>(o, i, apply_act(u, p.act));
+            for (int a = 0; a < K - 1; ++a) {
+                win[a][i] = win[a + 1][i];
+                u = fmaf(w[a][i], win[a][i], u);
             }
-            store_vec<T, V>(p.y.data, yb + (t + k) * p.y.s1, o);
+            win[K - 1][i] = at<T, V>(row, i);
+            u = fmaf(w[K - 1][i], win[K - 1][i], u);
+            put<T, V>(o, i, apply_act(u, p.act));
         }
+        return o;
+    };
+    if (whole_wavefront(t1 - q.t0 == p.strip)) {
+        int64_t xa = q.b * p.x.s0 + q.t0 * p.x.s1 + q.c, ya = yb + q.t0 * p.y.s1;
+        vec_t<T, V> v[2][RB];
+        auto fetch = [&](vec_t<T, V>(&r)[RB]) {
+#pragma unroll
+            for (int k = 0; k < RB; ++k, xa += p.x.s1) r[k] = load_vec<T, V>(p.x.data, xa);
+        };
+        auto run = [&](vec_t<T, V>(&r)[RB], bool more) {
+            vec_t<T, V> o[RB];
+#pragma unroll
+            for (int k = 0; k < RB; ++k) o[k] = token(r[k]);
+            if (more) fetch(r);
+#pragma unroll
+            for (int k = 0; k < RB; ++k, ya += p.y.s1) store_vec<T, V>(p.y.data, ya, o[k]);
+        };
+        fetch(v[0]);
+        fetch(v[1]);
+        for (int k = 0; k + 2 < p.strip / RB; k += 2) {
+            run(v[0], true);
+            run(v[1], true);
+        }
+        run(v[0], false);
+        run(v[1], false);
+    } else {
+        for (int64_t t = q.t0; t < t1; ++t)
+            store_vec<T, V>(p.y.data, yb + t * p.y.s1, token(load_vec<T, V>(p.x.data, q.b * p.x.s0 + t * p.x.s1 + q.c)));
     }
     for (int64_t t = max(q.t0, q.n); t < t2; ++t) store_vec<T, V>(p.y.data, yb + t * p.y.s1, vec_t<T, V>{});
-    if (K > 1 && p.fin.data && q.strip == 0) {      // (every row is read before one is written: fin may be init)
+    if (K > 1 && p.fin.data && q.strip == 0 && q.own) {      // (every row is read before one is written: fin may be init)
         vec_t<T, V> v[K];
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) v[j] = row_of<T, V, K>(p, q, q.n - (K - 1) + j);
@@ -121,7 +147,6 @@ template <typename T, int V, int K> __global__ __launch_bounds__(NT) void merit_
 {
     __shared__ float red[NT][V];
     const Place q = place<V>(p);
-    constexpr int RB = 4;
     float db[V], dw[K][V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -145,58 +170,109 @@ template <typename T, int V, int K> __global__ __launch_bounds__(NT) void merit_
                 }
             }
         }
-        for (int64_t s0 = q.t0; s0 < t1 + K - 1 && q.t0 < t1; s0 += RB) {
-            vec_t<T, V> xv[RB] = {}, yv[RB] = {};
+        float none[V];
 #pragma unroll
-            for (int k = 0; k < RB; ++k)
-                if (s0 + k < t1 + K - 1 && s0 + k < q.n) {
-                    xv[k] = load_vec<T, V>(p.x.data, xb + (s0 + k) * p.x.s1);
-                    yv[k] = load_vec<T, V>(p.dy.data, yb + (s0 + k) * p.dy.s1);
+        for (int i = 0; i < V; ++i) none[i] = 0.0f;
+        // token s: its u and du; `in`: it is there, `own`: it is the strip's; dx of the token K - 1 before it,
+        // `more` added
+        auto token = [&](const vec_t<T, V> &xrow, const vec_t<T, V> &yrow, bool in, bool own, const float (&more)[V]) {
+            vec_t<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float u = b[i];
+#pragma unroll
+                for (int a = 0; a < K - 1; ++a) {
+                    win[a][i] = win[a + 1][i];
+                    du[a][i] = du[a + 1][i];
+                    u = fmaf(w[a][i], win[a][i], u);
                 }
+                win[K - 1][i] = at<T, V>(xrow, i);
+                u = fmaf(w[K - 1][i], win[K - 1][i], u);
+                const float d = in ? at<T, V>(yrow, i) * act_slope(u, p.act) : 0.0f;
+                du[K - 1][i] = d;
+                if (own) {
+                    db[i] += d;
 #pragma unroll
-            for (int k = 0; k < RB; ++k) {
-                const int64_t s = s0 + k, t = s - (K - 1);
-                if (s >= t1 + K - 1) break;
-                vec_t<T, V> o;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float u = b[i];
-#pragma unroll
-                    for (int a = 0; a < K - 1; ++a) {
-                        win[a][i] = win[a + 1][i];
-                        du[a][i] = du[a + 1][i];
-                        u = fmaf(w[a][i], win[a][i], u);
-                    }
-                    win[K - 1][i] = at<T, V>(xv[k], i);
-                    u = fmaf(w[K - 1][i], win[K - 1][i], u);
-                    const float d = s < q.n ? at<T, V>(yv[k], i) * act_slope(u, p.act) : 0.0f;
-                    du[K - 1][i] = d;
-                    if (s < t1) {
-                        db[i] += d;
-#pragma unroll
-                        for (int a = 0; a < K; ++a) dw[a][i] = fmaf(d, win[a][i], dw[a][i]);
-                    }
-                    float g = 0.0f;
-#pragma unroll
-                    for (int a = 0; a < K; ++a) g = fmaf(w[a][i], du[K - 1 - a][i], g);
-                    if (p.dfin.data && t >= q.t0 && t >= q.n - (K - 1))
-                        g += (float)static_cast<const T *>(p.dfin.data)[q.b * p.dfin.s0 + (t - (q.n - (K - 1))) * p.dfin.s1 + q.c + i];
-                    put<T, V>(o, i, g);
+                    for (int a = 0; a < K; ++a) dw[a][i] = fmaf(d, win[a][i], dw[a][i]);
                 }
-                if (t >= q.t0) store_vec<T, V>(p.dx.data, ob + t * p.dx.s1, o);
+                float g = more[i];
+#pragma unroll
+                for (int a = 0; a < K; ++a) g = fmaf(w[a][i], du[K - 1 - a][i], g);
+                put<T, V>(o, i, g);
+            }
+            return o;
+        };
+        // (the gradient of the last tokens kept: rows at the end of a sequence)
+        if (whole_wavefront(t1 - q.t0 == p.strip && !p.dfin.data)) {
+            const int64_t last = q.n - 1;
+            auto rows = [&](int64_t s, vec_t<T, V> &x, vec_t<T, V> &y) {
+                const int64_t r = min(s, last);
+                x = load_vec<T, V>(p.x.data, xb + r * p.x.s1);
+                y = load_vec<T, V>(p.dy.data, yb + r * p.dy.s1);
+            };
+            if constexpr (K > 1) {                      // the first K - 1 tokens finish no dx of the strip
+                vec_t<T, V> x[K], y[K];
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k) rows(q.t0 + k, x[k], y[k]);
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k) token(x[k], y[k], q.t0 + k < q.n, true, none);
+            }
+            vec_t<T, V> x[2][RB], y[2][RB];
+            int64_t s = q.t0 + K - 1, oa = ob + q.t0 * p.dx.s1;
+            auto fetch = [&](int64_t from, vec_t<T, V>(&xr)[RB], vec_t<T, V>(&yr)[RB]) {
+#pragma unroll
+                for (int k = 0; k < RB; ++k) rows(from + k, xr[k], yr[k]);
+            };
+            auto run = [&](vec_t<T, V>(&xr)[RB], vec_t<T, V>(&yr)[RB], bool more) {
+                vec_t<T, V> o[RB];
+#pragma unroll
+                for (int k = 0; k < RB; ++k) o[k] = token(xr[k], yr[k], s + k < q.n, s + k < t1, none);
+                if (more) fetch(s + 2 * RB, xr, yr);
+#pragma unroll
+                for (int k = 0; k < RB; ++k, oa += p.dx.s1) store_vec<T, V>(p.dx.data, oa, o[k]);
+                s += RB;
+            };
+            fetch(s, x[0], y[0]);
+            fetch(s + RB, x[1], y[1]);
+            for (int k = 0; k + 2 < p.strip / RB; k += 2) {
+                run(x[0], y[0], true);
+                run(x[1], y[1], true);
+            }
+            run(x[0], y[0], false);
+            run(x[1], y[1], false);
+        } else if (q.t0 < t1) {
+            for (int64_t s = q.t0; s < t1 + K - 1; ++s) {
+                const int64_t t = s - (K - 1);
+                vec_t<T, V> xv{}, yv{};
+                if (s < q.n) {
+                    xv = load_vec<T, V>(p.x.data, xb + s * p.x.s1);
+                    yv = load_vec<T, V>(p.dy.data, yb + s * p.dy.s1);
+                }
+                float more[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) more[i] = 0.0f;
+                if (p.dfin.data && t >= q.t0 && t >= q.n - (K - 1)) {
+                    const T *f = static_cast<const T *>(p.dfin.data) + q.b * p.dfin.s0 + (t - (q.n - (K - 1))) * p.dfin.s1 + q.c;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) more[i] = (float)f[i];
+                }
+                const vec_t<T, V> o = token(xv, yv, s < q.n, s < t1, more);
+                if (t < q.t0) continue;
+                store_vec<T, V>(p.dx.data, ob + t * p.dx.s1, o);
             }
         }
         for (int64_t t = max(q.t0, q.n); t < t2; ++t) store_vec<T, V>(p.dx.data, ob + t * p.dx.s1, vec_t<T, V>{});
     }
     if (!p.dw && !p.db) return;
     float *out = p.part + q.row_block * (K + 1) * p.D;
+    const bool unit_own = q.own;                // (the first strip of a workgroup is there)
 #pragma unroll
     for (int a = 0; a <= K; ++a) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < V; ++i) red[threadIdx.x][i] = a < K ? dw[a < K ? a : 0][i] : db[i];
         __syncthreads();
-        if (q.sub == 0 && q.c < p.D) {
+        if (q.sub == 0 && unit_own) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 float s = red[threadIdx.x][i];
@@ -315,8 +391,8 @@ template <typename T, int V> hipError_t launch_v(const CconvParams &p, int pass,
 hipError_t launch_type(const CconvParams &p, int type, int pass, hipStream_t s)
 {
     if (type == MERIT_F32) return p.vec == 4 ? launch_v<float, 4>(p, pass, s) : launch_v<float, 1>(p, pass, s);
-    if (type == MERIT_F16) return p.vec == 8 ? launch_v<f16_t, 8>(p, pass, s) : launch_v<f16_t, 1>(p, pass, s);
-    return p.vec == 8 ? launch_v<bf16_t, 8>(p, pass, s) : launch_v<bf16_t, 1>(p, pass, s);
+    if (type == MERIT_F16) return p.vec == 4 ? launch_v<f16_t, 4>(p, pass, s) : launch_v<f16_t, 1>(p, pass, s);
+    return p.vec == 4 ? launch_v<bf16_t, 4>(p, pass, s) : launch_v<bf16_t, 1>(p, pass, s);
 }
 
 }  // namespace

@@ -4,13 +4,15 @@
 //     dx = rstd (g - mean(g) - xh mean(g xh)),   dw = sum du xh,   db = sum du
 // Bound by memory: 2 (forward) or 3 (backward) passes of the tensor over HBM where it is read once.
 //
-// Two forms.
+// Three forms.
 //  - one row a group (S = 1, a token's heads): a group is a run of channels of one row.  A run of lanes, a wavefront or a
 //    workgroup holds it in registers, so x is read once.  A wavefront keeps its columns and walks down the rows, which
 //    keeps weights and the parameter gradients' sums in registers.
+//  - a group a workgroup (the values of an image's group fit its registers): x is read once too.
 //  - chunks (any S): workgroups reduce row chunks to partial statistics, a second launch joins them and applies.
 // Variances are sums of squared distances from a mean that is known by then (of the row, or of the batch of values in
 // registers, batches joined by their counts): a mean far from zero costs no digits.
+#include "merit_internal.h"
 #include "tokens.h"
 
 namespace merit {
@@ -540,6 +542,163 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
 }
 
 // ---------------------------------------------------------------------------
+// a group a workgroup
+// ---------------------------------------------------------------------------
+// All of a group's values of one image stay in the workgroup's registers, U units of V channels a thread: x (and dy) are
+// read once and nothing waits for another workgroup.  Thread (row ty, unit tx) has rows ty, ty + rw, ...  A row of few
+// channels fills less than a cache line; its neighbours in the line belong to workgroups that run on the same XCD.
+struct Slab {
+    int64_t n;
+    int g, tx, ty, rw, c;
+    bool in;
+};
+template <int V, int NTH> __device__ __forceinline__ Slab slab_of(const NormParams &p)
+{
+    const int cu = p.Cg / V;
+    const uint32_t item = xcd_band_item(blockIdx.x, (int)(gridDim.x >> 3), (int)(gridDim.x & 7u)), n = item / (uint32_t)p.G;
+    Slab s;
+    s.n = n;
+    s.g = (int)(item - n * (uint32_t)p.G);
+    s.rw = NTH / cu;
+    s.ty = (int)threadIdx.x / cu;
+    s.tx = (int)threadIdx.x - s.ty * cu;
+    s.c = s.g * p.Cg + s.tx * V;
+    s.in = s.ty < s.rw;
+    return s;
+}
+// the sum over a workgroup; `slot`: LDS of its own for every sum
+template <int NTH> __device__ __forceinline__ float sum_block(float v, float *slot)
+{
+    v = sum_lanes(v, 64);
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NTH / 64; ++i) s += slot[i];
+    return s;
+}
+
+template <typename T, int V, int U, int NTH> __global__ __launch_bounds__(NTH) void merit_norm_slab(NormParams p)
+{
+    __shared__ float slots[2][NTH / 64];
+    const Slab s = slab_of<V, NTH>(p);
+    const int S = (int)p.S;
+    vec_t<T, V> v[U];
+    int64_t at0 = s.n * p.x.s0 + s.ty * p.x.s1 + s.c;
+#pragma unroll
+    for (int k = 0; k < U; ++k, at0 += s.rw * p.x.s1) {
+        v[k] = vec_t<T, V>{};
+        if (s.in && s.ty + k * s.rw < S) v[k] = load_vec<T, V>(p.x.data, at0);
+    }
+    float w[V], b[V];
+    load_params<T>(p.w, s.in ? s.c : 0, 1.0f, w);
+    load_params<T>(p.b, s.in ? s.c : 0, 0.0f, b);
+    float a = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) a += at<T, V>(v[k], i);     // (what is not there is 0)
+    const float inv = 1.0f / ((float)S * (float)p.Cg), mean = sum_block<NTH>(a, slots[0]) * inv;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const bool in = s.in && s.ty + k * s.rw < S;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float d = in ? at<T, V>(v[k], i) - mean : 0.0f;
+            q = fmaf(d, d, q);
+        }
+    }
+    const float rstd = __builtin_amdgcn_rsqf(sum_block<NTH>(q, slots[1]) * inv + p.eps);
+    if (threadIdx.x == 0) {
+        if (p.mean) p.mean[s.n * p.G + s.g] = mean;
+        if (p.rstd) p.rstd[s.n * p.G + s.g] = rstd;
+    }
+    int64_t yt = s.n * p.y.s0 + s.ty * p.y.s1 + s.c;
+#pragma unroll
+    for (int k = 0; k < U; ++k, yt += s.rw * p.y.s1) {
+        if (!s.in || s.ty + k * s.rw >= S) continue;
+        vec_t<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) put<T, V>(o, i, apply_act(fmaf((at<T, V>(v[k], i) - mean) * rstd, w[i], b[i]), p.act));
+        store_vec<T, V>(p.y.data, yt, o);
+    }
+}
+
+template <typename T, int V, int U, int NTH> __global__ __launch_bounds__(NTH) void merit_norm_slab_backward(NormParams p)
+{
+    __shared__ float slots[2][NTH / 64], red[NTH][V];
+    const Slab s = slab_of<V, NTH>(p);
+    const int S = (int)p.S;
+    vec_t<T, V> xv[U], dv[U];
+    int64_t xa = s.n * p.x.s0 + s.ty * p.x.s1 + s.c, da = s.n * p.dy.s0 + s.ty * p.dy.s1 + s.c;
+#pragma unroll
+    for (int k = 0; k < U; ++k, xa += s.rw * p.x.s1, da += s.rw * p.dy.s1) {
+        xv[k] = dv[k] = vec_t<T, V>{};
+        if (s.in && s.ty + k * s.rw < S) {
+            xv[k] = load_vec<T, V>(p.x.data, xa);
+            dv[k] = load_vec<T, V>(p.dy.data, da);
+        }
+    }
+    const float mean = p.mean[s.n * p.G + s.g], rstd = p.rstd[s.n * p.G + s.g];
+    float w[V], b[V], s1[V], s2[V];
+    load_params<T>(p.w, s.in ? s.c : 0, 1.0f, w);
+    load_params<T>(p.b, s.in ? s.c : 0, 0.0f, b);
+#pragma unroll
+    for (int i = 0; i < V; ++i) s1[i] = s2[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        if (!s.in || s.ty + k * s.rw >= S) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float xh = (at<T, V>(xv[k], i) - mean) * rstd;
+            const float du = at<T, V>(dv[k], i) * act_slope(fmaf(xh, w[i], b[i]), p.act);
+            s1[i] += du;
+            s2[i] = fmaf(du, xh, s2[i]);
+        }
+    }
+    float m1 = 0.0f, m2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        m1 = fmaf(w[i], s1[i], m1);
+        m2 = fmaf(w[i], s2[i], m2);
+    }
+    const float inv = 1.0f / ((float)S * (float)p.Cg);
+    m1 = sum_block<NTH>(s.in ? m1 : 0.0f, slots[0]) * inv;
+    m2 = sum_block<NTH>(s.in ? m2 : 0.0f, slots[1]) * inv;
+    int64_t ot = s.n * p.dx.s0 + s.ty * p.dx.s1 + s.c;
+#pragma unroll
+    for (int k = 0; k < U; ++k, ot += s.rw * p.dx.s1) {
+        if (!s.in || s.ty + k * s.rw >= S) continue;
+        vec_t<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float xh = (at<T, V>(xv[k], i) - mean) * rstd;
+            const float g1 = at<T, V>(dv[k], i) * act_slope(fmaf(xh, w[i], b[i]), p.act) * w[i];
+            put<T, V>(o, i, rstd * (g1 - m1 - xh * m2));
+        }
+        store_vec<T, V>(p.dx.data, ot, o);
+    }
+    if (!p.dw && !p.db) return;
+    // the rows' sums of a channel: lanes of a wavefront that have the same unit first where units are a power of two
+    float *out = p.part + s.n * 2 * p.C + s.g * p.Cg;
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        if (kind) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[threadIdx.x][i] = kind ? s2[i] : s1[i];
+        __syncthreads();
+        // a wavefront for each channel in turn
+        for (int c = threadIdx.x >> 6; c < p.Cg; c += NTH / 64) {
+            const int u = c / V, i = c - u * V, cu = p.Cg / V;
+            float v = 0.0f;
+            for (int r = threadIdx.x & 63; r < s.rw; r += 64) v += red[r * cu + u][i];
+            v = sum_lanes(v, 64);
+            if ((threadIdx.x & 63) == 0) out[kind * p.C + c] = v;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
 // sums over workgroups' partial results
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void merit_reduce_rows(ReduceParams p)
@@ -593,6 +752,17 @@ template <typename T, int V> hipError_t norm_forward(const NormParams &p, hipStr
         else merit_norm_rows<T, V, 4><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
         return hipGetLastError();
     }
+    if constexpr (V > 1)
+        if (p.slab) {
+            const unsigned grid = (unsigned)(p.N * p.G);
+            switch (p.slab) {
+            case 0x104: merit_norm_slab<T, V, 4, 256><<<grid, 256, 0, s>>>(p); break;
+            case 0x108: merit_norm_slab<T, V, 8, 256><<<grid, 256, 0, s>>>(p); break;
+            case 0x404: merit_norm_slab<T, V, 4, 1024><<<grid, 1024, 0, s>>>(p); break;
+            default: merit_norm_slab<T, V, 8, 1024><<<grid, 1024, 0, s>>>(p); break;
+            }
+            return hipGetLastError();
+        }
     const unsigned grid = (unsigned)(p.N * p.chunks * p.ctiles);
     merit_norm_stats<T, V><<<grid, NT, 0, s>>>(p);
     merit_norm_apply<T, V><<<grid, NT, 0, s>>>(p);
@@ -609,6 +779,15 @@ template <typename T, int V> hipError_t norm_backward(const NormParams &p, hipSt
         else if (f.U == 2) merit_norm_rows_backward<T, V, 2><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
         else merit_norm_rows_backward<T, V, 4><<<grid, NT, 0, s>>>(p, f.cu, f.lg, f.wpg);
         rows = p.chunks;
+    } else if (V > 1 && p.slab) {
+        const unsigned grid = (unsigned)(p.N * p.G);
+        if constexpr (V > 1) switch (p.slab) {
+            case 0x104: merit_norm_slab_backward<T, V, 4, 256><<<grid, 256, 0, s>>>(p); break;
+            case 0x108: merit_norm_slab_backward<T, V, 8, 256><<<grid, 256, 0, s>>>(p); break;
+            case 0x404: merit_norm_slab_backward<T, V, 4, 1024><<<grid, 1024, 0, s>>>(p); break;
+            default: merit_norm_slab_backward<T, V, 8, 1024><<<grid, 1024, 0, s>>>(p); break;
+            }
+        rows = p.N;
     } else {
         const unsigned grid = (unsigned)(p.N * p.chunks * p.ctiles);
         merit_norm_sums<T, V><<<grid, NT, 0, s>>>(p);

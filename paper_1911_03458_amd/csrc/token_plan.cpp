@@ -61,10 +61,10 @@ struct Views {
     }
 };
 
-// whether every row of `r` starts on a 16-byte boundary (n0, n1: its extents; the stride of an extent of 1 says nothing)
-bool wide(const Rows &r, int64_t n0, int64_t n1, int vec)
+// whether every row of `r` starts on a boundary of `vec` elements (n0, n1: its extents; the stride of an extent of 1 says nothing)
+bool wide(const Rows &r, int64_t n0, int64_t n1, int vec, int type)
 {
-    return !r.data || (reinterpret_cast<uintptr_t>(r.data) % 16 == 0 && (n0 <= 1 || r.s0 % vec == 0) &&
+    return !r.data || (reinterpret_cast<uintptr_t>(r.data) % (uintptr_t)(vec * elem_bytes(type)) == 0 && (n0 <= 1 || r.s0 % vec == 0) &&
                        (n1 <= 1 || r.s1 % vec == 0));
 }
 
@@ -79,6 +79,8 @@ merit_status scratch(int64_t need, void *workspace, int64_t bytes)
 merit_status done(hipError_t e) { return e == hipSuccess ? MERIT_OK : MERIT_ERR_HIP; }
 
 // ---- group norm ------------------------------------------------------------------------
+// groups from which on a workgroup each is the faster form
+constexpr int64_t NORM_SLAB_GROUPS = 64;
 // Column tiles and row chunks for `vec` channels a lane; returns the floats of scratch memory.
 int64_t norm_layout(NormParams &p, int vec, bool backward)
 {
@@ -95,6 +97,18 @@ int64_t norm_layout(NormParams &p, int vec, bool backward)
         p.chunks = rows < most ? rows : most;
         p.chunk_rows = 1;
         return backward ? p.chunks * 2 * p.C : 0;
+    }
+    p.slab = 0;
+    if (vec > 1 && p.N * p.G >= NORM_SLAB_GROUPS && cu <= 256 && p.S * cu >= 128) {
+        for (int form : {0x104, 0x108, 0x404, 0x408}) {
+            const int threads = form & 0x400 ? 1024 : 256, units = form & 0xFF;
+            if (p.S > (int64_t)(threads / cu) * units) continue;
+            p.slab = form;
+            p.ctiles = p.G;
+            p.chunks = 1;
+            p.chunk_rows = p.S;
+            return backward ? p.N * 2 * p.C : 0;
+        }
     }
     const int pieces = (int)cdiv(cu, 256), gt = pieces > 1 ? 1 : (p.G < 256 / cu ? p.G : 256 / cu);
     p.ctiles = pieces > 1 ? p.G * pieces : (int)cdiv(p.G, gt);
@@ -122,13 +136,18 @@ int64_t norm_bytes(const NormParams &p, int type, bool backward)
 }
 
 // ---- causal convolution ---------------------------------------------------------------------
-// Tokens of a strip: the longest that still gives every SIMD two wavefronts (a strip reads K - 1 rows again)
+// Channels a lane moves at once, whatever their type: with eight of 16 bits a lane's window, taps and sums take so many registers
+// that too few wavefronts are left to wait for memory (8x2048x2048 bfloat16, forward 36 us with 8, 29 with 4).
+constexpr int CONV_VEC = 4;
+// Tokens of a strip (it reads K - 1 rows again): the longest of 8, 16, 32 that gives every SIMD four wavefronts; backward of 8 to
+// 64 that gives it two (bfloat16, forward 3x4099x1536: 16 tokens 16.8 us, 32 18.8, 64 27; backward 8x2048x2048: 16 60 us, 32 54,
+// 64 50, 128 69).
 int64_t conv_layout(CconvParams &p, int vec, bool backward)
 {
     p.vec = vec;
     const int64_t cu = p.D / vec;
     p.strip = backward ? 64 : 32;
-    while (p.strip > 8 && p.B * cdiv(p.L, p.strip) * cu < 2 * 65536) p.strip /= 2;
+    while (p.strip > 8 && p.B * cdiv(p.L, p.strip) * cu < (backward ? 2 : 4) * 65536) p.strip /= 2;
     p.strips = p.L > 0 ? cdiv(p.L, p.strip) : 1;
     int ct = 1;
     while (ct < 64 && ct < cu) ct *= 2;
@@ -145,7 +164,7 @@ int64_t conv_blocks(const CconvParams &p)
 int64_t conv_bytes(const CconvParams &p, int type, bool backward)
 {
     CconvParams q = p;
-    const int vec = 16 / elem_bytes(type);
+    const int vec = CONV_VEC;
     int64_t most = conv_layout(q, 1, backward);
     if (p.D % vec == 0) {
         const int64_t n = conv_layout(q, vec, backward);
@@ -238,7 +257,7 @@ merit_status merit_plan_causal_conv(merit_dtype type, int64_t B, int64_t L, int6
     CconvParams &p = pl->conv;
     p.B = B; p.L = L; p.D = (int)D; p.K = (int)K;
     p.act = act;
-    for (int vec : {1, 16 / elem_bytes(type)}) {
+    for (int vec : {1, CONV_VEC}) {
         if (p.D % vec) continue;
         CconvParams q = p;
         conv_layout(q, vec, false);
@@ -313,6 +332,7 @@ merit_status merit_token_plan_kernel(const merit_token_plan *plan, merit_pass pa
         const int vec = 16 / elem_bytes(plan->type);
         norm_layout(q, q.Cg % vec == 0 ? vec : 1, backward);
         *name = q.rows_form ? (backward ? "merit_norm_rows_backward+merit_reduce_rows" : "merit_norm_rows")
+                : q.slab    ? (backward ? "merit_norm_slab_backward+merit_reduce_rows" : "merit_norm_slab")
                             : (backward ? "merit_norm_sums+merit_norm_apply_backward+merit_reduce_rows"
                                         : "merit_norm_stats+merit_norm_apply");
     } else if (plan->kind == CONV) {
@@ -348,7 +368,7 @@ merit_status merit_group_norm(const merit_token_plan *plan, const merit_group_no
     p.rstd = v.f32(a->rstd);
     if (v.st != MERIT_OK) return v.st;
     const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.Cg % vec == 0 && wide(p.x, p.N, p.S, vec) && wide(p.y, p.N, p.S, vec);
+    const bool fits = p.Cg % vec == 0 && wide(p.x, p.N, p.S, vec, plan->type) && wide(p.y, p.N, p.S, vec, plan->type);
     const int64_t need = 4 * norm_layout(p, fits ? vec : 1, false);
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
@@ -384,7 +404,7 @@ merit_status merit_group_norm_backward(const merit_token_plan *plan, const merit
         return done(launch_reduce_rows(r, s));
     }
     const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.Cg % vec == 0 && wide(p.x, p.N, p.S, vec) && wide(p.dy, p.N, p.S, vec) && wide(p.dx, p.N, p.S, vec);
+    const bool fits = p.Cg % vec == 0 && wide(p.x, p.N, p.S, vec, plan->type) && wide(p.dy, p.N, p.S, vec, plan->type) && wide(p.dx, p.N, p.S, vec, plan->type);
     const int64_t need = 4 * norm_layout(p, fits ? vec : 1, true);
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
@@ -408,9 +428,9 @@ merit_status merit_causal_conv(const merit_token_plan *plan, const merit_causal_
     p.y = v.rows(a->y, p.L > 0);
     p.fin = v.rows(a->final, false);
     if (v.st != MERIT_OK) return v.st;
-    const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.D % vec == 0 && wide(p.x, p.B, p.L, vec) && wide(p.y, p.B, p.L, vec) &&
-                      wide(p.init, p.B, p.K - 1, vec) && wide(p.fin, p.B, p.K - 1, vec);
+    const int vec = CONV_VEC;
+    const bool fits = p.D % vec == 0 && wide(p.x, p.B, p.L, vec, plan->type) && wide(p.y, p.B, p.L, vec, plan->type) &&
+                      wide(p.init, p.B, p.K - 1, vec, plan->type) && wide(p.fin, p.B, p.K - 1, vec, plan->type);
     conv_layout(p, fits ? vec : 1, false);
     return done(launch_cconv(p, plan->type, static_cast<hipStream_t>(stream)));
 }
@@ -444,9 +464,9 @@ merit_status merit_causal_conv_backward(const merit_token_plan *plan, const meri
         r.seg[1] = {p.db, 0, p.D};
         return done(launch_reduce_rows(r, s));
     }
-    const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.D % vec == 0 && wide(p.x, p.B, p.L, vec) && wide(p.dy, p.B, p.L, vec) && wide(p.dx, p.B, p.L, vec) &&
-                      wide(p.init, p.B, p.K - 1, vec);
+    const int vec = CONV_VEC;
+    const bool fits = p.D % vec == 0 && wide(p.x, p.B, p.L, vec, plan->type) && wide(p.dy, p.B, p.L, vec, plan->type) && wide(p.dx, p.B, p.L, vec, plan->type) &&
+                      wide(p.init, p.B, p.K - 1, vec, plan->type);
     const int64_t need = 4 * conv_layout(p, fits ? vec : 1, true);
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
@@ -469,9 +489,9 @@ merit_status merit_causal_conv_step(const merit_token_plan *plan, const merit_ca
     p.y = v.rows(a->y);
     p.fin = v.rows(a->kept_out, p.K > 1);
     if (v.st != MERIT_OK) return v.st;
-    const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.D % vec == 0 && wide(p.x, p.B, 1, vec) && wide(p.y, p.B, 1, vec) && wide(p.init, p.B, p.K - 1, vec) &&
-                      wide(p.fin, p.B, p.K - 1, vec);
+    const int vec = CONV_VEC;
+    const bool fits = p.D % vec == 0 && wide(p.x, p.B, 1, vec, plan->type) && wide(p.y, p.B, 1, vec, plan->type) && wide(p.init, p.B, p.K - 1, vec, plan->type) &&
+                      wide(p.fin, p.B, p.K - 1, vec, plan->type);
     p.vec = fits ? vec : 1;
     return done(launch_cconv_step(p, plan->type, static_cast<hipStream_t>(stream)));
 }

@@ -45,6 +45,7 @@ struct NormParams {
     float *mean, *rstd;    // [N, G]
     float *part;           // workspace
     int rows_form;         // one row a group
+    int slab;              // a group a workgroup: its threads / 256 << 8 | units a thread (0: not this form)
     int ctiles;            // column tiles
     int64_t chunks;        // row chunks of an image; one row a group: workgroups along the rows
     int64_t chunk_rows;
