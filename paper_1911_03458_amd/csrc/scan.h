@@ -188,16 +188,23 @@ template <int LPC> __device__ __forceinline__ void sum_to_tokens(const float (&v
     }
 }
 
-// four consecutive floats of LDS or one
+// one, two or four consecutive floats of LDS
 template <int SPL> __device__ __forceinline__ void read_states(const float *at, float (&v)[SPL])
 {
     if constexpr (SPL == 4) {
         const float4 q = *reinterpret_cast<const float4 *>(at);
         v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-    } else {
-#pragma unroll
-        for (int s = 0; s < SPL; ++s) v[s] = at[s];
-    }
+    } else if constexpr (SPL == 2) {
+        const float2 q = *reinterpret_cast<const float2 *>(at);
+        v[0] = q.x, v[1] = q.y;
+    } else v[0] = at[0];
+}
+
+template <int SPL> __device__ __forceinline__ void write_states(float *at, const float (&v)[SPL])
+{
+    if constexpr (SPL == 4) *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (SPL == 2) *reinterpret_cast<float2 *>(at) = make_float2(v[0], v[1]);
+    else at[0] = v[0];
 }
 
 // A state (or its adjoint) through `count` chunks from `q` on: their decay, then what they add.  Four chunks' loads go out
@@ -229,8 +236,9 @@ __device__ __forceinline__ void through_chunks(const ScanParams &p, const Where 
 template <typename F> hipError_t by_states(int N, F &&f)
 {
     if (N == 1) return f.template run<1, 1, false>();
-    if (N == 4) return f.template run<4, 1, false>();
-    if (N < 4) return f.template run<4, 1, true>();
+    if (N == 2) return f.template run<1, 2, false>();
+    if (N == 4) return f.template run<2, 2, false>();
+    if (N < 4) return f.template run<2, 2, true>();
     if (N == 8) return f.template run<4, 2, false>();
     if (N < 8) return f.template run<4, 2, true>();
     if (N == 16) return f.template run<4, 4, false>();

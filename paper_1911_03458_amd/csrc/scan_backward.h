@@ -9,6 +9,7 @@
 // halves the values too (15 exchanges for 16 sums of 16 lanes), then wavefronts through LDS, then workgroups through
 // memory in a second launch, in a fixed order.
 #pragma once
+#include "merit_internal.h"
 #include "scan.h"
 
 namespace merit {
@@ -43,25 +44,25 @@ template <int BIT> __device__ __forceinline__ float halve(float lo, float hi)
     }
 }
 
-// v[t], t < 16, summed over the lanes of a wavefront that have the same state (all but the lowest log2 LPC lane bits);
-// the lane keeps the sums of KEEP tokens, from first_token() on
+// Values of the 16 tokens summed over the lanes of a wavefront that have the same state (all but the lowest log2 LPC lane
+// bits): four tokens at a time over the highest two of these bits, the four results over the others.  The lane keeps the
+// sums of KEEP tokens, token(0), ...
 template <int LPC> struct Sums {
-    static constexpr int CW = 64 / LPC;                    // channels of a wavefront
-    static constexpr int KEEP = CW >= TT ? 1 : TT / CW;
-    static __device__ __forceinline__ int first_token()
+    static constexpr int KEEP = LPC <= 4 ? 1 : LPC / 4;
+    static __device__ __forceinline__ int token(int j)
     {
-        const int lane = threadIdx.x & 63;                 // bits 5, 4, ... of the lane are bits 3, 2, ... of the token
-        return ((lane >> 2) & 15) & ~(KEEP - 1);
+        const int lane = threadIdx.x, k = LPC <= 4 ? (lane >> 2) & 3 : LPC == 8 ? ((lane >> 2) & 2) + j : j;
+        return 4 * k + ((lane >> 4) & 3);
     }
-    static __device__ __forceinline__ void over_channels(float (&v)[TT])
+    static __device__ __forceinline__ float of_four(float a, float b, float c, float d)
     {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = halve<5>(v[i], v[i + 8]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = halve<4>(v[i], v[i + 4]);
+        return halve<4>(halve<5>(a, c), halve<5>(b, d));
+    }
+    static __device__ __forceinline__ void of_all(float (&v)[4])
+    {
         if constexpr (LPC <= 8) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) v[i] = halve<3>(v[i], v[i + 2]);
+            v[0] = halve<3>(v[0], v[2]);
+            v[1] = halve<3>(v[1], v[3]);
         }
         if constexpr (LPC <= 4) v[0] = halve<2>(v[0], v[1]);
         if constexpr (LPC <= 2) v[0] += lane_xor<1>(v[0]);
@@ -71,27 +72,34 @@ template <int LPC> struct Sums {
     static __device__ __forceinline__ bool writes() { return LPC >= 4 || (threadIdx.x & (3 & ~(LPC - 1))) == 0; }
 };
 
-template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_back(ScanParams p)
+// LDS of a workgroup: B and C of a tile, the wavefronts' sums for dB and dC, the states of the tile's tokens
+template <int SPL, int LPC> constexpr int back_lds()
+{
+    return (2 * TT * SPL * LPC + NT / 64 * TT * 2 * SPL * LPC + TT * NT * SPL) * 4;
+}
+
+// Two wavefronts a SIMD (a lone one issues plain arithmetic at half the rate), so 256 registers: the decays of a tile stay in
+// registers, its states in LDS.
+template <typename T, int SPL, int LPC, bool PAD>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2 : 1, 2))) void merit_scan_back(ScanParams p)
 {
     using S = Shape<SPL, LPC>;
     using Q = Sums<LPC>;
-    __shared__ __align__(16) float bl[TT * S::NP], cl[TT * S::NP];
-    __shared__ __align__(16) float red[NT / 64][TT * 2 * S::NP];
+    extern __shared__ __align__(16) float lds[];
+    float *const bl = lds, *const cl = bl + TT * S::NP, *const red = cl + TT * S::NP;
+    float *const hl = red + NT / 64 * TT * 2 * S::NP + threadIdx.x * SPL;      // token t: t * NT * SPL further
     const Where w = where<LPC>(p, 0, p.chunks);
     const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
-    float A[SPL], dA[SPL], carry[SPL];
+    float A2[SPL], dA[SPL], carry[SPL];                     // (A2: the exponentials are to the base 2)
     bool ok[SPL];
     const int64_t hat = (w.b * p.D + w.d) * p.N + n0;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
         ok[s] = w.in && (!PAD || n0 + s < p.N);
-        A[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] : 0.0f;
+        A2[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] * LOG2E : 0.0f;
         dA[s] = 0.0f;
         carry[s] = ok[s] && p.dh_last ? p.dh_last[hat + s] : 0.0f;     // a_{t+1} l_{t+1}
     }
-    float A2[SPL];
-#pragma unroll
-    for (int s = 0; s < SPL; ++s) A2[s] = A[s] * LOG2E;
     through_chunks<SPL>(p, w, n0, A2, ok, carry, p.chunks - 1, p.chunks - 1 - w.chunk, -1);
     const float bias = w.in && p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = w.in && p.skip ? p.skip[w.d] : 0.0f;
     float dskip = 0.0f, dbias = 0.0f;
@@ -132,125 +140,129 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
             store_walk<T, false>(ddw, tile, S::LQ, w.tok, p.L, od);
             if (p.z.data) store_walk<T, false>(dzw, tile, S::LQ, w.tok, p.L, oz);
         }
+        constexpr int R = TT * 2 * S::NP;
 #pragma unroll
-        for (int i = 0; i < (TT * 2 * S::NP + NT - 1) / NT; ++i) {
+        for (int i = 0; i < (R + NT - 1) / NT; ++i) {
             const int e = i * NT + (int)threadIdx.x, n = e % S::NP, k = e / S::NP;      // k = 2 t + (0: dB, 1: dC)
             const int64_t t = (int64_t)tile * TT + k / 2;
-            if (e < TT * 2 * S::NP && n < p.N && t < p.L)
-                bc[(t * 2 + (k & 1)) * p.N + n] = t < w.n ? (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]) : 0.0f;
+            if (e < R && n < p.N && t < p.L)
+                bc[(t * 2 + (k & 1)) * p.N + n] = t < w.n ? (red[e] + red[e + R]) + (red[e + 2 * R] + red[e + 3 * R]) : 0.0f;
         }
     };
     auto run = [&](int tile, auto all) {
         constexpr bool ALL = decltype(all)::value;
-        float x[S::TPL], raw[S::TPL], z[S::TPL], dy[S::TPL], dyo[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL], in_[S::TPL], da_[S::TPL];
+        // of a token: x, step, step x, dy', the step's slope, dy silu'(z)
+        float x[S::TPL], dt[S::TPL], dx[S::TPL], dy[S::TPL], slope[S::TPL], gz[S::TPL], y[S::TPL], in_[S::TPL], da_[S::TPL];
         values<T>(xr, x);
-        values<T>(dr, raw);
-        values<T>(yr, dyo);
-        values<T>(zr, z);
+        values<T>(dr, dt);
+        values<T>(yr, dy);
+        values<T>(zr, gz);
         lds_barrier();              // (the tile before is done with bl and cl, and red is whole)
         if (tile + 1 < w.tend) write(tile + 1);
         stage_states<T, SPL, LPC>(bl, p, w, tile, br);
         stage_states<T, SPL, LPC>(cl, p, w, tile, cr);
-        float hs[SPL], h[TT][SPL], a[TT][SPL];
+        float h[SPL], hs[SPL], a[TT][SPL];
 #pragma unroll
-        for (int s = 0; s < SPL; ++s) hs[s] = ok[s] ? hr[s] : 0.0f;
+        for (int s = 0; s < SPL; ++s) h[s] = hs[s] = ok[s] ? hr[s] : 0.0f;
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
             const bool in = w.in && (ALL || tile * TT + i * S::LQ + w.tok < w.n);
-            raw[i] += bias;
-            dt[i] = in ? (p.softplus ? softplusf(raw[i]) : raw[i]) : 0.0f;
+            const float v = dt[i] + bias, z = gz[i], g = dy[i];
+            slope[i] = p.softplus ? sigmoidf(v) : 1.0f;
+            dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
             dx[i] = in ? dt[i] * x[i] : 0.0f;
-            dy[i] = in ? (p.z.data ? dyo[i] * siluf(z[i]) : dyo[i]) : 0.0f;
+            dy[i] = in ? (p.z.data ? g * siluf(z) : g) : 0.0f;
+            gz[i] = in ? g * act_slope(z, MERIT_ACT_SILU) : 0.0f;
         }
         fetch(max(tile - 1, w.tile0), all);
         lds_barrier();
-        // the tile's states once more, four tokens at a time, what needs LDS asked for four tokens ahead
-        float Bv[2][4][SPL], Cv[2][4][SPL];
-        auto ahead = [&](int k) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                read_states<SPL>(bl + (4 * k + u) * S::NP + n0, Bv[k & 1][u]);
-                read_states<SPL>(cl + (4 * k + u) * S::NP + n0, Cv[k & 1][u]);
-            }
-        };
-        ahead(0);
+        // the tile's states once more, four tokens at a time; dC on the way
+        float sums[SPL][4];
 #pragma unroll
         for (int k = 0; k < TT / 4; ++k) {
             __builtin_amdgcn_sched_barrier(0);
-            if (k + 1 < TT / 4) ahead(k + 1);
-            float acc[4];
+            float acc[4], c4[SPL][4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int t = 4 * k + u;
                 const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
+                const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
+                float Bv[SPL], Cv[SPL];
+                read_states<SPL>(bl + t * S::NP + n0, Bv);
+                read_states<SPL>(cl + t * S::NP + n0, Cv);
                 acc[u] = 0.0f;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) {
                     a[t][s] = __builtin_amdgcn_exp2f(dtv * A2[s]);
-                    h[t][s] = fmaf(a[t][s], t ? h[t ? t - 1 : 0][s] : hs[s], dxv * Bv[k & 1][u][s]);
-                    if (PAD && !ok[s]) h[t][s] = 0.0f;
-                    acc[u] = fmaf(h[t][s], Cv[k & 1][u][s], acc[u]);
+                    h[s] = fmaf(a[t][s], h[s], dxv * Bv[s]);
+                    if (PAD && !ok[s]) h[s] = 0.0f;
+                    acc[u] = fmaf(h[s], Cv[s], acc[u]);
+                    c4[s][u] = h[s] * dyv;
                 }
+                write_states<SPL>(hl + t * NT * SPL, h);
             }
             sum_to_tokens<LPC>(acc, y + 4 * k / S::LQ);
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) sums[s][k] = Q::of_four(c4[s][0], c4[s][1], c4[s][2], c4[s][3]);
         }
-        // (the last four tokens' B and C are the first of the way back)
+        auto leave = [&](int kind) {
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) {
+                Q::of_all(sums[s]);
+                if (Q::writes())
+#pragma unroll
+                    for (int j = 0; j < Q::KEEP; ++j)
+                        red[wave * TT * 2 * S::NP + (2 * Q::token(j) + kind) * S::NP + n0 + s] = sums[s][j];
+            }
+        };
+        leave(1);
+        // (what the way back needs again it makes again: kept from above it would be more than the registers hold)
+#pragma unroll
+        for (int i = 0; i < S::TPL; ++i) asm volatile("" : "+v"(dt[i]), "+v"(dx[i]), "+v"(dy[i])::"memory");
+        // and back: the adjoint of the state
 #pragma unroll
         for (int k = TT / 4 - 1; k >= 0; --k) {
             __builtin_amdgcn_sched_barrier(0);
-            if (k) ahead(k - 1);
-            float u4[4], v4[4];
+            float u4[4], v4[4], b4[SPL][4];
 #pragma unroll
             for (int u = 3; u >= 0; --u) {
                 const int t = 4 * k + u;
                 const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
                 const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
+                float Bv[SPL], Cv[SPL];
+                read_states<SPL>(bl + t * S::NP + n0, Bv);
+                read_states<SPL>(cl + t * S::NP + n0, Cv);
+                if (t) read_states<SPL>(hl + (t - 1) * NT * SPL, h);
                 u4[u] = v4[u] = 0.0f;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) {
-                    float l = fmaf(Cv[k & 1][u][s], dyv, carry[s]);
+                    float l = fmaf(Cv[s], dyv, carry[s]);
                     if (PAD && !ok[s]) l = 0.0f;
-                    u4[u] = fmaf(l, Bv[k & 1][u][s], u4[u]);
+                    u4[u] = fmaf(l, Bv[s], u4[u]);
                     carry[s] = a[t][s] * l;
-                    const float q = carry[s] * (t ? h[t ? t - 1 : 0][s] : hs[s]);
-                    v4[u] = fmaf(q, A[s], v4[u]);
+                    const float q = carry[s] * (t ? h[s] : hs[s]);
+                    v4[u] = fmaf(q, A2[s], v4[u]);
                     dA[s] = fmaf(q, dtv, dA[s]);
-                    a[t][s] = l * dxv;                  // now dB's and dC's terms
-                    h[t][s] *= dyv;
+                    b4[s][u] = l * dxv;
                 }
             }
             sum_to_tokens<LPC>(u4, in_ + 4 * k / S::LQ);
             sum_to_tokens<LPC>(v4, da_ + 4 * k / S::LQ);
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) sums[s][k] = Q::of_four(b4[s][0], b4[s][1], b4[s][2], b4[s][3]);
         }
+        leave(0);
 #pragma unroll
         for (int i = 0; i < S::TPL; ++i) {
             const bool in = ALL || tile * TT + i * S::LQ + w.tok < w.n;
-            float ds = fmaf(in_[i], x[i], da_[i]);
-            if (p.softplus) ds *= sigmoidf(raw[i]);
-            const float y0 = p.skip ? fmaf(skip, x[i], y[i]) : y[i];
+            const float ds = fmaf(in_[i], x[i], da_[i] * (1.0f / LOG2E)) * slope[i], y0 = p.skip ? fmaf(skip, x[i], y[i]) : y[i];
             if (in) {
                 dskip = fmaf(dy[i], x[i], dskip);
                 dbias += ds;
             }
             ox[i] = in ? (p.skip ? fmaf(in_[i], dt[i], skip * dy[i]) : in_[i] * dt[i]) : 0.0f;
             od[i] = in ? ds : 0.0f;
-            oz[i] = in ? dyo[i] * y0 * act_slope(z[i], MERIT_ACT_SILU) : 0.0f;
-        }
-#pragma unroll
-        for (int s = 0; s < SPL; ++s) {
-            float vb[TT], vc[TT];
-#pragma unroll
-            for (int t = 0; t < TT; ++t) vb[t] = a[t][s], vc[t] = h[t][s];
-            Q::over_channels(vb);
-            Q::over_channels(vc);
-            if (Q::writes()) {
-#pragma unroll
-                for (int k = 0; k < Q::KEEP; ++k) {
-                    float *o = red[wave] + (Q::first_token() + k) * 2 * S::NP + n0 + s;
-                    o[0] = vb[k];
-                    o[S::NP] = vc[k];
-                }
-            }
+            oz[i] = in ? gz[i] * y0 : 0.0f;
         }
     };
     if (w.tile0 < w.tend) {
@@ -404,7 +416,11 @@ template <typename T> struct Backward {
     {
         if (p.chunks > 1)
             merit_scan_back_chunks<T, SPL, LPC, PAD><<<(unsigned)(p.B * (p.chunks - 1) * p.G * p.ctiles), NT, 0, s>>>(p);
-        merit_scan_back<T, SPL, LPC, PAD><<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, 0, s>>>(p);
+        static std::atomic<int> raised;
+        const hipError_t e = raise_lds_limit_once(reinterpret_cast<const void *>(merit_scan_back<T, SPL, LPC, PAD>), raised);
+        if (e != hipSuccess) return e;
+        merit_scan_back<T, SPL, LPC, PAD>
+            <<<(unsigned)(p.B * p.chunks * p.G * p.ctiles), NT, back_lds<SPL, LPC>(), s>>>(p);
         return hipGetLastError();
     }
 };

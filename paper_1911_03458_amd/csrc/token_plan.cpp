@@ -176,11 +176,12 @@ int64_t conv_bytes(const CconvParams &p, int type, bool backward)
 // ---- scan ----------------------------------------------------------------------------------------
 int64_t scan_part_bc(const ScanParams &p) { return (int64_t)p.G * p.ctiles * p.B * p.L * 2 * p.N; }
 int64_t scan_part_a(const ScanParams &p) { return p.B * p.chunks * ((int64_t)p.D * p.N + 2 * p.D); }
-// A sequence runs in one piece where that gives three of four compute units a workgroup (256 workgroups, 8x2048x2048 with 16
-// states: 237 us; as two chunks 272).  On fewer workgroups its chunks run side by side, which takes a launch more and most
-// of a chunk's arithmetic twice: forward two workgroups a unit (32 sequences' parts of 8191 tokens: 169 us in 16 chunks,
-// 875 in one), backward one (its registers allow no more).  A chunk is two tiles at least, and there are at most 4 sqrt(tiles) of
-// them: the last one passes through what all others left.  Below six tiles the second launch costs more than it saves.
+// On few workgroups a sequence's chunks run side by side, two workgroups a compute unit, which takes a launch more and most of a
+// chunk's arithmetic twice.  Forward that pays up to three workgroups for four units (bfloat16, 16 states, 32 workgroups,
+// 8191 tokens: 169 us in 16 chunks, 875 in one; 256 workgroups, 2048 tokens: 272 in two, 237 in one), backward up to three for
+// two units, since a chunk's first launch is a small part there (the latter: 614 in two, 719 in one).  A chunk is two tiles
+// at least, and there are at most 4 sqrt(tiles) of them: the last one passes through what all others left.  Below six tiles the
+// second launch costs more than it saves.
 int64_t scan_chunk_floats(const ScanParams &p) { return p.chunks > 1 ? p.B * p.chunks * (int64_t)p.D * (p.N + 1) : 0; }
 void scan_layout(ScanParams &p, bool backward)
 {
@@ -190,8 +191,8 @@ void scan_layout(ScanParams &p, bool backward)
     p.chunks = 1;
     p.chunk_tiles = p.tiles > 0 ? p.tiles : 1;
     const int64_t blocks = p.B * p.G * p.ctiles;
-    if (blocks == 0 || blocks > 192 || p.tiles < 6) return;
-    int64_t chunks = cdiv(backward ? 256 : 512, blocks);
+    if (blocks == 0 || blocks > (backward ? 384 : 192) || p.tiles < 6) return;
+    int64_t chunks = cdiv(512, blocks);
     if (chunks > p.tiles / 2) chunks = p.tiles / 2;
     while (chunks * chunks > 16 * p.tiles) --chunks;
     if (chunks < 2) return;

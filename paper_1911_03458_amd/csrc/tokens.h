@@ -87,9 +87,8 @@ struct ScanParams {
     float *part_a;         // [B * chunks][D * N + 2 D]: dA, dskip, ddt_bias of a sequence's chunk
     float *dA, *dskip, *ddt_bias;
 };
-// states of a channel that a lane holds, and lanes of a channel
-constexpr int scan_spl(int N) { return N == 1 ? 1 : 4; }
-constexpr int scan_lpc(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
+// lanes of a channel (scan.h: by_states)
+constexpr int scan_lpc(int N) { return N == 1 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 constexpr int SCAN_THREADS = 256;
 
 }  // namespace merit
