@@ -127,13 +127,13 @@ __device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, co
 // A barrier for LDS alone: loads from memory stay in flight across it, which a fence would wait for
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// log(1 + exp(v)) = max(v, 0) + log1p(exp(-|v|)); log1p by log(1 + e) e / ((1 + e) - 1), which keeps the digits of a
-// small e that the sum cuts off
+// log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|); log1p(e) = log(u) + (e - (u - 1)) / u, u the rounded 1 + e, which
+// gives back the digits of a small e that the sum cuts off
 __device__ __forceinline__ float softplusf(float v)
 {
-    const float e = __builtin_amdgcn_exp2f(-LOG2E * __builtin_fabsf(v)), u = 1.0f + e, d = u - 1.0f;
-    const float l = d > 0.0f ? __builtin_amdgcn_logf(u) * (1.0f / LOG2E) * (e * __builtin_amdgcn_rcpf(d)) : e;
-    return v != v ? v : fmaxf(v, 0.0f) + l;
+    const float e = __builtin_amdgcn_exp2f(-LOG2E * __builtin_fabsf(v)), u = 1.0f + e;
+    const float lost = e - (u - 1.0f);
+    return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(u), 1.0f / LOG2E, lost * __builtin_amdgcn_rcpf(u));
 }
 
 #define MERIT_DPP(v, ctrl) __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), ctrl, 0xF, 0xF, true))
