@@ -207,6 +207,19 @@ template <int SPL> __device__ __forceinline__ void write_states(float *at, const
     else at[0] = v[0];
 }
 
+// the same to memory, where a state need not start on more than its own boundary
+template <int SPL> __device__ __forceinline__ void store_states(float *at, const float (&v)[SPL])
+{
+    typedef float vec __attribute__((ext_vector_type(SPL == 1 ? 2 : SPL), aligned(4)));
+    if constexpr (SPL == 1) at[0] = v[0];
+    else {
+        vec q;
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) q[s] = v[s];
+        *reinterpret_cast<vec *>(at) = q;
+    }
+}
+
 // A state (or its adjoint) through `count` chunks from `q` on: their decay, then what they add.  Four chunks' loads go out
 // together.
 template <int SPL>

@@ -159,31 +159,44 @@ template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_
 
 template <typename T> __device__ __forceinline__ float load_el(const void *base, int64_t at) { return (float)static_cast<const T *>(base)[at]; }
 
+// One token: the state is read and written once, 8 bytes a state, and that is what bounds it (32 x 2048 channels, 16 states: 9 MB).
+// Every load goes out before the first value is used; lanes without a channel or a state read what their neighbours do.
 template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(NT) void merit_scan_token(ScanParams p)
 {
-    const int64_t id = (int64_t)blockIdx.x * NT + threadIdx.x, row = id / LPC;
-    const int lane = (int)id & (LPC - 1), n0 = lane * SPL;
-    const bool in = row < p.B * p.D;
-    const int64_t b = in ? row / p.D : 0;
-    const int d = in ? (int)(row - b * p.D) : 0, g = d / p.Dg;
-    const int64_t hat = (b * p.D + d) * p.N + n0;
-    const float v = load_el<T>(p.dt.data, b * p.dt.s0 + d) + (p.dt_bias ? p.dt_bias[d] : 0.0f);
-    const float x = load_el<T>(p.x.data, b * p.x.s0 + d), z = p.z.data ? load_el<T>(p.z.data, b * p.z.s0 + d) : 0.0f;
-    const float dt = p.softplus ? softplusf(v) : v, dx = dt * x;
+    const int64_t id = (int64_t)blockIdx.x * NT + threadIdx.x, rows = p.B * p.D, row = min(id / LPC, rows - 1);
+    const int lane = (int)threadIdx.x & (LPC - 1), n0 = lane * SPL;
+    const bool in = id / LPC < rows;
+    const uint32_t b = (uint32_t)((uint64_t)row / (uint32_t)p.D);
+    const int d = (int)(row - (int64_t)b * p.D), g = d / p.Dg;
+    float A[SPL], h[SPL], Bv[SPL], Cv[SPL];
+#pragma unroll
+    for (int s = 0; s < SPL; ++s) {
+        const int n = PAD ? min(n0 + s, p.N - 1) : n0 + s;
+        A[s] = p.A[(int64_t)d * p.N + n];
+        h[s] = p.h0[row * p.N + n];
+        Bv[s] = load_el<T>(p.Bm.data, b * p.Bm.s0 + (int64_t)g * p.N + n);
+        Cv[s] = load_el<T>(p.Cm.data, b * p.Cm.s0 + (int64_t)g * p.N + n);
+    }
+    const float x = load_el<T>(p.x.data, b * p.x.s0 + d), raw = load_el<T>(p.dt.data, b * p.dt.s0 + d);
+    const float z = p.z.data ? load_el<T>(p.z.data, b * p.z.s0 + d) : 0.0f;
+    const float bias = p.dt_bias ? p.dt_bias[d] : 0.0f, skip = p.skip ? p.skip[d] : 0.0f;
+    const float v = raw + bias, dt = p.softplus ? softplusf(v) : v, dx = dt * x;
     float acc = 0.0f;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
-        if (!in || (PAD && n0 + s >= p.N)) continue;
-        const float a = __builtin_amdgcn_exp2f(dt * p.A[(int64_t)d * p.N + n0 + s] * LOG2E);
-        const float h = fmaf(a, p.h0[hat + s], dx * load_el<T>(p.Bm.data, b * p.Bm.s0 + (int64_t)g * p.N + n0 + s));
-        p.h_last[hat + s] = h;
-        acc = fmaf(h, load_el<T>(p.Cm.data, b * p.Cm.s0 + (int64_t)g * p.N + n0 + s), acc);
+        h[s] = fmaf(__builtin_amdgcn_exp2f(dt * (A[s] * LOG2E)), h[s], dx * Bv[s]);
+        if (!PAD || n0 + s < p.N) acc = fmaf(h[s], Cv[s], acc);
     }
     acc = sum_channel<LPC>(acc);
-    if (!in || lane != 0) return;
-    float y = p.skip ? fmaf(p.skip[d], x, acc) : acc;
+    if (!in) return;
+    float y = p.skip ? fmaf(skip, x, acc) : acc;
     if (p.z.data) y *= siluf(z);
-    static_cast<T *>(p.y.data)[b * p.y.s0 + d] = (T)y;
+    if (lane == 0) static_cast<T *>(p.y.data)[b * p.y.s0 + d] = (T)y;
+    if (!PAD) store_states<SPL>(p.h_last + row * p.N + n0, h);
+    else
+#pragma unroll
+        for (int s = 0; s < SPL; ++s)
+            if (n0 + s < p.N) p.h_last[row * p.N + n0 + s] = h[s];
 }
 
 template <typename T> struct Forward {

@@ -189,6 +189,31 @@ def test_slices_and_broadcasts(mb):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("N", [16, 8, 4, 2, 5])
+def test_states_that_start_anywhere(mb, N):
+    """fp32 operands one element behind a 16-byte boundary, tensors of 16 bits behind an odd one."""
+    def off(t):
+        big = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        big[1:] = t.reshape(-1)
+        return big[1:].view(t.shape)
+
+    shape = (2, 35, 12, N, 2)
+    v = _inputs(shape, "f16", 12)
+    plan, plan1 = _plan(mb, shape, "f16"), _plan(mb, (2, 1, 12, N, 2), "f16")
+    u = {k: off(t) for k, t in v.items()}
+    names = ("skip", "z", "dt_bias", "h0", "lens")
+    results = []
+    for w in (v, u):
+        y, h, st = mb.merit_scan(plan, w["x"], w["dt"], w["A"], w["B"], w["C"], final=True, states=True, **_few(w, names))
+        g = mb.merit_scan_backward(plan, w["dy"], w["x"], w["dt"], w["A"], w["B"], w["C"], st if w is v else off(st), dh_last=w["dh"],
+                                   dh0=True, **_few(w, ("skip", "z", "dt_bias", "lens")))
+        s = mb.merit_scan_step(plan1, w["h0"], off(w["x"][:, 0]), off(w["dt"][:, 0]), w["A"], off(w["B"][:, 0]), off(w["C"][:, 0]),
+                               h_out=off(w["h0"]))
+        results.append([y, h, *g.values(), *s])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_what_lies_behind_an_end_is_not_read(mb):
     shape = (5, 40, 20, 16, 1)
     v = _inputs(shape, "f32", 6)
