@@ -15,6 +15,7 @@
 
 #include "merit.h"
 #include "merit_internal.h"
+#include "merit_tokens.h"
 
 namespace {
 
@@ -211,6 +212,65 @@ int sweep(uint64_t seed, int rounds)
     return made;
 }
 
+// the operators along a sequence of tokens: plans of any size, what they say, calls that end before a launch
+int take_tokens(merit_status st, merit_token_plan *plan)
+{
+    CHECK((st == MERIT_OK) == (plan != nullptr));
+    if (!plan) return 0;
+    int norm = 0;
+    for (int pass = 0; pass <= 3; ++pass) {
+        int64_t bytes = -1;
+        const char *name = nullptr;
+        const merit_status a = merit_token_plan_workspace(plan, (merit_pass)pass, &bytes);
+        const merit_status b = merit_token_plan_kernel(plan, (merit_pass)pass, &name);
+        CHECK(a == b && (a == MERIT_OK ? bytes >= 0 && name && std::strlen(name) > 0 : bytes <= 0));
+        if (pass == 2 && a != MERIT_OK) norm = 1;
+    }
+    // every operand absent: the first that is required (an empty batch: nothing to do)
+    merit_scan_backward_args none;
+    std::memset(static_cast<void *>(&none), 0, sizeof(none));
+    const void *v = &none;
+    int taken = 0;
+    auto refused = [&](merit_status st) {
+        CHECK(st == MERIT_ERR_NULL || st == MERIT_ERR_INVALID_ARG || st == MERIT_OK);
+        taken += st != MERIT_ERR_INVALID_ARG;
+    };
+    refused(merit_causal_conv_step(plan, static_cast<const merit_causal_conv_step_args *>(v), nullptr, 0, nullptr));
+    refused(merit_scan_step(plan, static_cast<const merit_scan_step_args *>(v), nullptr, 0, nullptr));
+    CHECK(taken == 1 - norm);
+    CHECK(merit_token_plan_destroy(plan) == MERIT_OK);
+    return 1;
+}
+
+int sweep_tokens(uint64_t seed, int rounds)
+{
+    Rng r{seed};
+    int made = 0;
+    auto size = [&](int bits) { return (int64_t)(r.next() & ((1ull << r.in(0, bits)) - 1)); };
+    for (int i = 0; i < rounds; ++i) {
+        const merit_dtype type = (merit_dtype)r.in(0, 3);
+        merit_token_plan *p = nullptr;
+        const int64_t G = r.in(0, 40);
+        merit_status st = merit_plan_group_norm(type, size(33) - 1, size(33) - 1, G * size(20) + r.in(0, 1), G, r.in(-1, 3) * 1e-5,
+                                                (merit_act)r.in(0, 3), &p);
+        made += take_tokens(st, p);
+        p = nullptr;
+        st = merit_plan_causal_conv(type, size(33) - 1, size(33) - 1, size(26), r.in(0, 9), (merit_act)r.in(0, 3), &p);
+        made += take_tokens(st, p);
+        p = nullptr;
+        st = merit_plan_scan(type, size(33) - 1, size(33) - 1, G * size(20), r.in(0, 66), G, r.in(0, 1), &p);
+        made += take_tokens(st, p);
+        // ordinary sizes
+        p = nullptr;
+        made += take_tokens(merit_plan_group_norm(MERIT_BF16, size(15), 1 + size(14), 8 * (1 + size(8)), 8, 1e-5, MERIT_ACT_SILU, &p), p);
+        p = nullptr;
+        made += take_tokens(merit_plan_causal_conv(MERIT_F16, size(6), size(15), 1 + size(12), 4, MERIT_ACT_SILU, &p), p);
+        p = nullptr;
+        made += take_tokens(merit_plan_scan(MERIT_F32, size(6), size(15), 4 * (1 + size(10)), 1 + (int64_t)r.in(0, 63), 4, 1, &p), p);
+    }
+    return made;
+}
+
 }  // namespace
 
 int main(int argc, char **argv)
@@ -219,7 +279,7 @@ int main(int argc, char **argv)
     int made = 0;
     check_moves();
     if (nthreads <= 1) {
-        made = sweep(1911, 120);
+        made = sweep(1911, 120) + sweep_tokens(1911, 400);
     } else {
         // one plan shared by every thread (queries only: merit.h allows that), next to the
         // private sweeps
@@ -229,7 +289,7 @@ int main(int argc, char **argv)
         std::vector<int> counts((size_t)nthreads, 0);
         for (int t = 0; t < nthreads; ++t)
             pool.emplace_back([&, t] {
-                counts[(size_t)t] = sweep(1911 + 7 * (uint64_t)t, 25);
+                counts[(size_t)t] = sweep(1911 + 7 * (uint64_t)t, 25) + sweep_tokens(1911 + 7 * (uint64_t)t, 50);
                 for (int k = 0; k < 200; ++k) {
                     merit_launch_info li;
                     int32_t nd;

@@ -14,6 +14,9 @@ namespace {
 constexpr int64_t MAX_CHANNELS = 1 << 24, MAX_ROWS = std::numeric_limits<int32_t>::max() - 1023;   // (rows are counted in 32 bits, past the last by up to four of a workgroup's)
 constexpr int64_t MAX_BLOCKS = 1 << 24;                 // of 256 threads: 2^32 threads a launch
 
+// elements of a tensor at most: scratch memory in bytes and every offset stay far from 2^63
+bool too_large(int64_t a, int64_t b, int64_t c) { return a != 0 && b != 0 && a > (1ll << 46) / b / c; }
+
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int elem_bytes(int type) { return type == MERIT_F32 ? 4 : 2; }
 bool type_ok(int type) { return type == MERIT_F16 || type == MERIT_BF16 || type == MERIT_F32; }
@@ -225,7 +228,7 @@ merit_status merit_plan_group_norm(merit_dtype type, int64_t N, int64_t S, int64
         !std::isfinite(eps))
         return MERIT_ERR_INVALID_ARG;
     if (C % groups != 0) return MERIT_ERR_SHAPE;
-    if (C > MAX_CHANNELS || N > MAX_ROWS || S > MAX_ROWS) return MERIT_ERR_UNSUPPORTED;
+    if (C > MAX_CHANNELS || N > MAX_ROWS || S > MAX_ROWS || too_large(N, S, C)) return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(NORM, type);
     if (!pl) return MERIT_ERR_INVALID_ARG;
     NormParams &p = pl->norm;
@@ -252,7 +255,8 @@ merit_status merit_plan_causal_conv(merit_dtype type, int64_t B, int64_t L, int6
     if (!out) return MERIT_ERR_NULL;
     *out = nullptr;
     if (!type_ok(type) || (int)act < 0 || (int)act > 2 || B < 0 || L < 0 || D < 1 || K < 1) return MERIT_ERR_INVALID_ARG;
-    if (K > MERIT_CONV_MAX_TAPS || D > MAX_CHANNELS || B > MAX_ROWS || L > MAX_ROWS) return MERIT_ERR_UNSUPPORTED;
+    if (K > MERIT_CONV_MAX_TAPS || D > MAX_CHANNELS || B > MAX_ROWS || L > MAX_ROWS || too_large(B, L, D))
+        return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(CONV, type);
     if (!pl) return MERIT_ERR_INVALID_ARG;
     CconvParams &p = pl->conv;
@@ -279,7 +283,8 @@ merit_status merit_plan_scan(merit_dtype type, int64_t B, int64_t L, int64_t D, 
     *out = nullptr;
     if (!type_ok(type) || B < 0 || L < 0 || D < 1 || N < 1 || groups < 1) return MERIT_ERR_INVALID_ARG;
     if (D % groups != 0) return MERIT_ERR_SHAPE;
-    if (N > MERIT_SCAN_MAX_STATES || D > MAX_CHANNELS || B > MAX_ROWS || L > MAX_ROWS) return MERIT_ERR_UNSUPPORTED;
+    if (N > MERIT_SCAN_MAX_STATES || D > MAX_CHANNELS || B > MAX_ROWS || L > MAX_ROWS || too_large(B, L, D))
+        return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(SCAN, type);
     if (!pl) return MERIT_ERR_INVALID_ARG;
     ScanParams &p = pl->scan;
