@@ -32,7 +32,7 @@ struct Where {
     int tend;              // the first of them that has no token of the sequence
 };
 // The workgroup's part: `chunks` chunks of every sequence, from `first` on
-template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, int first, int chunks)
+template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, int first, int chunks, int thread)
 {
     Where w;
     uint32_t r = blockIdx.x;
@@ -42,8 +42,8 @@ template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, i
     r /= (uint32_t)p.G;
     w.chunk = first + (int)(r % (uint32_t)chunks);
     w.b = r / (uint32_t)chunks;
-    const int cl = w.ct * (NT / LPC) + (int)threadIdx.x / LPC;
-    w.lane = (int)threadIdx.x & (LPC - 1);
+    const int cl = w.ct * (NT / LPC) + thread / LPC;
+    w.lane = thread & (LPC - 1);
     w.tok = w.lane & 3;
     w.in = cl < p.Dg;
     w.d = w.g * p.Dg + min(cl, p.Dg - 1);
@@ -54,11 +54,11 @@ template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, i
     return w;
 }
 
-// How the kernels move tiles.  Loads go out a tile before their use and stay raw (a 16-bit element in the low half) until
+// How the kernels move tiles.  Loads go out two tiles before their use (backward one) and stay raw (a 16-bit element in the low half) until
 // then.  Loads and stores share one counter and the wait for a load waits for what was issued before it, so a tile's results
 // are written while the next tile is under way, before its own loads are issued: a store is never younger than a load that
 // is waited for.  The barrier between staging and reading LDS waits for LDS alone (lds_barrier).
-// (Results written at once and a barrier that waits for everything: 8x2048x2048, 16 states, MEASURED_BEFORE us.)
+// (Results written at once and a barrier that waits for everything took a forward pass from 263 to 373 us.)
 // A tensor as a lane walks it: the address (in global memory: a flat load would count as one from LDS too) of its first
 // element of tile 0, bytes from token to token.
 typedef __attribute__((address_space(1))) char *gptr;
@@ -73,10 +73,10 @@ template <typename T> __device__ __forceinline__ Walk walk_rows(const Rows &r, c
     return Walk{(gptr)r.data + (w.b * r.s0 + w.tok * r.s1 + w.d) * es, r.s1 * es};
 }
 // (thread e of a tile's TT x NP elements of B or C, further ones NT elements on)
-template <typename T, int NP> __device__ __forceinline__ Walk walk_states(const Rows &r, const ScanParams &p, const Where &w)
+template <typename T, int NP> __device__ __forceinline__ Walk walk_states(const Rows &r, const ScanParams &p, const Where &w, int thread)
 {
     constexpr int64_t es = sizeof(T);
-    const int e = (int)threadIdx.x & (TT * NP - 1);
+    const int e = thread & (TT * NP - 1);
     return Walk{(gptr)r.data + (w.b * r.s0 + (e / NP) * r.s1 + w.g * p.N + min(e % NP, p.N - 1)) * es, r.s1 * es};
 }
 // COUNT elements, `every` tokens apart, the first token `first` of tile `tile`.  WHOLE: all of the tile's tokens are there
@@ -112,14 +112,14 @@ template <typename T, int COUNT> __device__ __forceinline__ void values(const ra
 }
 
 template <typename T, int SPL, int LPC>
-__device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, const Where &w, int tile, const raw_t<T> (&raw)[Shape<SPL, LPC>::EB])
+__device__ __forceinline__ void stage_states(float *lds, const ScanParams &p, const Where &w, int thread, int tile, const raw_t<T> (&raw)[Shape<SPL, LPC>::EB])
 {
     constexpr int NP = Shape<SPL, LPC>::NP;
     float v[Shape<SPL, LPC>::EB];
     values<T>(raw, v);
 #pragma unroll
     for (int i = 0; i < Shape<SPL, LPC>::EB; ++i) {
-        const int e = i * NT + (int)threadIdx.x;
+        const int e = i * NT + thread;
         if (e < TT * NP) lds[e] = e % NP < p.N && tile * TT + e / NP < w.n ? v[i] : 0.0f;
     }
 }

@@ -3,11 +3,15 @@
 //     h_t[d,n] = exp(s A[d,n]) h_{t-1}[d,n] + s x B_t[n]
 //     y[t,d]   = (sum_n C_t[n] h_t[d,n] + skip[d] x) silu(z)
 // Per state and token an exponential, two products, two multiply-adds: bound by the vector ALUs at 16 states (4 tensors of
-// 2 bytes a channel and token against 16 exponentials), by memory below about 8.
+// 2 bytes a channel and token against 16 exponentials), by memory below about 4.
 // A lane has four states of a channel, N / 4 lanes a channel, 256 threads 1024 / N channels of one sequence; tokens go in
-// tiles of 16.  Of a tile a lane loads x, dt and z of every N / 4-th token, so that steps and gates are computed once; a
-// token's values reach the channel's other lanes inside the multiplying instructions (DPP).  B and C of a tile, the same
-// for all channels, are staged in LDS as fp32.
+// tiles of 16.  Steps, gates and the movement of x, dt, z and y, once per token and channel, are the work of 256 threads more.
+// A token's step reaches the channel's lanes inside the multiplying instruction (DPP); B and C of a tile, the same for all
+// channels, are staged in LDS as fp32.
+// Measured (bfloat16, gated, 16 states): 8x2048x2048 176 us (271 MB: 1.5 TB/s; 0.54 G states x tokens: 3.1 T/s, exponentials and
+// plain operations alone would allow 7.9 T/s); 1x8191x2048 in 16 chunks 84 us and 56 us for the chunks' first states.
+// Without the second half of the workgroup, its work done by the first: 235 us, and 104 + 64.
+#include "merit_internal.h"
 #include "scan.h"
 
 namespace merit {
@@ -20,13 +24,124 @@ namespace {
 // that it adds (from a state of 0) and the sum of its steps, from which the next launch's chunks find their first states
 enum { RESULTS, KEEP_STATES, CHUNK_STATES };
 
-template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_bounds__(NT) void merit_scan_tiles(ScanParams p)
+// LDS of a workgroup, in floats, twice each for alternating tiles: (step, step x) and sums of 16 tokens x CPB channels, B and C
+template <int SPL, int LPC> struct Room {
+    using S = Shape<SPL, LPC>;
+    static constexpr int PITCH = S::CPB + 8;               // (lanes that read neighbouring tokens: other banks)
+    static constexpr int TOKENS = TT * PITCH * 2, SUMS = TT * PITCH, STATES = TT * S::NP;
+    static constexpr int BYTES = 4 * 2 * (TOKENS + SUMS + 2 * STATES);
+};
+
+// A workgroup is two halves.  The first 256 threads run the recurrence: they read steps, B and C from LDS and leave the tokens'
+// sums there.  The other 256 do what is done once per token and channel -- loads from memory, steps, gates, results --
+// a tile ahead of the first half and a tile behind it.  So a SIMD has a wavefront of either kind, and one's waits are the other's
+// arithmetic; the recurrence itself has no loads from memory to wait for.
+template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_bounds__(2 * NT) void merit_scan_tiles(ScanParams p)
 {
     using S = Shape<SPL, LPC>;
+    using R = Room<SPL, LPC>;
     constexpr bool KEEP = WHAT == KEEP_STATES, SUMS = WHAT == CHUNK_STATES;
-    __shared__ __align__(16) float bl[2][TT * S::NP], cl[SUMS ? 1 : 2][SUMS ? 4 : TT * S::NP];
-    const Where w = where<LPC>(p, 0, SUMS ? p.chunks - 1 : p.chunks);
-    const int n0 = w.lane * SPL;
+    extern __shared__ __align__(16) float lds[];
+    float *const tokens = lds, *const sums = tokens + 2 * R::TOKENS, *const bl = sums + 2 * R::SUMS, *const cl = bl + 2 * R::STATES;
+    Where w = where<LPC>(p, 0, SUMS ? p.chunks - 1 : p.chunks, (int)threadIdx.x & (NT - 1));
+    const int count = max(0, w.tend - w.tile0);            // tiles; a step for each, one before and one after them
+
+    if (threadIdx.x >= NT) {
+        constexpr int IP = TT / LPC;                        // tokens of a tile that a thread has: first, first + LPC, ...
+        const int thread = (int)threadIdx.x - NT, c = thread % S::CPB, first = thread / S::CPB;
+        w.d = w.g * p.Dg + min(w.ct * S::CPB + c, p.Dg - 1);
+        w.tok = first;
+        const float bias = p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = p.skip ? p.skip[w.d] : 0.0f;
+        const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), zw = p.z.data ? walk_rows<T>(p.z, w) : xw,
+                   yw = walk_rows<T>(p.y, w), bw = walk_states<T, S::NP>(p.Bm, p, w, thread), cw = walk_states<T, S::NP>(p.Cm, p, w, thread);
+        struct Raw {
+            raw_t<T> x[IP], dt[IP], z[IP], b[S::EB], c[S::EB];
+        };
+        Raw raw[4];                                         // tiles i, i + 4, ...: from their loads to their results
+        float steps = 0.0f;
+        auto fetch = [&](Raw &r, int tile, auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            const int state = (thread & (TT * S::NP - 1)) / S::NP;
+            load_walk<T, WHOLE>(xw, tile, LPC, first, w.n - 1, r.x);
+            load_walk<T, WHOLE>(dw, tile, LPC, first, w.n - 1, r.dt);
+            if (!SUMS) load_walk<T, WHOLE>(zw, tile, LPC, first, w.n - 1, r.z);
+            load_walk<T, WHOLE>(bw, tile, NT / S::NP, state, w.n - 1, r.b);
+            if (!SUMS) load_walk<T, WHOLE>(cw, tile, NT / S::NP, state, w.n - 1, r.c);
+        };
+        // Step s: results of tile s - 2 (kept in `last`), tile s made ready from `now`, tile s + 2 asked for (into `last`).
+        // all: these tiles are there and whole
+        auto step = [&](int s, Raw &now, Raw &last, auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            const int tile = w.tile0 + s;
+            if (!SUMS && (ALL || s >= 2)) {
+                float x[IP], z[IP], y[IP];
+                values<T>(last.x, x);
+                values<T>(last.z, z);
+#pragma unroll
+                for (int i = 0; i < IP; ++i) {
+                    y[i] = sums[(s & 1) * R::SUMS + (first + i * LPC) * R::PITCH + c];
+                    if (p.skip) y[i] = fmaf(skip, x[i], y[i]);          // (absent: not 0 times an infinite x)
+                    if (p.z.data) y[i] *= siluf(z[i]);
+                    if (!ALL && (tile - 2) * TT + first + i * LPC >= w.n) y[i] = 0.0f;
+                }
+                store_walk<T, ALL>(yw, tile - 2, LPC, first, p.L, y);
+            }
+            if (ALL || s < count) {
+                float x[IP], dt[IP];
+                values<T>(now.x, x);
+                values<T>(now.dt, dt);
+                float *const to = tokens + (s & 1) * R::TOKENS;
+#pragma unroll
+                for (int i = 0; i < IP; ++i) {
+                    const bool in = ALL || tile * TT + first + i * LPC < w.n;
+                    const float v = dt[i] + bias;
+                    dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
+                    steps += dt[i];
+                    *reinterpret_cast<float2 *>(to + 2 * ((first + i * LPC) * R::PITCH + c)) = make_float2(dt[i], in ? dt[i] * x[i] : 0.0f);
+                }
+                stage_states<T, SPL, LPC>(bl + (s & 1) * R::STATES, p, w, thread, tile, now.b);
+                if constexpr (!SUMS) stage_states<T, SPL, LPC>(cl + (s & 1) * R::STATES, p, w, thread, tile, now.c);
+            }
+            if (ALL) fetch(last, tile + 2, all);
+            else if (count) fetch(last, min(tile + 2, w.tend - 1), all);
+            lds_barrier();
+        };
+        if (count) {
+            fetch(raw[0], w.tile0, std::false_type{});
+            fetch(raw[1], min(w.tile0 + 1, w.tend - 1), std::false_type{});
+        }
+        const int total = count + 2, whole = min(w.tend, w.n / TT) - w.tile0;       // tiles 0 ... whole - 1 are whole
+        step(0, raw[0], raw[2], std::false_type{});
+        step(1, raw[1], raw[3], std::false_type{});
+        int s = 2;
+        for (; s + 5 < whole; s += 4) {
+            step(s, raw[2], raw[0], std::true_type{});
+            step(s + 1, raw[3], raw[1], std::true_type{});
+            step(s + 2, raw[0], raw[2], std::true_type{});
+            step(s + 3, raw[1], raw[3], std::true_type{});
+        }
+        for (; s < total; s += 4) {
+            step(s, raw[2], raw[0], std::false_type{});
+            if (s + 1 < total) step(s + 1, raw[3], raw[1], std::false_type{});
+            if (s + 2 < total) step(s + 2, raw[0], raw[2], std::false_type{});
+            if (s + 3 < total) step(s + 3, raw[1], raw[3], std::false_type{});
+        }
+        if (SUMS) {                                         // the chunk's steps, over the threads of a channel
+            tokens[first * S::CPB + c] = steps;
+            lds_barrier();
+            if (first == 0) {
+#pragma unroll
+                for (int i = 1; i < LPC; ++i) steps += tokens[i * S::CPB + c];
+                p.chunk_dt[(w.b * p.chunks + w.chunk) * p.D + w.d] = steps;
+            }
+        } else {
+            for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + first; t < min((int64_t)w.tile1 * TT, p.L); t += LPC)
+                static_cast<T *>(p.y.data)[w.b * p.y.s0 + t * p.y.s1 + w.d] = (T)0.0f;
+        }
+        return;
+    }
+
+    const int n0 = w.lane * SPL, c = (int)threadIdx.x / LPC;
     float A[SPL], h[SPL];
     bool ok[SPL];
     const int64_t hat = (w.b * p.D + w.d) * p.N + n0;
@@ -36,61 +151,34 @@ template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_
         A[s] = ok[s] ? p.A[(int64_t)w.d * p.N + n0 + s] * LOG2E : 0.0f;
         h[s] = !SUMS && ok[s] && p.h0 ? p.h0[hat + s] : 0.0f;
     }
-    float steps = 0.0f;
     if (!SUMS) through_chunks<SPL>(p, w, n0, A, ok, h, 0, w.chunk, 1);
-    const float bias = p.dt_bias ? p.dt_bias[w.d] : 0.0f, skip = p.skip ? p.skip[w.d] : 0.0f;
-    const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), zw = p.z.data ? walk_rows<T>(p.z, w) : xw,
-               yw = walk_rows<T>(p.y, w), bw = walk_states<T, S::NP>(p.Bm, p, w), cw = walk_states<T, S::NP>(p.Cm, p, w);
-
-    // Two tiles in flight: a tile's arithmetic is over before a load of it comes back
-    struct Raw {
-        raw_t<T> x[S::TPL], dt[S::TPL], z[S::TPL], b[S::EB], c[S::EB];
-    };
-    Raw even, odd;
-    auto fetch = [&](Raw &r, int tile, auto whole) {
-        constexpr bool WHOLE = decltype(whole)::value;
-        load_walk<T, WHOLE>(xw, tile, S::LQ, w.tok, w.n - 1, r.x);
-        load_walk<T, WHOLE>(dw, tile, S::LQ, w.tok, w.n - 1, r.dt);
-        if (!SUMS) load_walk<T, WHOLE>(zw, tile, S::LQ, w.tok, w.n - 1, r.z);
-        const int first = ((int)threadIdx.x & (TT * S::NP - 1)) / S::NP;
-        load_walk<T, WHOLE>(bw, tile, NT / S::NP, first, w.n - 1, r.b);
-        if (!SUMS) load_walk<T, WHOLE>(cw, tile, NT / S::NP, first, w.n - 1, r.c);
-    };
-    float out[S::TPL];                          // results of the tile before
-    // all: this tile and the one after the next are whole
-    auto run = [&](Raw &r, float *bt, float *ct, int tile, auto all) {
-        constexpr bool ALL = decltype(all)::value;
-        stage_states<T, SPL, LPC>(bt, p, w, tile, r.b);
-        if constexpr (!SUMS) stage_states<T, SPL, LPC>(ct, p, w, tile, r.c);
-        float x[S::TPL], z[S::TPL], dt[S::TPL], dx[S::TPL], y[S::TPL];
-        values<T>(r.x, x);
-        if constexpr (!SUMS) values<T>(r.z, z);
-        values<T>(r.dt, dt);
-#pragma unroll
-        for (int i = 0; i < S::TPL; ++i) {
-            const bool in = ALL || tile * TT + i * S::LQ + w.tok < w.n;
-            const float v = dt[i] + bias;
-            dt[i] = in ? (p.softplus ? softplusf(v) : v) : 0.0f;
-            dx[i] = in ? dt[i] * x[i] : 0.0f;
-            steps += dt[i];
-        }
-        if (!SUMS && tile > w.tile0) store_walk<T, true>(yw, tile - 1, S::LQ, w.tok, p.L, out);
+    lds_barrier();
+    for (int i = 0; i < count; ++i) {
+        const int tile = w.tile0 + i;
+        const float *const bt = bl + (i & 1) * R::STATES + n0, *const ct = cl + (i & 1) * R::STATES + n0,
+                    *const tt = tokens + (i & 1) * R::TOKENS + 2 * (w.tok * R::PITCH + c);
+        float *const st = sums + (i & 1) * R::SUMS + w.tok * R::PITCH + c;
         if (KEEP) {
             float *o = p.states + ((w.b * p.tiles + tile) * p.D + w.d) * p.N + n0;
 #pragma unroll
             for (int s = 0; s < SPL; ++s)
                 if (!PAD || ok[s]) o[s] = h[s];
         }
-        fetch(r, ALL ? tile + 2 : min(tile + 2, w.tend - 1), all);
-        lds_barrier();
+        float dt[S::TPL], dx[S::TPL];
+#pragma unroll
+        for (int k = 0; k < S::TPL; ++k) {
+            const float2 v = *reinterpret_cast<const float2 *>(tt + 2 * k * S::LQ * R::PITCH);
+            dt[k] = v.x;
+            dx[k] = v.y;
+        }
         // Four tokens at a time; what needs LDS or an exponential is asked for four tokens ahead
         float Bv[2][4][SPL], Cv[2][4][SPL], a[2][4][SPL];
         auto ahead = [&](int k) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int t = 4 * k + u;
-                read_states<SPL>(bt + t * S::NP + n0, Bv[k & 1][u]);
-                if (!SUMS) read_states<SPL>(ct + t * S::NP + n0, Cv[k & 1][u]);
+                read_states<SPL>(bt + t * S::NP, Bv[k & 1][u]);
+                if (!SUMS) read_states<SPL>(ct + t * S::NP, Cv[k & 1][u]);
                 const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ);
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) a[k & 1][u][s] = __builtin_amdgcn_exp2f(dtv * A[s]);
@@ -101,7 +189,7 @@ template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_
         for (int k = 0; k < TT / 4; ++k) {
             __builtin_amdgcn_sched_barrier(0);
             if (k + 1 < TT / 4) ahead(k + 1);
-            float acc[4];
+            float acc[4], y[4 / S::LQ];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int t = 4 * k + u;
@@ -114,47 +202,21 @@ template <typename T, int SPL, int LPC, bool PAD, int WHAT> __global__ __launch_
                     if (!SUMS) acc[u] = fmaf(h[s], Cv[k & 1][u][s], acc[u]);
                 }
             }
-            if (!SUMS) sum_to_tokens<LPC>(acc, y + 4 * k / S::LQ);
-        }
-        if (SUMS) return;
+            if (SUMS) continue;
+            sum_to_tokens<LPC>(acc, y);
 #pragma unroll
-        for (int i = 0; i < S::TPL; ++i) {
-            if (p.skip) y[i] = fmaf(skip, x[i], y[i]);          // (absent: not 0 times an infinite x)
-            if (p.z.data) y[i] *= siluf(z[i]);
-            out[i] = ALL || tile * TT + i * S::LQ + w.tok < w.n ? y[i] : 0.0f;
+            for (int j = 0; j < 4 / S::LQ; ++j) st[(4 * k + j * S::LQ) * R::PITCH] = y[j];
         }
-    };
-    if (w.tile0 < w.tend) {
-        fetch(even, w.tile0, std::false_type{});
-        fetch(odd, min(w.tile0 + 1, w.tend - 1), std::false_type{});
-        const int whole = min(w.tend, w.n / TT);                // tiles before this one are whole
-        int tile = w.tile0;
-        for (; tile + 3 < whole; tile += 2) {
-            run(even, bl[0], cl[0], tile, std::true_type{});
-            run(odd, bl[1], cl[SUMS ? 0 : 1], tile + 1, std::true_type{});
-        }
-        for (; tile < w.tend; tile += 2) {
-            run(even, bl[0], cl[0], tile, std::false_type{});
-            if (tile + 1 < w.tend) run(odd, bl[1], cl[SUMS ? 0 : 1], tile + 1, std::false_type{});
-        }
-        if (!SUMS) store_walk<T, false>(yw, w.tend - 1, S::LQ, w.tok, p.L, out);
+        lds_barrier();
     }
-    if (SUMS) {
-        const int64_t at = (w.b * p.chunks + w.chunk) * p.D + w.d;
-        steps = sum_channel<S::LQ>(steps);      // (a channel's further quads have the same tokens)
-        if (w.lane == 0) p.chunk_dt[at] = steps;
+    lds_barrier();
+    if (SUMS) lds_barrier();                                // (the other half adds up the steps)
+    float *const out = SUMS ? p.chunk_h + ((w.b * p.chunks + w.chunk) * p.D + w.d) * p.N + n0
+                            : p.h_last && w.chunk == p.chunks - 1 ? p.h_last + hat : nullptr;
+    if (out)
 #pragma unroll
         for (int s = 0; s < SPL; ++s)
-            if (ok[s]) p.chunk_h[at * p.N + n0 + s] = h[s];
-        return;
-    }
-    for (int64_t t = (int64_t)max(w.tend, w.tile0) * TT + w.lane; t < min((int64_t)w.tile1 * TT, p.L); t += LPC)
-        static_cast<T *>(p.y.data)[w.b * p.y.s0 + t * p.y.s1 + w.d] = (T)0.0f;
-    if (p.h_last && w.chunk == p.chunks - 1) {
-#pragma unroll
-        for (int s = 0; s < SPL; ++s)
-            if (ok[s]) p.h_last[hat + s] = h[s];
-    }
+            if (ok[s]) out[s] = h[s];
 }
 
 template <typename T> __device__ __forceinline__ float load_el(const void *base, int64_t at) { return (float)static_cast<const T *>(base)[at]; }
@@ -205,9 +267,19 @@ template <typename T> struct Forward {
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
         const unsigned per = (unsigned)(p.B * p.G * p.ctiles);
-        if (p.chunks > 1) merit_scan_tiles<T, SPL, LPC, PAD, CHUNK_STATES><<<per * (p.chunks - 1), NT, 0, s>>>(p);
-        if (p.states) merit_scan_tiles<T, SPL, LPC, PAD, KEEP_STATES><<<per * p.chunks, NT, 0, s>>>(p);
-        else merit_scan_tiles<T, SPL, LPC, PAD, RESULTS><<<per * p.chunks, NT, 0, s>>>(p);
+        if (p.chunks > 1) {
+            const hipError_t e = launch<SPL, LPC, PAD, CHUNK_STATES>(per * (p.chunks - 1));
+            if (e != hipSuccess) return e;
+        }
+        return p.states ? launch<SPL, LPC, PAD, KEEP_STATES>(per * p.chunks) : launch<SPL, LPC, PAD, RESULTS>(per * p.chunks);
+    }
+    template <int SPL, int LPC, bool PAD, int WHAT> hipError_t launch(unsigned grid)
+    {
+        static std::atomic<int> raised;
+        const auto kernel = merit_scan_tiles<T, SPL, LPC, PAD, WHAT>;
+        const hipError_t e = raise_lds_limit_once(reinterpret_cast<const void *>(kernel), raised);
+        if (e != hipSuccess) return e;
+        kernel<<<grid, 2 * NT, Room<SPL, LPC>::BYTES, s>>>(p);
         return hipGetLastError();
     }
 };

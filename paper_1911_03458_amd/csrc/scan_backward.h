@@ -88,7 +88,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
     extern __shared__ __align__(16) float lds[];
     float *const bl = lds, *const cl = bl + TT * S::NP, *const red = cl + TT * S::NP;
     float *const hl = red + NT / 64 * TT * 2 * S::NP + threadIdx.x * SPL;      // token t: t * NT * SPL further
-    const Where w = where<LPC>(p, 0, p.chunks);
+    const Where w = where<LPC>(p, 0, p.chunks, threadIdx.x);
     const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
     float A2[SPL], dA[SPL], carry[SPL];                     // (A2: the exponentials are to the base 2)
     bool ok[SPL];
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
     for (int64_t e = (int64_t)max(w.tend, w.tile0) * TT * 2 * p.N + threadIdx.x; e < min((int64_t)w.tile1 * TT, p.L) * 2 * p.N; e += NT) bc[e] = 0.0f;
 
     const Walk xw = walk_rows<T>(p.x, w), dw = walk_rows<T>(p.dt, w), yw = walk_rows<T>(p.dy, w),
-               zw = p.z.data ? walk_rows<T>(p.z, w) : xw, bw = walk_states<T, S::NP>(p.Bm, p, w),
-               cw = walk_states<T, S::NP>(p.Cm, p, w), dxw = walk_rows<T>(p.dx, w), ddw = walk_rows<T>(p.ddt, w),
+               zw = p.z.data ? walk_rows<T>(p.z, w) : xw, bw = walk_states<T, S::NP>(p.Bm, p, w, threadIdx.x),
+               cw = walk_states<T, S::NP>(p.Cm, p, w, threadIdx.x), dxw = walk_rows<T>(p.dx, w), ddw = walk_rows<T>(p.ddt, w),
                dzw = walk_rows<T>(p.dz, w);
     raw_t<T> xr[S::TPL], dr[S::TPL], yr[S::TPL], zr[S::TPL], br[S::EB], cr[S::EB];
     float hr[SPL];
@@ -159,8 +159,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
         values<T>(zr, gz);
         lds_barrier();              // (the tile before is done with bl and cl, and red is whole)
         if (tile + 1 < w.tend) write(tile + 1);
-        stage_states<T, SPL, LPC>(bl, p, w, tile, br);
-        stage_states<T, SPL, LPC>(cl, p, w, tile, cr);
+        stage_states<T, SPL, LPC>(bl, p, w, threadIdx.x, tile, br);
+        stage_states<T, SPL, LPC>(cl, p, w, threadIdx.x, tile, cr);
         float h[SPL], hs[SPL], a[TT][SPL];
 #pragma unroll
         for (int s = 0; s < SPL; ++s) h[s] = hs[s] = ok[s] ? hr[s] : 0.0f;
@@ -295,7 +295,7 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
 {
     using S = Shape<SPL, LPC>;
     __shared__ __align__(16) float cl[2][TT * S::NP];
-    const Where w = where<LPC>(p, 1, p.chunks - 1);
+    const Where w = where<LPC>(p, 1, p.chunks - 1, threadIdx.x);
     const int n0 = w.lane * SPL;
     float A[SPL], carry[SPL], steps = 0.0f;
     bool ok[SPL];
@@ -307,7 +307,7 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
     }
     const float bias = p.dt_bias ? p.dt_bias[w.d] : 0.0f;
     const Walk dw = walk_rows<T>(p.dt, w), yw = walk_rows<T>(p.dy, w), zw = p.z.data ? walk_rows<T>(p.z, w) : yw,
-               cw = walk_states<T, S::NP>(p.Cm, p, w);
+               cw = walk_states<T, S::NP>(p.Cm, p, w, threadIdx.x);
     struct Raw {
         raw_t<T> dt[S::TPL], dy[S::TPL], z[S::TPL], c[S::EB];
     };
@@ -321,7 +321,7 @@ template <typename T, int SPL, int LPC, bool PAD> __global__ __launch_bounds__(N
     };
     auto run = [&](Raw &r, float *ct, int tile, auto all) {
         constexpr bool ALL = decltype(all)::value;
-        stage_states<T, SPL, LPC>(ct, p, w, tile, r.c);
+        stage_states<T, SPL, LPC>(ct, p, w, threadIdx.x, tile, r.c);
         float dt[S::TPL], dy[S::TPL], z[S::TPL];
         values<T>(r.dt, dt);
         values<T>(r.dy, dy);

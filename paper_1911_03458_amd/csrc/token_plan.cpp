@@ -181,7 +181,7 @@ int64_t scan_part_bc(const ScanParams &p) { return (int64_t)p.G * p.ctiles * p.B
 int64_t scan_part_a(const ScanParams &p) { return p.B * p.chunks * ((int64_t)p.D * p.N + 2 * p.D); }
 // On few workgroups a sequence's chunks run side by side, two workgroups a compute unit, which takes a launch more and most of a
 // chunk's arithmetic twice.  Forward that pays up to three workgroups for four units (bfloat16, 16 states, 32 workgroups,
-// 8191 tokens: 169 us in 16 chunks, 875 in one; 256 workgroups, 2048 tokens: 272 in two, 237 in one), backward up to three for
+// 8191 tokens: 139 us in 16 chunks; 256 workgroups, 2048 tokens: 176 us in one piece, about 225 in two), backward up to three for
 // two units, since a chunk's first launch is a small part there (the latter: 614 in two, 719 in one).  A chunk is two tiles
 // at least, and there are at most 4 sqrt(tiles) of them: the last one passes through what all others left.  Below six tiles the
 // second launch costs more than it saves.
