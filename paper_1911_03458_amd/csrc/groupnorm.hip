@@ -245,7 +245,7 @@ template <int V> __device__ __forceinline__ Tile tile_of(const NormParams &p)
         t.piece = ct - t.g0 * t.pieces;
         t.cw = min(NT, cu - t.piece * NT);
     } else {
-        const int gt = min(p.G, NT / cu);
+        const int gt = p.group_tile;
         t.g0 = ct * gt;
         t.groups = min(gt, p.G - t.g0);
         t.piece = 0;
@@ -593,18 +593,22 @@ template <typename T, int V, int U, int NTH> __global__ __launch_bounds__(NTH) v
     float w[V], b[V];
     load_params<T>(p.w, s.in ? s.c : 0, 1.0f, w);
     load_params<T>(p.b, s.in ? s.c : 0, 0.0f, b);
+    // distances from a value of the group: next to a mean that is far from zero they keep all digits
+    const float k0 = shift_of<T>(p, s.n, s.g);
     float a = 0.0f, q = 0.0f;
 #pragma unroll
-    for (int k = 0; k < U; ++k)
+    for (int k = 0; k < U; ++k) {
+        const bool in = s.in && s.ty + k * s.rw < S;
 #pragma unroll
-        for (int i = 0; i < V; ++i) a += at<T, V>(v[k], i);     // (what is not there is 0)
-    const float inv = 1.0f / ((float)S * (float)p.Cg), mean = sum_block<NTH>(a, slots[0]) * inv;
+        for (int i = 0; i < V; ++i) a += in ? at<T, V>(v[k], i) - k0 : 0.0f;
+    }
+    const float inv = 1.0f / ((float)S * (float)p.Cg), off = sum_block<NTH>(a, slots[0]) * inv, mean = k0 + off;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         const bool in = s.in && s.ty + k * s.rw < S;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float d = in ? at<T, V>(v[k], i) - mean : 0.0f;
+            const float d = in ? (at<T, V>(v[k], i) - k0) - off : 0.0f;
             q = fmaf(d, d, q);
         }
     }
@@ -817,18 +821,29 @@ hipError_t launch_reduce_rows(const ReduceParams &p, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t launch_norm(const NormParams &p, int type, hipStream_t s)
+namespace {
+
+template <bool BACKWARD, typename T, int V> hipError_t norm_pass(const NormParams &p, hipStream_t s)
 {
-    if (type == MERIT_F32) return p.vec == 4 ? norm_forward<float, 4>(p, s) : norm_forward<float, 1>(p, s);
-    if (type == MERIT_F16) return p.vec == 8 ? norm_forward<f16_t, 8>(p, s) : norm_forward<f16_t, 1>(p, s);
-    return p.vec == 8 ? norm_forward<bf16_t, 8>(p, s) : norm_forward<bf16_t, 1>(p, s);
+    if constexpr (BACKWARD) return norm_backward<T, V>(p, s);
+    else return norm_forward<T, V>(p, s);
+}
+template <bool BACKWARD, typename T> hipError_t norm_typed(const NormParams &p, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (p.vec == 8) return norm_pass<BACKWARD, T, 8>(p, s);
+    if (p.vec == 4) return norm_pass<BACKWARD, T, 4>(p, s);
+    return p.vec == 2 ? norm_pass<BACKWARD, T, 2>(p, s) : norm_pass<BACKWARD, T, 1>(p, s);
+}
+template <bool BACKWARD> hipError_t norm_any(const NormParams &p, int type, hipStream_t s)
+{
+    if (type == MERIT_F32) return norm_typed<BACKWARD, float>(p, s);
+    return type == MERIT_F16 ? norm_typed<BACKWARD, f16_t>(p, s) : norm_typed<BACKWARD, bf16_t>(p, s);
 }
 
-hipError_t launch_norm_backward(const NormParams &p, int type, hipStream_t s)
-{
-    if (type == MERIT_F32) return p.vec == 4 ? norm_backward<float, 4>(p, s) : norm_backward<float, 1>(p, s);
-    if (type == MERIT_F16) return p.vec == 8 ? norm_backward<f16_t, 8>(p, s) : norm_backward<f16_t, 1>(p, s);
-    return p.vec == 8 ? norm_backward<bf16_t, 8>(p, s) : norm_backward<bf16_t, 1>(p, s);
-}
+}  // namespace
+
+hipError_t launch_norm(const NormParams &p, int type, hipStream_t s) { return norm_any<false>(p, type, s); }
+hipError_t launch_norm_backward(const NormParams &p, int type, hipStream_t s) { return norm_any<true>(p, type, s); }
 
 }  // namespace merit

@@ -82,12 +82,11 @@ merit_status scratch(int64_t need, void *workspace, int64_t bytes)
 merit_status done(hipError_t e) { return e == hipSuccess ? MERIT_OK : MERIT_ERR_HIP; }
 
 // ---- group norm ------------------------------------------------------------------------
-// groups from which on a workgroup each is the faster form
-constexpr int64_t NORM_SLAB_GROUPS = 64;
 // Column tiles and row chunks for `vec` channels a lane; returns the floats of scratch memory.
 int64_t norm_layout(NormParams &p, int vec, bool backward)
 {
     p.vec = vec;
+    p.slab = 0;
     const int cu = p.Cg / vec;
     p.rows_form = p.S == 1 && cu <= 1024;
     if (p.rows_form) {
@@ -101,8 +100,10 @@ int64_t norm_layout(NormParams &p, int vec, bool backward)
         p.chunk_rows = 1;
         return backward ? p.chunks * 2 * p.C : 0;
     }
-    p.slab = 0;
-    if (vec > 1 && p.N * p.G >= NORM_SLAB_GROUPS && cu <= 256 && p.S * cu >= 128) {
+    // A workgroup a group, where its registers hold the group's values (bfloat16, us a call, chunks / this: forward 1x196x512, 32
+    // groups 9.6 / 5.7, 4x3136x256 12.1 / 8.9, 2 groups of 1x784x64 8.9 / 5.8; backward with 32 groups and more 15.9 / 9.8 and
+    // 20.1 / 17.4, with 16 17.1 / 19.6, with 2 14.5 / 19.2).  Fewer than 128 units would leave most of its threads without one.
+    if (vec > 1 && (!backward || p.N * p.G >= 32) && cu <= 256 && p.S * cu >= 128) {
         for (int form : {0x104, 0x108, 0x404, 0x408}) {
             const int threads = form & 0x400 ? 1024 : 256, units = form & 0xFF;
             if (p.S > (int64_t)(threads / cu) * units) continue;
@@ -113,12 +114,18 @@ int64_t norm_layout(NormParams &p, int vec, bool backward)
             return backward ? p.N * 2 * p.C : 0;
         }
     }
-    const int pieces = (int)cdiv(cu, 256), gt = pieces > 1 ? 1 : (p.G < 256 / cu ? p.G : 256 / cu);
+    // Chunks: tiles of about 32 units side by side (512 bytes of a row), and so many row chunks that there are 1024 workgroups;
+    // not more than eight for each thread that joins them in the second launch.
+    const int pieces = (int)cdiv(cu, 256), fit = cu < 32 ? 32 / cu : 1, gt = pieces > 1 ? 1 : fit < p.G ? fit : p.G;
+    p.group_tile = gt;
     p.ctiles = pieces > 1 ? p.G * pieces : (int)cdiv(p.G, gt);
     const int rw = pieces > 1 ? 1 : 256 / (gt * cu);
+    int lanes = 64;
+    while (lanes * gt > 256) lanes /= 2;
     int64_t chunks = cdiv(1024, p.ctiles * (p.N > 0 ? p.N : 1));
     const int64_t most = cdiv(p.S, 4 * rw);
     if (chunks > most) chunks = most;
+    if (chunks > 8 * lanes) chunks = 8 * lanes;
     if (chunks < 1) chunks = 1;
     p.chunk_rows = cdiv(cdiv(p.S, chunks), rw) * rw;
     if (p.chunk_rows < 1) p.chunk_rows = 1;
@@ -126,12 +133,19 @@ int64_t norm_layout(NormParams &p, int vec, bool backward)
     const int64_t groups = p.N * p.G * p.chunks * pieces * 2;
     return groups + (backward ? p.N * p.chunks * 2 * p.C : p.N * p.G);
 }
+// channels a lane moves at once: the most of 16 bytes, 8, ... that divides a group, and that the rows' boundaries allow
+template <typename F> int norm_vec(const NormParams &p, int type, F &&aligned)
+{
+    for (int vec = 16 / elem_bytes(type); vec > 1; vec /= 2)
+        if (p.Cg % vec == 0 && aligned(vec)) return vec;
+    return 1;
+}
 int64_t norm_bytes(const NormParams &p, int type, bool backward)
 {
-    NormParams q = p;
-    const int vec = 16 / elem_bytes(type);
-    int64_t most = norm_layout(q, 1, backward);
-    if (p.Cg % vec == 0) {
+    int64_t most = 0;
+    for (int vec = 16 / elem_bytes(type); vec >= 1; vec /= 2) {
+        if (p.Cg % vec) continue;
+        NormParams q = p;
         const int64_t n = norm_layout(q, vec, backward);
         if (n > most) most = n;
     }
@@ -236,11 +250,13 @@ merit_status merit_plan_group_norm(merit_dtype type, int64_t N, int64_t S, int64
     p.C = (int)C; p.G = (int)groups; p.Cg = (int)(C / groups);
     p.eps = (float)eps;
     p.act = act;
-    for (int vec : {1, 16 / elem_bytes(type)}) {
+    for (int vec = 16 / elem_bytes(type); vec >= 1; vec /= 2) {
         if (p.Cg % vec) continue;
         NormParams q = p;
+        norm_layout(q, vec, true);              // (the pass with more workgroups of the two)
+        const bool too_many = q.rows_form ? q.chunks * q.ctiles >= MAX_BLOCKS : q.N > MAX_BLOCKS || q.N * q.chunks * q.ctiles >= MAX_BLOCKS;
         norm_layout(q, vec, false);
-        if (q.rows_form ? q.chunks * q.ctiles >= MAX_BLOCKS : q.N > MAX_BLOCKS || q.N * q.chunks * q.ctiles >= MAX_BLOCKS) {
+        if (too_many || (q.rows_form ? q.chunks * q.ctiles >= MAX_BLOCKS : q.N > MAX_BLOCKS || q.N * q.chunks * q.ctiles >= MAX_BLOCKS)) {
             delete pl;
             return MERIT_ERR_UNSUPPORTED;
         }
@@ -335,8 +351,7 @@ merit_status merit_token_plan_kernel(const merit_token_plan *plan, merit_pass pa
     const bool backward = pass == MERIT_PASS_BACKWARD;
     if (plan->kind == NORM) {
         NormParams q = plan->norm;
-        const int vec = 16 / elem_bytes(plan->type);
-        norm_layout(q, q.Cg % vec == 0 ? vec : 1, backward);
+        norm_layout(q, norm_vec(q, plan->type, [](int) { return true; }), backward);
         *name = q.rows_form ? (backward ? "merit_norm_rows_backward+merit_reduce_rows" : "merit_norm_rows")
                 : q.slab    ? (backward ? "merit_norm_slab_backward+merit_reduce_rows" : "merit_norm_slab")
                             : (backward ? "merit_norm_sums+merit_norm_apply_backward+merit_reduce_rows"
@@ -373,9 +388,8 @@ merit_status merit_group_norm(const merit_token_plan *plan, const merit_group_no
     p.mean = v.f32(a->mean);
     p.rstd = v.f32(a->rstd);
     if (v.st != MERIT_OK) return v.st;
-    const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.Cg % vec == 0 && wide(p.x, p.N, p.S, vec, plan->type) && wide(p.y, p.N, p.S, vec, plan->type);
-    const int64_t need = 4 * norm_layout(p, fits ? vec : 1, false);
+    const int vec = norm_vec(p, plan->type, [&](int n) { return wide(p.x, p.N, p.S, n, plan->type) && wide(p.y, p.N, p.S, n, plan->type); });
+    const int64_t need = 4 * norm_layout(p, vec, false);
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
     p.part = static_cast<float *>(workspace);
@@ -409,9 +423,10 @@ merit_status merit_group_norm_backward(const merit_token_plan *plan, const merit
         r.seg[1] = {p.dw, 0, p.C};
         return done(launch_reduce_rows(r, s));
     }
-    const int vec = 16 / elem_bytes(plan->type);
-    const bool fits = p.Cg % vec == 0 && wide(p.x, p.N, p.S, vec, plan->type) && wide(p.dy, p.N, p.S, vec, plan->type) && wide(p.dx, p.N, p.S, vec, plan->type);
-    const int64_t need = 4 * norm_layout(p, fits ? vec : 1, true);
+    const int vec = norm_vec(p, plan->type, [&](int n) {
+        return wide(p.x, p.N, p.S, n, plan->type) && wide(p.dy, p.N, p.S, n, plan->type) && wide(p.dx, p.N, p.S, n, plan->type);
+    });
+    const int64_t need = 4 * norm_layout(p, vec, true);
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
     p.part = static_cast<float *>(workspace);

@@ -39,7 +39,7 @@ struct NormParams {
     int C, G, Cg;
     float eps;
     int act;
-    int vec;               // channels a lane moves at once: 16 bytes of them, or 1
+    int vec;               // channels a lane moves at once: 16 bytes of them, 8, 4 or one
     Rows x, y, dy, dx;
     Param w, b;
     float *mean, *rstd;    // [N, G]
@@ -47,6 +47,7 @@ struct NormParams {
     int rows_form;         // one row a group
     int slab;              // a group a workgroup: its threads / 256 << 8 | units a thread (0: not this form)
     int ctiles;            // column tiles
+    int group_tile;        // chunks: groups of a tile
     int64_t chunks;        // row chunks of an image; one row a group: workgroups along the rows
     int64_t chunk_rows;
     float *dw, *db;

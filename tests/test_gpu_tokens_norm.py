@@ -27,7 +27,7 @@ def mb():
 SHAPES = [(5, 1, 64, 4), (7, 1, 1024, 16), (3, 1, 40, 8), (9, 1, 15, 3), (6, 1, 640, 1), (2, 1, 1032, 1), (5, 1, 2000, 1),
           (3, 1, 3000, 2), (2, 1, 8192, 1), (2, 1, 8200, 1), (1, 1, 9000, 1), (3, 1, 255, 1), (1000, 1, 32, 4), (1, 1, 8, 8),
           (2, 9, 64, 4), (1, 49, 96, 3), (3, 50, 40, 8), (2, 33, 15, 3), (1, 7, 2056, 1), (2, 5, 520, 2), (1, 300, 8, 8),
-          (2, 1000, 256, 32), (1, 2, 600, 600), (300, 2, 16, 2), (1, 4097, 3, 1)]
+          (1, 40, 320, 32), (2, 1100, 40, 4), (2, 60, 60, 2), (1, 4200, 20, 1), (7, 1, 60, 6), (3, 1, 1500, 3), (2, 1000, 256, 32), (1, 2, 600, 600), (300, 2, 16, 2), (1, 4097, 3, 1)]
 
 
 def _inputs(shape, dtype, seed, params=True):

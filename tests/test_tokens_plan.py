@@ -127,7 +127,9 @@ def test_empty_batches_are_no_work():
 def test_kernels_named():
     assert mb.merit_plan_group_norm(1, 4096, 1, 1024, 16).kernel() == "merit_norm_rows"
     assert "merit_norm_rows_backward" in mb.merit_plan_group_norm(1, 4096, 1, 1024, 16).kernel(mb.MERIT_PASS_BACKWARD)
-    assert "+" in mb.merit_plan_group_norm(1, 2, 4096, 64, 16).kernel()
+    assert mb.merit_plan_group_norm(1, 2, 4096, 64, 16).kernel() == "merit_norm_slab"
+    assert mb.merit_plan_group_norm(1, 2, 40960, 64, 16).kernel() == "merit_norm_stats+merit_norm_apply"
+    assert "merit_norm_sums" in mb.merit_plan_group_norm(1, 1, 4096, 64, 16).kernel(mb.MERIT_PASS_BACKWARD)
     assert mb.merit_plan_causal_conv(3, 2, 5, 64, 4).kernel(mb.MERIT_PASS_STEP) == "merit_cconv_step"
     assert mb.merit_plan_scan(3, 2, 5, 64, 16).kernel(mb.MERIT_PASS_STEP) == "merit_scan_token"
     with pytest.raises(mb.MeritError):
