@@ -193,13 +193,22 @@ int64_t conv_bytes(const CconvParams &p, int type, bool backward)
 // ---- scan ----------------------------------------------------------------------------------------
 int64_t scan_part_bc(const ScanParams &p) { return (int64_t)p.G * p.ctiles * p.B * p.L * 2 * p.N; }
 int64_t scan_part_a(const ScanParams &p) { return p.B * p.chunks * ((int64_t)p.D * p.N + 2 * p.D); }
-// On few workgroups a sequence's chunks run side by side, two workgroups a compute unit, which takes a launch more and most of a
-// chunk's arithmetic twice.  Forward that pays up to three workgroups for four units (bfloat16, 16 states, 32 workgroups,
-// 8191 tokens: 139 us in 16 chunks; 256 workgroups, 2048 tokens: 176 us in one piece, about 225 in two), backward up to three for
-// two units, since a chunk's first launch is a small part there (the latter: 614 in two, 719 in one).  A chunk is two tiles
-// at least, and there are at most 4 sqrt(tiles) of them: the last one passes through what all others left.  Below six tiles the
-// second launch costs more than it saves.
 int64_t scan_chunk_floats(const ScanParams &p) { return p.chunks > 1 ? p.B * p.chunks * (int64_t)p.D * (p.N + 1) : 0; }
+// A sequence's chunks can run side by side, for a launch more that finds the state before each (the state that a chunk adds:
+// most of a forward pass's arithmetic, a tenth of a backward one's) and a chunk's way through what those before it left.  What
+// `chunks` cost, in hundredths of the time of a tile: 512 workgroups run at once, two a compute unit, and up to 256 of them
+// take half of that time (8 states) or a little more.
+int64_t scan_cost(const ScanParams &p, int64_t blocks, int64_t chunk_tiles, int64_t chunks, bool backward)
+{
+    const int64_t w = blocks * chunks, rest = w % 512;
+    const int64_t half = p.N <= 8 ? 50 : backward && p.N <= 16 ? 60 : 55;
+    const int64_t runs = chunk_tiles * (w / 512 * 100 + (rest == 0 ? 0 : rest <= 256 ? half : 100));
+    if (chunks == 1) return runs;
+    return backward ? runs + runs / 10 + 5 * chunks + 100 : runs + runs * 4 / 5 + 25 * chunks + 400;
+}
+// The cheapest of 1 to 4 sqrt(tiles) chunks of two tiles and more (bfloat16, D 2048, 16 states, us in one piece / in chunks /
+// those: forward 1x8191 553 / 122 / 16, 1x512 39 / 17 / 8, 3x2048 141 / 93 / 8, 4x2048 142 / 119 / 4, but 6x2048 144 / 171 / 8;
+// backward 1x8191 2753 / 327 / 16, 6x2048 713 / 473 / 8, 8x2048 720 / 595 / 2, but 16x1024 508 / 568 / 2).
 void scan_layout(ScanParams &p, bool backward)
 {
     const int cpb = SCAN_THREADS / scan_lpc(p.N);
@@ -208,13 +217,18 @@ void scan_layout(ScanParams &p, bool backward)
     p.chunks = 1;
     p.chunk_tiles = p.tiles > 0 ? p.tiles : 1;
     const int64_t blocks = p.B * p.G * p.ctiles;
-    if (blocks == 0 || blocks > (backward ? 384 : 192) || p.tiles < 6) return;
-    int64_t chunks = cdiv(512, blocks);
-    if (chunks > p.tiles / 2) chunks = p.tiles / 2;
-    while (chunks * chunks > 16 * p.tiles) --chunks;
-    if (chunks < 2) return;
-    p.chunk_tiles = cdiv(p.tiles, chunks);
-    p.chunks = (int)cdiv(p.tiles, p.chunk_tiles);
+    if (blocks == 0 || blocks > 1024 || p.tiles < 4) return;
+    int64_t most = cdiv(2048, blocks);
+    if (most > p.tiles / 2) most = p.tiles / 2;
+    while (most * most > 16 * p.tiles) --most;
+    int64_t least = scan_cost(p, blocks, p.tiles, 1, backward);
+    for (int64_t k = 2; k <= most; ++k) {
+        const int64_t tiles = cdiv(p.tiles, k), chunks = cdiv(p.tiles, tiles), cost = scan_cost(p, blocks, tiles, chunks, backward);
+        if (cost >= least) continue;
+        least = cost;
+        p.chunk_tiles = tiles;
+        p.chunks = (int)chunks;
+    }
 }
 
 merit_token_plan *new_plan(int kind, int type)
@@ -307,7 +321,9 @@ merit_status merit_plan_scan(merit_dtype type, int64_t B, int64_t L, int64_t D, 
     p.B = B; p.L = L; p.D = (int)D; p.N = (int)N; p.G = (int)groups; p.Dg = (int)(D / groups);
     p.softplus = softplus != 0;
     p.type = type;
+    pl->scan_back = p;
     scan_layout(p, false);
+    scan_layout(pl->scan_back, true);
     const int64_t per = (int64_t)p.chunks * p.G * p.ctiles, lanes = (int64_t)D * scan_lpc(p.N), bc = groups * 2 * N;
     // (the last: launch_reduce_rows over A's gradient, 1024 threads for 64 sums)
     if (B > MAX_BLOCKS || D * (N + 2) > MAX_BLOCKS * 8 || B * per >= MAX_BLOCKS || cdiv(B * lanes, 256) >= MAX_BLOCKS ||
@@ -336,8 +352,7 @@ merit_status merit_token_plan_workspace(const merit_token_plan *plan, merit_pass
     if (plan->kind == NORM) *bytes = norm_bytes(plan->norm, plan->type, backward);
     else if (plan->kind == CONV) *bytes = conv_bytes(plan->conv, plan->type, backward);
     else {
-        ScanParams q = plan->scan;
-        scan_layout(q, backward);
+        const ScanParams &q = backward ? plan->scan_back : plan->scan;
         *bytes = 4 * (scan_chunk_floats(q) + (backward ? scan_part_bc(q) + scan_part_a(q) : 0));
     }
     return MERIT_OK;
@@ -359,9 +374,7 @@ merit_status merit_token_plan_kernel(const merit_token_plan *plan, merit_pass pa
     } else if (plan->kind == CONV) {
         *name = pass == MERIT_PASS_STEP ? "merit_cconv_step" : backward ? "merit_cconv_backward+merit_reduce_rows" : "merit_cconv";
     } else {
-        ScanParams q = plan->scan;
-        scan_layout(q, backward);
-        const bool split = q.chunks > 1;
+        const bool split = (backward ? plan->scan_back : plan->scan).chunks > 1;
         *name = pass == MERIT_PASS_STEP ? "merit_scan_token"
                 : backward              ? (split ? "merit_scan_back_chunks+merit_scan_back+merit_scan_sum_bc+merit_reduce_rows"
                                                  : "merit_scan_back+merit_scan_sum_bc+merit_reduce_rows")
@@ -540,7 +553,6 @@ merit_status merit_scan(const merit_token_plan *plan, const merit_scan_args *a, 
     p.h_last = v.f32(a->h_last);
     p.states = v.f32(a->states);
     if (v.st != MERIT_OK) return v.st;
-    scan_layout(p, false);
     const merit_status st = scratch(4 * scan_chunk_floats(p), workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
     p.chunk_dt = static_cast<float *>(workspace);
@@ -553,7 +565,7 @@ merit_status merit_scan_backward(const merit_token_plan *plan, const merit_scan_
 {
     if (!plan || !a) return MERIT_ERR_NULL;
     if (plan->kind != SCAN) return MERIT_ERR_INVALID_ARG;
-    ScanParams p = plan->scan;
+    ScanParams p = plan->scan_back;
     const bool some = p.B > 0 && p.L > 0;
     Views v{plan->type};
     p.dy = v.rows(a->dy, some);
@@ -578,7 +590,6 @@ merit_status merit_scan_backward(const merit_token_plan *plan, const merit_scan_
     p.ddt_bias = v.f32(a->ddt_bias);
     p.dh0 = v.f32(a->dh0);
     if (v.st != MERIT_OK) return v.st;
-    scan_layout(p, true);
     const int64_t need = 4 * (scan_part_bc(p) + scan_part_a(p) + scan_chunk_floats(p));
     const merit_status st = scratch(need, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;

@@ -99,7 +99,7 @@ struct merit_token_plan {
     int type;              // merit_dtype
     merit::NormParams norm;
     merit::CconvParams conv;
-    merit::ScanParams scan;
+    merit::ScanParams scan, scan_back;     // (in how many chunks: one choice for each direction)
 };
 
 namespace merit {
