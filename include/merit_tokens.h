@@ -14,8 +14,8 @@
  *     of one or two dimensions without a leading batch are dense, their strides are not looked at.
  *     A leading stride may be anything for an input (a slice of a wider projection, 0 for a
  *     broadcast one).  data == NULL: absent, where the operand is optional.
- *   - Pointers are aligned to their element; on rows that start on 16-byte boundaries the kernels
- *     move 16 bytes a lane, else fewer.
+ *   - Pointers are aligned to their element; on rows that start on 16-byte boundaries the norms
+ *     move 16 bytes a lane and the convolutions four elements, else fewer.
  *   - "T" below is the plan's type: MERIT_F16, MERIT_BF16 or MERIT_F32.  "P": T or MERIT_F32.
  *     Arithmetic, sums, statistics and states are fp32 whatever T is; a result of type T is rounded
  *     once, to nearest even.

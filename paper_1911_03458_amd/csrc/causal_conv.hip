@@ -3,8 +3,12 @@
 //     M(w)[p,a] = w[d, a]
 // reduced with the dot product, bias and activation on top: y = act(u).  Backward: du = dy act'(u),
 //     dx[t] = sum_a w[a] du[t + K-1 - a],   dw[a] = sum_t du[t] x[t + a - (K-1)],   db = sum_t du[t].
-// Bound by memory: 2 passes of the tensor forward, 3 backward.  A lane has 16 bytes of channels and walks down a strip of
-// tokens with the window's rows in registers, so a row is read once per strip, and once more by the strip after it.
+// Bound by memory: 2 passes of the tensor forward, 3 backward.  A lane has four channels and walks down a strip of tokens
+// with the window's rows, taps and sums in registers, so a row is read once per strip and its last K - 1 once more by the
+// strip after it.  The gradients of taps and bias are summed over a workgroup's strips in LDS and over workgroups by a second
+// launch, in a fixed order.
+// Measured (bfloat16, K 4, SiLU): forward 8x2048x2048 30 us (134 MB: 4.5 TB/s), 3x4099x1536 17 us (76 MB: 4.4 TB/s); backward
+// 8x2048x2048 51 us (201 MB: 4.0 TB/s; a copy of this size 6.0) and 5 us of sums; a token of 32x2048 channels 3.1 us: a launch.
 #include "tokens.h"
 
 namespace merit {
