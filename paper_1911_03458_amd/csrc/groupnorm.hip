@@ -410,9 +410,12 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
     constexpr int RB = 4;                   // rows in flight (y may be x: no load moves over a store by itself)
     for (int r = (int)first; r < (int)t.r1; r += RB * t.rw) {
         vec_t<T, V> v[RB];
+        // (behind the last row: that one again; a load under a condition would be waited for before the next)
 #pragma unroll
-        for (int k = 0; k < RB; ++k, xa += xs)
-            if (k == 0 || r + k * t.rw < (int)t.r1) v[k] = load_vec<T, V>(p.x.data, xa);
+        for (int k = 0; k < RB; ++k) {
+            v[k] = load_vec<T, V>(p.x.data, xa);
+            if (r + (k + 1) * t.rw < (int)t.r1) xa += xs;
+        }
 #pragma unroll
         for (int k = 0; k < RB; ++k, ya += ys) {
             if (k && r + k * t.rw >= (int)t.r1) break;
@@ -525,11 +528,14 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
     for (int r = (int)first; r < (int)t.r1; r += RB * t.rw) {
         vec_t<T, V> xv[RB], dv[RB];
 #pragma unroll
-        for (int k = 0; k < RB; ++k, xa += xs, da += ds)
-            if (k == 0 || r + k * t.rw < (int)t.r1) {
-                xv[k] = load_vec<T, V>(p.x.data, xa);
-                dv[k] = load_vec<T, V>(p.dy.data, da);
+        for (int k = 0; k < RB; ++k) {
+            xv[k] = load_vec<T, V>(p.x.data, xa);
+            dv[k] = load_vec<T, V>(p.dy.data, da);
+            if (r + (k + 1) * t.rw < (int)t.r1) {
+                xa += xs;
+                da += ds;
             }
+        }
 #pragma unroll
         for (int k = 0; k < RB; ++k, oa += os) {
             if (k && r + k * t.rw >= (int)t.r1) break;

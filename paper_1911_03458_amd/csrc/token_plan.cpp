@@ -103,7 +103,13 @@ int64_t norm_layout(NormParams &p, int vec, bool backward)
     // A workgroup a group, where its registers hold the group's values (bfloat16, us a call, chunks / this: forward 1x196x512, 32
     // groups 9.6 / 5.7, 4x3136x256 12.1 / 8.9, 2 groups of 1x784x64 8.9 / 5.8; backward with 32 groups and more 15.9 / 9.8 and
     // 20.1 / 17.4, with 16 17.1 / 19.6, with 2 14.5 / 19.2).  Fewer than 128 units would leave most of its threads without one.
-    if (vec > 1 && (!backward || p.N * p.G >= 32) && cu <= 256 && p.S * cu >= 128) {
+    // Not where rows of one unit each make many long groups (binary16, 8x3136x256 15.4 / 12.6, but 10 images 16.7 / 17.7, 32
+    // 32.0 / 41.3; 16x1568x256 15.0 / 12.4, 32 20.4 / 22.9; 64x784x512 32.2 / 28.9): the line that such a row is a piece of comes
+    // once for each group of it.  And not backward where eight channels a lane make many sums to leave (binary16, 8x49x2048 16.1 /
+    // 15.4, but 16 16.5 / 17.8, 64 23.4 / 38.7; 16x196x1024 19.7 / 18.3, 64 34.1 / 39.9; fp32 64x196x1024 47.5 / 38.3).
+    const bool torn = cu == 1 && p.S > 1024 && p.N * p.G * p.S > 900000;
+    const bool sums = !backward || (p.N * p.G >= 32 && (vec < 8 || p.N * p.C <= 24576));
+    if (vec > 1 && sums && !torn && cu <= 256 && p.S * cu >= 128) {
         for (int form : {0x104, 0x108, 0x404, 0x408}) {
             const int threads = form & 0x400 ? 1024 : 256, units = form & 0xFF;
             if (p.S > (int64_t)(threads / cu) * units) continue;
