@@ -12,8 +12,8 @@
 //  - a group a workgroup (the values of an image's group fit its registers): x is read once too.  bfloat16, 8x3136x256 in 32
 //    groups 13.9 us (1.8 TB/s: 256 workgroups, so that every one loads, reduces and stores at the same time as all others).
 //  - chunks (any S): workgroups reduce row chunks to partial statistics, a second launch joins them and applies; its read of x
-//    comes from the cache behind the L2 where that holds the tensor.  binary16, 16x12544x64 in 8 groups (26 MB): 9.2 + 12.9 us
-//    (5.2 TB/s, reads of both launches and the result); backward 15.6 + 16.3 us (4.0 TB/s) and 5 us of sums.
+//    comes from the cache behind the L2 where that holds the tensor.  binary16, 16x12544x64 in 8 groups (26 MB): 8.8 + 12.6 us
+//    (3.6 TB/s, reads of both launches and the result); backward 15.1 + 16.0 us (4.1 TB/s) and 5 us of sums.
 // Variances are sums of squared distances from a mean that is known by then (of the row, or of the batch of values in
 // registers, batches joined by their counts): a mean far from zero costs no digits.
 #include "merit_internal.h"
