@@ -35,7 +35,7 @@ struct Where {
 template <int LPC> __device__ __forceinline__ Where where(const ScanParams &p, int first, int chunks, int thread)
 {
     Where w;
-    uint32_t r = blockIdx.x;
+    uint32_t r = p.block0 + blockIdx.x;
     w.ct = (int)(r % (uint32_t)p.ctiles);
     r /= (uint32_t)p.ctiles;
     w.g = (int)(r % (uint32_t)p.G);

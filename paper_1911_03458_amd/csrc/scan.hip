@@ -267,21 +267,26 @@ template <typename T> struct Forward {
     hipStream_t s;
     template <int SPL, int LPC, bool PAD> hipError_t run()
     {
-        const unsigned per = (unsigned)(p.B * p.G * p.ctiles);
+        const int64_t per = p.B * p.G * p.ctiles;
         if (p.chunks > 1) {
             const hipError_t e = launch<SPL, LPC, PAD, CHUNK_STATES>(per * (p.chunks - 1));
             if (e != hipSuccess) return e;
         }
         return p.states ? launch<SPL, LPC, PAD, KEEP_STATES>(per * p.chunks) : launch<SPL, LPC, PAD, RESULTS>(per * p.chunks);
     }
-    template <int SPL, int LPC, bool PAD, int WHAT> hipError_t launch(unsigned grid)
+    template <int SPL, int LPC, bool PAD, int WHAT> hipError_t launch(int64_t blocks)
     {
         static std::atomic<int> raised;
         const auto kernel = merit_scan_tiles<T, SPL, LPC, PAD, WHAT>;
-        const hipError_t e = raise_lds_limit_once(reinterpret_cast<const void *>(kernel), raised);
-        if (e != hipSuccess) return e;
-        kernel<<<grid, 2 * NT, Room<SPL, LPC>::BYTES, s>>>(p);
-        return hipGetLastError();
+        hipError_t e = raise_lds_limit_once(reinterpret_cast<const void *>(kernel), raised);
+        ScanParams q = p;
+        for (int64_t at = 0; at < blocks && e == hipSuccess; at += SCAN_FORWARD_BLOCKS) {
+            const int64_t rest = blocks - at;
+            q.block0 = (uint32_t)at;
+            kernel<<<(unsigned)(rest < SCAN_FORWARD_BLOCKS ? rest : SCAN_FORWARD_BLOCKS), 2 * NT, Room<SPL, LPC>::BYTES, s>>>(q);
+            e = hipGetLastError();
+        }
+        return e;
     }
 };
 template <typename T> struct Token {

@@ -12,7 +12,7 @@ using namespace merit;
 namespace {
 
 constexpr int64_t MAX_CHANNELS = 1 << 24, MAX_ROWS = std::numeric_limits<int32_t>::max() - 1023;   // (rows are counted in 32 bits, past the last by up to four of a workgroup's)
-constexpr int64_t MAX_BLOCKS = 1 << 24;                 // of 256 threads: 2^32 threads a launch
+constexpr int64_t MAX_BLOCKS = 1 << 24;                 // of 256 threads: a launch holds fewer than 2^32
 
 // elements of a tensor at most: scratch memory in bytes and every offset stay far from 2^63
 bool too_large(int64_t a, int64_t b, int64_t c) { return a != 0 && b != 0 && a > (1ll << 46) / b / c; }
@@ -380,11 +380,14 @@ merit_status merit_token_plan_kernel(const merit_token_plan *plan, merit_pass pa
     } else if (plan->kind == CONV) {
         *name = pass == MERIT_PASS_STEP ? "merit_cconv_step" : backward ? "merit_cconv_backward+merit_reduce_rows" : "merit_cconv";
     } else {
-        const bool split = (backward ? plan->scan_back : plan->scan).chunks > 1;
+        const ScanParams &q = backward ? plan->scan_back : plan->scan;
+        const bool split = q.chunks > 1;        // (then the workgroups are few: SCAN_FORWARD_BLOCKS is for unsplit sequences)
+        const int64_t launches = split ? 2 : cdiv(q.B * q.G * q.ctiles, SCAN_FORWARD_BLOCKS);
         *name = pass == MERIT_PASS_STEP ? "merit_scan_token"
                 : backward              ? (split ? "merit_scan_back_chunks+merit_scan_back+merit_scan_sum_bc+merit_reduce_rows"
                                                  : "merit_scan_back+merit_scan_sum_bc+merit_reduce_rows")
-                : split                 ? "merit_scan_tiles+merit_scan_tiles"
+                : launches > 2          ? "merit_scan_tiles+merit_scan_tiles+merit_scan_tiles"
+                : launches == 2         ? "merit_scan_tiles+merit_scan_tiles"
                                         : "merit_scan_tiles";
     }
     return MERIT_OK;

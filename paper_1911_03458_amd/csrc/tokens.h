@@ -74,6 +74,7 @@ struct ScanParams {
     int D, N, G, Dg;       // Dg = D / G channels share B and C
     int softplus;
     int type;              // merit_dtype of x, dt, B, C, z, y, ...
+    uint32_t block0;       // workgroups of the launches before this one
     Rows x, dt, Bm, Cm, z, y, dy, dx, ddt, dz, dB, dC;
     const float *A, *skip, *dt_bias, *h0, *dh_last;
     const int32_t *lens;
@@ -91,6 +92,9 @@ struct ScanParams {
 // lanes of a channel (scan.h: by_states)
 constexpr int scan_lpc(int N) { return N == 1 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 constexpr int SCAN_THREADS = 256;
+// The forward pass has two halves of SCAN_THREADS in a workgroup, and a launch holds fewer than 2^32 threads: more workgroups go
+// in launches of this many, one after the other.
+constexpr int64_t SCAN_FORWARD_BLOCKS = (1ll << 32) / (2 * SCAN_THREADS) - 1;
 
 }  // namespace merit
 
