@@ -12,7 +12,8 @@ using namespace merit;
 namespace {
 
 constexpr int64_t MAX_CHANNELS = 1 << 24, MAX_ROWS = std::numeric_limits<int32_t>::max() - 1023;   // (rows are counted in 32 bits, past the last by up to four of a workgroup's)
-constexpr int64_t MAX_BLOCKS = 1 << 24;                 // of 256 threads: a launch holds fewer than 2^32
+constexpr int64_t MAX_THREADS = 1ll << 32;              // a launch holds fewer
+constexpr int64_t MAX_BLOCKS = MAX_THREADS / 256;       // workgroups of 256 threads (where a kernel has more: at its rule)
 
 // elements of a tensor at most: scratch memory in bytes and every offset stay far from 2^63
 bool too_large(int64_t a, int64_t b, int64_t c) { return a != 0 && b != 0 && a > (1ll << 46) / b / c; }
@@ -112,7 +113,7 @@ int64_t norm_layout(NormParams &p, int vec, bool backward)
     if (vec > 1 && sums && !torn && cu <= 256 && p.S * cu >= 128) {
         for (int form : {0x104, 0x108, 0x404, 0x408}) {
             const int threads = form & 0x400 ? 1024 : 256, units = form & 0xFF;
-            if (p.S > (int64_t)(threads / cu) * units) continue;
+            if (p.S > (int64_t)(threads / cu) * units || p.N * p.G * threads >= MAX_THREADS) continue;
             p.slab = form;
             p.ctiles = p.G;
             p.chunks = 1;

@@ -20,3 +20,17 @@ def test_scan_over_many_short_sequences(B, G, launches):
     assert _launches(plan) == ["merit_scan_tiles"] * launches
     assert _launches(plan, mb.MERIT_PASS_STEP) == ["merit_scan_token"]
     assert _launches(plan, mb.MERIT_PASS_BACKWARD)[0] == "merit_scan_back"
+
+
+@pytest.mark.parametrize("N, S, C, G, slab", [
+    ((1 << 22) - 1, 681, 6, 1, True),                    # 1024 threads a group
+    (1 << 22, 681, 6, 1, False),                         # 2^32 threads
+    (1 << 20, 681, 24, 4, False),
+    (1 << 22, 340, 6, 1, True),                          # 256 threads a group
+    ((1 << 24) - 1, 128, 4, 1, True),
+])
+def test_norm_over_many_images(N, S, C, G, slab):
+    """Where the groups' workgroups would be too many, chunks take them."""
+    plan = mb.merit_plan_group_norm(mb.MERIT_F16, N, S, C, G)
+    assert _launches(plan) == (["merit_norm_slab"] if slab else ["merit_norm_stats", "merit_norm_apply"])
+    assert _launches(plan, mb.MERIT_PASS_BACKWARD)[0] == ("merit_norm_slab_backward" if slab else "merit_norm_sums")
