@@ -77,10 +77,11 @@ template <int LPC> struct Sums {
     static __device__ __forceinline__ bool writes() { return LPC >= 4 || (threadIdx.x & (3 & ~(LPC - 1))) == 0; }
 };
 
-// LDS of a workgroup: B and C of a tile, the wavefronts' sums for dB and dC, the states of the tile's tokens
+// LDS of a workgroup: B and C of a tile, the wavefronts' sums for dB and dC, the states of the tile's tokens, zeros in the place
+// of B and C
 template <int SPL, int LPC> constexpr int back_lds()
 {
-    return (2 * TT * SPL * LPC + NT / 64 * TT * 2 * SPL * LPC + TT * NT * SPL) * 4;
+    return (4 * TT * SPL * LPC + NT / 64 * TT * 2 * SPL * LPC + TT * NT * SPL) * 4;
 }
 
 // Two wavefronts a SIMD (a lone one issues plain arithmetic at half the rate), so 256 registers: the decays of a tile stay in
@@ -93,8 +94,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
     extern __shared__ __align__(16) float lds[];
     float *const bl = lds, *const cl = bl + TT * S::NP, *const red = cl + TT * S::NP;
     float *const hl = red + NT / 64 * TT * 2 * S::NP + threadIdx.x * SPL;      // token t: t * NT * SPL further
+    float *const none = red + NT / 64 * TT * 2 * S::NP + TT * NT * SPL;
     const Where w = where<LPC>(p, 0, p.chunks, threadIdx.x);
     const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
+    // Lanes without a channel take part in the sums over channels: their x, dt and dy are zeros, and so are their B and C, of
+    // which an infinity times 0 would be a NaN
+    for (int e = threadIdx.x; e < 2 * TT * S::NP; e += NT) none[e] = 0.0f;
+    const float *const bt = (w.in ? bl : none) + n0, *const ct = bt + TT * S::NP;
     float A2[SPL], dA[SPL], carry[SPL];                     // (A2: the exponentials are to the base 2)
     bool ok[SPL];
     const int64_t hat = (w.b * p.D + w.d) * p.N + n0;
@@ -193,8 +199,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
                 const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
                 const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
                 float Bv[SPL], Cv[SPL];
-                read_states<SPL>(bl + t * S::NP + n0, Bv);
-                read_states<SPL>(cl + t * S::NP + n0, Cv);
+                read_states<SPL>(bt + t * S::NP, Bv);
+                read_states<SPL>(ct + t * S::NP, Cv);
                 acc[u] = 0.0f;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) {
@@ -235,8 +241,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
                 const float dtv = from_lane<S::LQ>(dt[t / S::LQ], t % S::LQ), dxv = from_lane<S::LQ>(dx[t / S::LQ], t % S::LQ);
                 const float dyv = from_lane<S::LQ>(dy[t / S::LQ], t % S::LQ);
                 float Bv[SPL], Cv[SPL];
-                read_states<SPL>(bl + t * S::NP + n0, Bv);
-                read_states<SPL>(cl + t * S::NP + n0, Cv);
+                read_states<SPL>(bt + t * S::NP, Bv);
+                read_states<SPL>(ct + t * S::NP, Cv);
                 if (t) read_states<SPL>(hl + (t - 1) * NT * SPL, h);
                 u4[u] = v4[u] = 0.0f;
 #pragma unroll

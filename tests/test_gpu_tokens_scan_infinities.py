@@ -1,0 +1,46 @@
+"""Infinities in what a group's channels share, where the channels do not fill their workgroup: what the definition says about
+them, and nothing from lanes that have no channel."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from oracle import tokens as ot                        # noqa: E402
+from token_helpers import DEV, TYPES, Gen, check, host     # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def mb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1911_03458_amd import binding
+    binding.lib()
+    return binding
+
+
+@pytest.mark.parametrize("D, G", [(10, 1), (64, 1), (70, 1), (6, 2)])
+@pytest.mark.parametrize("N", [1, 3, 8, 16, 17, 64])
+@pytest.mark.parametrize("what", ["B", "C"])
+def test_gradients_of_tokens(mb, what, N, D, G):
+    """All operands positive, so that no sum of the definition has infinities of both signs: a result is infinite, or it is as
+    near as ever, and a NaN only where the definition has one (0 times an infinite state).  Chain: 3 (4 L + N + 16) + D / G."""
+    B, L = 2, 37
+    g = Gen(31)
+    u = {k: g.uniform(*s, lo=0.2, hi=1.0) for k, s in dict(x=(B, L, D), dt=(B, L, D), B=(B, L, G, N), C=(B, L, G, N), dy=(B, L, D)).items()}
+    A = -g.uniform(D, N, lo=0.1, hi=2.0)
+    u[what][1, 20, G - 1, N - 1] = float("inf")
+    plan = mb.merit_plan_scan(TYPES["f32"][1], B, L, D, N, G)
+    _, st = mb.merit_scan(plan, u["x"], u["dt"], A, u["B"], u["C"], states=True)
+    got = mb.merit_scan_backward(plan, u["dy"], u["x"], u["dt"], A, u["B"], u["C"], st)
+    with np.errstate(invalid="ignore"):
+        want = ot.scan_backward(host(u["dy"]), host(u["x"]), host(u["dt"]), host(A), host(u["B"]), host(u["C"]))
+    for k in ("dx", "ddt", "dB", "dC"):
+        w, t = want[k], host(got[k])
+        assert np.array_equal(np.isnan(t), np.isnan(w)), k
+        far = np.isinf(w)
+        assert np.array_equal(t[far], w[far]), k
+        finite = np.isfinite(w)
+        check(got[k].cpu()[torch.from_numpy(finite)], w[finite], 3 * (4 * L + N + 16) + D // G, k)
+    assert np.isinf(want["dC" if what == "B" else "dB"]).any()
