@@ -251,7 +251,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
                     if (PAD && !ok[s]) l = 0.0f;
                     u4[u] = fmaf(l, Bv[s], u4[u]);
                     carry[s] = a[t][s] * l;
-                    const float q = carry[s] * (t ? h[s] : hs[s]);
+                    float q = carry[s] * (t ? h[s] : hs[s]);
+                    if (!ALL && tile * TT + t >= w.n) q = 0.0f;         // (behind the end: an infinite state times 0)
                     v4[u] = fmaf(q, A2[s], v4[u]);
                     dA[s] = fmaf(q, dtv, dA[s]);
                     b4[s][u] = l * dxv;

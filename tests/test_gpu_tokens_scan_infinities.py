@@ -44,3 +44,27 @@ def test_gradients_of_tokens(mb, what, N, D, G):
         finite = np.isfinite(w)
         check(got[k].cpu()[torch.from_numpy(finite)], w[finite], 3 * (4 * L + N + 16) + D // G, k)
     assert np.isinf(want["dC" if what == "B" else "dB"]).any()
+
+
+@pytest.mark.parametrize("L, lens", [(37, None), (48, None), (48, (48, 40, 17))])
+@pytest.mark.parametrize("N", [1, 3, 16, 64])
+@pytest.mark.parametrize("last", [True, False])
+def test_gradient_of_decays(mb, last, N, L, lens):
+    """A state that becomes infinite at a sequence's last token has no part in dA (the decays multiply the states before it);
+    one that does so earlier makes that entry infinite.  Chain: 3 (4 L + N + 16) + B L."""
+    B, D = 3, 20
+    g = Gen(32)
+    u = {k: g.uniform(*s, lo=0.2, hi=1.0) for k, s in dict(x=(B, L, D), dt=(B, L, D), B=(B, L, 1, N), C=(B, L, 1, N), dy=(B, L, D)).items()}
+    A = -g.uniform(D, N, lo=0.1, hi=2.0)
+    ends = [L] * B if lens is None else lens
+    u["x"][1, ends[1] - 1 if last else 9, 5] = float("inf")
+    n = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    plan = mb.merit_plan_scan(TYPES["f32"][1], B, L, D, N)
+    _, st = mb.merit_scan(plan, u["x"], u["dt"], A, u["B"], u["C"], lens=n, states=True)
+    got = host(mb.merit_scan_backward(plan, u["dy"], u["x"], u["dt"], A, u["B"], u["C"], st, lens=n)["dA"])
+    with np.errstate(invalid="ignore"):
+        want = ot.scan_backward(*(host(u[k]) for k in ("dy", "x", "dt")), host(A), host(u["B"]), host(u["C"]), lens=ends)["dA"]
+    assert np.isfinite(want).all() if last else np.isinf(want[5]).all() and np.isfinite(np.delete(want, 5, 0)).all()
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    finite = np.isfinite(want)
+    check(torch.from_numpy(got[finite]).float(), want[finite], 3 * (4 * L + N + 16) + B * L, "dA")
