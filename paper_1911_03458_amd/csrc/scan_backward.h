@@ -94,13 +94,14 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
     extern __shared__ __align__(16) float lds[];
     float *const bl = lds, *const cl = bl + TT * S::NP, *const red = cl + TT * S::NP;
     float *const hl = red + NT / 64 * TT * 2 * S::NP + threadIdx.x * SPL;      // token t: t * NT * SPL further
-    float *const none = red + NT / 64 * TT * 2 * S::NP + TT * NT * SPL;
     const Where w = where<LPC>(p, 0, p.chunks, threadIdx.x);
     const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
     // Lanes without a channel take part in the sums over channels: their x, dt and dy are zeros, and so are their B and C, of
     // which an infinity times 0 would be a NaN
-    for (int e = threadIdx.x; e < 2 * TT * S::NP; e += NT) none[e] = 0.0f;
-    const float *const bt = (w.in ? bl : none) + n0, *const ct = bt + TT * S::NP;
+    // (an offset, of which the compiler sees what it is a multiple of: a pointer chosen took 8 % more time at one state)
+    constexpr int NONE = 2 * TT * S::NP + NT / 64 * TT * 2 * S::NP + TT * NT * SPL;
+    for (int e = threadIdx.x; e < 2 * TT * S::NP; e += NT) lds[NONE + e] = 0.0f;
+    const float *const bt = lds + (w.in ? 0 : NONE) + n0, *const ct = bt + TT * S::NP;
     float A2[SPL], dA[SPL], carry[SPL];                     // (A2: the exponentials are to the base 2)
     bool ok[SPL];
     const int64_t hat = (w.b * p.D + w.d) * p.N + n0;
