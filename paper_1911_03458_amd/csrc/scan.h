@@ -221,7 +221,7 @@ template <int SPL> __device__ __forceinline__ void store_states(float *at, const
 }
 
 // A state (or its adjoint) through `count` chunks from `q` on: their decay, then what they add.  Four chunks' loads go out
-// together.
+// together.  No decay is 0: an infinite state stays one where fp32 cannot hold a chunk's.
 template <int SPL>
 __device__ __forceinline__ void through_chunks(const ScanParams &p, const Where &w, int n0, const float (&A2)[SPL], const bool (&ok)[SPL],
                                                float (&h)[SPL], int q, int count, int dir)
@@ -241,7 +241,10 @@ __device__ __forceinline__ void through_chunks(const ScanParams &p, const Where 
             if (k < count)
 #pragma unroll
                 for (int s = 0; s < SPL; ++s)
-                    if (ok[s]) h[s] = fmaf(__builtin_amdgcn_exp2f(sum[k] * A2[s]), h[s], add[k][s]);
+                    if (ok[s]) {
+                        const float decay = __builtin_amdgcn_exp2f(sum[k] * A2[s]);
+                        h[s] = fmaf(decay == 0.0f && __builtin_isinf(h[s]) ? 1.0f : decay, h[s], add[k][s]);
+                    }
     }
 }
 

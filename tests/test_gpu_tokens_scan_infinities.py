@@ -68,3 +68,29 @@ def test_gradient_of_decays(mb, last, N, L, lens):
     assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
     finite = np.isfinite(want)
     check(torch.from_numpy(got[finite]).float(), want[finite], 3 * (4 * L + N + 16) + B * L, "dA")
+
+
+@pytest.mark.parametrize("N", [1, 3, 16, 64])
+def test_an_infinite_state_through_chunks(mb, N):
+    """An infinite state stays one, however much of it has decayed: also where a sequence runs in chunks, over which the decay is
+    less than fp32 can hold (steps of at least 0.31 and A of -12: 5 to 11 bits a token)."""
+    B, L, D = 1, 400, 20
+    g = Gen(33)
+    u = {k: g.uniform(*s, lo=0.2, hi=1.0) for k, s in dict(x=(B, L, D), dt=(B, L, D), B=(B, L, 1, N), C=(B, L, 1, N), dy=(B, L, D)).items()}
+    u["dt"] -= 1.2
+    A = torch.full((D, N), -12.0, device=DEV)
+    plan = mb.merit_plan_scan(TYPES["f32"][1], B, L, D, N)
+    assert "+" in plan.kernel() and plan.kernel(mb.MERIT_PASS_BACKWARD).startswith("merit_scan_back_chunks")
+    x, dy = u["x"].clone(), u["dy"].clone()
+    x[0, 7, 4] = dy[0, 390, 9] = float("inf")
+    y, h = mb.merit_scan(plan, x, u["dt"], A, u["B"], u["C"], final=True)
+    clean, _ = mb.merit_scan(plan, u["x"], u["dt"], A, u["B"], u["C"], final=True)
+    assert torch.isposinf(y[0, 7:, 4]).all() and torch.isposinf(h[0, 4]).all()
+    y[0, 7:, 4] = clean[0, 7:, 4]
+    assert torch.equal(y, clean)
+    _, st = mb.merit_scan(plan, u["x"], u["dt"], A, u["B"], u["C"], states=True)
+    got = mb.merit_scan_backward(plan, dy, u["x"], u["dt"], A, u["B"], u["C"], st, dh0=True)
+    clean = mb.merit_scan_backward(plan, u["dy"], u["x"], u["dt"], A, u["B"], u["C"], st, dh0=True)
+    assert torch.isposinf(got["dx"][0, :391, 9]).all() and torch.isposinf(got["dh0"][0, 9]).all()
+    got["dx"][0, :391, 9] = clean["dx"][0, :391, 9]
+    assert torch.equal(got["dx"], clean["dx"])
