@@ -5,8 +5,9 @@
  *
  * All tensors are channels last: a token's channels lie side by side.  The convolution is a ranged
  * inner product, k = (b, t, d | a) with a moving along t at offset -(K-1); the scan is a recurrence
- * over its result; the norm closes the block (every token with statistics of its own), or follows a
- * convolution layer whose result lies channels last (H * W positions share the statistics).
+ * over its result; the norm closes the block (every token with statistics of its own), or normalises
+ * an image that lies channels last (H * W positions share the statistics; the image layers of merit.h
+ * leave planes, whose channels do not lie side by side).
  *
  * Conventions
  *   - An operand is a merit_view: a DEVICE pointer owned by the caller, the element strides of its
@@ -25,6 +26,8 @@
  *     (merit_token_plan_workspace; 16-byte aligned; free for other use when the call's work is done).
  *   - A plan is immutable host memory, may be shared between threads and streams.
  *   - Results do not depend on the order in which workgroups run: the same call gives the same bits.
+ *   - Sizes that a launch cannot hold are MERIT_ERR_UNSUPPORTED when the plan is made: fewer than 2^32
+ *     threads a launch, which is 2^24 workgroups for most passes, and B L groups N < 2^31 for a scan.
  *   - Every function returns a merit_status; on an error nothing was launched (MERIT_ERR_HIP apart:
  *     of a call of several launches the first may have been).
  */
@@ -67,7 +70,8 @@ merit_status merit_plan_scan(merit_dtype type, int64_t B, int64_t L, int64_t D, 
 merit_status merit_token_plan_destroy(merit_token_plan *plan);
 /* Scratch memory that a pass needs, in bytes (0: none). */
 merit_status merit_token_plan_workspace(const merit_token_plan *plan, merit_pass pass, int64_t *bytes);
-/* The kernels a pass runs ("a+b": two launches), for rows on 16-byte boundaries. */
+/* The kernels a pass runs ("a+b": two launches), for rows on 16-byte boundaries and with every gradient wanted but that
+ * of `init`, which is a launch more (merit_cconv_dinit). */
 merit_status merit_token_plan_kernel(const merit_token_plan *plan, merit_pass pass, const char **name);
 
 /* y = act((x - mean) rstd weight + bias), rstd = 1 / sqrt(var + eps), var with the divisor S C / groups. */

@@ -10,10 +10,10 @@
 //    keeps weights and the parameter gradients' sums in registers.  bfloat16, 16384 x 16 groups of 128 channels: 29 us
 //    (4.7 TB/s); backward 41 us (4.9 TB/s) and 5 us of sums.  16 x 16 groups of 64: 3.5 us, a launch.
 //  - a group a workgroup (the values of an image's group fit its registers): x is read once too.  bfloat16, 8x3136x256 in 32
-//    groups 13.9 us (1.8 TB/s: 256 workgroups, so that every one loads, reduces and stores at the same time as all others).
+//    groups 14.1 us (1.8 TB/s: 256 workgroups, so that every one loads, reduces and stores at the same time as all others).
 //  - chunks (any S): workgroups reduce row chunks to partial statistics, a second launch joins them and applies; its read of x
-//    comes from the cache behind the L2 where that holds the tensor.  binary16, 16x12544x64 in 8 groups (26 MB): 8.8 + 12.6 us
-//    (3.6 TB/s, reads of both launches and the result); backward 15.1 + 16.0 us (4.1 TB/s) and 5 us of sums.
+//    comes from the cache behind the L2 where that holds the tensor.  binary16, 16x12544x64 in 8 groups (26 MB): 9.1 + 12.5 us
+//    (3.6 TB/s, reads of both launches and the result); backward 15.6 + 16.2 us (4.0 TB/s) and 5 us of sums.
 // Variances are sums of squared distances from a mean that is known by then (of the row, or of the batch of values in
 // registers, batches joined by their counts): a mean far from zero costs no digits.
 #include "merit_internal.h"
@@ -555,7 +555,8 @@ template <typename T, int V> __global__ __launch_bounds__(NT) void merit_norm_ap
 // a group a workgroup
 // ---------------------------------------------------------------------------
 // All of a group's values of one image stay in the workgroup's registers, U units of V channels a thread: x (and dy) are
-// read once and nothing waits for another workgroup.  Thread (row ty, unit tx) has rows ty, ty + rw, ...  A row of few
+// read once and nothing waits for another workgroup.  (Eight units of eight channels in 1024 threads spill: 42 registers forward,
+// 2 backward.)  Thread (row ty, unit tx) has rows ty, ty + rw, ...  A row of few
 // channels fills less than a cache line; its neighbours in the line belong to workgroups that run on the same XCD.
 struct Slab {
     int64_t n;
@@ -693,7 +694,7 @@ template <typename T, int V, int U, int NTH> __global__ __launch_bounds__(NTH) v
         store_vec<T, V>(p.dx.data, ot, o);
     }
     if (!p.dw && !p.db) return;
-    // the rows' sums of a channel: lanes of a wavefront that have the same unit first where units are a power of two
+    // the rows' sums of a channel
     float *out = p.part + s.n * 2 * p.C + s.g * p.Cg;
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {

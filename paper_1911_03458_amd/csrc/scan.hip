@@ -10,8 +10,9 @@
 // channels, are staged in LDS as fp32.
 // Measured (bfloat16, gated, 16 states; traced launch by launch): 8x2048x2048 176 us (271 MB: 1.5 TB/s; 0.54 G states x tokens:
 // 3.1 T/s, exponentials and plain operations alone would allow 7.9 T/s), 150 us a call where calls follow one another;
-// 1x8191x2048 in 16 chunks 84 us and 56 us for the chunks' first states, 121 a call; a token of 32x2048 channels 4.3 us.
+// 1x8191x2048 in 16 chunks 87 us and 58 us for the chunks' first states, 121 a call; a token of 32x2048 channels 4.3 us.
 // Without the second half of the workgroup, its work done by the first: 235 us, and 104 + 64.
+// (With one state the second half, 16 tokens of a tile a thread, spills 77 registers.)
 #include "merit_internal.h"
 #include "scan.h"
 

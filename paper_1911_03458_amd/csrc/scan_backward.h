@@ -4,15 +4,15 @@
 //     u = sum_n l_t B_t,  q[n] = l_t a_t h_{t-1},  ds = u x + sum_n q A,  dx = u s + skip dy'
 //     ddt = ds sigmoid(dt + dt_bias),  dA[n] = sum_{b,t} q s,  dz = dy (C_t h_t + skip x) silu'(z)
 // Tiles of 16 tokens from the last to the first; a tile starts from the state that the forward pass kept before it, so the
-// states of its tokens are computed once more and stay in registers with their decays.  dB and dC are sums over
+// states of its tokens are computed once more and stay, the decays in registers, the states in LDS.  dB and dC are sums over
 // channels, which are lanes: the 16 tokens' values of a state are added across lanes so that every halving of the lanes
 // halves the values too (15 exchanges for 16 sums of 16 lanes), then wavefronts through LDS, then workgroups through
 // memory in a second launch, in a fixed order.
 // Bound by the vector ALUs: a state and token take an exponential, 13 plain operations and two sums across lanes of 15/16 of
 // an exchange and an addition each, about 51 cycles a wavefront and SIMD: 190 us for 8x2048x2048 and 16 states.  Measured there
-// (bfloat16, gated): 528 us, in two chunks a sequence with 92 us for their first adjoints; 16 us for the sums of dB and dC and
-// 5 us for those of dA.  (Two workgroups a compute unit is what registers and LDS allow; a wait of one has but the other to
-// fill it.)
+// (bfloat16, gated): 531 us, in two chunks a sequence with 90 us for their first adjoints; 16 us for the sums of dB and dC and
+// 5 us for those of dA.  (Two workgroups a compute unit is what registers and LDS allow at 9 to 16 states; a wait of one has but
+// the other to fill it.  At 3 to 8 states registers allow one, 270 to 348 of them, and from 17 on LDS does, 88 or 112 KB.)
 #pragma once
 #include "merit_internal.h"
 #include "scan.h"
@@ -84,8 +84,8 @@ template <int SPL, int LPC> constexpr int back_lds()
     return (4 * TT * SPL * LPC + NT / 64 * TT * 2 * SPL * LPC + TT * NT * SPL) * 4;
 }
 
-// Two wavefronts a SIMD (a lone one issues plain arithmetic at half the rate), so 256 registers: the decays of a tile stay in
-// registers, its states in LDS.
+// Two wavefronts a SIMD (a lone one issues plain arithmetic at half the rate) for 9 to 16 states, so 256 registers: the decays of
+// a tile stay in registers, its states in LDS.  From 33 states on 5 to 8 registers spill.
 template <typename T, int SPL, int LPC, bool PAD>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2 : 1, 2))) void merit_scan_back(ScanParams p)
 {
@@ -97,8 +97,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(LPC >= 4 ? 2
     const Where w = where<LPC>(p, 0, p.chunks, threadIdx.x);
     const int n0 = w.lane * SPL, wave = threadIdx.x >> 6;
     // Lanes without a channel take part in the sums over channels: their x, dt and dy are zeros, and so are their B and C, of
-    // which an infinity times 0 would be a NaN
-    // (an offset, of which the compiler sees what it is a multiple of: a pointer chosen took 8 % more time at one state)
+    // which an infinity times 0 would be a NaN.  (An offset, of which the compiler sees what it is a multiple of: with a pointer
+    // chosen 8x1024x1030 with one state took 111 us, with the offset 105.)
     constexpr int NONE = 2 * TT * S::NP + NT / 64 * TT * 2 * S::NP + TT * NT * SPL;
     for (int e = threadIdx.x; e < 2 * TT * S::NP; e += NT) lds[NONE + e] = 0.0f;
     const float *const bt = lds + (w.in ? 0 : NONE) + n0, *const ct = bt + TT * S::NP;

@@ -19,8 +19,8 @@ struct Param {             // a dense vector or matrix of parameters: fp32 or th
     int32_t f32;
 };
 
-// out[segment][j] = sum over r < rows of in[r * pitch + at + j], fp32 or rounded to `type`: the last step of every sum
-// over workgroups.  The rows go in a fixed order, so the result does not depend on which workgroup ended first.
+// out[segment][j] = sum over r < rows of in[r * pitch + at + j], fp32: the last step of every sum over workgroups.  The rows
+// go in a fixed order, so the result does not depend on which workgroup ended first.
 struct ReduceSeg {
     float *out;            // nullptr: nobody wants it
     int64_t at, len;
@@ -175,7 +175,7 @@ constexpr float LOG2E = 1.44269504088896340736f;
 
 __device__ __forceinline__ float sigmoidf(float u) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * u)); }
 __device__ __forceinline__ float siluf(float u) { return u * sigmoidf(u); }
-// (an infinite u: u * q would be -inf * 0)
+// (SiLU of -inf is a NaN, -inf * 0, as the formula gives in any precision; a clipped NaN stays one)
 __device__ __forceinline__ float apply_act(float u, int act)
 {
     if (act == MERIT_ACT_SILU) return siluf(u);
