@@ -215,7 +215,7 @@ def _run_own(s):
         return {"y": y, "h": h}
     if kind == "delta_train":
         y, h, states = mb.merit_delta_rule(plan, s["q"], s["k"], s["v"], s["g"], s["beta"], lens=s["lens"], final=True, states=True)
-        d = mb.merit_delta_rule_backward(plan, s["dy"], s["q"], s["k"], s["v"], s["g"], s["beta"], states, lens=s["lens"])
+        d = mb.merit_delta_rule_backward(plan, s["dy"], s["q"], s["k"], s["g"], s["beta"], states, lens=s["lens"])
         return {"y": y, "h": h, **{k: d[k] for k in ("dq", "dk", "dv", "dg", "dbeta")}}
     vectors = dict(after_weight=s["aw"], after_bias=s["ab"], scale=s["scale"], before_weight=s["bw"], before_bias=s["bb"])
     if kind == "norm":
