@@ -222,7 +222,7 @@ def _run_own(s):
         out, n = mb.merit_block_norm(plan, s["x"], s["z"], s["r"], **vectors)
         return {"out": out, "n": n}
     out, n, stats = mb.merit_block_norm(plan, s["x"], s["z"], s["r"], stats=True, **vectors)
-    d = mb.merit_block_norm_backward(plan, s["dout"], s["dn"], s["x"], s["z"], out, stats, dr=s["r"] is not None, **vectors)
+    d = mb.merit_block_norm_backward(plan, s["dout"], s["dn"], s["x"], s["z"], s["r"], stats, dr=s["r"] is not None, **vectors)
     return {"out": out, "n": n, **d}
 
 
