@@ -1,6 +1,7 @@
 /*
  * merit_tokens.h -- operators along a sequence of tokens: a short causal convolution, a selective
- * state space scan, a group norm with an activation.  Forward and backward passes for whole
+ * state space scan, the gated delta rule, a group norm with an activation, the norms before and
+ * after a block with its gate and residual scale.  Forward and backward passes for whole
  * sequences, and the forms that continue a sequence by one token.
  *
  * All tensors are channels last: a token's channels lie side by side.  The convolution is a ranged
@@ -47,7 +48,8 @@ typedef struct {
     int32_t reserved;        /* 0 */
 } merit_view;
 
-typedef enum { MERIT_ACT_NONE = 0, MERIT_ACT_RELU = 1, MERIT_ACT_SILU = 2 } merit_act;
+typedef enum { MERIT_ACT_NONE = 0, MERIT_ACT_RELU = 1, MERIT_ACT_SILU = 2,
+               MERIT_ACT_SIGMOID = 3 /* the gate of merit_block_norm only */ } merit_act;
 typedef enum { MERIT_PASS_FORWARD = 0, MERIT_PASS_BACKWARD = 1, MERIT_PASS_STEP = 2 } merit_pass;
 
 typedef struct merit_token_plan merit_token_plan;   /* opaque, host memory only */
@@ -55,6 +57,10 @@ typedef struct merit_token_plan merit_token_plan;   /* opaque, host memory only 
 #define MERIT_CONV_MAX_TAPS   8
 #define MERIT_SCAN_MAX_STATES 64
 #define MERIT_SCAN_TILE       16     /* tokens between two kept states of a forward pass */
+#define MERIT_DELTA_MAX_KEYS  128    /* values of a key */
+#define MERIT_DELTA_CHUNK     64     /* tokens between two kept states of a forward pass */
+#define MERIT_DELTA_EPS       1e-6f  /* beside the square of a length that divides */
+#define MERIT_BLOCK_NORM_MAX_CHANNELS 16384
 
 /* Group norm of x[N, S, C]: the S positions x C / groups channels of a group share mean and variance.
  * S = 1: every token by itself; S = H * W: an image, channels last.  eps >= 0. */
@@ -67,6 +73,15 @@ merit_status merit_plan_causal_conv(merit_dtype type, int64_t B, int64_t L, int6
  * a group share the tokens' B and C.  softplus != 0: the step is log(1 + exp(dt + dt_bias)), else dt + dt_bias. */
 merit_status merit_plan_scan(merit_dtype type, int64_t B, int64_t L, int64_t D, int64_t N, int64_t groups, int softplus,
                              merit_token_plan **out);
+/* Gated delta rule of q, k[B, L, key_heads, Dk] and v[B, L, heads, Dv], Dk <= MERIT_DELTA_MAX_KEYS; heads / key_heads value
+ * heads share a key head.  normalize != 0: q and k count by their direction, x / sqrt(|x|^2 + MERIT_DELTA_EPS). */
+merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64_t heads, int64_t key_heads, int64_t Dk, int64_t Dv,
+                                   double scale, int normalize, merit_token_plan **out);
+/* The end of a block over rows x[B, L, C], C <= MERIT_BLOCK_NORM_MAX_CHANNELS: norm, gate, scale, residual sum, norm (below).
+ * type: of x, z, n and their gradients; stream: of the residual stream r, out and their gradients, `type` or MERIT_F32.
+ * layer != 0: norms subtract the mean; after, before != 0: which of the two norms there are (one at least). */
+merit_status merit_plan_block_norm(merit_dtype type, merit_dtype stream, int64_t B, int64_t L, int64_t C, double eps, int layer,
+                                   merit_act act, int after, int before, merit_token_plan **out);
 merit_status merit_token_plan_destroy(merit_token_plan *plan);
 /* Scratch memory that a pass needs, in bytes (0: none). */
 merit_status merit_token_plan_workspace(const merit_token_plan *plan, merit_pass pass, int64_t *bytes);
@@ -207,6 +222,109 @@ typedef struct {
 } merit_scan_step_args;
 merit_status merit_scan_step(const merit_token_plan *plan, const merit_scan_step_args *args, void *workspace,
                              int64_t workspace_bytes, void *hip_stream);
+
+/* S_t = a_t S_{t-1} + k_t u_t^T,  u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  y_t = scale S_t^T q_t,  a_t = exp(g_t).
+ * The states start from h0, or 0.  lens[b]: tokens of sequence b (cut to [0, L]); behind them nothing is read, y is 0 and the
+ * state stays.  states: for every MERIT_DELTA_CHUNK-th token the state before it (Dk rows) and what the tokens from it on add
+ * along their keys, each for beta = 1 (MERIT_DELTA_CHUNK rows), for the backward pass; not written behind a sequence's last chunk.
+ * A value that is not finite (an infinity, a NaN) makes NaN of what depends on it: q of its token's y, v of its column from its
+ * token on, k, g (but -inf, which is a decay of 0) and beta of the head from there on. */
+typedef struct {
+    merit_view q;            /* T [B, L, key_heads, Dk]                       */
+    merit_view k;            /* T [B, L, key_heads, Dk]                       */
+    merit_view v;            /* T [B, L, heads, Dv]                           */
+    merit_view g;            /* F32 [B, L, heads], optional (0: no decay)     */
+    merit_view beta;         /* P [B, L, heads]                               */
+    merit_view h0;           /* F32 [B, heads, Dk, Dv] dense, optional (0)    */
+    merit_view lens;         /* int32 [B], optional                           */
+    merit_view y;            /* T [B, L, heads, Dv]                           */
+    merit_view h_last;       /* F32 [B, heads, Dk, Dv] dense, optional; may be h0 */
+    merit_view states;       /* F32 [B, ceil(L / MERIT_DELTA_CHUNK), heads, Dk + MERIT_DELTA_CHUNK, Dv] dense, optional */
+} merit_delta_rule_args;
+merit_status merit_delta_rule(const merit_token_plan *plan, const merit_delta_rule_args *args, void *workspace,
+                              int64_t workspace_bytes, void *hip_stream);
+
+typedef struct {
+    merit_view dy;           /* T [B, L, heads, Dv]; not read behind lens     */
+    merit_view q;            /* T [B, L, key_heads, Dk]                       */
+    merit_view k;            /* T [B, L, key_heads, Dk]                       */
+    merit_view g;            /* F32 [B, L, heads], optional                   */
+    merit_view beta;         /* P [B, L, heads]                               */
+    merit_view states;       /* F32, as the forward pass left them            */
+    merit_view lens;         /* int32 [B], optional                           */
+    merit_view dh_last;      /* F32 [B, heads, Dk, Dv] dense, optional        */
+    merit_view dq;           /* T [B, L, key_heads, Dk]; these five: 0 behind lens */
+    merit_view dk;           /* T [B, L, key_heads, Dk]                       */
+    merit_view dv;           /* T [B, L, heads, Dv]                           */
+    merit_view dg;           /* F32 [B, L, heads], optional                   */
+    merit_view dbeta;        /* F32 [B, L, heads]                             */
+    merit_view dh0;          /* F32 [B, heads, Dk, Dv] dense, optional        */
+} merit_delta_rule_backward_args;
+merit_status merit_delta_rule_backward(const merit_token_plan *plan, const merit_delta_rule_backward_args *args, void *workspace,
+                                       int64_t workspace_bytes, void *hip_stream);
+
+/* One more token of every sequence (the plan's L is not looked at).  Operands but the states: stride[0] between sequences. */
+typedef struct {
+    merit_view h;            /* F32 [B, heads, Dk, Dv] dense                  */
+    merit_view q;            /* T [B, key_heads, Dk]                          */
+    merit_view k;            /* T [B, key_heads, Dk]                          */
+    merit_view v;            /* T [B, heads, Dv]                              */
+    merit_view g;            /* F32 [B, heads], optional                      */
+    merit_view beta;         /* P [B, heads]                                  */
+    merit_view y;            /* T [B, heads, Dv]                              */
+    merit_view h_out;        /* F32 [B, heads, Dk, Dv] dense; may be h        */
+} merit_delta_rule_step_args;
+merit_status merit_delta_rule_step(const merit_token_plan *plan, const merit_delta_rule_step_args *args, void *workspace,
+                                   int64_t workspace_bytes, void *hip_stream);
+
+/* u = norm(x) after_weight + after_bias (x where the plan has no norm after the block);  t = u act(z), or u;
+ * out = r + scale t;  n = norm(out) before_weight + before_bias, from `out` before it is rounded.
+ * norm(x) = x / sqrt(mean(x^2) + eps), or (x - mean) / sqrt(var + eps); weights, scale: 1, biases, r: 0 where absent, and absent
+ * where the plan has no such norm.  The strides of z may be 0: a gate for each sequence. */
+typedef struct {
+    merit_view x;            /* T [B, L, C]                                   */
+    merit_view z;            /* T [B, L, C], optional (no gate)               */
+    merit_view r;            /* stream [B, L, C], optional                    */
+    merit_view after_weight; /* P [C], optional                               */
+    merit_view after_bias;   /* P [C], optional                               */
+    merit_view scale;        /* P [C], optional                               */
+    merit_view before_weight;/* P [C], optional                               */
+    merit_view before_bias;  /* P [C], optional                               */
+    merit_view out;          /* stream [B, L, C]; may be r                    */
+    merit_view n;            /* T [B, L, C], where the plan has the norm before the next block; may be x */
+    merit_view after_mean;   /* F32 [B, L], these four optional: kept for backward */
+    merit_view after_rstd;   /* F32 [B, L]                                    */
+    merit_view before_mean;  /* F32 [B, L]                                    */
+    merit_view before_rstd;  /* F32 [B, L]                                    */
+} merit_block_norm_args;
+merit_status merit_block_norm(const merit_token_plan *plan, const merit_block_norm_args *args, void *workspace,
+                              int64_t workspace_bytes, void *hip_stream);
+
+typedef struct {
+    merit_view dout;         /* stream [B, L, C], optional (0)                */
+    merit_view dn;           /* T [B, L, C], where the plan has that norm     */
+    merit_view x;            /* T [B, L, C]                                   */
+    merit_view z;            /* T [B, L, C], optional                         */
+    merit_view r;            /* stream [B, L, C], optional; not read where the plan has no norm before the next block */
+    merit_view after_weight; /* P [C], optional                               */
+    merit_view after_bias;   /* P [C], optional                               */
+    merit_view scale;        /* P [C], optional                               */
+    merit_view before_weight;/* P [C], optional                               */
+    merit_view after_mean;   /* F32 [B, L], as the forward pass left them: rstd where the plan has the norm, mean besides */
+    merit_view after_rstd;   /* F32 [B, L]  where it is a layer norm          */
+    merit_view before_mean;  /* F32 [B, L]                                    */
+    merit_view before_rstd;  /* F32 [B, L]                                    */
+    merit_view dx;           /* T [B, L, C]                                   */
+    merit_view dz;           /* T [B, L, C], present where z is: a gradient for each row, also where rows share a gate */
+    merit_view dr;           /* stream [B, L, C], optional; may be dout       */
+    merit_view dafter_weight;/* F32 [C], these five optional                  */
+    merit_view dafter_bias;  /* F32 [C]                                       */
+    merit_view dscale;       /* F32 [C]                                       */
+    merit_view dbefore_weight;/* F32 [C]                                      */
+    merit_view dbefore_bias; /* F32 [C]                                       */
+} merit_block_norm_backward_args;
+merit_status merit_block_norm_backward(const merit_token_plan *plan, const merit_block_norm_backward_args *args, void *workspace,
+                                       int64_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

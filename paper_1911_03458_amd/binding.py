@@ -18,7 +18,11 @@ import threading
 import warnings
 
 from . import build as _build
-from . import tokens
+from . import mixers, tokens
+from .mixers import (  # noqa: F401
+    MERIT_ACT_SIGMOID, MERIT_BLOCK_NORM_MAX_CHANNELS, MERIT_DELTA_CHUNK, MERIT_DELTA_MAX_KEYS, merit_block_norm,
+    merit_block_norm_backward, merit_delta_rule, merit_delta_rule_backward, merit_delta_rule_step, merit_plan_block_norm,
+    merit_plan_delta_rule)
 from .tokens import (  # noqa: F401  (the operators along a sequence of tokens)
     MERIT_ACT_NONE, MERIT_ACT_RELU, MERIT_ACT_SILU, MERIT_BF16, MERIT_CONV_MAX_TAPS, MERIT_PASS_BACKWARD,
     MERIT_PASS_FORWARD, MERIT_PASS_STEP, MERIT_SCAN_MAX_STATES, MERIT_SCAN_TILE, TokenPlan, merit_causal_conv,
@@ -134,6 +138,7 @@ def lib():
                  "merit_conv2d_packed", "merit_conv2d_packed_noalloc"):
         getattr(L, name).restype = c_int
     tokens._declare(L)
+    mixers._declare(L)
     L.merit_status_string.argtypes = [c_int]
     L.merit_status_string.restype = ctypes.c_char_p
     _lib = L

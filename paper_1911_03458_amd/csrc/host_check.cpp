@@ -237,6 +237,7 @@ int take_tokens(merit_status st, merit_token_plan *plan)
     };
     refused(merit_causal_conv_step(plan, static_cast<const merit_causal_conv_step_args *>(v), nullptr, 0, nullptr));
     refused(merit_scan_step(plan, static_cast<const merit_scan_step_args *>(v), nullptr, 0, nullptr));
+    refused(merit_delta_rule_step(plan, static_cast<const merit_delta_rule_step_args *>(v), nullptr, 0, nullptr));
     CHECK(taken == 1 - norm);
     CHECK(merit_token_plan_destroy(plan) == MERIT_OK);
     return 1;
@@ -260,7 +261,18 @@ int sweep_tokens(uint64_t seed, int rounds)
         p = nullptr;
         st = merit_plan_scan(type, size(33) - 1, size(33) - 1, G * size(20), r.in(0, 66), G, r.in(0, 1), &p);
         made += take_tokens(st, p);
+        p = nullptr;
+        st = merit_plan_delta_rule(type, size(33) - 1, size(33) - 1, G * size(12), G, size(9), size(26), r.in(-1, 1) * 0.5, r.in(0, 1), &p);
+        made += take_tokens(st, p);
+        p = nullptr;
+        st = merit_plan_block_norm(type, (merit_dtype)r.in(0, 3), size(33) - 1, size(33) - 1, size(16), r.in(-1, 3) * 1e-5, r.in(0, 1),
+                                   (merit_act)r.in(0, 3), r.in(0, 1), r.in(0, 1), &p);
+        made += take_tokens(st, p);
         // ordinary sizes
+        p = nullptr;
+        made += take_tokens(merit_plan_delta_rule(MERIT_BF16, size(6), size(15), 2 * (1 + size(4)), 2, 1 + (int64_t)r.in(0, 127), 1 + size(9), 1.0, 1, &p), p);
+        p = nullptr;
+        made += take_tokens(merit_plan_block_norm(MERIT_BF16, MERIT_F32, size(6), size(15), 1 + size(14), 1e-6, 0, MERIT_ACT_SILU, 1, 1, &p), p);
         p = nullptr;
         made += take_tokens(merit_plan_group_norm(MERIT_BF16, size(15), 1 + size(14), 8 * (1 + size(8)), 8, 1e-5, MERIT_ACT_SILU, &p), p);
         p = nullptr;

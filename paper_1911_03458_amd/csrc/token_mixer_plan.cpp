@@ -1,0 +1,352 @@
+// Plans and entry points of the gated delta rule and of the norms before and after a block (include/merit_tokens.h): what is
+// accepted, how a pass is split into workgroups, how much scratch memory it takes.  Host code only.
+#include "token_plan.h"
+
+using namespace merit;
+
+namespace {
+
+Rows rows_of(Views &v, const merit_view &view, int type, bool required)
+{
+    const int own = v.type;
+    v.type = type;
+    const Rows r = v.rows(view, required);
+    v.type = own;
+    return r;
+}
+
+// ---- gated delta rule ------------------------------------------------------------------------
+// Scratch memory, in the order of its parts; every part is a multiple of 16 bytes but the last
+struct DeltaScratch {
+    int64_t scal, tri, mix, dx, ds, part, bytes;
+};
+DeltaScratch delta_scratch(const DeltaParams &p, bool backward)
+{
+    constexpr int64_t square = (int64_t)MERIT_DELTA_CHUNK * MERIT_DELTA_CHUNK * 2;
+    const int64_t chunks = p.B * p.n * p.H;
+    DeltaScratch s = {};
+    s.tri = chunks * DELTA_SCALAR_FLOATS * 4;
+    s.mix = s.tri + chunks * 3 * square;
+    s.dx = s.mix + chunks * (backward || p.type == MERIT_F32 ? 3 : 2) * square;
+    s.bytes = s.dx;
+    if (!backward) return s;
+    s.ds = s.dx + chunks * MERIT_DELTA_CHUNK * p.Dv * 4;
+    s.part = s.ds + chunks * ((int64_t)p.Dk * p.Dv * 4 + 15) / 16 * 16;
+    s.bytes = s.part + (p.each > 1 ? 2 * p.B * p.L * p.H * p.Dk * 4 : 0);
+    return s;
+}
+void delta_use(DeltaParams &p, void *workspace, bool backward)
+{
+    const DeltaScratch s = delta_scratch(p, backward);
+    char *at = static_cast<char *>(workspace);
+    p.scal = reinterpret_cast<float *>(at + s.scal);
+    p.tri = at + s.tri;
+    p.mix = at + s.mix;
+    if (!backward) return;
+    p.dx = reinterpret_cast<float *>(at + s.dx);
+    p.ds = reinterpret_cast<float *>(at + s.ds);
+    p.part = p.each > 1 ? reinterpret_cast<float *>(at + s.part) : nullptr;
+}
+void delta_gates(Views &v, DeltaParams &p, const merit_view &g, const merit_view &beta)
+{
+    p.g = rows_of(v, g, MERIT_F32, false);
+    p.beta_f32 = beta.dtype == MERIT_F32;
+    p.beta = rows_of(v, beta, p.beta_f32 ? MERIT_F32 : v.type, true);
+}
+bool in_16_bytes(const Rows &r, int64_t n0, int64_t n1, int type) { return wide(r, n0, n1, 16 / elem_bytes(type), type); }
+bool address_16(const void *a) { return reinterpret_cast<uintptr_t>(a) % 16 == 0; }
+
+// ---- the norms before and after a block -----------------------------------------------------
+// The threads of a row for `vec` channels each: a run of lanes up to 64 vectors, else a workgroup.
+void block_layout(BlockNormParams &p, int vec, bool backward)
+{
+    p.vec = vec;
+    const int cu = p.C / vec;
+    p.lanes = 0;
+    p.units = 1;
+    p.threads = cu <= 256 ? 256 : cu <= 512 ? 512 : 1024;
+    if (cu <= 64) {
+        p.lanes = 1;
+        while (p.lanes < cu) p.lanes *= 2;
+    }
+    while (p.threads * p.units < cu) p.units *= 2;
+    const int64_t at_once = p.lanes ? 256 / p.lanes : 1;
+    const int64_t most = (backward ? 131072 : 524288) / p.threads;
+    p.blocks = cdiv(p.rows, at_once);
+    if (p.blocks > most) p.blocks = most;
+}
+template <typename F> int block_vec(const BlockNormParams &p, F &&fits)
+{
+    const int most = 16 / elem_bytes(p.type);
+    for (int vec : {most, 2})
+        if (p.C % vec == 0 && fits(vec)) return vec;
+    return 1;
+}
+bool block_rows(const BlockNormParams &p, const Rows &r, int vec, int type)
+{
+    return wide(r, p.B, p.L, type == MERIT_F32 && vec > 4 ? 4 : vec, type);
+}
+int64_t block_bytes(const BlockNormParams &p)
+{
+    int64_t most = 0;
+    for (int vec : {16 / elem_bytes(p.type), 2, 1}) {
+        if (p.C % vec) continue;
+        BlockNormParams q = p;
+        block_layout(q, vec, true);
+        const int64_t n = q.blocks * 5 * p.C * 4;
+        if (n > most) most = n;
+    }
+    return most;
+}
+
+}  // namespace
+
+namespace merit {
+
+merit_status mixer_workspace(const merit_token_plan *plan, merit_pass pass, int64_t *bytes)
+{
+    if ((int)pass < 0 || (int)pass > 2 || (plan->kind == BLOCK && pass == MERIT_PASS_STEP)) return MERIT_ERR_INVALID_ARG;
+    if (pass == MERIT_PASS_STEP) return MERIT_OK;
+    const bool backward = pass == MERIT_PASS_BACKWARD;
+    if (plan->kind == DELTA) *bytes = delta_scratch(plan->delta, backward).bytes;
+    else *bytes = backward ? block_bytes(plan->block) : 0;
+    return MERIT_OK;
+}
+
+merit_status mixer_kernel(const merit_token_plan *plan, merit_pass pass, const char **name)
+{
+    if ((int)pass < 0 || (int)pass > 2 || (plan->kind == BLOCK && pass == MERIT_PASS_STEP)) return MERIT_ERR_INVALID_ARG;
+    const bool backward = pass == MERIT_PASS_BACKWARD;
+    if (plan->kind == BLOCK)
+        *name = backward ? "merit_block_norm_rows_backward+merit_reduce_rows" : "merit_block_norm_rows";
+    else
+        *name = pass == MERIT_PASS_STEP   ? "merit_delta_token"
+                : !backward               ? "merit_delta_prepare+merit_delta_chunks"
+                : plan->delta.each > 1    ? "merit_delta_prepare+merit_delta_back_chunks+merit_delta_grads+merit_delta_sum_heads"
+                                          : "merit_delta_prepare+merit_delta_back_chunks+merit_delta_grads";
+    return MERIT_OK;
+}
+
+}  // namespace merit
+
+extern "C" {
+
+merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64_t heads, int64_t key_heads, int64_t Dk, int64_t Dv,
+                                   double scale, int normalize, merit_token_plan **out)
+{
+    if (!out) return MERIT_ERR_NULL;
+    *out = nullptr;
+    if (!type_ok(type) || B < 0 || L < 0 || heads < 1 || key_heads < 1 || Dk < 1 || Dv < 1 || !std::isfinite(scale))
+        return MERIT_ERR_INVALID_ARG;
+    if (heads % key_heads != 0) return MERIT_ERR_SHAPE;
+    if (Dk > MERIT_DELTA_MAX_KEYS || Dv > MAX_CHANNELS || heads > MAX_CHANNELS / Dv || heads > MAX_CHANNELS / Dk || B > MAX_ROWS ||
+        L > MAX_ROWS || too_large(B, L, heads * (Dk + Dv)))
+        return MERIT_ERR_UNSUPPORTED;
+    const int64_t n = cdiv(L, MERIT_DELTA_CHUNK);
+    // workgroups of every pass, at the narrowest tiles; the sum over heads, a thread a value; states of all chunks
+    if (B > MAX_BLOCKS / heads || B * heads * (n > cdiv(Dv, 16) ? n : cdiv(Dv, 16)) >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + 64) * Dv) ||
+        (L > 0 && B > MAX_BLOCKS / L * 256 / (key_heads * Dk)))
+        return MERIT_ERR_UNSUPPORTED;
+    merit_token_plan *pl = new_plan(DELTA, type);
+    if (!pl) return MERIT_ERR_INVALID_ARG;
+    DeltaParams &p = pl->delta;
+    p.B = B; p.L = L;
+    p.H = (int)heads; p.K = (int)key_heads; p.each = (int)(heads / key_heads);
+    p.Dk = (int)Dk; p.Dv = (int)Dv;
+    p.scale = (float)scale;
+    p.unit = normalize != 0;
+    p.type = type;
+    p.n = (int)n;
+    *out = pl;
+    return MERIT_OK;
+}
+
+merit_status merit_plan_block_norm(merit_dtype type, merit_dtype stream, int64_t B, int64_t L, int64_t C, double eps, int layer,
+                                   merit_act act, int after, int before, merit_token_plan **out)
+{
+    if (!out) return MERIT_ERR_NULL;
+    *out = nullptr;
+    if (!type_ok(type) || (stream != type && stream != MERIT_F32) || (int)act < 0 || (int)act > 3 || B < 0 || L < 0 || C < 1 ||
+        !(eps >= 0.0) || !std::isfinite(eps) || !(after || before))
+        return MERIT_ERR_INVALID_ARG;
+    if (C > MERIT_BLOCK_NORM_MAX_CHANNELS || B > MAX_ROWS || L > MAX_ROWS || (L > 0 && B > MAX_ROWS / L)) return MERIT_ERR_UNSUPPORTED;
+    merit_token_plan *pl = new_plan(BLOCK, type);
+    if (!pl) return MERIT_ERR_INVALID_ARG;
+    BlockNormParams &p = pl->block;
+    p.B = B; p.L = L; p.rows = B * L;
+    p.C = (int)C;
+    p.eps = (float)eps;
+    p.layer = layer != 0;
+    p.act = act;
+    p.after = after != 0;
+    p.before = before != 0;
+    p.type = type;
+    p.stream = stream;
+    *out = pl;
+    return MERIT_OK;
+}
+
+// ---- gated delta rule ---------------------------------------------------------------------------
+merit_status merit_delta_rule(const merit_token_plan *plan, const merit_delta_rule_args *a, void *workspace, int64_t workspace_bytes,
+                              void *stream)
+{
+    if (!plan || !a) return MERIT_ERR_NULL;
+    if (plan->kind != DELTA) return MERIT_ERR_INVALID_ARG;
+    DeltaParams p = plan->delta;
+    if (p.B == 0) return MERIT_OK;
+    const bool some = p.L > 0;
+    Views v{plan->type};
+    p.q = v.rows(a->q, some);
+    p.k = v.rows(a->k, some);
+    p.v = v.rows(a->v, some);
+    if (some) delta_gates(v, p, a->g, a->beta);
+    p.h0 = v.f32(a->h0);
+    p.lens = v.lens(a->lens);
+    p.y = v.rows(a->y, some);
+    p.h_last = v.f32(a->h_last);
+    p.states = v.f32(a->states);
+    if (v.st != MERIT_OK) return v.st;
+    const merit_status st = scratch(delta_scratch(p, false).bytes, workspace, workspace_bytes);
+    if (st != MERIT_OK) return st;
+    delta_use(p, workspace, false);
+    p.wide_qk = p.Dk % 8 == 0 && in_16_bytes(p.q, p.B, p.L, p.type) && in_16_bytes(p.k, p.B, p.L, p.type);
+    return done(launch_delta(p, static_cast<hipStream_t>(stream)));
+}
+
+merit_status merit_delta_rule_backward(const merit_token_plan *plan, const merit_delta_rule_backward_args *a, void *workspace,
+                                       int64_t workspace_bytes, void *stream)
+{
+    if (!plan || !a) return MERIT_ERR_NULL;
+    if (plan->kind != DELTA) return MERIT_ERR_INVALID_ARG;
+    DeltaParams p = plan->delta;
+    if (p.B == 0) return MERIT_OK;
+    const bool some = p.L > 0;
+    Views v{plan->type};
+    p.dy = v.rows(a->dy, some);
+    p.q = v.rows(a->q, some);
+    p.k = v.rows(a->k, some);
+    if (some) delta_gates(v, p, a->g, a->beta);
+    p.states = v.f32(a->states, some);
+    p.lens = v.lens(a->lens);
+    p.dh_last = v.f32(a->dh_last);
+    p.dq = v.rows(a->dq, some);
+    p.dk = v.rows(a->dk, some);
+    p.dv = v.rows(a->dv, some);
+    p.dg = rows_of(v, a->dg, MERIT_F32, false);
+    p.dbeta = rows_of(v, a->dbeta, MERIT_F32, some);
+    p.dh0 = v.f32(a->dh0);
+    if (v.st != MERIT_OK) return v.st;
+    const merit_status st = scratch(delta_scratch(p, true).bytes, workspace, workspace_bytes);
+    if (st != MERIT_OK) return st;
+    delta_use(p, workspace, true);
+    p.wide_qk = p.Dk % 8 == 0 && in_16_bytes(p.q, p.B, p.L, p.type) && in_16_bytes(p.k, p.B, p.L, p.type);
+    p.wide_v = p.Dv % 8 == 0 && in_16_bytes(p.dy, p.B, p.L, p.type) && address_16(p.states);
+    return done(launch_delta_backward(p, static_cast<hipStream_t>(stream)));
+}
+
+merit_status merit_delta_rule_step(const merit_token_plan *plan, const merit_delta_rule_step_args *a, void *, int64_t, void *stream)
+{
+    if (!plan || !a) return MERIT_ERR_NULL;
+    if (plan->kind != DELTA) return MERIT_ERR_INVALID_ARG;
+    DeltaParams p = plan->delta;
+    if (p.B == 0) return MERIT_OK;
+    Views v{plan->type};
+    p.h0 = v.f32(a->h, true);
+    p.q = v.rows(a->q);
+    p.k = v.rows(a->k);
+    p.v = v.rows(a->v);
+    delta_gates(v, p, a->g, a->beta);
+    p.y = v.rows(a->y);
+    p.h_last = v.f32(a->h_out, true);
+    if (v.st != MERIT_OK) return v.st;
+    p.wide_state = p.Dv % 4 == 0 && address_16(p.h0) && address_16(p.h_last);
+    return done(launch_delta_step(p, static_cast<hipStream_t>(stream)));
+}
+
+// ---- the norms before and after a block -----------------------------------------------------------
+merit_status merit_block_norm(const merit_token_plan *plan, const merit_block_norm_args *a, void *, int64_t, void *stream)
+{
+    if (!plan || !a) return MERIT_ERR_NULL;
+    if (plan->kind != BLOCK) return MERIT_ERR_INVALID_ARG;
+    BlockNormParams p = plan->block;
+    if (p.rows == 0) return MERIT_OK;
+    Views v{plan->type};
+    p.x = v.rows(a->x);
+    p.z = v.rows(a->z, false);
+    p.r = rows_of(v, a->r, p.stream, false);
+    p.aw = v.param(a->after_weight);
+    p.ab = v.param(a->after_bias);
+    p.scale = v.param(a->scale);
+    p.bw = v.param(a->before_weight);
+    p.bb = v.param(a->before_bias);
+    p.out = rows_of(v, a->out, p.stream, true);
+    p.n = v.rows(a->n, p.before);
+    p.am = v.f32(a->after_mean);
+    p.ar = v.f32(a->after_rstd);
+    p.bm = v.f32(a->before_mean);
+    p.br = v.f32(a->before_rstd);
+    if (v.st != MERIT_OK) return v.st;
+    if ((!p.after && (p.aw.data || p.ab.data)) || (!p.before && (p.bw.data || p.bb.data || p.n.data))) return MERIT_ERR_INVALID_ARG;
+    const int vec = block_vec(p, [&](int n) {
+        return block_rows(p, p.x, n, p.type) && block_rows(p, p.z, n, p.type) && block_rows(p, p.n, n, p.type) &&
+               block_rows(p, p.r, n, p.stream) && block_rows(p, p.out, n, p.stream);
+    });
+    block_layout(p, vec, false);
+    return done(launch_block_norm(p, static_cast<hipStream_t>(stream)));
+}
+
+merit_status merit_block_norm_backward(const merit_token_plan *plan, const merit_block_norm_backward_args *a, void *workspace,
+                                       int64_t workspace_bytes, void *stream)
+{
+    if (!plan || !a) return MERIT_ERR_NULL;
+    if (plan->kind != BLOCK) return MERIT_ERR_INVALID_ARG;
+    BlockNormParams p = plan->block;
+    const bool some = p.rows > 0;
+    Views v{plan->type};
+    p.dout = rows_of(v, a->dout, p.stream, false);
+    p.dn = v.rows(a->dn, some && p.before);
+    p.x = v.rows(a->x, some);
+    p.z = v.rows(a->z, false);
+    p.r = rows_of(v, a->r, p.stream, false);
+    p.aw = v.param(a->after_weight);
+    p.ab = v.param(a->after_bias);
+    p.scale = v.param(a->scale);
+    p.bw = v.param(a->before_weight);
+    p.am = v.f32(a->after_mean, some && p.after && p.layer);
+    p.ar = v.f32(a->after_rstd, some && p.after);
+    p.bm = v.f32(a->before_mean, some && p.before && p.layer);
+    p.br = v.f32(a->before_rstd, some && p.before);
+    p.dx = v.rows(a->dx, some);
+    p.dz = v.rows(a->dz, some && p.z.data);
+    p.dr = rows_of(v, a->dr, p.stream, false);
+    p.daw = v.f32(a->dafter_weight);
+    p.dab = v.f32(a->dafter_bias);
+    p.dscale = v.f32(a->dscale);
+    p.dbw = v.f32(a->dbefore_weight);
+    p.dbb = v.f32(a->dbefore_bias);
+    if (v.st != MERIT_OK) return v.st;
+    if ((!p.after && (p.aw.data || p.ab.data || p.daw || p.dab)) || (!p.before && (p.bw.data || p.dbw || p.dbb || p.dn.data)) ||
+        (!p.z.data && p.dz.data))
+        return MERIT_ERR_INVALID_ARG;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!some) {                                        // no gradient from nothing: zeros
+        ReduceParams r = {};
+        for (float *o : {p.daw, p.dab, p.dscale, p.dbw, p.dbb})
+            if (o) r.seg[r.nseg++] = {o, 0, p.C};
+        return r.nseg ? done(launch_reduce_rows(r, s)) : MERIT_OK;
+    }
+    const int vec = block_vec(p, [&](int n) {
+        for (const Rows *r : {&p.x, &p.z, &p.dn, &p.dx, &p.dz})
+            if (!block_rows(p, *r, n, p.type)) return false;
+        for (const Rows *r : {&p.dout, &p.r, &p.dr})
+            if (!block_rows(p, *r, n, p.stream)) return false;
+        return true;
+    });
+    block_layout(p, vec, true);
+    const merit_status st = scratch(p.blocks * 5 * p.C * 4, workspace, workspace_bytes);
+    if (st != MERIT_OK) return st;
+    p.part = static_cast<float *>(workspace);
+    return done(launch_block_norm_backward(p, s));
+}
+
+}  // extern "C"

@@ -28,7 +28,7 @@ struct ReduceSeg {
 struct ReduceParams {
     const float *in;
     int64_t rows, pitch;
-    ReduceSeg seg[4];
+    ReduceSeg seg[5];
     int nseg;
 };
 hipError_t launch_reduce_rows(const ReduceParams &p, hipStream_t s);
@@ -96,14 +96,58 @@ constexpr int SCAN_THREADS = 256;
 // in launches of this many, one after the other.
 constexpr int64_t SCAN_FORWARD_BLOCKS = (1ll << 32) / (2 * SCAN_THREADS) - 1;
 
+// ---- gated delta rule ----------------------------------------------------------------
+struct DeltaParams {
+    int64_t B, L;
+    int H, K, each, Dk, Dv;    // each = H / K value heads share a key head
+    float scale;
+    int unit;              // q and k count by their direction
+    int type;
+    int n;                 // chunks of MERIT_DELTA_CHUNK tokens
+    int slices;            // workgroups along v's columns
+    int wide_qk, wide_v, wide_state;    // whether rows can be read in 16-byte pieces
+    Rows q, k, v, y, dy, dq, dk, dv;
+    Rows g, beta, dg, dbeta;            // a number a head
+    int beta_f32;
+    const float *h0, *dh_last;
+    float *h_last, *states, *dh0;
+    const int32_t *lens;
+    void *tri, *mix;       // workspace: a chunk's two triangular matrices, in terms
+    float *scal;           // factors of its tokens
+    float *dx, *ds;        // backward: x of its tokens, the gradient of the state behind it
+    float *part;           // dq, dk of a value head, where value heads share keys
+};
+constexpr int DELTA_SCALAR_FLOATS = 8 * MERIT_DELTA_CHUNK;
+
+// ---- the norms before and after a block ------------------------------------------------
+struct BlockNormParams {
+    int64_t B, L, rows;    // rows = B L
+    int C;
+    float eps;
+    int layer, act, after, before;
+    int type, stream;
+    int vec;               // channels a lane moves at once
+    int threads;           // of a workgroup; lanes of a row where it is a wavefront or less
+    int lanes;             // (0: a workgroup a row)
+    int units;             // vectors a thread
+    int64_t blocks;
+    Rows x, z, r, out, n, dout, dn, dx, dz, dr;
+    Param aw, ab, scale, bw, bb;
+    float *am, *ar, *bm, *br;           // [B, L]
+    float *part;           // backward: [blocks][5][C]
+    float *daw, *dab, *dscale, *dbw, *dbb;
+};
+
 }  // namespace merit
 
 struct merit_token_plan {
-    int kind;              // 0 norm, 1 convolution, 2 scan
+    int kind;              // 0 norm, 1 convolution, 2 scan, 3 delta rule, 4 block norm
     int type;              // merit_dtype
     merit::NormParams norm;
     merit::CconvParams conv;
     merit::ScanParams scan, scan_back;     // (in how many chunks: one choice for each direction)
+    merit::DeltaParams delta;
+    merit::BlockNormParams block;
 };
 
 namespace merit {
@@ -115,6 +159,14 @@ hipError_t launch_cconv_step(const CconvParams &p, int type, hipStream_t s);
 hipError_t launch_scan(const ScanParams &p, hipStream_t s);
 hipError_t launch_scan_backward(const ScanParams &p, hipStream_t s);
 hipError_t launch_scan_step(const ScanParams &p, hipStream_t s);
+hipError_t launch_delta(const DeltaParams &p, hipStream_t s);
+hipError_t launch_delta_backward(const DeltaParams &p, hipStream_t s);
+hipError_t launch_delta_step(const DeltaParams &p, hipStream_t s);
+hipError_t launch_block_norm(const BlockNormParams &p, hipStream_t s);
+hipError_t launch_block_norm_backward(const BlockNormParams &p, hipStream_t s);
+// What a plan of the last two kinds answers to merit_token_plan_workspace and _kernel (token_mixer_plan.cpp)
+merit_status mixer_workspace(const merit_token_plan *plan, merit_pass pass, int64_t *bytes);
+merit_status mixer_kernel(const merit_token_plan *plan, merit_pass pass, const char **name);
 }  // namespace merit
 
 #ifdef __HIPCC__
