@@ -13,211 +13,172 @@ namespace merit {
 namespace delta {
 
 // ---------------------------------------------------------------------------
-// one chunk after the other, from the last: a workgroup 16 NC columns of a head's Z
+// one chunk after the other, from the last: a wavefront 16 columns of a head's Z
 // ---------------------------------------------------------------------------
-template <typename T, int KF, int NC>
+// Split as merit_delta_chunks is: a wavefront has its columns of Z and of all tokens in registers, LDS holds K, Q and the transposes
+// of the triangular matrices, of which a row of blocks begins at the diagonal.
+template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(true), RT = KF < 2 ? 1 : KF / 2;
+    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(true), RT = C / 16, DT = 2 * KF;
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
-    typedef Tile<NK, C, KF * 32> TK;
-    typedef Tile<3, NC * 16, KF * 32> TS;
-    typedef Tile<3, NC * 16, C> TX;
-    typedef Tile<NK, NC * 16, C> TY;
+    typedef Mixed<NK, KF * 32> TK;
     const TK kt{smem}, qt{kt.at + TK::bytes / 2};
-    const TS zt{qt.at + TK::bytes / 2};
-    const TX ut{zt.at + TS::bytes / 2}, it{ut.at + TX::bytes / 2};     // it: i dy and then i dv
-    const TY yt{it.at + TX::bytes / 2};
+    const Mixed<3, C> tt{qt.at + TK::bytes / 2};
+    const Mixed<NP, C> mt{tt.at + Mixed<3, C>::bytes / 2};
+    float *const sc = reinterpret_cast<float *>(mt.at + Mixed<NP, C>::bytes / 2);
 
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
-    const int c0 = (int)(id % (uint32_t)p.slices) * NC * 16, kh = (int)h / p.each;
-    const int len = tokens_of(p, b), n = (len + C - 1) / C;
+    const int kh = (int)h / p.each, len = tokens_of(p, b), n = (len + C - 1) / C;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
-    const int row4 = 16 * wave + 4 * quad;
     const int64_t head = b * p.H + h, Dv = p.Dv;
-    const bool has_rows = wave < 2 * KF;
+    const int c0 = (int)(id % (uint32_t)p.slices) * 64, c = c0 + 16 * wave + l16;
+    const bool busy = c0 + 16 * wave < Dv, in = c < Dv;
 
-    f32x4 Z[RT][NC];
+    f32x4 Z[DT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 16 * (wave + 4 * rt) + 4 * quad + r, dv = c0 + 16 * ct + l16;
-                Z[rt][ct][r] = p.dh_last && dk < p.Dk && dv < Dv ? p.dh_last[(head * p.Dk + dk) * Dv + dv] : 0.0f;
-            }
-    auto to_lds = [&]() __attribute__((always_inline)) {
-        if (has_rows)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct) {
-                    const float e[4] = {Z[rt][ct][0], Z[rt][ct][1], Z[rt][ct][2], Z[rt][ct][3]};
-                    zt.put4(16 * ct + l16, 16 * (wave + 4 * rt) + 4 * quad, e);
-                }
-    };
-    auto to_memory = [&](float *out) __attribute__((always_inline)) {
-        if (has_rows)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int dk = 16 * (wave + 4 * rt) + 4 * quad + r, dv = c0 + 16 * ct + l16;
-                        if (dk < p.Dk && dv < Dv) out[dk * Dv + dv] = Z[rt][ct][r];
-                    }
-    };
-
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 16 * d + 4 * quad + r;
+            Z[d][r] = p.dh_last && dk < p.Dk && in ? p.dh_last[(head * p.Dk + dk) * Dv + c] : 0.0f;
+        }
+    const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);
     ChunkRows<T, KF> kr, qr;
-    if (n > 0) {
-        kr.load(p.k, b, (int64_t)(n - 1) * C, len - (n - 1) * C, kh, p.Dk, p.wide_qk);
-        qr.load(p.q, b, (int64_t)(n - 1) * C, len - (n - 1) * C, kh, p.Dk, p.wide_qk);
-    }
-    to_lds();
-    for (int i = n - 1; i >= 0; --i) {
-        const int64_t t0 = (int64_t)i * C, chunk = (b * p.n + i) * p.H + h;
-        const int m = min(C, len - (int)t0);
-        const float *scal = p.scal + chunk * SCALAR_FLOATS;
-        const f32x4 in_k = *reinterpret_cast<const f32x4 *>(scal + IN_K * C + row4);
-        const f32x4 in_q = *reinterpret_cast<const f32x4 *>(scal + IN_Q * C + row4);
-        const f32x4 out_k = *reinterpret_cast<const f32x4 *>(scal + OUT_K * C + row4);
-        const f32x4 beta = *reinterpret_cast<const f32x4 *>(scal + BETA * C + row4);
-        const float whole = exp_of(reinterpret_cast<const double *>(scal + SCALARS * C)[C - 1]);
-        kr.store(kt);
-        qr.store(qt);
+    Square<3> tr;
+    Square<NP> mr;
+    f32x4 sr;
+    ChunkColumn<T> dy;
+    auto load = [&](int i, auto full) __attribute__((always_inline)) {
+        const int64_t chunk = (b * p.n + i) * p.H + h;
+        const int m = min(C, len - i * C);
+        kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
+        qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
+        tr.load(p.tri, chunk);
+        mr.load(p.mix, chunk);
+        sr = reinterpret_cast<const f32x4 *>(p.scal + chunk * SCALAR_FLOATS)[tid % (SCALAR_FLOATS / 4)];
+    };
+    auto load_dy = [&](int i, auto full) __attribute__((always_inline)) {
+        dy.template load<full.value>(p.dy, b, (int64_t)i * C, min(C, len - i * C), mine);
+    };
+    auto scalar = [&](int which, int rt) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4 *>(sc + which * C + 16 * rt + 4 * quad);
+    };
+    // Z += (rows of keys)^T w
+    auto into_state = [&](const TK &t, const f32x4 (&w)[RT]) __attribute__((always_inline)) {
+        bf16x8 o[2][3];
 #pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            float dy[4], in[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dv = c0 + 16 * ct + l16;
-                dy[r] = row4 + r < m && dv < Dv
-                            ? (float)static_cast<const T *>(p.dy.data)[b * p.dy.s0 + (t0 + row4 + r) * p.dy.s1 + h * Dv + dv] : 0.0f;
-                in[r] = in_q[r] * dy[r];
-            }
-            yt.put4(16 * ct + l16, row4, dy);
-            it.put4(16 * ct + l16, row4, in);
-        }
-        to_memory(p.ds + chunk * p.Dk * Dv);
-        __syncthreads();
-        if (i > 0) {
-            kr.load(p.k, b, t0 - C, C, kh, p.Dk, p.wide_qk);
-            qr.load(p.q, b, t0 - C, C, kh, p.Dk, p.wide_qk);
-        }
-
-        // what reaches u: through the state behind the chunk, and through y (from the diagonal's block of 32 on)
-        f32x4 U[NC];
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) U[ct] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int f = 0; f < KF; ++f) {
-            bf16x8 ka[NK];
-            kt.rows(16 * wave, 32 * f, ka);
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                bf16x8 z[3];
-                zt.rows(16 * ct, 32 * f, z);
-                multiply<3>(U[ct], ka, z);
-            }
-        }
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) U[ct] *= out_k;
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            if (2 * f + 1 < wave) continue;
-            bf16x8 mix[NP];
-#pragma unroll
-            for (int k = 0; k < NP; ++k)
-                mix[k] = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(p.mix) + (chunk * NP + k) * C * C +
-                                                           (16 * wave + l16) * C + 32 * f + 8 * quad);
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                bf16x8 y[NK];
-                yt.rows(16 * ct, 32 * f, y);
-                multiply<3>(U[ct], mix, y);
-            }
-        }
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            const float e[4] = {U[ct][0], U[ct][1], U[ct][2], U[ct][3]};
-            ut.put4(16 * ct + l16, row4, e);
-        }
-        // Q^T (i dy): before `it` takes i dv
-        if (has_rows)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                bf16x8 qa[2][NK];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) qt.cols(32 * f, 16 * (wave + 4 * rt), qa[f]);
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct) {
-                    f32x4 s = Z[rt][ct] * whole;
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        bf16x8 o[3];
-                        it.rows(16 * ct, 32 * f, o);
-                        multiply<3>(s, qa[f], o);
-                    }
-                    Z[rt][ct] = s;
-                }
-            }
-        __syncthreads();
-
-        bf16x8 tri[2][3];
+        for (int f = 0; f < 2; ++f) operand<3>(w[2 * f], w[2 * f + 1], o[f]);
 #pragma unroll
         for (int f = 0; f < 2; ++f)
-            if (2 * f + 1 >= wave)
 #pragma unroll
-                for (int k = 0; k < 3; ++k)
-                    tri[f][k] = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(p.tri) + (chunk * 3 + k) * C * C +
-                                                                  (16 * wave + l16) * C + 32 * f + 8 * quad);
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            f32x4 X = {0, 0, 0, 0};
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                if (2 * f + 1 < wave) continue;
-                bf16x8 u[3];
-                ut.rows(16 * ct, 32 * f, u);
-                multiply<3>(X, tri[f], u);
+            for (int g = 0; g < DT / 2; ++g) {
+                bf16x8 a[2][NK];
+                f32x4 two[2] = {Z[2 * g], Z[2 * g + 1]};
+                t.cols(f, 2 * g, a[0]);
+                t.cols(f, 2 * g + 1, a[1]);
+                multiply_rows<3>(two, a, o[f]);
+                Z[2 * g] = two[0];
+                Z[2 * g + 1] = two[1];
             }
-            float e[4];
-            const int dv = c0 + 16 * ct + l16;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float dr = beta[r] * X[r];
-                e[r] = -in_k[r] * dr;
-                if (dv >= Dv) continue;
-                p.dx[(chunk * C + row4 + r) * Dv + dv] = X[r];
-                if (t0 + row4 + r < p.L)
-                    static_cast<T *>(p.dv.data)[b * p.dv.s0 + (t0 + row4 + r) * p.dv.s1 + h * Dv + dv] = (T)(row4 + r < m ? dr : 0.0f);
-            }
-            it.put4(16 * ct + l16, row4, e);
-        }
+    };
+
+    // Chunk i; `full`: whole, and so is chunk `then`, whose operands go out here
+    auto step = [&](int i, int then, auto full) __attribute__((always_inline)) {
+        const int64_t t0 = (int64_t)i * C, chunk = (b * p.n + i) * p.H + h;
+        const int m = min(C, len - i * C);
+        kr.store(kt);
+        qr.store(qt);
+        tr.store(tt);
+        mr.store(mt);
+        if (tid < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid] = sr;
         __syncthreads();
-        if (has_rows)
+        if constexpr (full.value) load(then, full);
+        if (busy) {
+            put_state<DT>(Z, p.ds + chunk * p.Dk * Dv + c, p.Dk, Dv, in);
+            // what reaches u: through the state behind the chunk, and through y
+            f32x4 U[RT], W[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) U[rt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int f = 0; f < KF; ++f) {
+                bf16x8 z[3], a[RT][NK];
+                operand<3>(Z[2 * f], Z[2 * f + 1], z);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) kt.rows(rt, f, a[rt]);
+                multiply_rows<3>(U, a, z);
+            }
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                bf16x8 ka[2][NK];
+                U[rt] *= scalar(OUT_K, rt);
 #pragma unroll
-                for (int f = 0; f < 2; ++f) kt.cols(32 * f, 16 * (wave + 4 * rt), ka[f]);
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        bf16x8 o[3];
-                        it.rows(16 * ct, 32 * f, o);
-                        multiply<3>(Z[rt][ct], ka[f], o);
-                    }
+                for (int r = 0; r < 4; ++r) W[rt][r] = (float)dy.v[rt][r];
             }
-        to_lds();
+            if constexpr (full.value) load_dy(then, full);
+            {
+                bf16x8 y[2][NK], a[RT][NP], au[2][NP];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) operand<NK>(W[2 * f], W[2 * f + 1], y[f]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) mt.rows(rt, 1, a[rt]);
+                multiply_rows<3>(U, a, y[1]);
+                f32x4 upper[2] = {U[0], U[1]};
+                mt.rows(0, 0, au[0]);
+                mt.rows(1, 0, au[1]);
+                multiply_rows<3>(upper, au, y[0]);
+                U[0] = upper[0];
+                U[1] = upper[1];
+            }
+            const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) Z[d] *= whole;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) W[rt] *= scalar(IN_Q, rt);
+            into_state(qt, W);
+
+            f32x4 X[RT];
+            {
+                bf16x8 u[2][3], a[RT][3], au[2][3];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) operand<3>(U[2 * f], U[2 * f + 1], u[f]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    X[rt] = f32x4{0, 0, 0, 0};
+                    tt.rows(rt, 1, a[rt]);
+                }
+                multiply_rows<3>(X, a, u[1]);
+                f32x4 upper[2] = {X[0], X[1]};
+                tt.rows(0, 0, au[0]);
+                tt.rows(1, 0, au[1]);
+                multiply_rows<3>(upper, au, u[0]);
+                X[0] = upper[0];
+                X[1] = upper[1];
+            }
+            put_state<RT>(X, p.dx + chunk * C * Dv + c, C, Dv, in);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                X[rt] *= scalar(BETA, rt);
+                W[rt] = -scalar(IN_K, rt) * X[rt];
+            }
+            put_column<full.value, T>(X, p.dv, b, t0, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
+            into_state(kt, W);
+        }
         __syncthreads();
+    };
+    const int whole_chunks = len / C;
+    if (whole_chunks < n) {
+        load(n - 1, std::false_type());
+        load_dy(n - 1, std::false_type());
+        step(n - 1, n - 1, std::false_type());
     }
-    if (p.dh0) to_memory(p.dh0 + head * p.Dk * Dv);
-    const int cols = min(NC * 16, (int)Dv - c0);
+    if (whole_chunks > 0) {
+        load(whole_chunks - 1, std::true_type());
+        load_dy(whole_chunks - 1, std::true_type());
+        for (int i = whole_chunks - 1; i >= 0; --i) step(i, max(i - 1, 0), std::true_type());     // (the first one's again: no branch)
+    }
+    if (p.dh0) put_state<DT>(Z, p.dh0 + head * p.Dk * Dv + c, p.Dk, Dv, in);
+    const int cols = min(64, (int)Dv - c0);
     for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += NT) {
         const int64_t t = (int64_t)n * C + u / cols;
         static_cast<T *>(p.dv.data)[b * p.dv.s0 + t * p.dv.s1 + h * Dv + c0 + u % cols] = (T)0.0f;
@@ -379,9 +340,11 @@ __global__ __launch_bounds__(NT) void merit_delta_grads(DeltaParams p)
     __syncthreads();            // (the first part's LDS is free)
     {
         ChunkRows<T, KF> e;
-        e.load(p.k, b, t0, m, kh, p.Dk, p.wide_qk);
+        if (p.wide_qk) e.template load<false, true>(p.k, b, t0, m, kh, p.Dk);
+        else e.template load<false, false>(p.k, b, t0, m, kh, p.Dk);
         e.store(kt);
-        e.load(p.q, b, t0, m, kh, p.Dk, p.wide_qk);
+        if (p.wide_qk) e.template load<false, true>(p.q, b, t0, m, kh, p.Dk);
+        else e.template load<false, false>(p.q, b, t0, m, kh, p.Dk);
         e.store(qt);
     }
 #pragma unroll
@@ -523,14 +486,14 @@ template <typename T> __global__ __launch_bounds__(NT) void merit_delta_sum_head
     static_cast<T *>(p.dk.data)[b * p.dk.s0 + t * p.dk.s1 + (int64_t)kh * p.Dk + c] = (T)k;
 }
 
-template <typename T, int KF, int NC> hipError_t backward_chunks(DeltaParams p, hipStream_t s)
+template <typename T, int KF> hipError_t backward_chunks(DeltaParams p, hipStream_t s)
 {
-    constexpr int NK = Terms<T>::n;
-    constexpr int lds = 2 * Tile<NK, C, KF * 32>::bytes + Tile<3, NC * 16, KF * 32>::bytes + 2 * Tile<3, NC * 16, C>::bytes +
-                        Tile<NK, NC * 16, C>::bytes;
+    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + Mixed<3, C>::bytes + Mixed<mix_terms<T>(true), C>::bytes + SCALAR_FLOATS * 4;
     static_assert(lds <= 160 * 1024, "");
-    p.slices = (int)((p.Dv + 16 * NC - 1) / (16 * NC));
-    merit_delta_back_chunks<T, KF, NC><<<(unsigned)(p.B * p.H * p.slices), NT, lds, s>>>(p);
+    p.slices = (p.Dv + 63) / 64;
+    const unsigned grid = (unsigned)(p.B * p.H * p.slices);
+    if (p.wide_qk) merit_delta_back_chunks<T, KF, true><<<grid, NT, lds, s>>>(p);
+    else merit_delta_back_chunks<T, KF, false><<<grid, NT, lds, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int KF> hipError_t grads_of(const DeltaParams &p, hipStream_t s)
@@ -545,8 +508,8 @@ template <typename T, int KF> hipError_t grads_of(const DeltaParams &p, hipStrea
 }
 template <typename T, int KF> hipError_t backward_of(const DeltaParams &p, hipStream_t s)
 {
-    constexpr int NC = KF == 4 && Terms<T>::n == 3 ? 1 : 2;     // (what LDS holds)
-    if (hipError_t e = p.Dv <= 16 ? backward_chunks<T, KF, 1>(p, s) : backward_chunks<T, KF, NC>(p, s)) return e;
+    if (hipError_t e = prepare_of<T, KF, true>(p, s)) return e;
+    if (hipError_t e = backward_chunks<T, KF>(p, s)) return e;
     if (p.n == 0) return hipSuccess;
     if (hipError_t e = grads_of<T, KF>(p, s)) return e;
     if (!p.part) return hipSuccess;
@@ -564,10 +527,7 @@ enum { FORWARD, BACKWARD, STEP };
 template <typename T> hipError_t passes(const DeltaParams &p, int pass, hipStream_t s)
 {
     if (pass == FORWARD) return forward_typed<T>(p, s);
-    if (pass == STEP) return token_typed<T>(p, s);
-    if (p.n > 0)
-        if (hipError_t e = prepare_back_typed<T>(p, s)) return e;
-    return backward_typed<T>(p, s);
+    return pass == STEP ? token_typed<T>(p, s) : backward_typed<T>(p, s);
 }
 hipError_t passes_f32(const DeltaParams &p, int pass, hipStream_t s);
 hipError_t passes_f16(const DeltaParams &p, int pass, hipStream_t s);

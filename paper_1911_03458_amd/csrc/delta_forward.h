@@ -10,14 +10,14 @@ namespace delta {
 // ---------------------------------------------------------------------------
 // chunks side by side: a workgroup a chunk of a head
 // ---------------------------------------------------------------------------
-// Forward it leaves X = (1 + N diag(b))^-1 and P = scale f o Q K^T, rows side by side; backward the transposes of
-// (1 + diag(b) N)^-1 and P.  Blocks of 16 x 16 above the diagonal are not written but where a product of 32 reads them.
-template <typename T, int KF, bool BACK>
+// Forward it leaves X = (1 + N diag(b))^-1 and P = scale f o Q K^T, their columns interleaved (delta.h); backward the transposes of
+// (1 + diag(b) N)^-1 and P.  Blocks of 16 x 16 of P beyond the diagonal are not written but where a product of 32 reads them.
+template <typename T, int KF, bool BACK, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 {
     constexpr int NK = Terms<T>::n, NP = mix_terms<T>(BACK);
     __shared__ __attribute__((aligned(16))) __bf16 kmem[Tile<NK, C, KF * 32>::bytes / 2];
-    __shared__ __attribute__((aligned(16))) float a[C][C + 4];
+    __shared__ __attribute__((aligned(16))) float a[C][C + 4], x[C][C + 4];
     __shared__ double G[C];
     __shared__ float beta[C], invk[C], invq[C];
     __shared__ int bad;             // the first token whose row of the triangular matrix is not finite
@@ -33,14 +33,12 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 
     // Two rows' loads in a wavefront: keys to LDS, their squares' sums over the lanes of a row
     ChunkRows<T, KF> kr;
-    kr.load(p.k, b, t0, m, kh, p.Dk, p.wide_qk);
-    const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + 16 * wave + l16) * p.q.s1 + (int64_t)kh * p.Dk;
+    kr.template load<false, WIDE>(p.k, b, t0, m, kh, p.Dk);
+    const int own = 16 * wave + l16;
+    const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + min(own, m - 1)) * p.q.s1 + (int64_t)kh * p.Dk;
     Eight<T> qe[KF];
 #pragma unroll
-    for (int f = 0; f < KF; ++f) {
-        qe[f] = zero8<T>();
-        if (16 * wave + l16 < m) qe[f] = load8<T>(qrow, 32 * f + 8 * quad, p.Dk, p.wide_qk);
-    }
+    for (int f = 0; f < KF; ++f) qe[f] = take8<WIDE, T>(qrow, 32 * f + 8 * quad, own < m ? p.Dk : 0);
     if (wave == 0) {
         double g = 0.0;
         float bt = 0.0f;
@@ -129,9 +127,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
                 atomicMin(&bad, t);
                 w = 0.0f;
             }
-            // (backward the columns of the inverse are wanted side by side, forward its rows)
-            if constexpr (BACK) a[t][j] = w;
-            else a[j][t] = w;
+            a[t][j] = w;
             __bf16 s[NP];
             split<NP>(j <= t ? f * p.scale * invq[t] * invk[j] * qk[r] : 0.0f, s);
 #pragma unroll
@@ -141,281 +137,297 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 #pragma unroll
             for (int n = 0; n < NP; ++n) {
                 __bf16 *to = mix + n * C * C +
-                             (BACK ? (16 * jb + l16) * C + 16 * wave + 4 * quad : (16 * wave + l16) * C + 16 * jb + 4 * quad);
+                             (BACK ? (16 * jb + l16) * C + interleaved(16 * wave + 4 * quad) : (16 * wave + l16) * C + interleaved(16 * jb + 4 * quad));
                 *reinterpret_cast<bf16x4 *>(to) = out[n];
             }
     }
     __syncthreads();
 
-    // The inverse: lane c has column c (backward), or row c (forward), and takes one value after the other
-    if (wave == 0) {
-        float x[C];
+    // The inverse x of 1 + a, in blocks of 16 x 16.  On the diagonal: lane c of wavefront w has column c of block w and takes one
+    // row after the other (powers of a block, which would do it with products, cancel where keys are alike).
+    {
+        float d[16];
 #pragma unroll
-        for (int s = 0; s < C; ++s) {
-            const int r = BACK ? s : C - 1 - s;
-            float v0 = r == lane ? 1.0f : 0.0f, v1 = 0.0f, v2 = 0.0f, v3 = 0.0f;
-            if constexpr (BACK) {
+        for (int r = 0; r < 16; ++r) {
+            float v0 = r == l16 ? 1.0f : 0.0f, v1 = 0.0f;
 #pragma unroll
-                for (int j = 0; j < r; j += 4) {
-                    const f32x4 w = *reinterpret_cast<const f32x4 *>(&a[r][j]);
-                    v0 = fmaf(-w[0], x[j], v0);
-                    if (j + 1 < r) v1 = fmaf(-w[1], x[j + 1], v1);
-                    if (j + 2 < r) v2 = fmaf(-w[2], x[j + 2], v2);
-                    if (j + 3 < r) v3 = fmaf(-w[3], x[j + 3], v3);
-                }
-            } else {
-#pragma unroll
-                for (int j = r / 4 * 4; j < C; j += 4) {
-                    const f32x4 w = *reinterpret_cast<const f32x4 *>(&a[r][j]);
-                    if (j > r) v0 = fmaf(-w[0], x[j], v0);
-                    if (j + 1 > r) v1 = fmaf(-w[1], x[j + 1], v1);
-                    if (j + 2 > r) v2 = fmaf(-w[2], x[j + 2], v2);
-                    if (j + 3 > r) v3 = fmaf(-w[3], x[j + 3], v3);
-                }
+            for (int j = 0; j < r; j += 4) {
+                const f32x4 w = *reinterpret_cast<const f32x4 *>(&a[16 * wave + r][16 * wave + j]);
+                v0 = fmaf(-w[0], d[j], v0);
+                if (j + 1 < r) v1 = fmaf(-w[1], d[j + 1], v1);
+                if (j + 2 < r) v0 = fmaf(-w[2], d[j + 2], v0);
+                if (j + 3 < r) v1 = fmaf(-w[3], d[j + 3], v1);
             }
-            x[r] = (v0 + v1) + (v2 + v3);
+            d[r] = v0 + v1;
         }
-        __bf16 *to = static_cast<__bf16 *>(p.tri) + (int64_t)id * 3 * C * C + lane * C;
-        const bool lost = !BACK && lane >= bad;
+        if (quad == 0)
 #pragma unroll
-        for (int c = 0; c < C; c += 8) {
-            float e[8];
+            for (int r = 0; r < 16; ++r) x[16 * wave + r][16 * wave + l16] = d[r];
+    }
+    __syncthreads();
+    // Below it, a diagonal of blocks at a time: x_ij = -x_ii (a_ij x_jj + .. + a_i,i-1 x_i-1,j), fp32 products.  Step s of a product
+    // sums over the numbers 4 q + s of quad q's lanes, which is how a result lies in them: it goes on without a move.
 #pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = lost ? __builtin_nanf("") : x[c + k];
+    for (int dist = 1; dist < 4; ++dist) {
+        const int bi_ = wave + dist, bj = wave;
+        if (bi_ < 4) {
+            f32x4 sum = {0, 0, 0, 0}, out = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < dist; ++k)
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(a[16 * bi_ + l16][16 * (bj + k) + 4 * quad + s],
+                                                               x[16 * (bj + k) + 4 * quad + s][16 * bj + l16], sum, 0, 0, 0);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                out = __builtin_amdgcn_mfma_f32_16x16x4f32(-x[16 * bi_ + l16][16 * bi_ + 4 * quad + s], sum[s], out, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[16 * bi_ + 4 * quad + r][16 * bj + l16] = out[r];
+        }
+        __syncthreads();
+    }
+    // Its rows in three terms (backward: its columns), zeros above the diagonal's blocks
+    {
+        const int row = BACK ? tid & 63 : tid >> 2, c0 = 16 * (BACK ? tid >> 6 : tid & 3);
+        float e[2][8];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int t = BACK ? c0 + k : row, j = BACK ? row : c0 + k;
+            float v = t >> 4 >= j >> 4 ? x[t][j] : 0.0f;
+            if (!BACK && t >= bad) v = __builtin_nanf("");
+            e[k / 8][k % 8] = v;
+        }
+        __bf16 *to = static_cast<__bf16 *>(p.tri) + (int64_t)id * 3 * C * C + row * C;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
             bf16x8 o[3];
-            split8<3>(e, o);
+            split8<3>(e[k], o);
 #pragma unroll
-            for (int n = 0; n < 3; ++n) *reinterpret_cast<bf16x8 *>(to + n * C * C + c) = o[n];
+            for (int n = 0; n < 3; ++n) {
+                *reinterpret_cast<bf16x4 *>(to + n * C * C + interleaved(c0 + 8 * k)) = __builtin_shufflevector(o[n], o[n], 0, 1, 2, 3);
+                *reinterpret_cast<bf16x4 *>(to + n * C * C + interleaved(c0 + 8 * k + 4)) = __builtin_shufflevector(o[n], o[n], 4, 5, 6, 7);
+            }
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// one chunk after the other: a workgroup 16 NC columns of a head's state
+// one chunk after the other: a wavefront 16 columns of a head's state
 // ---------------------------------------------------------------------------
-// The columns of a state do not depend on each other.  A wavefront has 16 of the chunk's tokens, and 16 or 32 rows of the state
-// in registers, from which it goes to LDS in three terms for the next chunk's products.
-template <typename T, int KF, int NC>
+// The columns of a state do not depend on each other.  A wavefront has 16 of them, all of a chunk's tokens and all rows of the state,
+// in registers: results go from product to product as they lie (delta.h: Mixed).  LDS holds the other operands, K, Q and the two
+// triangular matrices, for the four wavefronts of a workgroup; the next chunk's are on their way in registers meanwhile.
+template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(false), RT = KF < 2 ? 1 : KF / 2, ORD = NP;
+    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(false), ORD = NP, RT = C / 16, DT = 2 * KF;
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
-    typedef Tile<NK, C, KF * 32> TK;
-    typedef Tile<3, NC * 16, KF * 32> TS;
-    typedef Tile<3, NC * 16, C> TX;
-    typedef Tile<NP, NC * 16, C> TU;
-    const TK kt{smem};
-    const TS st{kt.at + TK::bytes / 2};
-    const TX xt{st.at + TS::bytes / 2}, ot{xt.at + TX::bytes / 2};
-    const TU ut{ot.at + TX::bytes / 2};
-    // The first token of a chunk from which a column is not finite: such values go into products as zeros, because those of
-    // earlier tokens have them too, times 0.  (Set once: the chunks behind it start from a state that is not finite.)
-    __shared__ int bad[NC * 16];
+    typedef Mixed<NK, KF * 32> TK;
+    const TK kt{smem}, qt{kt.at + TK::bytes / 2};
+    const Mixed<3, C> tt{qt.at + TK::bytes / 2};
+    const Mixed<NP, C> mt{tt.at + Mixed<3, C>::bytes / 2};
+    float *const sc = reinterpret_cast<float *>(mt.at + Mixed<NP, C>::bytes / 2);
 
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
-    const int c0 = (int)(id % (uint32_t)p.slices) * NC * 16, kh = (int)h / p.each;
-    const int len = tokens_of(p, b), n = (len + C - 1) / C;
+    const int kh = (int)h / p.each, len = tokens_of(p, b), n = (len + C - 1) / C;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
-    const int row4 = 16 * wave + 4 * quad;                     // the first of a lane's four tokens in a result of 16 x 16
     const int64_t head = b * p.H + h, Dv = p.Dv;
-    const bool has_rows = wave < 2 * KF;
+    const int c0 = (int)(id % (uint32_t)p.slices) * 64, c = c0 + 16 * wave + l16;
+    const bool busy = c0 + 16 * wave < Dv, in = c < Dv;            // (the wavefront, the lane has columns)
 
-    f32x4 S[RT][NC];
+    f32x4 S[DT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int ct = 0; ct < NC; ++ct)
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 16 * d + 4 * quad + r;
+            S[d][r] = p.h0 && dk < p.Dk && in ? p.h0[(head * p.Dk + dk) * Dv + c] : 0.0f;
+        }
+    const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);         // (a lane without a column: any that is there)
+    ChunkRows<T, KF> kr, qr;
+    Square<3> tr;
+    Square<NP> mr;
+    f32x4 sr;
+    ChunkColumn<T> v;
+    auto load = [&](int i, auto full) __attribute__((always_inline)) {
+        const int64_t chunk = (b * p.n + i) * p.H + h;
+        const int m = min(C, len - i * C);
+        kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
+        qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
+        tr.load(p.tri, chunk);
+        mr.load(p.mix, chunk);
+        sr = reinterpret_cast<const f32x4 *>(p.scal + chunk * SCALAR_FLOATS)[tid % (SCALAR_FLOATS / 4)];
+    };
+    auto load_v = [&](int i, auto full) __attribute__((always_inline)) {
+        v.template load<full.value>(p.v, b, (int64_t)i * C, min(C, len - i * C), mine);
+    };
+    auto scalar = [&](int which, int rt) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4 *>(sc + which * C + 16 * rt + 4 * quad);
+    };
+    // Values that are not finite go into products as zeros, because those of earlier tokens have them too, times 0; `bad` is the
+    // first token of the chunk from which the lane's column has some, and everything from there on becomes a NaN.
+    int bad = C;
+    auto finite = [&](f32x4 (&x)[RT]) __attribute__((always_inline)) {
+        bool all = true;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 16 * (wave + 4 * rt) + 4 * quad + r, dv = c0 + 16 * ct + l16;
-                S[rt][ct][r] = p.h0 && dk < p.Dk && dv < Dv ? p.h0[(head * p.Dk + dk) * Dv + dv] : 0.0f;
-            }
-    auto state_to_lds = [&]() __attribute__((always_inline)) {
-        if (has_rows)
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int r = 0; r < 4; ++r) all = all && isfinite(x[rt][r]);
+        if (__ballot(!all) == 0) return;
 #pragma unroll
-                for (int ct = 0; ct < NC; ++ct) {
-                    const float e[4] = {S[rt][ct][0], S[rt][ct][1], S[rt][ct][2], S[rt][ct][3]};
-                    st.put4(16 * ct + l16, 16 * (wave + 4 * rt) + 4 * quad, e);
+        for (int rt = RT - 1; rt >= 0; --rt)
+#pragma unroll
+            for (int r = 3; r >= 0; --r)
+                if (!isfinite(x[rt][r])) {
+                    bad = min(bad, 16 * rt + 4 * quad + r);
+                    x[rt][r] = 0.0f;
                 }
-    };
-    auto state_to = [&](float *out) __attribute__((always_inline)) {
-        if (has_rows)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int dk = 16 * (wave + 4 * rt) + 4 * quad + r, dv = c0 + 16 * ct + l16;
-                        if (dk < p.Dk && dv < Dv) out[dk * Dv + dv] = S[rt][ct][r];
-                    }
+        bad = min(bad, __shfl_xor(bad, 16));
+        bad = min(bad, __shfl_xor(bad, 32));
     };
 
-    ChunkRows<T, KF> kr;
-    if (n > 0) kr.load(p.k, b, 0, min(C, len), kh, p.Dk, p.wide_qk);
-    if (tid < NC * 16) bad[tid] = C;
-    state_to_lds();
-    for (int i = 0; i < n; ++i) {
+    // Chunk i; `full`: whole, and so is chunk `then`, whose operands go out here
+    auto step = [&](int i, int then, auto full) __attribute__((always_inline)) {
         const int64_t t0 = (int64_t)i * C, chunk = (b * p.n + i) * p.H + h;
-        const int m = min(C, len - (int)t0);
-        const float *scal = p.scal + chunk * SCALAR_FLOATS;
+        const int m = min(C, len - i * C);
         kr.store(kt);
+        qr.store(qt);
+        tr.store(tt);
+        mr.store(mt);
+        if (tid < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid] = sr;
         __syncthreads();
-        if (i + 1 < n) kr.load(p.k, b, t0 + C, min(C, len - (int)t0 - C), kh, p.Dk, p.wide_qk);
-
-        // K S and Q S
-        const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + 16 * wave + l16) * p.q.s1 + (int64_t)kh * p.Dk;
-        Eight<T> qe[KF];
+        if constexpr (full.value) load(then, full);
+        if (busy) {
+            // K S and Q S
+            f32x4 X[RT], Y[RT];
 #pragma unroll
-        for (int f = 0; f < KF; ++f) {
-            qe[f] = zero8<T>();
-            if (16 * wave + l16 < m) qe[f] = load8<T>(qrow, 32 * f + 8 * quad, p.Dk, p.wide_qk);
-        }
-        float v[NC][4];
+            for (int rt = 0; rt < RT; ++rt) X[rt] = Y[rt] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int ct = 0; ct < NC; ++ct)
+            for (int f = 0; f < KF; ++f) {
+                bf16x8 s[3], a[RT][NK];
+                operand<3>(S[2 * f], S[2 * f + 1], s);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dv = c0 + 16 * ct + l16;
-                v[ct][r] = row4 + r < m && dv < Dv
-                               ? (float)static_cast<const T *>(p.v.data)[b * p.v.s0 + (t0 + row4 + r) * p.v.s1 + h * Dv + dv] : 0.0f;
+                for (int rt = 0; rt < RT; ++rt) kt.rows(rt, f, a[rt]);
+                multiply_rows<3>(X, a, s);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) qt.rows(rt, f, a[rt]);
+                multiply_rows<ORD>(Y, a, s);
             }
-        const f32x4 in_k = *reinterpret_cast<const f32x4 *>(scal + IN_K * C + row4);
-        const f32x4 in_q = *reinterpret_cast<const f32x4 *>(scal + IN_Q * C + row4);
-        const f32x4 out_k = *reinterpret_cast<const f32x4 *>(scal + OUT_K * C + row4);
-        const f32x4 beta = *reinterpret_cast<const f32x4 *>(scal + BETA * C + row4);
-        const float whole = exp_of(reinterpret_cast<const double *>(scal + SCALARS * C)[C - 1]);
-        bf16x8 tri[2][3], mix[2][NP];
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            const int64_t at = (16 * wave + l16) * C + 32 * f + 8 * quad;
-            if (2 * f > wave) continue;
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-                tri[f][k] = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(p.tri) + (chunk * 3 + k) * C * C + at);
-#pragma unroll
-            for (int k = 0; k < NP; ++k)
-                mix[f][k] = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(p.mix) + (chunk * NP + k) * C * C + at);
-        }
-
-        f32x4 R[NC], Y[NC];
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) R[ct] = Y[ct] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int f = 0; f < KF; ++f) {
-            bf16x8 ka[NK], qa[NK];
-            kt.rows(16 * wave, 32 * f, ka);
-            terms8<T>(qe[f], qa);
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                bf16x8 s[3];
-                st.rows(16 * ct, 32 * f, s);
-                multiply<3>(R[ct], ka, s);
-                multiply<ORD>(Y[ct], qa, s);
-            }
-        }
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            float e[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                e[r] = fmaf(-in_k[r], R[ct][r], v[ct][r]);
-                if (!isfinite(e[r])) {
-                    atomicMin(&bad[16 * ct + l16], row4 + r);
-                    e[r] = 0.0f;
-                }
-            }
-            xt.put4(16 * ct + l16, row4, e);
-        }
-        __syncthreads();
-
-        // d, u
-        f32x4 D[NC];
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            D[ct] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                if (2 * f > wave) continue;
-                bf16x8 x[3];
-                xt.rows(16 * ct, 32 * f, x);
-                multiply<3>(D[ct], tri[f], x);
-            }
-            float u[4], o[4];
-            const int from = bad[16 * ct + l16];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (row4 + r >= from) D[ct][r] = __builtin_nanf("");
-                u[r] = beta[r] * D[ct][r];
-                if (!isfinite(u[r])) {
-                    atomicMin(&bad[16 * ct + l16], row4 + r);
-                    u[r] = 0.0f;
-                }
-                o[r] = out_k[r] * u[r];
-            }
-            ut.put4(16 * ct + l16, row4, u);
-            ot.put4(16 * ct + l16, row4, o);
-        }
-        if (p.states) {
-            float *out = p.states + chunk * (p.Dk + C) * Dv;
-            state_to(out);
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int dv = c0 + 16 * ct + l16;
-                    if (dv < Dv) out[(p.Dk + row4 + r) * Dv + dv] = D[ct][r];
-                }
-        }
-        __syncthreads();
-
-        // y, and the state behind the chunk
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct) {
-            f32x4 y = {0, 0, 0, 0};
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                if (2 * f > wave) continue;
-                bf16x8 u[NP];
-                ut.rows(16 * ct, 32 * f, u);
-                multiply<ORD>(y, mix[f], u);
-            }
-            const int dv = c0 + 16 * ct + l16, from = bad[16 * ct + l16];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float f = row4 + r >= from ? __builtin_nanf("") : fmaf(in_q[r], Y[ct][r], y[r]);
-                if (dv < Dv && t0 + row4 + r < p.L)
-                    static_cast<T *>(p.y.data)[b * p.y.s0 + (t0 + row4 + r) * p.y.s1 + h * Dv + dv] = (T)(row4 + r < m ? f : 0.0f);
-            }
-        }
-        if (has_rows)
+            if (p.states) put_state<DT>(S, p.states + chunk * (p.Dk + C) * Dv + c, p.Dk, Dv, in);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                bf16x8 ka[2][NK];
+                const f32x4 in_k = scalar(IN_K, rt);
 #pragma unroll
-                for (int f = 0; f < 2; ++f) kt.cols(32 * f, 16 * (wave + 4 * rt), ka[f]);
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct) {
-                    f32x4 s = S[rt][ct] * whole;
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        bf16x8 o[3];
-                        ot.rows(16 * ct, 32 * f, o);
-                        multiply<3>(s, ka[f], o);
-                    }
-                    if (bad[16 * ct + l16] < C) s = f32x4{1, 1, 1, 1} * __builtin_nanf("");
-                    S[rt][ct] = s;
-                }
+                for (int r = 0; r < 4; ++r) X[rt][r] = fmaf(-in_k[r], X[rt][r], (float)v.v[rt][r]);
             }
-        state_to_lds();
+            if constexpr (full.value) load_v(then, full);
+            finite(X);
+
+            // d, u
+            f32x4 D[RT], U[RT];
+            bf16x8 x[2][3];
+#pragma unroll
+            for (int f = 0; f < 2; ++f) operand<3>(X[2 * f], X[2 * f + 1], x[f]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) D[rt] = f32x4{0, 0, 0, 0};
+            {
+                bf16x8 a[RT][3];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) tt.rows(rt, 0, a[rt]);
+                multiply_rows<3>(D, a, x[0]);
+                f32x4 lower[2] = {D[2], D[3]};
+                bf16x8 al[2][3];
+                tt.rows(2, 1, al[0]);
+                tt.rows(3, 1, al[1]);
+                multiply_rows<3>(lower, al, x[1]);
+                D[2] = lower[0];
+                D[3] = lower[1];
+            }
+            if (__ballot(bad < C) != 0)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * rt + 4 * quad + r >= bad) D[rt][r] = __builtin_nanf("");
+            if (p.states) {
+                put_state<RT>(D, p.states + (chunk * (p.Dk + C) + p.Dk) * Dv + c, C, Dv, in);
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) U[rt] = D[rt] * scalar(BETA, rt);
+            finite(U);
+
+            // the state behind the chunk
+            const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
+            {
+                bf16x8 o[2][3];
+                f32x4 w[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) w[rt] = U[rt] * scalar(OUT_K, rt);
+#pragma unroll
+                for (int f = 0; f < 2; ++f) operand<3>(w[2 * f], w[2 * f + 1], o[f]);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) S[d] *= whole;
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int g = 0; g < DT / 2; ++g) {
+                        bf16x8 a[2][NK];
+                        f32x4 two[2] = {S[2 * g], S[2 * g + 1]};
+                        kt.cols(f, 2 * g, a[0]);
+                        kt.cols(f, 2 * g + 1, a[1]);
+                        multiply_rows<3>(two, a, o[f]);
+                        S[2 * g] = two[0];
+                        S[2 * g + 1] = two[1];
+                    }
+            }
+            // y
+            {
+                bf16x8 u[2][NP], a[RT][NP], al[2][NP];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) operand<NP>(U[2 * f], U[2 * f + 1], u[f]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    Y[rt] *= scalar(IN_Q, rt);
+                    mt.rows(rt, 0, a[rt]);
+                }
+                multiply_rows<ORD>(Y, a, u[0]);
+                f32x4 lower[2] = {Y[2], Y[3]};
+                mt.rows(2, 1, al[0]);
+                mt.rows(3, 1, al[1]);
+                multiply_rows<ORD>(lower, al, u[1]);
+                Y[2] = lower[0];
+                Y[3] = lower[1];
+            }
+            if (__ballot(bad < C) != 0 && bad < C) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * rt + 4 * quad + r >= bad) Y[rt][r] = __builtin_nanf("");
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[d][r] = __builtin_nanf("");
+            }
+            put_column<full.value, T>(Y, p.y, b, t0, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
+        }
         __syncthreads();
+    };
+    const int whole_chunks = len / C;
+    if (whole_chunks > 0) {
+        load(0, std::true_type());
+        load_v(0, std::true_type());
+        for (int i = 0; i < whole_chunks; ++i) step(i, min(i + 1, whole_chunks - 1), std::true_type());    // (the last one's again: no branch)
     }
-    if (p.h_last) state_to(p.h_last + head * p.Dk * Dv);
+    if (whole_chunks < n) {
+        load(n - 1, std::false_type());
+        load_v(n - 1, std::false_type());
+        step(n - 1, n - 1, std::false_type());
+    }
+    if (p.h_last) put_state<DT>(S, p.h_last + head * p.Dk * Dv + c, p.Dk, Dv, in);
     // zeros behind the sequence's last chunk
-    const int cols = min(NC * 16, (int)Dv - c0);
+    const int cols = min(64, (int)Dv - c0);
     for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += NT) {
         const int64_t t = (int64_t)n * C + u / cols;
         static_cast<T *>(p.y.data)[b * p.y.s0 + t * p.y.s1 + h * Dv + c0 + u % cols] = (T)0.0f;
@@ -514,36 +526,28 @@ __global__ __launch_bounds__(NT) void merit_delta_token(DeltaParams p, int lanes
     }
 }
 
-template <typename T, int KF, int NC> hipError_t forward_chunks(DeltaParams p, hipStream_t s)
+template <typename T, int KF, bool BACK> hipError_t prepare_of(const DeltaParams &p, hipStream_t s)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(false);
-    constexpr int lds = Tile<NK, C, KF * 32>::bytes + Tile<3, NC * 16, KF * 32>::bytes + 2 * Tile<3, NC * 16, C>::bytes +
-                        Tile<NP, NC * 16, C>::bytes;
-    static_assert(lds <= 160 * 1024, "");
-    p.slices = (int)((p.Dv + 16 * NC - 1) / (16 * NC));
-    merit_delta_chunks<T, KF, NC><<<(unsigned)(p.B * p.H * p.slices), NT, lds, s>>>(p);
+    const unsigned grid = (unsigned)(p.B * p.n * p.H);
+    if (grid == 0) return hipSuccess;
+    if (p.wide_qk) merit_delta_prepare<T, KF, BACK, true><<<grid, NT, 0, s>>>(p);
+    else merit_delta_prepare<T, KF, BACK, false><<<grid, NT, 0, s>>>(p);
     return hipGetLastError();
 }
-template <typename T, int KF> hipError_t forward_of(const DeltaParams &p, hipStream_t s)
+template <typename T, int KF> hipError_t forward_of(DeltaParams p, hipStream_t s)
 {
-    if (p.n > 0) {
-        merit_delta_prepare<T, KF, false><<<(unsigned)(p.B * p.n * p.H), NT, 0, s>>>(p);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
-    return p.Dv <= 16 ? forward_chunks<T, KF, 1>(p, s) : forward_chunks<T, KF, 2>(p, s);
+    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + Mixed<3, C>::bytes + Mixed<mix_terms<T>(false), C>::bytes + SCALAR_FLOATS * 4;
+    static_assert(lds <= 160 * 1024, "");
+    if (hipError_t e = prepare_of<T, KF, false>(p, s)) return e;
+    p.slices = (p.Dv + 63) / 64;
+    const unsigned grid = (unsigned)(p.B * p.H * p.slices);
+    if (p.wide_qk) merit_delta_chunks<T, KF, true><<<grid, NT, lds, s>>>(p);
+    else merit_delta_chunks<T, KF, false><<<grid, NT, lds, s>>>(p);
+    return hipGetLastError();
 }
 template <typename T> hipError_t forward_typed(const DeltaParams &p, hipStream_t s)
 {
     return p.Dk <= 32 ? forward_of<T, 1>(p, s) : p.Dk <= 64 ? forward_of<T, 2>(p, s) : forward_of<T, 4>(p, s);
-}
-
-template <typename T> hipError_t prepare_back_typed(const DeltaParams &p, hipStream_t s)
-{
-    const unsigned grid = (unsigned)(p.B * p.n * p.H);
-    if (p.Dk <= 32) merit_delta_prepare<T, 1, true><<<grid, NT, 0, s>>>(p);
-    else if (p.Dk <= 64) merit_delta_prepare<T, 2, true><<<grid, NT, 0, s>>>(p);
-    else merit_delta_prepare<T, 4, true><<<grid, NT, 0, s>>>(p);
-    return hipGetLastError();
 }
 
 template <typename T> hipError_t token_typed(const DeltaParams &p, hipStream_t s)
