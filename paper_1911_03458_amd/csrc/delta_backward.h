@@ -188,47 +188,69 @@ __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
 // ---------------------------------------------------------------------------
 // chunks side by side: the gradients of q, k, g and beta; a workgroup a chunk of a head
 // ---------------------------------------------------------------------------
-// First the products along v's columns, 32 of them at a time (states, u and x come through LDS in terms); then those along the
-// chunk's tokens, for which LDS holds q, k and the matrices of 64 x 64.  A wavefront has 16 tokens' rows of all results.
-template <typename T, int KF>
-__global__ __launch_bounds__(NT) void merit_delta_grads(DeltaParams p)
+// First the products along v's columns, 32 of them at a time: a wavefront takes 16 of the keys' columns of S_0 and Z straight from
+// memory, LDS holds dy, x and u in terms.  Then those along the chunk's tokens, for which it holds K, Q and one matrix of 64 x 64
+// after the other.  Results are kept times what a row goes through at the end: dQ scale / |q|, rows / |k|, cols / |k|, for which the
+// matrices have the lengths of both of their tokens, and serve both ways round.  Through LDS they come into rows of eight values a
+// thread, for the sums along the keys and the stores.
+template <int KF> constexpr int grad_waves() { return KF < 4 ? 4 : 8; }
+template <typename T, int KF, bool WIDE>
+__global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(DeltaParams p)
 {
-    constexpr int NK = Terms<T>::n, DT = 2 * KF;
+    constexpr int NK = Terms<T>::n, RT = C / 16, WAVES = grad_waves<KF>(), THREADS = 64 * WAVES, OP = KF * 32 + 4;
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
-    __shared__ double G[C], suffix[C], dots[4];
+    __shared__ double G[C], sums[2][WAVES], suffix[C];
     __shared__ float invk[C], invq[C], beta[C];
-    typedef Tile<3, KF * 32, 32> TS;
     typedef Tile<3, C, 32> TU;
     typedef Tile<NK, C, KF * 32> TK;
-    typedef Tile<3, C, C> TM;
-    const TS st{smem}, zt{st.at + TS::bytes / 2};
-    const TU ut{zt.at + TS::bytes / 2};
+    const Tile<NK, C, 32> yt{smem};
+    const TU xt{yt.at + Tile<NK, C, 32>::bytes / 2}, ut{xt.at + TU::bytes / 2};
     const TK kt{smem}, qt{kt.at + TK::bytes / 2};
-    const TM pt{qt.at + TK::bytes / 2}, mt{pt.at + TM::bytes / 2};
+    const Tile<3, C, C> wt{qt.at + TK::bytes / 2};
+    float *const ot = reinterpret_cast<float *>(wt.at);        // [C][OP], in the place of the matrices
 
     const uint32_t id = blockIdx.x, h = id % (uint32_t)p.H, bi = id / (uint32_t)p.H;
     const uint32_t i = bi % (uint32_t)p.n;
     const int64_t b = bi / (uint32_t)p.n, t0 = (int64_t)i * C, Dv = p.Dv;
-    const int kh = (int)h / p.each, m = min(C, tokens_of(p, b) - (int)t0), here = min(C, (int)(p.L - t0));
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4, row4 = 16 * wave + 4 * quad;
-    float *part_q = p.part ? p.part + ((b * p.L + t0) * p.H + h) * p.Dk : nullptr;
-    float *part_k = p.part ? part_q + p.B * p.L * p.H * p.Dk : nullptr;
-    auto put = [&](int r, int c, float q, float k) __attribute__((always_inline)) {
+    const int kh = (int)h / p.each, m = min(C, tokens_of(p, b) - (int)t0), here = (int)min((int64_t)C, p.L - t0);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
+    // rows t of dq or dk, as they lie: the tensor's, or the value head's part in fp32
+    auto put8 = [&](const Rows &out, int64_t which, int t, int c, const float (&v)[8]) __attribute__((always_inline)) {
         if (p.part) {
-            part_q[(int64_t)r * p.H * p.Dk + c] = q;
-            part_k[(int64_t)r * p.H * p.Dk + c] = k;
+            float *to = p.part + ((which * p.B * p.L + b * p.L + t0 + t) * p.H + h) * p.Dk + c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < p.Dk) to[e] = v[e];
+            return;
+        }
+        T *to = static_cast<T *>(out.data) + b * out.s0 + (t0 + t) * out.s1 + (int64_t)kh * p.Dk + c;
+        if (p.wide_out) {
+            if (c >= p.Dk) return;
+            typename Eight<T>::vec o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = (T)v[e];
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+                u32x4 w;
+                __builtin_memcpy(&w, reinterpret_cast<const char *>(&o) + 16 * k, 16);
+                reinterpret_cast<u32x4 *>(to)[k] = w;
+            }
         } else {
-            static_cast<T *>(p.dq.data)[b * p.dq.s0 + (t0 + r) * p.dq.s1 + (int64_t)kh * p.Dk + c] = (T)q;
-            static_cast<T *>(p.dk.data)[b * p.dk.s0 + (t0 + r) * p.dk.s1 + (int64_t)kh * p.Dk + c] = (T)k;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < p.Dk) to[e] = (T)v[e];
         }
     };
-    auto put_gates = [&](int r, float dg, float db) __attribute__((always_inline)) {
-        if (p.dg.data) static_cast<float *>(p.dg.data)[b * p.dg.s0 + (t0 + r) * p.dg.s1 + h] = dg;
-        static_cast<float *>(p.dbeta.data)[b * p.dbeta.s0 + (t0 + r) * p.dbeta.s1 + h] = db;
-    };
     if (m <= 0) {
-        for (int u = tid; u < here * p.Dk; u += NT) put(u / p.Dk, u % p.Dk, 0.0f, 0.0f);
-        if (tid < here) put_gates(tid, 0.0f, 0.0f);
+        const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int u = tid; u < here * KF * 4; u += THREADS) {
+            put8(p.dq, 0, u / (KF * 4), u % (KF * 4) * 8, none);
+            put8(p.dk, 1, u / (KF * 4), u % (KF * 4) * 8, none);
+        }
+        if (tid < here) {
+            if (p.dg.data) static_cast<float *>(p.dg.data)[b * p.dg.s0 + (t0 + tid) * p.dg.s1 + h] = 0.0f;
+            static_cast<float *>(p.dbeta.data)[b * p.dbeta.s0 + (t0 + tid) * p.dbeta.s1 + h] = 0.0f;
+        }
         return;
     }
     const float *scal = p.scal + (int64_t)id * SCALAR_FLOATS;
@@ -239,233 +261,295 @@ __global__ __launch_bounds__(NT) void merit_delta_grads(DeltaParams p)
         beta[tid] = scal[BETA * C + tid];
     }
     const float *state = p.states + (int64_t)id * (p.Dk + C) * Dv, *kept = state + p.Dk * Dv;
-    const float *z = p.ds + (int64_t)id * p.Dk * Dv, *x = p.dx + (int64_t)id * C * Dv;
-    const int own = 16 * wave + l16;
-    const float bt = scal[BETA * C + own];
-    const T *dyrow = static_cast<const T *>(p.dy.data) + b * p.dy.s0 + (t0 + own) * p.dy.s1 + h * Dv;
+    const float *zs = p.ds + (int64_t)id * p.Dk * Dv, *xs = p.dx + (int64_t)id * C * Dv;
+    // a thread of the first four wavefronts moves eight values of a token of dy and x, of the last four (they may be the same) of u;
+    // and every lane eight of the rows of S_0 and Z that are its own
+    const bool first = tid < NT, second = tid >= THREADS - NT;
+    const int tr = (tid & (NT - 1)) >> 2, tc = (tid & 3) * 8;
+    const T *dyrow = static_cast<const T *>(p.dy.data) + b * p.dy.s0 + (t0 + min(tr, m - 1)) * p.dy.s1 + h * Dv;
+    const float bt = scal[BETA * C + tr];
+    const int row = 16 * wave + l16;
+    const bool keys = wave < 2 * KF;                           // (the wavefront has a tile of keys)
+    Eight<T> dy;
+    Eight<float> x, d, s, z;
+    auto load = [&](int c0) __attribute__((always_inline)) {
+        const int left = (int)Dv - c0;
+        dy = take8<WIDE, T>(dyrow + c0, tc, tr < m ? left : 0);
+        x = take8<WIDE, float>(xs + tr * Dv + c0, tc, left);
+        d = take8<WIDE, float>(kept + tr * Dv + c0, tc, left);
+        const int64_t at = (int64_t)min(row, p.Dk - 1) * Dv + c0;
+        const int there = row < p.Dk ? left : 0;
+        s = take8<WIDE, float>(state + at, 8 * quad, there);
+        z = take8<WIDE, float>(zs + at, 8 * quad, there);
+    };
 
-    f32x4 dq[DT], rows[DT], cols[DT], dP[4], dM[4];
+    f32x4 dq[RT], rows[RT], cols[RT], dP[RT], dM[RT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) dq[d] = rows[d] = cols[d] = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) dP[j] = dM[j] = f32x4{0, 0, 0, 0};
+    for (int rt = 0; rt < RT; ++rt) dP[rt] = dM[rt] = dq[rt] = rows[rt] = cols[rt] = f32x4{0, 0, 0, 0};
+    // With eight wavefronts the first four have the rows of dP, the others those of dM
+    const int own = wave & 3;
+    const bool has_p = wave < 4, has_m = WAVES == 4 || wave >= 4;
     float db = 0.0f;
     double sz = 0.0;
+    load(0);
     for (int c0 = 0; c0 < Dv; c0 += 32) {
         __syncthreads();
-        float szp = 0.0f;
-        for (int u = tid; u < KF * 32 * 4; u += NT) {
-            const int r = u / 4, c = u % 4 * 8;
-            Eight<float> s = zero8<float>(), g = zero8<float>();
-            if (r < p.Dk) {
-                s = load8<float>(state + r * Dv + c0, c, p.Dv - c0, p.wide_v);
-                g = load8<float>(z + r * Dv + c0, c, p.Dv - c0, p.wide_v);
+        bf16x8 st[3], zt[3];
+        {
+            bf16x8 o[NK], o3[3];
+            if (first) {
+                terms8<T>(dy, o);
+                yt.put8(tr, tc, o);
+                terms8<float>(x, o3);
+                xt.put8(tr, tc, o3);
             }
-            bf16x8 o[3];
-            terms8<float>(s, o);
-            st.put8(r, c, o);
-            terms8<float>(g, o);
-            zt.put8(r, c, o);
+            if (second) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) szp = fmaf(s.v[e], g.v[e], szp);
-        }
-        sz += (double)szp;
-        {
-            const int r = tid / 4, c = tid % 4 * 8;
-            Eight<float> d = load8<float>(kept + r * Dv + c0, c, p.Dv - c0, p.wide_v);
-            const float f = scal[BETA * C + r];
+                for (int e = 0; e < 8; ++e) db = fmaf(x.v[e], d.v[e], db);
+                d.v *= bt;
+                terms8<float>(d, o3);
+                ut.put8(tr, tc, o3);
+            }
+            float f = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d.v[e] *= f;
-            bf16x8 o[3];
-            terms8<float>(d, o);
-            ut.put8(r, c, o);
+            for (int e = 0; e < 8; ++e) f = fmaf(s.v[e], z.v[e], f);
+            sz += (double)f;
+            terms8<float>(s, st);
+            terms8<float>(z, zt);
         }
-        bf16x8 ya[NK], xa[3], ua[3];
-        {
-            Eight<T> y = zero8<T>();
-            if (own < m) y = load8<T>(dyrow + c0, 8 * quad, p.Dv - c0, p.wide_v);
-            terms8<T>(y, ya);
-            const Eight<float> xe = load8<float>(x + own * Dv + c0, 8 * quad, p.Dv - c0, p.wide_v);
-            const Eight<float> d = load8<float>(kept + own * Dv + c0, 8 * quad, p.Dv - c0, p.wide_v);
-            terms8<float>(xe, xa);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) db = fmaf(xe.v[e], d.v[e], db);
-        }
+        load(c0 + 32 < Dv ? c0 + 32 : c0);              // (the last ones again: no branch)
         __syncthreads();
-        ut.rows(16 * wave, 0, ua);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            bf16x8 o[3];
-            st.rows(16 * d, 0, o);
-            multiply<3>(dq[d], ya, o);
-            multiply<3>(rows[d], xa, o);
-            zt.rows(16 * d, 0, o);
-            multiply<3>(cols[d], ua, o);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j > wave) continue;
-            bf16x8 o[3];
-            ut.rows(16 * j, 0, o);
-            multiply<3>(dP[j], ya, o);
-            multiply<3>(dM[j], xa, o);
+        for (int rt = 0; rt < RT; ++rt) {
+            bf16x8 a[NK], a3[3], u[3];
+            yt.rows(16 * rt, 0, a);
+            xt.rows(16 * rt, 0, a3);
+            ut.rows(16 * rt, 0, u);
+            if (keys) {
+                multiply<3>(dq[rt], a, st);
+                multiply<3>(rows[rt], a3, st);
+                multiply<3>(cols[rt], u, zt);
+            }
+            if (rt <= own) {
+                if (has_p) {
+                    yt.rows(16 * own, 0, a);
+                    multiply<3>(dP[rt], a, u);
+                }
+                if (has_m) {
+                    xt.rows(16 * own, 0, a3);
+                    multiply<3>(dM[rt], a3, u);
+                }
+            }
         }
     }
-    (void)bt;
-    db += lane_xor<4>(db);
-    db += lane_xor<5>(db);
+    db += lane_xor<0>(db);
+    db += lane_xor<1>(db);
+    if (!keys) sz = 0.0;
 #pragma unroll
-    for (int s = 1; s < 64; s *= 2) sz += __shfl_xor(sz, s);
-    if (lane == 0) dots[wave] = sz;
-
-    // scales of rows; K and Q; the matrices of 64 x 64, rows side by side
-    float in[4], out[4], ik[4], iq[4], bb[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const double g = G[row4 + r];
-        in[r] = exp_of(g);
-        out[r] = exp_of(G[C - 1] - g);
-        ik[r] = invk[row4 + r];
-        iq[r] = invq[row4 + r];
-        bb[r] = beta[row4 + r];
-    }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            dq[d][r] *= in[r];
-            rows[d][r] *= -in[r] * bb[r];
-            cols[d][r] *= out[r];
-        }
+    for (int k = 1; k < 64; k *= 2) sz += __shfl_xor(sz, k);
+    if (lane == 0) sums[0][wave] = sz;
     __syncthreads();            // (the first part's LDS is free)
     {
-        ChunkRows<T, KF> e;
-        if (p.wide_qk) e.template load<false, true>(p.k, b, t0, m, kh, p.Dk);
-        else e.template load<false, false>(p.k, b, t0, m, kh, p.Dk);
-        e.store(kt);
-        if (p.wide_qk) e.template load<false, true>(p.q, b, t0, m, kh, p.Dk);
-        else e.template load<false, false>(p.q, b, t0, m, kh, p.Dk);
-        e.store(qt);
-    }
+        // a unit of eight values of K and Q a thread and turn
+        constexpr int units = C * KF * 4 / THREADS;
+        static_assert(units >= 1, "");
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (j > (wave | 1)) continue;
-        const int c = 16 * j + l16;
+        for (int n = 0; n < units; ++n) {
+            const int u = tid + n * THREADS, r = u / (KF * 4), c = u % (KF * 4) * 8, there = r < m ? p.Dk : 0;
+            const T *krow = static_cast<const T *>(p.k.data) + b * p.k.s0 + (t0 + min(r, m - 1)) * p.k.s1 + (int64_t)kh * p.Dk;
+            const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + min(r, m - 1)) * p.q.s1 + (int64_t)kh * p.Dk;
+            const Eight<T> e = p.wide_qk ? take8<true, T>(krow, c, there) : take8<false, T>(krow, c, there);
+            const Eight<T> g = p.wide_qk ? take8<true, T>(qrow, c, there) : take8<false, T>(qrow, c, there);
+            bf16x8 o[NK];
+            terms8<T>(e, o);
+            kt.put8(r, c, o);
+            terms8<T>(g, o);
+            qt.put8(r, c, o);
+        }
+    }
+    // the matrices' rows of the wavefront
+    {
+        float tk[4], tq[4], tb[4];
+        double gt[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int t = row4 + r;
-            const float f = c <= t ? exp_of(G[t] - G[c]) : 0.0f;
-            dP[j][r] = c <= t ? f * dP[j][r] : 0.0f;
-            dM[j][r] = c < t ? -f * bb[r] * dM[j][r] : 0.0f;
-            pt.put1(t, c, dP[j][r] * invk[c]);
-            mt.put1(t, c, dM[j][r] * invk[c]);
+            const int t = 16 * own + 4 * quad + r;
+            tk[r] = invk[t];
+            tq[r] = invq[t] * p.scale;
+            tb[r] = -beta[t] * tk[r];
+            gt[r] = G[t];
         }
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {
+            if (j > (own | 1)) continue;
+            const int c = 16 * j + l16;
+            const float ck = invk[c];
+            const double gc = G[c];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * own + 4 * quad + r;
+                const float f = c <= t ? exp_of(gt[r] - gc) * ck : 0.0f;
+                dP[j][r] = c <= t ? f * tq[r] * dP[j][r] : 0.0f;
+                dM[j][r] = c < t ? f * tb[r] * dM[j][r] : 0.0f;
+                if (has_p) wt.put1(t, c, dP[j][r]);
+            }
+        }
+    }
+    // rows' factors
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const f32x4 in_q = *reinterpret_cast<const f32x4 *>(scal + IN_Q * C + 16 * rt + 4 * quad);
+        const f32x4 in_k = *reinterpret_cast<const f32x4 *>(scal + IN_K * C + 16 * rt + 4 * quad);
+        const f32x4 out_k = *reinterpret_cast<const f32x4 *>(scal + OUT_K * C + 16 * rt + 4 * quad);
+        const f32x4 bb = *reinterpret_cast<const f32x4 *>(scal + BETA * C + 16 * rt + 4 * quad);
+        dq[rt] *= in_q;
+        rows[rt] *= -in_k * bb;
+        cols[rt] *= out_k;
     }
     __syncthreads();
     // K.(o u Z^T), for the last token's G
-    float kz = 0.0f;
+    double kz = 0.0;
+    if (keys) {
+        float f = 0.0f;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) kz = fmaf(ik[r] * kt.value(row4 + r, 16 * d + l16), cols[d][r], kz);
-    double kzd = (double)kz;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) kzd += __shfl_xor(kzd, s);
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-        if (2 * f > wave) continue;
-        bf16x8 pa[3], ma[3];
-        pt.rows(16 * wave, 32 * f, pa);
-        mt.rows(16 * wave, 32 * f, ma);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            bf16x8 o[NK];
-            kt.cols(32 * f, 16 * d, o);
-            multiply<3>(dq[d], pa, o);
-            multiply<3>(rows[d], ma, o);
-        }
-    }
-    __syncthreads();
-    // their transposes
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (j > (wave | 1)) continue;
-        float e[4], g[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            e[r] = dP[j][r] * iq[r] * p.scale;
-            g[r] = dM[j][r] * ik[r];
-        }
-        pt.put4(16 * j + l16, row4, e);
-        mt.put4(16 * j + l16, row4, g);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-        if (2 * f + 1 < wave) continue;
-        bf16x8 pa[3], ma[3];
-        pt.rows(16 * wave, 32 * f, pa);
-        mt.rows(16 * wave, 32 * f, ma);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            bf16x8 o[NK];
-            qt.cols(32 * f, 16 * d, o);
-            multiply<3>(cols[d], pa, o);
-            kt.cols(32 * f, 16 * d, o);
-            multiply<3>(cols[d], ma, o);
-        }
-    }
-    // dots of a row along the keys, through the length, results
-    float dotq[4], dotr[4], dotc[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) dotq[r] = dotr[r] = dotc[r] = 0.0f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float kv = kt.value(row4 + r, 16 * d + l16), qv = qt.value(row4 + r, 16 * d + l16);
-            dotq[r] = fmaf(qv, dq[d][r], dotq[r]);
-            dotr[r] = fmaf(kv, rows[d][r], dotr[r]);
-            dotc[r] = fmaf(kv, cols[d][r], dotc[r]);
-        }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        dotq[r] = sum_lanes(dotq[r], 16) * iq[r] * p.scale;
-        dotr[r] = sum_lanes(dotr[r], 16) * ik[r];
-        dotc[r] = sum_lanes(dotc[r], 16) * ik[r];
-        if (l16 == 0) suffix[row4 + r] = (double)dotq[r] + (double)dotr[r] - (double)dotc[r];
+            for (int r = 0; r < 4; ++r) f = fmaf(kt.value(16 * rt + 4 * quad + r, row), cols[rt][r], f);
+        kz = (double)f;
     }
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int k = 1; k < 64; k *= 2) kz += __shfl_xor(kz, k);
+    if (lane == 0) sums[1][wave] = kz;
+
+    // to += W B (rows at or before the diagonal), and += W^T B
+    auto along = [&](f32x4 (&to)[RT], const bf16x8 (&o)[2][NK]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int c = 16 * d + l16;
-            if (row4 + r >= here || c >= p.Dk) continue;
-            float q = dq[d][r] * p.scale, k = rows[d][r] + cols[d][r];
-            if (p.unit) {
-                q = iq[r] * (q - iq[r] * qt.value(row4 + r, c) * dotq[r]);
-                k = ik[r] * (k - ik[r] * kt.value(row4 + r, c) * (dotr[r] + dotc[r]));
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int rt = 2 * f; rt < RT; ++rt) {
+                bf16x8 a[3];
+                wt.rows(16 * rt, 32 * f, a);
+                multiply<3>(to[rt], a, o[f]);
             }
-            const bool live = row4 + r < m;
-            put(row4 + r, c, live ? q : 0.0f, live ? k : 0.0f);
+    };
+    auto across = [&](f32x4 (&to)[RT], const bf16x8 (&o)[2][NK]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int rt = 0; rt < 2 * f + 2; ++rt) {
+                bf16x8 a[3];
+                wt.cols(32 * f, 16 * rt, a);
+                multiply<3>(to[rt], a, o[f]);
+            }
+    };
+    bf16x8 ko[2][NK];
+    if (keys) {
+        bf16x8 qo[2][NK];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            kt.cols(32 * f, 16 * wave, ko[f]);
+            qt.cols(32 * f, 16 * wave, qo[f]);
         }
-    __shared__ double last[4];
-    if (lane == 0) last[wave] = kzd;
+        along(dq, ko);
+        across(cols, qo);
+    }
+    __syncthreads();
+    if (has_m)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {
+            if (j > (own | 1)) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) wt.put1(16 * own + 4 * quad + r, 16 * j + l16, dM[j][r]);
+        }
+    __syncthreads();
+    if (keys) {
+        along(rows, ko);
+        across(cols, ko);
+    }
+    // Eight values of a token's row a thread and turn, for the sums along the keys (its KF * 4 lanes have the row) and the stores
+    constexpr int units = C * KF * 4 / THREADS;
+    auto by_rows = [&](const f32x4 (&v)[RT], float (&o)[units][8]) __attribute__((always_inline)) {
+        __syncthreads();
+        if (keys)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) ot[(16 * rt + 4 * quad + r) * OP + row] = v[rt][r];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < units; ++n) {
+            const int u = tid + n * THREADS;
+            const f32x4 *from = reinterpret_cast<const f32x4 *>(ot + u / (KF * 4) * OP + u % (KF * 4) * 8);
+            const f32x4 lo = from[0], hi = from[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o[n][e] = lo[e];
+                o[n][4 + e] = hi[e];
+            }
+        }
+    };
+    auto values = [&](const TK &t, int r, int c, float (&o)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll
+        for (int k = NK - 1; k >= 0; --k) {
+            const bf16x8 w = *reinterpret_cast<const bf16x8 *>(t.at + k * TK::plane + r * TK::pitch + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += (float)w[e];
+        }
+    };
+    auto dot = [&](const float (&a)[8], const float (&b)[8]) __attribute__((always_inline)) {
+        float v = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v = fmaf(a[e], b[e], v);
+        return sum_lanes(v, KF * 4);
+    };
+    float vq[units][8], va[units][8], vc[units][8];
+    by_rows(dq, vq);
+    by_rows(rows, va);
+    by_rows(cols, vc);
+#pragma unroll
+    for (int n = 0; n < units; ++n) {
+        const int u = tid + n * THREADS, t = u / (KF * 4), c = u % (KF * 4) * 8;
+        float qv[8], kv[8];
+        values(qt, t, c, qv);
+        values(kt, t, c, kv);
+        const float dotq = dot(qv, vq[n]), dota = dot(kv, va[n]), dotc = dot(kv, vc[n]);
+        if (c == 0) suffix[t] = (double)dotq + (double)dota - (double)dotc;
+        // through the lengths
+        const float fq = p.unit ? invq[t] * invq[t] * dotq : 0.0f, fk = p.unit ? invk[t] * invk[t] * (dota + dotc) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            vq[n][e] = t < m ? fmaf(-fq, qv[e], vq[n][e]) : 0.0f;
+            va[n][e] = t < m ? fmaf(-fk, kv[e], va[n][e] + vc[n][e]) : 0.0f;
+        }
+        if (t < here) {
+            put8(p.dq, 0, t, c, vq[n]);
+            put8(p.dk, 1, t, c, va[n]);
+        }
+    }
     __syncthreads();
     if (wave == 0) {
-        double s = suffix[lane];
-        if (lane == C - 1)
-            s += (double)exp_of(G[C - 1]) * ((dots[0] + dots[1]) + (dots[2] + dots[3])) + (last[0] + last[1]) + (last[2] + last[3]);
+        double a = suffix[lane];
+        if (lane == C - 1) {
+            double f = 0.0, g = 0.0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                f += sums[0][w];
+                g += sums[1][w];
+            }
+            a += (double)exp_of(G[C - 1]) * f + g;
+        }
 #pragma unroll
         for (int k = 1; k < C; k *= 2) {
-            const double o = __shfl_down(s, k);
-            if (lane + k < C) s += o;
+            const double o = __shfl_down(a, k);
+            if (lane + k < C) a += o;
         }
         if (lane < here && p.dg.data)
-            static_cast<float *>(p.dg.data)[b * p.dg.s0 + (t0 + lane) * p.dg.s1 + h] = lane < m ? (float)s : 0.0f;
+            static_cast<float *>(p.dg.data)[b * p.dg.s0 + (t0 + lane) * p.dg.s1 + h] = lane < m ? (float)a : 0.0f;
     }
-    if (quad == 0 && own < here)
-        static_cast<float *>(p.dbeta.data)[b * p.dbeta.s0 + (t0 + own) * p.dbeta.s1 + h] = own < m ? db : 0.0f;
+    if (second && (tid & 3) == 0 && tr < here)
+        static_cast<float *>(p.dbeta.data)[b * p.dbeta.s0 + (t0 + tr) * p.dbeta.s1 + h] = tr < m ? db : 0.0f;
 }
 
 // dq, dk of a key head: the sum over its value heads
@@ -499,11 +583,14 @@ template <typename T, int KF> hipError_t backward_chunks(DeltaParams p, hipStrea
 template <typename T, int KF> hipError_t grads_of(const DeltaParams &p, hipStream_t s)
 {
     constexpr int NK = Terms<T>::n;
-    constexpr int one = 2 * Tile<3, KF * 32, 32>::bytes + Tile<3, C, 32>::bytes;
-    constexpr int two = 2 * Tile<NK, C, KF * 32>::bytes + 2 * Tile<3, C, C>::bytes;
+    constexpr int one = Tile<NK, C, 32>::bytes + 2 * Tile<3, C, 32>::bytes;
+    constexpr int matrix = Tile<3, C, C>::bytes, out = C * (KF * 32 + 4) * 4;
+    constexpr int two = 2 * Tile<NK, C, KF * 32>::bytes + (matrix > out ? matrix : out);
     constexpr int lds = one > two ? one : two;
     static_assert(lds + 3 * 1024 <= 160 * 1024, "");
-    merit_delta_grads<T, KF><<<(unsigned)(p.B * p.n * p.H), NT, lds, s>>>(p);
+    const unsigned grid = (unsigned)(p.B * p.n * p.H);
+    if (p.wide_v) merit_delta_grads<T, KF, true><<<grid, 64 * grad_waves<KF>(), lds, s>>>(p);
+    else merit_delta_grads<T, KF, false><<<grid, 64 * grad_waves<KF>(), lds, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int KF> hipError_t backward_of(const DeltaParams &p, hipStream_t s)

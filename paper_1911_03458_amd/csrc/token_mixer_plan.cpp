@@ -143,8 +143,8 @@ merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64
         L > MAX_ROWS || too_large(B, L, heads * (Dk + Dv)))
         return MERIT_ERR_UNSUPPORTED;
     const int64_t n = cdiv(L, MERIT_DELTA_CHUNK);
-    // workgroups of every pass, at the narrowest tiles; the sum over heads, a thread a value; states of all chunks
-    if (B > MAX_BLOCKS / heads || B * heads * (n > cdiv(Dv, 16) ? n : cdiv(Dv, 16)) >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + 64) * Dv) ||
+    // workgroups of every pass, at the narrowest tiles and up to 512 threads a chunk; the sum over heads, a thread a value; states of all chunks
+    if (B > MAX_BLOCKS / heads || B * heads * (2 * n > cdiv(Dv, 16) ? 2 * n : cdiv(Dv, 16)) >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + 64) * Dv) ||
         (L > 0 && B > MAX_BLOCKS / L * 256 / (key_heads * Dk)))
         return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(DELTA, type);
@@ -240,6 +240,7 @@ merit_status merit_delta_rule_backward(const merit_token_plan *plan, const merit
     if (st != MERIT_OK) return st;
     delta_use(p, workspace, true);
     p.wide_qk = p.Dk % 8 == 0 && in_16_bytes(p.q, p.B, p.L, p.type) && in_16_bytes(p.k, p.B, p.L, p.type);
+    p.wide_out = p.Dk % 8 == 0 && in_16_bytes(p.dq, p.B, p.L, p.type) && in_16_bytes(p.dk, p.B, p.L, p.type);
     p.wide_v = p.Dv % 8 == 0 && in_16_bytes(p.dy, p.B, p.L, p.type) && address_16(p.states);
     return done(launch_delta_backward(p, static_cast<hipStream_t>(stream)));
 }

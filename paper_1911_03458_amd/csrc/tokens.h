@@ -105,7 +105,7 @@ struct DeltaParams {
     int type;
     int n;                 // chunks of MERIT_DELTA_CHUNK tokens
     int slices;            // workgroups along v's columns
-    int wide_qk, wide_v, wide_state;    // whether rows can be read in 16-byte pieces
+    int wide_qk, wide_v, wide_out, wide_state;      // whether rows can be moved in 16-byte pieces (wide_out: dq, dk)
     Rows q, k, v, y, dy, dq, dk, dv;
     Rows g, beta, dg, dbeta;            // a number a head
     int beta_f32;
