@@ -59,6 +59,7 @@ typedef struct merit_token_plan merit_token_plan;   /* opaque, host memory only 
 #define MERIT_SCAN_TILE       16     /* tokens between two kept states of a forward pass */
 #define MERIT_DELTA_MAX_KEYS  128    /* values of a key */
 #define MERIT_DELTA_CHUNK     64     /* tokens between two kept states of a forward pass */
+#define MERIT_DELTA_KEPT      9728   /* values that the forward pass keeps of a chunk besides its state and tokens */
 #define MERIT_DELTA_EPS       1e-6f  /* beside the square of a length that divides */
 #define MERIT_BLOCK_NORM_MAX_CHANNELS 16384
 
@@ -225,8 +226,10 @@ merit_status merit_scan_step(const merit_token_plan *plan, const merit_scan_step
 
 /* S_t = a_t S_{t-1} + k_t u_t^T,  u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  y_t = scale S_t^T q_t,  a_t = exp(g_t).
  * The states start from h0, or 0.  lens[b]: tokens of sequence b (cut to [0, L]); behind them nothing is read, y is 0 and the
- * state stays.  states: for every MERIT_DELTA_CHUNK-th token the state before it (Dk rows) and what the tokens from it on add
- * along their keys, each for beta = 1 (MERIT_DELTA_CHUNK rows), for the backward pass; not written behind a sequence's last chunk.
+ * state stays.  states: what the backward pass takes of every MERIT_DELTA_CHUNK tokens of a head (a chunk), from a 16-byte boundary on:
+ * MERIT_DELTA_KEPT values of how they act on each other, the state before them, and for each of them the row of Dv values that it
+ * would add to the state along its key for beta = 1; in all M = MERIT_DELTA_KEPT + (Dk + MERIT_DELTA_CHUNK) Dv values, rounded up to
+ * a multiple of 4.  Of chunks behind a sequence's end nothing is written.
  * A value that is not finite (an infinity, a NaN) makes NaN of what depends on it: q of its token's y, v of its column from its
  * token on, k, g (but -inf, which is a decay of 0) and beta of the head from there on. */
 typedef struct {
@@ -239,7 +242,7 @@ typedef struct {
     merit_view lens;         /* int32 [B], optional                           */
     merit_view y;            /* T [B, L, heads, Dv]                           */
     merit_view h_last;       /* F32 [B, heads, Dk, Dv] dense, optional; may be h0 */
-    merit_view states;       /* F32 [B, ceil(L / MERIT_DELTA_CHUNK), heads, Dk + MERIT_DELTA_CHUNK, Dv] dense, optional */
+    merit_view states;       /* F32 [B, ceil(L / MERIT_DELTA_CHUNK), heads, M] dense, optional */
 } merit_delta_rule_args;
 merit_status merit_delta_rule(const merit_token_plan *plan, const merit_delta_rule_args *args, void *workspace,
                               int64_t workspace_bytes, void *hip_stream);

@@ -3,9 +3,11 @@
 //     S_t = a_t S_{t-1} + k_t u_t^T,   u_t = b_t d_t,   d_t = v_t - a_t S_{t-1}^T k_t,   y_t = scale S_t^T q_t,   a_t = exp(g_t)
 //
 // A chunk of C = 64 tokens at once, G_t = g_1 + .. + g_t inside it, f_tj = exp(G_t - G_j), N_tj = f_tj k_t.k_j below the diagonal:
-//     d = (1 + N diag(b))^-1 (v - exp(G) K S_0),    y = scale (exp(G) Q S_0 + (f o Q K^T) u),    S_C = exp(G_C) S_0 + K^T (exp(G_C - G) u)
-// so that a token's dependence on those before it is a triangular matrix (found by merit_delta_prepare for all chunks side by
-// side), and the rest are matrix products.
+//     (1 + N diag(b)) d = r = v - exp(G) K S_0,    y = scale (exp(G) Q S_0 + (f o Q K^T) u),    S_C = exp(G_C) S_0 + K^T (exp(G_C - G) u)
+// so that a token's dependence on those before it is a triangular matrix, and the rest are matrix products.  With
+//     W = (1 + N diag(b))^-1 N,   (1 + N diag(b))^-1 = 1 - W diag(b),   (1 + diag(b) N)^-1 = 1 - diag(b) W
+// one matrix serves the forward pass, d = r - W (b r), and the backward pass, x = y - W^T (b y), whatever b is (0 too).
+// merit_delta_prepare finds it and P = scale f o Q K^T for all chunks side by side.
 //
 // Products run on v_mfma_f32_16x16x32_bf16.  An fp32 operand goes in as three bfloat16 terms of 8 bits each (x = x0 + x1 + x2 with
 // the rounding error of the one before in each), a binary16 one as two, a bfloat16 one as it is, and terms whose product is below
@@ -34,9 +36,9 @@ template <typename T> struct Terms { static constexpr int n = 3; };
 template <> struct Terms<f16_t> { static constexpr int n = 2; };
 template <> struct Terms<bf16_t> { static constexpr int n = 1; };
 
-// Terms of P and u where they give y, which is rounded to T: two leave 2^-17, next to the 2^-12 of a rounding to binary16; the
-// gradients that P gives go on into sums in fp32
-template <typename T> constexpr int mix_terms(bool backward) { return backward || Terms<T>::n == 3 ? 3 : 2; }
+// Terms of P and u where they give y, which is rounded to T: two leave 2^-17, next to the 2^-12 of a rounding to binary16 (the
+// gradients that P gives go on into sums in fp32: three)
+template <typename T> constexpr int mix_terms() { return Terms<T>::n == 3 ? 3 : 2; }
 
 template <int N> __device__ __forceinline__ void split(float x, __bf16 (&o)[N])
 {
@@ -264,25 +266,48 @@ template <int N> __device__ __forceinline__ void operand(const f32x4 &top, const
     split8<N>(x, o);
 }
 
-// A matrix of C x C in terms, as merit_delta_prepare leaves it (its columns interleaved), on its way into LDS
-template <int PLANES> struct Square {
-    static constexpr int units = PLANES * C * 8 / NT;
+// A triangular matrix of C x C in terms, as merit_delta_prepare leaves it: its columns interleaved, of the upper half of its rows the
+// left half.
+__device__ __forceinline__ int triangle_at(int t, int c) { return t < C / 2 ? t * (C / 2) + c : C * C / 4 + (t - C / 2) * C + c; }
+constexpr int TRIANGLE = C * C * 3 / 4;
+// The first PLANES of its terms on their way into LDS
+template <int PLANES> struct Triangle {
+    static constexpr int per = TRIANGLE / 8, all = PLANES * per, units = (all + NT - 1) / NT;
     bf16x8 e[units];
-    __device__ __forceinline__ void load(const void *base, int64_t chunk)
+    __device__ __forceinline__ void load(const __bf16 *from)
     {
-        const bf16x8 *from = static_cast<const bf16x8 *>(base) + chunk * PLANES * C * 8 + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < units; ++i) e[i] = from[i * NT];
+        for (int i = 0; i < units; ++i) {
+            const int u = (int)threadIdx.x + i * NT;
+            e[i] = reinterpret_cast<const bf16x8 *>(from)[u < all ? u : all - 1];
+        }
     }
     __device__ __forceinline__ void store(const Mixed<PLANES, C> &t) const
     {
 #pragma unroll
         for (int i = 0; i < units; ++i) {
-            const int u = (int)threadIdx.x + i * NT;
-            *reinterpret_cast<bf16x8 *>(t.at + u / (C * 8) * t.plane + u / 8 % C * t.pitch + u % 8 * 8) = e[i];
+            const int u = (int)threadIdx.x + i * NT, v = u % per, w = v - per / 3;
+            const int at = v < per / 3 ? (v >> 2) * t.pitch + (v & 3) * 8 : (C / 2 + (w >> 3)) * t.pitch + (w & 7) * 8;
+            if (u < all) *reinterpret_cast<bf16x8 *>(t.at + u / per * t.plane + at) = e[i];
         }
     }
 };
+// What merit_delta_prepare leaves of a chunk of a head
+struct Prepared {
+    __bf16 *w, *mix;        // -W and P, three terms each (of P two, where nothing but y of a 16-bit type is made of it)
+    float *scal;
+};
+constexpr int PREPARED_FLOATS = DELTA_PREPARED_FLOATS;
+static_assert(PREPARED_FLOATS == 3 * TRIANGLE + DELTA_SCALAR_FLOATS, "");
+__device__ __forceinline__ Prepared prepared(const DeltaParams &p, int64_t chunk)
+{
+    float *at = p.prep + chunk * p.prep_stride;
+    Prepared r;
+    r.scal = at;
+    r.w = reinterpret_cast<__bf16 *>(at + DELTA_SCALAR_FLOATS);
+    r.mix = r.w + 3 * TRIANGLE;
+    return r;
+}
 
 // Eight values of a row of n, from column c on, zeros from column n on; nothing stands in a branch, so that loads of many rows go out
 // together.  WIDE: rows start on 16 bytes and n is a multiple of 8.

@@ -1,10 +1,10 @@
 // The gated delta rule, backward (the formulas and the representation of operands: delta.h).  With Z the gradient of the state
-// behind a chunk, T = (1 + diag(b) N)^-1, K and Q of unit length (Q scaled), i = exp(G), o = exp(G_C - G):
-//     x = T^T (P^T dy + o K Z),   dv = b x,   Z_before = exp(G_C) Z + Q^T (i dy) - K^T (i dv)              one chunk after the other
+// behind a chunk, K and Q of unit length (Q scaled), i = exp(G), o = exp(G_C - G):
+//     y = P^T dy + o K Z,   x = y - W^T (b y),   dv = b x,   Z_before = exp(G_C) Z + Q^T (i dy) - K^T (i dv)              one chunk after the other
 //     dQ = i (dy S_0^T) + (f o dy u^T) K                                                                   chunks side by side
 //     dK = rows + cols,  rows = M K - i (dv S_0^T),  cols = (f o dy u^T)^T Q + M^T K + o (u Z^T),  M = -b f o (x u^T) below the diagonal
 //     db = x.d,   dG = Q.dQ + K.rows - K.cols, at the last token besides exp(G_C) <S_0, Z> + K.(o u Z^T),   dg_t = sum of dG from t on
-// d and S_0 come from the forward pass.
+// d, S_0, W and P come from the forward pass.
 #pragma once
 
 #include "delta_forward.h"
@@ -15,18 +15,18 @@ namespace delta {
 // ---------------------------------------------------------------------------
 // one chunk after the other, from the last: a wavefront 16 columns of a head's Z
 // ---------------------------------------------------------------------------
-// Split as merit_delta_chunks is: a wavefront has its columns of Z and of all tokens in registers, LDS holds K, Q and the transposes
-// of the triangular matrices, of which a row of blocks begins at the diagonal.
+// Split as merit_delta_chunks is: a wavefront has its columns of Z and of all tokens in registers, LDS holds K, Q and the
+// triangular matrices, whose transposes come out of transposing reads.
 template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(true), RT = C / 16, DT = 2 * KF;
+    constexpr int NK = Terms<T>::n, RT = C / 16, DT = 2 * KF;
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
     typedef Mixed<NK, KF * 32> TK;
     const TK kt{smem}, qt{kt.at + TK::bytes / 2};
     const Mixed<3, C> tt{qt.at + TK::bytes / 2};
-    const Mixed<NP, C> mt{tt.at + Mixed<3, C>::bytes / 2};
-    float *const sc = reinterpret_cast<float *>(mt.at + Mixed<NP, C>::bytes / 2);
+    const Mixed<3, C> mt{tt.at + Mixed<3, C>::bytes / 2};
+    float *const sc = reinterpret_cast<float *>(mt.at + Mixed<3, C>::bytes / 2);
 
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
@@ -46,8 +46,7 @@ __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
         }
     const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);
     ChunkRows<T, KF> kr, qr;
-    Square<3> tr;
-    Square<NP> mr;
+    Triangle<3> tr, mr;
     f32x4 sr;
     ChunkColumn<T> dy;
     auto load = [&](int i, auto full) __attribute__((always_inline)) {
@@ -55,9 +54,10 @@ __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
         const int m = min(C, len - i * C);
         kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
         qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
-        tr.load(p.tri, chunk);
-        mr.load(p.mix, chunk);
-        sr = reinterpret_cast<const f32x4 *>(p.scal + chunk * SCALAR_FLOATS)[tid % (SCALAR_FLOATS / 4)];
+        const Prepared from = prepared(p, chunk);
+        tr.load(from.w);
+        mr.load(from.mix);
+        sr = reinterpret_cast<const f32x4 *>(from.scal)[tid % (SCALAR_FLOATS / 4)];
     };
     auto load_dy = [&](int i, auto full) __attribute__((always_inline)) {
         dy.template load<full.value>(p.dy, b, (int64_t)i * C, min(C, len - i * C), mine);
@@ -117,15 +117,15 @@ __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
             }
             if constexpr (full.value) load_dy(then, full);
             {
-                bf16x8 y[2][NK], a[RT][NP], au[2][NP];
+                bf16x8 y[2][NK], a[RT][3], au[2][3];
 #pragma unroll
                 for (int f = 0; f < 2; ++f) operand<NK>(W[2 * f], W[2 * f + 1], y[f]);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) mt.rows(rt, 1, a[rt]);
+                for (int rt = 0; rt < RT; ++rt) mt.cols(1, rt, a[rt]);
                 multiply_rows<3>(U, a, y[1]);
                 f32x4 upper[2] = {U[0], U[1]};
-                mt.rows(0, 0, au[0]);
-                mt.rows(1, 0, au[1]);
+                mt.cols(0, 0, au[0]);
+                mt.cols(0, 1, au[1]);
                 multiply_rows<3>(upper, au, y[0]);
                 U[0] = upper[0];
                 U[1] = upper[1];
@@ -141,16 +141,17 @@ __global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
             {
                 bf16x8 u[2][3], a[RT][3], au[2][3];
 #pragma unroll
-                for (int f = 0; f < 2; ++f) operand<3>(U[2 * f], U[2 * f + 1], u[f]);
-#pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    X[rt] = f32x4{0, 0, 0, 0};
-                    tt.rows(rt, 1, a[rt]);
+                    X[rt] = U[rt];
+                    U[rt] *= scalar(BETA, rt);
+                    tt.cols(1, rt, a[rt]);
                 }
+#pragma unroll
+                for (int f = 0; f < 2; ++f) operand<3>(U[2 * f], U[2 * f + 1], u[f]);
                 multiply_rows<3>(X, a, u[1]);
                 f32x4 upper[2] = {X[0], X[1]};
-                tt.rows(0, 0, au[0]);
-                tt.rows(1, 0, au[1]);
+                tt.cols(0, 0, au[0]);
+                tt.cols(0, 1, au[1]);
                 multiply_rows<3>(upper, au, u[0]);
                 X[0] = upper[0];
                 X[1] = upper[1];
@@ -253,14 +254,14 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
         }
         return;
     }
-    const float *scal = p.scal + (int64_t)id * SCALAR_FLOATS;
+    const float *scal = prepared(p, id).scal;
     if (tid < C) {
         G[tid] = reinterpret_cast<const double *>(scal + SCALARS * C)[tid];
         invk[tid] = scal[INV_K * C + tid];
         invq[tid] = scal[INV_Q * C + tid];
         beta[tid] = scal[BETA * C + tid];
     }
-    const float *state = p.states + (int64_t)id * (p.Dk + C) * Dv, *kept = state + p.Dk * Dv;
+    const float *state = p.states + (int64_t)id * p.prep_stride + PREPARED_FLOATS, *kept = state + p.Dk * Dv;
     const float *zs = p.ds + (int64_t)id * p.Dk * Dv, *xs = p.dx + (int64_t)id * C * Dv;
     // a thread of the first four wavefronts moves eight values of a token of dy and x, of the last four (they may be the same) of u;
     // and every lane eight of the rows of S_0 and Z that are its own
@@ -572,7 +573,7 @@ template <typename T> __global__ __launch_bounds__(NT) void merit_delta_sum_head
 
 template <typename T, int KF> hipError_t backward_chunks(DeltaParams p, hipStream_t s)
 {
-    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + Mixed<3, C>::bytes + Mixed<mix_terms<T>(true), C>::bytes + SCALAR_FLOATS * 4;
+    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + 2 * Mixed<3, C>::bytes + SCALAR_FLOATS * 4;
     static_assert(lds <= 160 * 1024, "");
     p.slices = (p.Dv + 63) / 64;
     const unsigned grid = (unsigned)(p.B * p.H * p.slices);
@@ -595,7 +596,6 @@ template <typename T, int KF> hipError_t grads_of(const DeltaParams &p, hipStrea
 }
 template <typename T, int KF> hipError_t backward_of(const DeltaParams &p, hipStream_t s)
 {
-    if (hipError_t e = prepare_of<T, KF, true>(p, s)) return e;
     if (hipError_t e = backward_chunks<T, KF>(p, s)) return e;
     if (p.n == 0) return hipSuccess;
     if (hipError_t e = grads_of<T, KF>(p, s)) return e;

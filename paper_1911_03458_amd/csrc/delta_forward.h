@@ -10,17 +10,19 @@ namespace delta {
 // ---------------------------------------------------------------------------
 // chunks side by side: a workgroup a chunk of a head
 // ---------------------------------------------------------------------------
-// Forward it leaves X = (1 + N diag(b))^-1 and P = scale f o Q K^T, their columns interleaved (delta.h); backward the transposes of
-// (1 + diag(b) N)^-1 and P.  Blocks of 16 x 16 of P beyond the diagonal are not written but where a product of 32 reads them.
-template <typename T, int KF, bool BACK, bool WIDE>
+// It leaves -W and P in terms, their columns interleaved, and the tokens' factors.
+template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(BACK);
-    __shared__ __attribute__((aligned(16))) __bf16 kmem[Tile<NK, C, KF * 32>::bytes / 2];
-    __shared__ __attribute__((aligned(16))) float a[C][C + 4], x[C][C + 4];
+    constexpr int NK = Terms<T>::n, LINE = C + 4;
+    // K, and where it is not needed any more W
+    constexpr int first = Tile<NK, C, KF * 32>::bytes > C * LINE * 4 ? Tile<NK, C, KF * 32>::bytes : C * LINE * 4;
+    __shared__ __attribute__((aligned(16))) __bf16 kmem[first / 2];
+    __shared__ __attribute__((aligned(16))) float a[C][LINE];
+    float (*const x)[LINE] = reinterpret_cast<float (*)[LINE]>(kmem);
     __shared__ double G[C];
-    __shared__ float beta[C], invk[C], invq[C];
-    __shared__ int bad;             // the first token whose row of the triangular matrix is not finite
+    __shared__ __attribute__((aligned(16))) float beta[C], finite_beta[C], invk[C], invq[C];
+    __shared__ int bad;             // the first token whose row of N is not finite
     const Tile<NK, C, KF * 32> kt{kmem};
 
     const uint32_t id = blockIdx.x, h = id % (uint32_t)p.H, bi = id / (uint32_t)p.H;
@@ -29,7 +31,8 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
     const int kh = (int)h / p.each, m = min(C, tokens_of(p, b) - (int)t0);
     if (m <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
-    float *scal = p.scal + (int64_t)id * SCALAR_FLOATS;
+    const Prepared to = prepared(p, id);
+    float *const scal = to.scal;
 
     // Two rows' loads in a wavefront: keys to LDS, their squares' sums over the lanes of a row
     ChunkRows<T, KF> kr;
@@ -55,6 +58,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         }
         G[lane] = g;
         beta[lane] = bt;
+        finite_beta[lane] = isfinite(bt) ? bt : 0.0f;     // (the rows that it reaches are lost anyway)
     }
     if (p.unit) {
 #pragma unroll
@@ -92,14 +96,17 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         reinterpret_cast<double *>(scal + SCALARS * C)[tid] = g;
     }
 
-    // Rows or columns 16 wave .. of K K^T and Q K^T, up to the diagonal's block
-    __bf16 *mix = static_cast<__bf16 *>(p.mix) + (int64_t)id * NP * C * C;
+    // Rows 16 wave .. of K K^T and Q K^T, transposed (the lane then has four values of a row side by side), up to the diagonal's block
     bf16x8 qa[KF][NK], ka[KF][NK];
 #pragma unroll
     for (int f = 0; f < KF; ++f) {
         terms8<T>(qe[f], qa[f]);
         kt.rows(16 * wave, 32 * f, ka[f]);
     }
+    const int t = own;                                  // the token that reads
+    const double gt = G[t];
+    const float kt_len = invk[t], qt_len = invq[t] * p.scale;
+#pragma unroll
     for (int jb = 0; jb < 4; ++jb) {
         f32x4 kk = {0, 0, 0, 0}, qk = {0, 0, 0, 0};
         if (jb <= wave)
@@ -107,49 +114,44 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
             for (int f = 0; f < KF; ++f) {
                 bf16x8 o[NK];
                 kt.rows(16 * jb, 32 * f, o);
-                // backward: the lane has a column of four rows, whose transpose lies side by side; forward the other way round
-                if constexpr (BACK) {
-                    multiply<3>(kk, ka[f], o);
-                    multiply<3>(qk, qa[f], o);
-                } else {
-                    multiply<3>(kk, o, ka[f]);
-                    multiply<3>(qk, o, qa[f]);
-                }
+                multiply<3>(kk, o, ka[f]);
+                multiply<3>(qk, o, qa[f]);
             }
-        bf16x4 out[NP];
+        const int j0 = 16 * jb + 4 * quad;              // the tokens that were written
+        const f32x4 lens = *reinterpret_cast<const f32x4 *>(&invk[j0]);
+        f32x4 n;
+        bf16x4 out[3];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int t = BACK ? 16 * wave + 4 * quad + r : 16 * wave + l16;          // the token that reads
-            const int j = BACK ? 16 * jb + l16 : 16 * jb + 4 * quad + r;              // the token that was written
-            const float f = j <= t ? exp_of(G[t] - G[j]) : 0.0f;
-            float w = j < t ? f * invk[t] * invk[j] * (BACK ? beta[t] : beta[j]) * kk[r] : 0.0f;
-            if (!isfinite(w)) {     // (0 times it would reach the tokens before)
+            const int j = j0 + r;
+            const float f = j <= t ? exp_of(gt - G[j]) * lens[r] : 0.0f;
+            float w = j < t ? f * kt_len * kk[r] : 0.0f;
+            if (j < t && !isfinite(w * beta[j])) {      // (0 times it would reach the tokens before)
                 atomicMin(&bad, t);
                 w = 0.0f;
             }
-            a[t][j] = w;
-            __bf16 s[NP];
-            split<NP>(j <= t ? f * p.scale * invq[t] * invk[j] * qk[r] : 0.0f, s);
+            n[r] = w;
+            __bf16 s[3];
+            split<3>(j <= t ? f * qt_len * qk[r] : 0.0f, s);
 #pragma unroll
-            for (int n = 0; n < NP; ++n) out[n][r] = s[n];
+            for (int k = 0; k < 3; ++k) out[k][r] = s[k];
         }
+        *reinterpret_cast<f32x4 *>(&a[t][j0]) = n;
         if (jb <= (wave | 1))
 #pragma unroll
-            for (int n = 0; n < NP; ++n) {
-                __bf16 *to = mix + n * C * C +
-                             (BACK ? (16 * jb + l16) * C + interleaved(16 * wave + 4 * quad) : (16 * wave + l16) * C + interleaved(16 * jb + 4 * quad));
-                *reinterpret_cast<bf16x4 *>(to) = out[n];
-            }
+            for (int k = 0; k < 3; ++k)
+                if (k < p.mix_terms) *reinterpret_cast<bf16x4 *>(to.mix + k * TRIANGLE + triangle_at(t, interleaved(j0))) = out[k];
     }
     __syncthreads();
 
-    // The inverse x of 1 + a, in blocks of 16 x 16.  On the diagonal: lane c of wavefront w has column c of block w and takes one
-    // row after the other (powers of a block, which would do it with products, cancel where keys are alike).
+    // W in blocks of 16 x 16.  On the diagonal: lane c of wavefront w has column c of block w and takes one row after the other,
+    // W_rc = N_rc - sum over c < j < r of N_rj b_j W_jc (powers of a block, which would do it with products, cancel where keys are
+    // alike).
     {
-        float d[16];
+        float d[16];                // b W
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            float v0 = r == l16 ? 1.0f : 0.0f, v1 = 0.0f;
+            float v0 = a[16 * wave + r][16 * wave + l16], v1 = 0.0f;        // (0 from the diagonal on)
 #pragma unroll
             for (int j = 0; j < r; j += 4) {
                 const f32x4 w = *reinterpret_cast<const f32x4 *>(&a[16 * wave + r][16 * wave + j]);
@@ -158,55 +160,57 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
                 if (j + 2 < r) v0 = fmaf(-w[2], d[j + 2], v0);
                 if (j + 3 < r) v1 = fmaf(-w[3], d[j + 3], v1);
             }
-            d[r] = v0 + v1;
+            const float v = v0 + v1;
+            d[r] = finite_beta[16 * wave + r] * v;
+            if (quad == 0) x[16 * wave + r][16 * wave + l16] = v;
         }
-        if (quad == 0)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[16 * wave + r][16 * wave + l16] = d[r];
     }
     __syncthreads();
-    // Below it, a diagonal of blocks at a time: x_ij = -x_ii (a_ij x_jj + .. + a_i,i-1 x_i-1,j), fp32 products.  Step s of a product
-    // sums over the numbers 4 q + s of quad q's lanes, which is how a result lies in them: it goes on without a move.
+    // Below it, a diagonal of blocks at a time: W_ij = M - W_ii (b M), M = N_ij - N_ij (b W_jj) - .. - N_i,i-1 (b W_i-1,j), fp32
+    // products.  Step s of a product sums over the numbers 4 q + s of quad q's lanes, which is how a result lies in them: it goes
+    // on without a move.
 #pragma unroll
     for (int dist = 1; dist < 4; ++dist) {
         const int bi_ = wave + dist, bj = wave;
         if (bi_ < 4) {
-            f32x4 sum = {0, 0, 0, 0}, out = {0, 0, 0, 0};
+            f32x4 mm;
 #pragma unroll
-            for (int k = 0; k < dist; ++k)
+            for (int r = 0; r < 4; ++r) mm[r] = a[16 * bi_ + 4 * quad + r][16 * bj + l16];
+#pragma unroll
+            for (int k = 0; k < dist; ++k) {
+                const f32x4 bk = *reinterpret_cast<const f32x4 *>(&finite_beta[16 * (bj + k) + 4 * quad]);
+                const f32x4 ak = *reinterpret_cast<const f32x4 *>(&a[16 * bi_ + l16][16 * (bj + k) + 4 * quad]);
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
-                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(a[16 * bi_ + l16][16 * (bj + k) + 4 * quad + s],
-                                                               x[16 * (bj + k) + 4 * quad + s][16 * bj + l16], sum, 0, 0, 0);
+                    mm = __builtin_amdgcn_mfma_f32_16x16x4f32(-ak[s], bk[s] * x[16 * (bj + k) + 4 * quad + s][16 * bj + l16], mm, 0, 0, 0);
+            }
+            const f32x4 bm = *reinterpret_cast<const f32x4 *>(&finite_beta[16 * bi_ + 4 * quad]) * mm;
+            const f32x4 wi = *reinterpret_cast<const f32x4 *>(&x[16 * bi_ + l16][16 * bi_ + 4 * quad]);
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                out = __builtin_amdgcn_mfma_f32_16x16x4f32(-x[16 * bi_ + l16][16 * bi_ + 4 * quad + s], sum[s], out, 0, 0, 0);
+            for (int s = 0; s < 4; ++s) mm = __builtin_amdgcn_mfma_f32_16x16x4f32(-wi[s], bm[s], mm, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[16 * bi_ + 4 * quad + r][16 * bj + l16] = out[r];
+            for (int r = 0; r < 4; ++r) x[16 * bi_ + 4 * quad + r][16 * bj + l16] = mm[r];
         }
         __syncthreads();
     }
-    // Its rows in three terms (backward: its columns), zeros above the diagonal's blocks
+    // -W in three terms, zeros above the diagonal's blocks: a thread has 16 values of a row
     {
-        const int row = BACK ? tid & 63 : tid >> 2, c0 = 16 * (BACK ? tid >> 6 : tid & 3);
-        float e[2][8];
+        const int r = tid >> 2, c0 = 16 * (tid & 3);
+        if (r < C / 2 && c0 >= C / 2) return;
+        const bool lost = r >= bad, below = r >> 4 >= c0 >> 4;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const int t = BACK ? c0 + k : row, j = BACK ? row : c0 + k;
-            float v = t >> 4 >= j >> 4 ? x[t][j] : 0.0f;
-            if (!BACK && t >= bad) v = __builtin_nanf("");
-            e[k / 8][k % 8] = v;
-        }
-        __bf16 *to = static_cast<__bf16 *>(p.tri) + (int64_t)id * 3 * C * C + row * C;
+        for (int k = 0; k < 4; ++k) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(&x[r][c0 + 4 * k]);
+            bf16x4 o[3];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            bf16x8 o[3];
-            split8<3>(e[k], o);
+            for (int e = 0; e < 4; ++e) {
+                __bf16 s[3];
+                split<3>(lost ? __builtin_nanf("") : below ? -v[e] : 0.0f, s);
 #pragma unroll
-            for (int n = 0; n < 3; ++n) {
-                *reinterpret_cast<bf16x4 *>(to + n * C * C + interleaved(c0 + 8 * k)) = __builtin_shufflevector(o[n], o[n], 0, 1, 2, 3);
-                *reinterpret_cast<bf16x4 *>(to + n * C * C + interleaved(c0 + 8 * k + 4)) = __builtin_shufflevector(o[n], o[n], 4, 5, 6, 7);
+                for (int n = 0; n < 3; ++n) o[n][e] = s[n];
             }
+#pragma unroll
+            for (int n = 0; n < 3; ++n) *reinterpret_cast<bf16x4 *>(to.w + n * TRIANGLE + triangle_at(r, interleaved(c0 + 4 * k))) = o[n];
         }
     }
 }
@@ -220,7 +224,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(false), ORD = NP, RT = C / 16, DT = 2 * KF;
+    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(), ORD = NP, RT = C / 16, DT = 2 * KF;
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
     typedef Mixed<NK, KF * 32> TK;
     const TK kt{smem}, qt{kt.at + TK::bytes / 2};
@@ -246,8 +250,8 @@ __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
         }
     const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);         // (a lane without a column: any that is there)
     ChunkRows<T, KF> kr, qr;
-    Square<3> tr;
-    Square<NP> mr;
+    Triangle<3> tr;
+    Triangle<NP> mr;
     f32x4 sr;
     ChunkColumn<T> v;
     auto load = [&](int i, auto full) __attribute__((always_inline)) {
@@ -255,9 +259,10 @@ __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
         const int m = min(C, len - i * C);
         kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
         qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
-        tr.load(p.tri, chunk);
-        mr.load(p.mix, chunk);
-        sr = reinterpret_cast<const f32x4 *>(p.scal + chunk * SCALAR_FLOATS)[tid % (SCALAR_FLOATS / 4)];
+        const Prepared from = prepared(p, chunk);
+        tr.load(from.w);
+        mr.load(from.mix);
+        sr = reinterpret_cast<const f32x4 *>(from.scal)[tid % (SCALAR_FLOATS / 4)];
     };
     auto load_v = [&](int i, auto full) __attribute__((always_inline)) {
         v.template load<full.value>(p.v, b, (int64_t)i * C, min(C, len - i * C), mine);
@@ -314,7 +319,7 @@ __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
                 for (int rt = 0; rt < RT; ++rt) qt.rows(rt, f, a[rt]);
                 multiply_rows<ORD>(Y, a, s);
             }
-            if (p.states) put_state<DT>(S, p.states + chunk * (p.Dk + C) * Dv + c, p.Dk, Dv, in);
+            if (p.states) put_state<DT>(S, p.states + chunk * p.prep_stride + PREPARED_FLOATS + c, p.Dk, Dv, in);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const f32x4 in_k = scalar(IN_K, rt);
@@ -322,15 +327,18 @@ __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
                 for (int r = 0; r < 4; ++r) X[rt][r] = fmaf(-in_k[r], X[rt][r], (float)v.v[rt][r]);
             }
             if constexpr (full.value) load_v(then, full);
-            finite(X);
 
             // d, u
             f32x4 D[RT], U[RT];
             bf16x8 x[2][3];
 #pragma unroll
-            for (int f = 0; f < 2; ++f) operand<3>(X[2 * f], X[2 * f + 1], x[f]);
+            for (int rt = 0; rt < RT; ++rt) {
+                D[rt] = X[rt];
+                X[rt] *= scalar(BETA, rt);
+            }
+            finite(X);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) D[rt] = f32x4{0, 0, 0, 0};
+            for (int f = 0; f < 2; ++f) operand<3>(X[2 * f], X[2 * f + 1], x[f]);
             {
                 bf16x8 a[RT][3];
 #pragma unroll
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
                     for (int r = 0; r < 4; ++r)
                         if (16 * rt + 4 * quad + r >= bad) D[rt][r] = __builtin_nanf("");
             if (p.states) {
-                put_state<RT>(D, p.states + (chunk * (p.Dk + C) + p.Dk) * Dv + c, C, Dv, in);
+                put_state<RT>(D, p.states + chunk * p.prep_stride + PREPARED_FLOATS + p.Dk * Dv + c, C, Dv, in);
             }
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) U[rt] = D[rt] * scalar(BETA, rt);
@@ -526,19 +534,20 @@ __global__ __launch_bounds__(NT) void merit_delta_token(DeltaParams p, int lanes
     }
 }
 
-template <typename T, int KF, bool BACK> hipError_t prepare_of(const DeltaParams &p, hipStream_t s)
+template <typename T, int KF> hipError_t prepare_of(const DeltaParams &p, hipStream_t s)
 {
     const unsigned grid = (unsigned)(p.B * p.n * p.H);
     if (grid == 0) return hipSuccess;
-    if (p.wide_qk) merit_delta_prepare<T, KF, BACK, true><<<grid, NT, 0, s>>>(p);
-    else merit_delta_prepare<T, KF, BACK, false><<<grid, NT, 0, s>>>(p);
+    if (p.wide_qk) merit_delta_prepare<T, KF, true><<<grid, NT, 0, s>>>(p);
+    else merit_delta_prepare<T, KF, false><<<grid, NT, 0, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int KF> hipError_t forward_of(DeltaParams p, hipStream_t s)
 {
-    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + Mixed<3, C>::bytes + Mixed<mix_terms<T>(false), C>::bytes + SCALAR_FLOATS * 4;
+    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + Mixed<3, C>::bytes + Mixed<mix_terms<T>(), C>::bytes + SCALAR_FLOATS * 4;
     static_assert(lds <= 160 * 1024, "");
-    if (hipError_t e = prepare_of<T, KF, false>(p, s)) return e;
+    p.mix_terms = p.states ? 3 : mix_terms<T>();
+    if (hipError_t e = prepare_of<T, KF>(p, s)) return e;
     p.slices = (p.Dv + 63) / 64;
     const unsigned grid = (unsigned)(p.B * p.H * p.slices);
     if (p.wide_qk) merit_delta_chunks<T, KF, true><<<grid, NT, lds, s>>>(p);

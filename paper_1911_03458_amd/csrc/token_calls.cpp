@@ -41,7 +41,7 @@ struct Operand {
     Kind kind;
     Role role;
     int n, lead;
-    int64_t shape[5];
+    int64_t shape[4];
     at::IntArrayRef ref() const { return at::IntArrayRef(shape, static_cast<size_t>(n)); }
 };
 struct Spec {
@@ -76,7 +76,7 @@ bool read_spec(PyObject *const *args, Spec *s)
         o.kind = static_cast<Kind>(kind);
         o.role = static_cast<Role>(role);
         o.lead = lead;
-        if (PyTuple_GET_SIZE(shape) > 5 || lead > 2) return false;
+        if (PyTuple_GET_SIZE(shape) > 4 || lead > 2) return false;
         o.n = static_cast<int>(PyTuple_GET_SIZE(shape));
         for (int k = 0; k < o.n; ++k) o.shape[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, k));
         if (PyErr_Occurred()) return false;

@@ -16,36 +16,25 @@ Rows rows_of(Views &v, const merit_view &view, int type, bool required)
 }
 
 // ---- gated delta rule ------------------------------------------------------------------------
-// Scratch memory, in the order of its parts; every part is a multiple of 16 bytes but the last
+// Floats that the forward pass keeps of a chunk of a head
+int64_t delta_kept(const DeltaParams &p) { return cdiv(DELTA_PREPARED_FLOATS + (int64_t)(p.Dk + MERIT_DELTA_CHUNK) * p.Dv, 4) * 4; }
+// Scratch memory.  Forward: what the chunks' tokens do to each other (a call that keeps states has it there instead).  Backward: x, the
+// gradients of the states, and the value heads' parts of dq and dk; each a multiple of 16 bytes but the last.
 struct DeltaScratch {
-    int64_t scal, tri, mix, dx, ds, part, bytes;
+    int64_t dx, ds, part, bytes;
 };
 DeltaScratch delta_scratch(const DeltaParams &p, bool backward)
 {
-    constexpr int64_t square = (int64_t)MERIT_DELTA_CHUNK * MERIT_DELTA_CHUNK * 2;
     const int64_t chunks = p.B * p.n * p.H;
     DeltaScratch s = {};
-    s.tri = chunks * DELTA_SCALAR_FLOATS * 4;
-    s.mix = s.tri + chunks * 3 * square;
-    s.dx = s.mix + chunks * (backward || p.type == MERIT_F32 ? 3 : 2) * square;
-    s.bytes = s.dx;
-    if (!backward) return s;
+    if (!backward) {
+        s.bytes = chunks * DELTA_PREPARED_FLOATS * 4;
+        return s;
+    }
     s.ds = s.dx + chunks * MERIT_DELTA_CHUNK * p.Dv * 4;
-    s.part = s.ds + chunks * ((int64_t)p.Dk * p.Dv * 4 + 15) / 16 * 16;
+    s.part = s.ds + (chunks * p.Dk * p.Dv * 4 + 15) / 16 * 16;
     s.bytes = s.part + (p.each > 1 ? 2 * p.B * p.L * p.H * p.Dk * 4 : 0);
     return s;
-}
-void delta_use(DeltaParams &p, void *workspace, bool backward)
-{
-    const DeltaScratch s = delta_scratch(p, backward);
-    char *at = static_cast<char *>(workspace);
-    p.scal = reinterpret_cast<float *>(at + s.scal);
-    p.tri = at + s.tri;
-    p.mix = at + s.mix;
-    if (!backward) return;
-    p.dx = reinterpret_cast<float *>(at + s.dx);
-    p.ds = reinterpret_cast<float *>(at + s.ds);
-    p.part = p.each > 1 ? reinterpret_cast<float *>(at + s.part) : nullptr;
 }
 void delta_gates(Views &v, DeltaParams &p, const merit_view &g, const merit_view &beta)
 {
@@ -122,8 +111,8 @@ merit_status mixer_kernel(const merit_token_plan *plan, merit_pass pass, const c
     else
         *name = pass == MERIT_PASS_STEP   ? "merit_delta_token"
                 : !backward               ? "merit_delta_prepare+merit_delta_chunks"
-                : plan->delta.each > 1    ? "merit_delta_prepare+merit_delta_back_chunks+merit_delta_grads+merit_delta_sum_heads"
-                                          : "merit_delta_prepare+merit_delta_back_chunks+merit_delta_grads";
+                : plan->delta.each > 1    ? "merit_delta_back_chunks+merit_delta_grads+merit_delta_sum_heads"
+                                          : "merit_delta_back_chunks+merit_delta_grads";
     return MERIT_OK;
 }
 
@@ -144,7 +133,7 @@ merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64
         return MERIT_ERR_UNSUPPORTED;
     const int64_t n = cdiv(L, MERIT_DELTA_CHUNK);
     // workgroups of every pass, at the narrowest tiles and up to 512 threads a chunk; the sum over heads, a thread a value; states of all chunks
-    if (B > MAX_BLOCKS / heads || B * heads * (2 * n > cdiv(Dv, 16) ? 2 * n : cdiv(Dv, 16)) >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + 64) * Dv) ||
+    if (B > MAX_BLOCKS / heads || B * heads * (2 * n > cdiv(Dv, 16) ? 2 * n : cdiv(Dv, 16)) >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + MERIT_DELTA_CHUNK) * Dv + MERIT_DELTA_KEPT) ||
         (L > 0 && B > MAX_BLOCKS / L * 256 / (key_heads * Dk)))
         return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(DELTA, type);
@@ -206,9 +195,11 @@ merit_status merit_delta_rule(const merit_token_plan *plan, const merit_delta_ru
     p.h_last = v.f32(a->h_last);
     p.states = v.f32(a->states);
     if (v.st != MERIT_OK) return v.st;
+    if (p.states && reinterpret_cast<uintptr_t>(p.states) % 16 != 0) return MERIT_ERR_ALIGNMENT;
     const merit_status st = scratch(delta_scratch(p, false).bytes, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
-    delta_use(p, workspace, false);
+    p.prep = p.states ? p.states : static_cast<float *>(workspace);
+    p.prep_stride = p.states ? delta_kept(p) : DELTA_PREPARED_FLOATS;
     p.wide_qk = p.Dk % 8 == 0 && in_16_bytes(p.q, p.B, p.L, p.type) && in_16_bytes(p.k, p.B, p.L, p.type);
     return done(launch_delta(p, static_cast<hipStream_t>(stream)));
 }
@@ -236,12 +227,19 @@ merit_status merit_delta_rule_backward(const merit_token_plan *plan, const merit
     p.dbeta = rows_of(v, a->dbeta, MERIT_F32, some);
     p.dh0 = v.f32(a->dh0);
     if (v.st != MERIT_OK) return v.st;
-    const merit_status st = scratch(delta_scratch(p, true).bytes, workspace, workspace_bytes);
+    if (some && reinterpret_cast<uintptr_t>(p.states) % 16 != 0) return MERIT_ERR_ALIGNMENT;
+    const DeltaScratch at = delta_scratch(p, true);
+    const merit_status st = scratch(at.bytes, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
-    delta_use(p, workspace, true);
+    char *const base = static_cast<char *>(workspace);
+    p.dx = reinterpret_cast<float *>(base + at.dx);
+    p.ds = reinterpret_cast<float *>(base + at.ds);
+    p.part = p.each > 1 ? reinterpret_cast<float *>(base + at.part) : nullptr;
+    p.prep = p.states;
+    p.prep_stride = delta_kept(p);
     p.wide_qk = p.Dk % 8 == 0 && in_16_bytes(p.q, p.B, p.L, p.type) && in_16_bytes(p.k, p.B, p.L, p.type);
     p.wide_out = p.Dk % 8 == 0 && in_16_bytes(p.dq, p.B, p.L, p.type) && in_16_bytes(p.dk, p.B, p.L, p.type);
-    p.wide_v = p.Dv % 8 == 0 && in_16_bytes(p.dy, p.B, p.L, p.type) && address_16(p.states);
+    p.wide_v = p.Dv % 8 == 0 && in_16_bytes(p.dy, p.B, p.L, p.type);
     return done(launch_delta_backward(p, static_cast<hipStream_t>(stream)));
 }
 

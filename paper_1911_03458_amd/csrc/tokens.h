@@ -112,12 +112,15 @@ struct DeltaParams {
     const float *h0, *dh_last;
     float *h_last, *states, *dh0;
     const int32_t *lens;
-    void *tri, *mix;       // workspace: a chunk's two triangular matrices, in terms
-    float *scal;           // factors of its tokens
+    float *prep;           // what merit_delta_prepare leaves of a chunk of a head (in scratch memory, or kept with its state),
+    int64_t prep_stride;   // floats from one to the next
+    int mix_terms;         // terms of P to leave
     float *dx, *ds;        // backward: x of its tokens, the gradient of the state behind it
     float *part;           // dq, dk of a value head, where value heads share keys
 };
 constexpr int DELTA_SCALAR_FLOATS = 8 * MERIT_DELTA_CHUNK;
+constexpr int DELTA_PREPARED_FLOATS = DELTA_SCALAR_FLOATS + 2 * 3 * (MERIT_DELTA_CHUNK * MERIT_DELTA_CHUNK * 3 / 4) / 2;
+static_assert(DELTA_PREPARED_FLOATS == MERIT_DELTA_KEPT, "");
 
 // ---- the norms before and after a block ------------------------------------------------
 struct BlockNormParams {

@@ -10,6 +10,7 @@ from .tokens import MERIT_ACT_NONE, TokenPlan, _binding, _bits, _call, _F32, _I3
 MERIT_ACT_SIGMOID = 3                   # the gate of merit_block_norm only
 MERIT_DELTA_MAX_KEYS = 128
 MERIT_DELTA_CHUNK = 64
+MERIT_DELTA_KEPT = 9728
 MERIT_BLOCK_NORM_MAX_CHANNELS = 16384
 
 _ENTRIES = ("merit_delta_rule", "merit_delta_rule_backward", "merit_delta_rule_step", "merit_block_norm", "merit_block_norm_backward")
@@ -37,7 +38,7 @@ def merit_plan_delta_rule(dtype, B, L, heads, key_heads, Dk, Dv, *, scale=None, 
     b._check(b.lib().merit_plan_delta_rule(dtype, B, L, heads, key_heads, Dk, Dv, scale, int(bool(normalize)), ctypes.byref(h)),
              "merit_plan_delta_rule")
     qk, v, gate, state = (B, L, key_heads, Dk), (B, L, heads, Dv), (B, L, heads), (B, heads, Dk, Dv)
-    kept = (B, -(-L // MERIT_DELTA_CHUNK), heads, Dk + MERIT_DELTA_CHUNK, Dv)
+    kept = (B, -(-L // MERIT_DELTA_CHUNK), heads, -(-(MERIT_DELTA_KEPT + (Dk + MERIT_DELTA_CHUNK) * Dv) // 4) * 4)
     qk1, v1, gate1 = (B, key_heads, Dk), (B, heads, Dv), (B, heads)
     return TokenPlan(h, dtype, {
         "merit_delta_rule": (0, [("q", _T, qk, 2, "in"), ("k", _T, qk, 2, "in"), ("v", _T, v, 2, "in"), ("g", _F32, gate, 2, "opt"),

@@ -257,7 +257,7 @@ def test_empty(mb):
     q, v, s = torch.empty(2, 0, 1, 8, device=DEV), torch.empty(2, 0, 2, 12, device=DEV), torch.empty(2, 0, 2, device=DEV)
     h0 = g.normal(2, 2, 8, 12)
     y, h, st = mb.merit_delta_rule(plan, q, q, v, s, s, h0=h0, final=True, states=True)
-    assert y.shape == (2, 0, 2, 12) and torch.equal(h, h0) and st.shape == (2, 0, 2, 72, 12)
+    assert y.shape == (2, 0, 2, 12) and torch.equal(h, h0) and st.shape[:3] == (2, 0, 2)
     d = mb.merit_delta_rule_backward(plan, v, q, q, s, s, st, dh_last=h0, dh0=True)
     assert torch.equal(d["dh0"], h0)
     plan = _plan(mb, (0, 5, 2, 1, 8, 12), "f32")

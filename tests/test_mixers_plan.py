@@ -115,8 +115,8 @@ def test_scratch_and_kernels():
     plan = mb.merit_plan_delta_rule(mb.MERIT_BF16, 2, 130, 4, 2, 64, 64)
     assert plan.workspace(1) > plan.workspace(0) > 0 and plan.workspace(2) == 0
     assert plan.kernel() == "merit_delta_prepare+merit_delta_chunks"
-    assert plan.kernel(mb.MERIT_PASS_BACKWARD).endswith("merit_delta_grads+merit_delta_sum_heads")
     assert plan.kernel(mb.MERIT_PASS_STEP) == "merit_delta_token"
+    assert plan.kernel(mb.MERIT_PASS_BACKWARD) == "merit_delta_back_chunks+merit_delta_grads+merit_delta_sum_heads"
     assert mb.merit_plan_delta_rule(mb.MERIT_BF16, 2, 0, 4, 2, 64, 64).workspace(1) == 0
     norm = mb.merit_plan_block_norm(mb.MERIT_BF16, 2, 130, 64)
     assert norm.workspace(0) == 0 and norm.workspace(1) > 0
