@@ -49,14 +49,35 @@ template <int N> __device__ __forceinline__ void split(float x, __bf16 (&o)[N])
         o[i] = (__bf16)x;
     }
 }
+// Eight values side by side.  Three terms of 8 bits each, cut off instead of rounded, are the value itself (24 bits), and take no
+// conversions; of fewer the last is rounded.
 template <int N> __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&o)[N])
 {
+    if constexpr (N == 3) {
+        unsigned w[3][4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        __bf16 t[N];
-        split<N>(x[e], t);
+        for (int e = 0; e < 8; e += 2) {
+            float a = x[e], b = x[e + 1];
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i][e] = t[i];
+            for (int i = 0; i < 3; ++i) {
+                const unsigned ua = __builtin_bit_cast(unsigned, a), ub = __builtin_bit_cast(unsigned, b);
+                w[i][e / 2] = __builtin_amdgcn_perm(ub, ua, 0x07060302);       // the upper halves of both
+                if (i < 2) {
+                    a -= __builtin_bit_cast(float, ua & 0xFFFF0000u);
+                    b -= __builtin_bit_cast(float, ub & 0xFFFF0000u);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) __builtin_memcpy(&o[i], w[i], 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            __bf16 t[N];
+            split<N>(x[e], t);
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i][e] = t[i];
+        }
     }
 }
 
@@ -215,79 +236,98 @@ template <int PLANES, int ROWS, int COLS> struct Tile {
     }
 };
 
-// The same with every 32 columns in the order in which two results of 16 x 16, one under the other, lie in a lane: 8 values side by
-// side are 4 q .. 4 q + 3 of the first 16 and of the second.  A product then takes results as they come out of other products
-// (`operand`): what a wavefront computes for its columns never leaves its registers.
-__device__ __forceinline__ int interleaved(int c) { return (c & ~31) + 8 * ((c & 15) >> 2) + 4 * ((c >> 4) & 1) + (c & 3); }
-template <int PLANES, int COLS> struct Mixed {
-    static constexpr int pitch = COLS + 8;
-    static constexpr int plane = C * pitch;
-    static constexpr int bytes = PLANES * plane * 2;
+// Products of chunks.  Row i of a result of 16 x 16 stands for token (or key value) 32 h + 8 (i / 4) + 4 s + i % 4: of two results, s = 0
+// and 1, a lane then has eight that follow each other, which is how it has to have them for a sum along them (`operand`).  What a
+// wavefront computes for its columns so goes from product to product in its registers; the other operands' rows are read in that
+// order from LDS, where they lie as in memory.
+__device__ __forceinline__ int row_of(int half, int sub) { const int i = threadIdx.x & 15; return 32 * half + 8 * (i >> 2) + 4 * sub + (i & 3); }
+
+// Two results of 16 x 16 as an operand whose sum runs down their rows
+template <int N> __device__ __forceinline__ void operand(const f32x4 &s0, const f32x4 &s1, bf16x8 (&o)[N])
+{
+    const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+    split8<N>(x, o);
+}
+// A transposing read takes four rows of 16 columns from 16 lanes, each of which names 8 bytes (row i / 4, columns 4 (i % 4) ..), and leaves
+// lane i the i-th column.
+__device__ __forceinline__ bf16x8 transposed(const __bf16 *lo, const __bf16 *hi)
+{
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) short4v *lds4;
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)lo), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)hi);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A chunk's keys or queries in LDS
+template <int PLANES, int COLS> struct Keys {
+    static constexpr int pitch = COLS + 8, plane = C * pitch, bytes = PLANES * plane * 2;
     __bf16 *at;
 
-    // Sums along the rows: lane l has row 16 rt + l % 16 and the 32 columns of f
-    __device__ __forceinline__ void rows(int rt, int f, bf16x8 (&o)[PLANES]) const
+    // tokens of (half, sub), the 32 columns of f
+    __device__ __forceinline__ void rows(int half, int sub, int f, bf16x8 (&o)[PLANES]) const
     {
-        const int lane = threadIdx.x & 63;
-        const __bf16 *p = at + (16 * rt + (lane & 15)) * pitch + 32 * f + 8 * (lane >> 4);
+        const __bf16 *p = at + row_of(half, sub) * pitch + 32 * f + 8 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
         for (int i = 0; i < PLANES; ++i) o[i] = *reinterpret_cast<const bf16x8 *>(p + i * plane);
     }
-    // Sums down the columns: lane l has column 16 ct + l % 16 and the 32 rows of f, in results' order.  A transposing read takes
-    // four rows of 16 columns from 16 lanes, each of which names 8 bytes, and leaves lane i the i-th column.
-    __device__ __forceinline__ void cols(int f, int ct, bf16x8 (&o)[PLANES]) const
+    // columns of (f, sub), the 32 tokens of `half`
+    __device__ __forceinline__ void cols(int f, int sub, int half, bf16x8 (&o)[PLANES]) const
     {
-        typedef short short4v __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) short4v *lds4;
         const int lane = threadIdx.x & 63;
-        const __bf16 *p = at + (32 * f + 4 * (lane >> 4) + ((lane & 15) >> 2)) * pitch + 32 * (ct >> 1) + 8 * (lane & 3) + 4 * (ct & 1);
+        const __bf16 *p = at + (32 * half + 8 * (lane >> 4) + ((lane & 15) >> 2)) * pitch + 32 * f + 8 * (lane & 3) + 4 * sub;
 #pragma unroll
-        for (int i = 0; i < PLANES; ++i) {
-            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + i * plane));
-            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + i * plane + 16 * pitch));
-            o[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
+        for (int i = 0; i < PLANES; ++i) o[i] = transposed(p + i * plane, p + i * plane + 4 * pitch);
     }
-    // Columns c .. c + 7 of a row
     __device__ __forceinline__ void put8(int r, int c, const bf16x8 (&o)[PLANES]) const
     {
-        __bf16 *p = at + r * pitch + interleaved(c);
 #pragma unroll
-        for (int i = 0; i < PLANES; ++i) {
-            *reinterpret_cast<bf16x4 *>(p + i * plane) = __builtin_shufflevector(o[i], o[i], 0, 1, 2, 3);
-            *reinterpret_cast<bf16x4 *>(p + i * plane + 8) = __builtin_shufflevector(o[i], o[i], 4, 5, 6, 7);
-        }
+        for (int i = 0; i < PLANES; ++i) *reinterpret_cast<bf16x8 *>(at + i * plane + r * pitch + c) = o[i];
     }
 };
-// Two results of 16 x 16, one under the other, as an operand whose sum runs down their rows
-template <int N> __device__ __forceinline__ void operand(const f32x4 &top, const f32x4 &bottom, bf16x8 (&o)[N])
-{
-    const float x[8] = {top[0], top[1], top[2], top[3], bottom[0], bottom[1], bottom[2], bottom[3]};
-    split8<N>(x, o);
-}
 
-// A triangular matrix of C x C in terms, as merit_delta_prepare leaves it: its columns interleaved, of the upper half of its rows the
-// left half.
+// A triangular matrix of C x C: of the upper half of its rows the left half
 __device__ __forceinline__ int triangle_at(int t, int c) { return t < C / 2 ? t * (C / 2) + c : C * C / 4 + (t - C / 2) * C + c; }
 constexpr int TRIANGLE = C * C * 3 / 4;
-// The first PLANES of its terms on their way into LDS
+// in LDS
 template <int PLANES> struct Triangle {
-    static constexpr int per = TRIANGLE / 8, all = PLANES * per, units = (all + NT - 1) / NT;
+    static constexpr int upper = C / 2 + 8, lower = C + 8, plane = C / 2 * (upper + lower), bytes = PLANES * plane * 2;
+    __bf16 *at;
+
+    static __device__ __forceinline__ int line(int half, int r) { return half ? C / 2 * upper + r * lower : r * upper; }
+    // tokens of (half, sub), the 32 columns of f (not the right half of the upper rows)
+    __device__ __forceinline__ void rows(int half, int sub, int f, bf16x8 (&o)[PLANES]) const
+    {
+        const __bf16 *p = at + line(half, row_of(0, sub)) + 32 * f + 8 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i) o[i] = *reinterpret_cast<const bf16x8 *>(p + i * plane);
+    }
+    // columns of (f, sub), the 32 rows of `half`
+    __device__ __forceinline__ void cols(int f, int sub, int half, bf16x8 (&o)[PLANES]) const
+    {
+        const int lane = threadIdx.x & 63, r = 8 * (lane >> 4) + ((lane & 15) >> 2);
+        const __bf16 *p = at + line(half, r) + 32 * f + 8 * (lane & 3) + 4 * sub;
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i) o[i] = transposed(p + i * plane, p + i * plane + 4 * (half ? lower : upper));
+    }
+};
+// and its first PLANES terms on their way there, from where merit_delta_prepare leaves them
+template <int PLANES, int THREADS> struct TriangleRows {
+    static constexpr int per = TRIANGLE / 8, all = PLANES * per, units = (all + THREADS - 1) / THREADS;
     bf16x8 e[units];
     __device__ __forceinline__ void load(const __bf16 *from)
     {
 #pragma unroll
         for (int i = 0; i < units; ++i) {
-            const int u = (int)threadIdx.x + i * NT;
+            const int u = (int)(threadIdx.x % THREADS) + i * THREADS;
             e[i] = reinterpret_cast<const bf16x8 *>(from)[u < all ? u : all - 1];
         }
     }
-    __device__ __forceinline__ void store(const Mixed<PLANES, C> &t) const
+    __device__ __forceinline__ void store(const Triangle<PLANES> &t) const
     {
 #pragma unroll
         for (int i = 0; i < units; ++i) {
-            const int u = (int)threadIdx.x + i * NT, v = u % per, w = v - per / 3;
-            const int at = v < per / 3 ? (v >> 2) * t.pitch + (v & 3) * 8 : (C / 2 + (w >> 3)) * t.pitch + (w & 7) * 8;
+            const int u = (int)(threadIdx.x % THREADS) + i * THREADS, v = u % per, w = v - per / 3;
+            const int at = v < per / 3 ? t.line(0, v >> 2) + (v & 3) * 8 : t.line(1, w >> 3) + (w & 7) * 8;
             if (u < all) *reinterpret_cast<bf16x8 *>(t.at + u / per * t.plane + at) = e[i];
         }
     }
@@ -309,42 +349,50 @@ __device__ __forceinline__ Prepared prepared(const DeltaParams &p, int64_t chunk
     return r;
 }
 
-// Eight values of a row of n, from column c on, zeros from column n on; nothing stands in a branch, so that loads of many rows go out
-// together.  WIDE: rows start on 16 bytes and n is a multiple of 8.
+// Eight values of a row of n, from column c on.  Nothing stands in a branch, so that loads of many rows go out together, and what is read
+// in the place of values that are not there is not looked at before `keep8` makes zeros of it, where the values are used: a select
+// right behind a load waits for it.  WIDE: rows start on 16 bytes and n is a multiple of 8.
 template <bool WIDE, typename T> __device__ __forceinline__ Eight<T> take8(const T *row, int c, int n)
 {
     Eight<T> r;
     if constexpr (WIDE) {
         const u32x4 *from = reinterpret_cast<const u32x4 *>(row + (c < n ? c : 0));
         if constexpr (sizeof(T) == 2) {
-            u32x4 a = from[0];
-            if (c >= n) a = u32x4{0, 0, 0, 0};
-            r.v = __builtin_bit_cast(typename Eight<T>::vec, a);
+            r.v = __builtin_bit_cast(typename Eight<T>::vec, from[0]);
         } else {
-            u32x4 a = from[0], b = from[1];
-            if (c >= n) a = b = u32x4{0, 0, 0, 0};
+            const u32x4 a = from[0], b = from[1];
             r.v = __builtin_bit_cast(typename Eight<T>::vec, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const T x = row[max(min(c + e, n - 1), 0)];        // (n may be 0: a row of zeros, of which the first value is there)
-            r.v[e] = c + e < n ? x : (T)0.0f;
-        }
+        for (int e = 0; e < 8; ++e) r.v[e] = row[max(min(c + e, n - 1), 0)];       // (n may be 0: the row's first value is there)
+    }
+    return r;
+}
+template <bool WIDE, typename T> __device__ __forceinline__ Eight<T> keep8(const Eight<T> &x, int c, int n)
+{
+    Eight<T> r = zero8<T>();
+    if constexpr (WIDE) {
+        if (c < n) r = x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < n) r.v[e] = x.v[e];
     }
     return r;
 }
 
-// A chunk's rows of q or k: unit u of a thread is row u / (KF * 4) of the tile and eight columns.  FULL: all C rows are there, else m,
-// at least one, the others zeros.
-template <typename T, int KF> struct ChunkRows {
-    static constexpr int units = C * KF * 4 / NT, step = NT / (KF * 4);
+// A chunk's rows of q or k: unit u of a thread is row u / (KF * 4) of the tile and eight columns (with more threads than units some have
+// the same).  FULL: all C rows are there, else m, at least one, the others zeros.
+template <typename T, int KF, int THREADS> struct ChunkRows {
+    static constexpr int all = C * KF * 4, units = (all + THREADS - 1) / THREADS, step = THREADS / (KF * 4);
     Eight<T> e[units];
 
+    static __device__ __forceinline__ int unit() { return (int)(threadIdx.x % THREADS) % all; }
     template <bool FULL, bool WIDE>
     __device__ __forceinline__ void load(const Rows &x, int64_t b, int64_t t0, int m, int head, int D)
     {
-        const int r0 = (int)threadIdx.x / (KF * 4), c = (int)threadIdx.x % (KF * 4) * 8;
+        const int r0 = unit() / (KF * 4), c = unit() % (KF * 4) * 8;
         const T *from = static_cast<const T *>(x.data) + b * x.s0 + t0 * x.s1 + (int64_t)head * D;
         const T *row = from + r0 * x.s1;
 #pragma unroll
@@ -352,79 +400,93 @@ template <typename T, int KF> struct ChunkRows {
             if constexpr (FULL) {
                 e[i] = take8<WIDE, T>(row + i * step * x.s1, c, D);
             } else {
-                const int r = r0 + i * step;
-                e[i] = take8<WIDE, T>(from + min(r, m - 1) * x.s1, c, r < m ? D : 0);
+                e[i] = take8<WIDE, T>(from + min(r0 + i * step, m - 1) * x.s1, c, D);
             }
         }
     }
-    template <typename M> __device__ __forceinline__ void store(const M &t) const
+    // (zeros in the place of what is not there)
+    template <bool FULL, bool WIDE> __device__ __forceinline__ Eight<T> value(int i, int m, int D) const
+    {
+        const int r = unit() / (KF * 4) + i * step, c = unit() % (KF * 4) * 8;
+        return keep8<WIDE, T>(e[i], c, FULL || r < m ? D : 0);
+    }
+    template <bool FULL, bool WIDE, typename M> __device__ __forceinline__ void store(const M &t, int m, int D) const
     {
 #pragma unroll
         for (int i = 0; i < units; ++i) {
-            const int u = (int)threadIdx.x + i * NT;
             bf16x8 o[Terms<T>::n];
-            terms8<T>(e[i], o);
-            t.put8(u / (KF * 4), u % (KF * 4) * 8, o);
+            terms8<T>(value<FULL, WIDE>(i, m, D), o);
+            t.put8(unit() / (KF * 4) + i * step, unit() % (KF * 4) * 8, o);
         }
     }
 };
 
-// A lane's sixteen values of a column of v or dy, in the order of four results one under the other
-template <typename T> struct ChunkColumn {
-    T v[C / 16][4];
+// A lane's values of a column of v or dy: N halves of a chunk from `half` on (each two results, sub 0 and 1, of four rows).  16-bit
+// values stay as they were loaded, each in a register: putting two into one would wait for them.
+template <typename T, int N> struct ChunkColumn {
+    typedef typename std::conditional<sizeof(T) == 2, uint16_t, float>::type M;
+    typedef typename std::conditional<sizeof(T) == 2, uint32_t, float>::type Word;
+    Word v[2 * N][4];
 
     // `c`: a column that is there
-    template <bool FULL> __device__ __forceinline__ void load(const Rows &x, int64_t b, int64_t t0, int m, int64_t c)
+    template <bool FULL> __device__ __forceinline__ void load(const Rows &x, int64_t b, int64_t t0, int half, int m, int64_t c)
     {
-        const int quad = (threadIdx.x & 63) >> 4;
-        const T *from = static_cast<const T *>(x.data) + b * x.s0 + t0 * x.s1 + c, *row = from + 4 * quad * x.s1;
+        const int r0 = 32 * half + 8 * ((threadIdx.x & 63) >> 4);
+        const M *from = static_cast<const M *>(x.data) + b * x.s0 + t0 * x.s1 + c, *row = from + r0 * x.s1;
 #pragma unroll
-        for (int rt = 0; rt < C / 16; ++rt)
+        for (int k = 0; k < 2 * N; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
+                const int t = 32 * (k >> 1) + 4 * (k & 1) + r;
                 if constexpr (FULL) {
-                    v[rt][r] = row[(16 * rt + r) * x.s1];
+                    v[k][r] = row[t * x.s1];
                 } else {
-                    const int t = 16 * rt + 4 * quad + r;
-                    const T f = from[min(t, m - 1) * x.s1];
-                    v[rt][r] = t < m ? f : (T)0.0f;
+                    const Word f = from[min(r0 + t, m - 1) * x.s1];
+                    v[k][r] = r0 + t < m ? f : (Word)0;
                 }
             }
     }
+    __device__ __forceinline__ float value(int k, int r) const
+    {
+        if constexpr (sizeof(T) == 4) return v[k][r];
+        else return (float)__builtin_bit_cast(T, (uint16_t)v[k][r]);
+    }
 };
-// Sixteen results to a column of `x`: tokens from m on are zeros, those from `there` on are not
+// The results of half a chunk to a column of `x`: tokens from m on are zeros, those from `there` on are not
 template <bool FULL, typename T>
-__device__ __forceinline__ void put_column(const f32x4 (&v)[C / 16], const Rows &x, int64_t b, int64_t t0, int m, int there, int64_t c, bool in)
+__device__ __forceinline__ void put_column(const f32x4 (&v)[2], const Rows &x, int64_t b, int64_t t0, int half, int m, int there, int64_t c, bool in)
 {
-    const int quad = (threadIdx.x & 63) >> 4;
-    T *row = static_cast<T *>(x.data) + b * x.s0 + (t0 + 4 * quad) * x.s1 + c;
+    const int r0 = 32 * half + 8 * ((threadIdx.x & 63) >> 4);
+    T *row = static_cast<T *>(x.data) + b * x.s0 + (t0 + r0) * x.s1 + c;
     if (in)
 #pragma unroll
-        for (int rt = 0; rt < C / 16; ++rt)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = 16 * rt + 4 * quad + r;
-                if (FULL || t < there) row[(16 * rt + r) * x.s1] = (T)(FULL || t < m ? v[rt][r] : 0.0f);
+                const int t = 4 * k + r;
+                if (FULL || r0 + t < there) row[t * x.s1] = (T)(FULL || r0 + t < m ? v[k][r] : 0.0f);
             }
 }
-// A wavefront's 16 columns of a state, rows of Dv
-template <int DT> __device__ __forceinline__ void put_state(const f32x4 (&S)[DT], float *out, int Dk, int64_t Dv, bool in)
+// 32 rows of fp32, of which `there` are there, to a column of rows of Dv; and back
+__device__ __forceinline__ void put_rows(const f32x4 (&v)[2], float *out, int there, int64_t Dv, bool in)
 {
-    const int quad = (threadIdx.x & 63) >> 4;
-    float *row = out + 4 * quad * Dv;
+    const int r0 = 8 * ((threadIdx.x & 63) >> 4);
+    float *row = out + r0 * Dv;
     if (!in) return;
-    if (Dk == 16 * DT) {
+    if (there >= 32) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) row[(16 * d + r) * Dv] = S[d][r];
+        for (int t = 0; t < 8; ++t) row[t * Dv] = v[t >> 2][t & 3];
     } else {
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (16 * d + 4 * quad + r < Dk) row[(16 * d + r) * Dv] = S[d][r];
+        for (int t = 0; t < 8; ++t)
+            if (r0 + t < there) row[t * Dv] = v[t >> 2][t & 3];
     }
+}
+__device__ __forceinline__ void get_rows(f32x4 (&v)[2], const float *from, int there, int64_t Dv, bool in)
+{
+    const int r0 = 8 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t >> 2][t & 3] = from && in && r0 + t < there ? from[(r0 + t) * Dv] : 0.0f;
 }
 
 // What merit_delta_prepare leaves of a chunk of a head, 64 values each

@@ -13,177 +13,265 @@ namespace merit {
 namespace delta {
 
 // ---------------------------------------------------------------------------
-// one chunk after the other, from the last: a wavefront 16 columns of a head's Z
+// one chunk after the other, from the last: two wavefronts 16 columns of a head's Z
 // ---------------------------------------------------------------------------
-// Split as merit_delta_chunks is: a wavefront has its columns of Z and of all tokens in registers, LDS holds K, Q and the
-// triangular matrices, whose transposes come out of transposing reads.
-template <typename T, int KF, bool WIDE>
-__global__ __launch_bounds__(NT) void merit_delta_back_chunks(DeltaParams p)
+// Split as merit_delta_chunks is; here the second half's tokens come first.  The triangular matrices' transposes come out of transposing
+// reads.
+template <typename T, int KF> struct BackwardLds {
+    static constexpr int NK = Terms<T>::n;
+    static constexpr int k = 0, w = k + Keys<NK, KF * 32>::bytes, mix = w + Triangle<3>::bytes, scal = mix + Triangle<3>::bytes,
+                         q = scal + SCALAR_FLOATS * 4;
+    // handed over in a pair: 2 KB to each, b y of the second and then w of the first, w of the second
+    static constexpr bool shared = NK == 3 && KF == 4;
+    static constexpr int pair = (4 + 3 + 3) * 1024, hand = shared ? q : q + Keys<NK, KF * 32>::bytes;
+    static constexpr int bytes = hand + 4 * pair > q + Keys<NK, KF * 32>::bytes ? hand + 4 * pair : q + Keys<NK, KF * 32>::bytes;
+};
+// (a half at a time is compiled: every place in LDS is then a lane's base and a constant)
+template <typename T, int KF, bool WIDE, int half>
+__device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem)
 {
-    constexpr int NK = Terms<T>::n, RT = C / 16, DT = 2 * KF;
-    extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
-    typedef Mixed<NK, KF * 32> TK;
-    const TK kt{smem}, qt{kt.at + TK::bytes / 2};
-    const Mixed<3, C> tt{qt.at + TK::bytes / 2};
-    const Mixed<3, C> mt{tt.at + Mixed<3, C>::bytes / 2};
-    float *const sc = reinterpret_cast<float *>(mt.at + Mixed<3, C>::bytes / 2);
+    typedef BackwardLds<T, KF> L;
+    constexpr int NK = L::NK, KO = KF < 2 ? 1 : KF / 2;
+    char *const lds = reinterpret_cast<char *>(smem);
+    const Keys<NK, KF * 32> kt{reinterpret_cast<__bf16 *>(lds + L::k)}, qt{reinterpret_cast<__bf16 *>(lds + L::q)};
+    const Triangle<3> wt{reinterpret_cast<__bf16 *>(lds + L::w)}, mt{reinterpret_cast<__bf16 *>(lds + L::mix)};
+    float *const sc = reinterpret_cast<float *>(lds + L::scal);
 
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
     const int kh = (int)h / p.each, len = tokens_of(p, b), n = (len + C - 1) / C;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, tile = tid >> 6 & 3, l16 = lane & 15, quad = lane >> 4;
     const int64_t head = b * p.H + h, Dv = p.Dv;
-    const int c0 = (int)(id % (uint32_t)p.slices) * 64, c = c0 + 16 * wave + l16;
-    const bool busy = c0 + 16 * wave < Dv, in = c < Dv;
+    const int c0 = (int)(id % (uint32_t)p.slices) * p.width, c = c0 + 16 * tile + l16;
+    const bool busy = 16 * tile < p.width && c0 + 16 * tile < Dv, in = busy && c < Dv, has = half < KF;
+    f32x4 *const to_me = reinterpret_cast<f32x4 *>(lds + L::hand + tile * L::pair + half * 2048) + lane;
+    f32x4 *const to_other = reinterpret_cast<f32x4 *>(lds + L::hand + tile * L::pair + (1 - half) * 2048) + lane;
+    bf16x8 *const one = reinterpret_cast<bf16x8 *>(lds + L::hand + tile * L::pair + 4096) + lane;     // b y of the second, w of the first
+    bf16x8 *const two = one + 192;                                                                       // w of the second
 
-    f32x4 Z[DT];
+    f32x4 Z[KO][2];
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dk = 16 * d + 4 * quad + r;
-            Z[d][r] = p.dh_last && dk < p.Dk && in ? p.dh_last[(head * p.Dk + dk) * Dv + c] : 0.0f;
-        }
+    for (int o = 0; o < KO; ++o) {
+        const int dk = 32 * (half + 2 * o);
+        get_rows(Z[o], p.dh_last ? p.dh_last + (head * p.Dk + dk) * Dv + c : nullptr, p.Dk - dk, Dv, in);
+    }
     const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);
-    ChunkRows<T, KF> kr, qr;
-    Triangle<3> tr, mr;
+    // (the second half's wavefronts, which wait for the others later, move what the next chunk needs)
+    ChunkRows<T, KF, NT> kr, qr;
+    TriangleRows<3, NT> wr, mr;
     f32x4 sr;
-    ChunkColumn<T> dy;
+    ChunkColumn<T, 2> dy;
     auto load = [&](int i, auto full) __attribute__((always_inline)) {
-        const int64_t chunk = (b * p.n + i) * p.H + h;
         const int m = min(C, len - i * C);
         kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
         qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
-        const Prepared from = prepared(p, chunk);
-        tr.load(from.w);
+        const Prepared from = prepared(p, (b * p.n + i) * p.H + h);
+        wr.load(from.w);
         mr.load(from.mix);
         sr = reinterpret_cast<const f32x4 *>(from.scal)[tid % (SCALAR_FLOATS / 4)];
     };
     auto load_dy = [&](int i, auto full) __attribute__((always_inline)) {
-        dy.template load<full.value>(p.dy, b, (int64_t)i * C, min(C, len - i * C), mine);
+        dy.template load<full.value>(p.dy, b, (int64_t)i * C, 0, min(C, len - i * C), mine);
     };
-    auto scalar = [&](int which, int rt) __attribute__((always_inline)) {
-        return *reinterpret_cast<const f32x4 *>(sc + which * C + 16 * rt + 4 * quad);
+    auto scalar = [&](int which, int at, int sub) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4 *>(sc + which * C + 32 * at + 8 * quad + 4 * sub);
     };
-    // Z += (rows of keys)^T w
-    auto into_state = [&](const TK &t, const f32x4 (&w)[RT]) __attribute__((always_inline)) {
-        bf16x8 o[2][3];
+    // Z += (rows of keys)^T w over the tokens of half `f`
+    auto into_state = [&](const Keys<NK, KF * 32> &t, int f, const bf16x8 (&w)[3]) __attribute__((always_inline)) {
+        if (has)
 #pragma unroll
-        for (int f = 0; f < 2; ++f) operand<3>(w[2 * f], w[2 * f + 1], o[f]);
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int g = 0; g < DT / 2; ++g) {
+            for (int o = 0; o < KO; ++o) {
                 bf16x8 a[2][NK];
-                f32x4 two[2] = {Z[2 * g], Z[2 * g + 1]};
-                t.cols(f, 2 * g, a[0]);
-                t.cols(f, 2 * g + 1, a[1]);
-                multiply_rows<3>(two, a, o[f]);
-                Z[2 * g] = two[0];
-                Z[2 * g + 1] = two[1];
+                t.cols(half + 2 * o, 0, f, a[0]);
+                t.cols(half + 2 * o, 1, f, a[1]);
+                multiply_rows<3>(Z[o], a, w);
+                __builtin_amdgcn_sched_barrier(0);
             }
     };
 
-    // Chunk i; `full`: whole, and so is chunk `then`, whose operands go out here
+    // Chunk i; `full`: whole, and so is chunk `then`, whose operands go out on the way
     auto step = [&](int i, int then, auto full) __attribute__((always_inline)) {
         const int64_t t0 = (int64_t)i * C, chunk = (b * p.n + i) * p.H + h;
         const int m = min(C, len - i * C);
-        kr.store(kt);
-        qr.store(qt);
-        tr.store(tt);
-        mr.store(mt);
-        if (tid < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid] = sr;
+        if constexpr (half == 1) {
+            kr.template store<full.value, WIDE>(kt, m, p.Dk);
+            qr.template store<full.value, WIDE>(qt, m, p.Dk);
+            wr.store(wt);
+            mr.store(mt);
+            if (tid - NT < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid - NT] = sr;
+        }
         __syncthreads();
-        if constexpr (full.value) load(then, full);
-        if (busy) {
-            put_state<DT>(Z, p.ds + chunk * p.Dk * Dv + c, p.Dk, Dv, in);
-            // what reaches u: through the state behind the chunk, and through y
-            f32x4 U[RT], W[RT];
+
+        // K Z over the own rows: Y[0], [1] for the own tokens, [2], [3] for the other's
+        const f32x4 out_k[2] = {scalar(OUT_K, half, 0), scalar(OUT_K, half, 1)}, beta[2] = {scalar(BETA, half, 0), scalar(BETA, half, 1)};
+        f32x4 Y[4];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) U[rt] = f32x4{0, 0, 0, 0};
+        for (int k = 0; k < 4; ++k) Y[k] = f32x4{0, 0, 0, 0};
+        if (busy && has)
 #pragma unroll
-            for (int f = 0; f < KF; ++f) {
-                bf16x8 z[3], a[RT][NK];
-                operand<3>(Z[2 * f], Z[2 * f + 1], z);
+            for (int o = 0; o < KO; ++o) {
+                bf16x8 z[3], a[4][NK];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) kt.rows(rt, f, a[rt]);
-                multiply_rows<3>(U, a, z);
+                for (int k = 0; k < 4; ++k) kt.rows(half ^ (k >> 1), k & 1, half + 2 * o, a[k]);
+                operand<3>(Z[o][0], Z[o][1], z);
+                multiply_rows<3>(Y, a, z);
+                __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                U[rt] *= scalar(OUT_K, rt);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) W[rt][r] = (float)dy.v[rt][r];
-            }
-            if constexpr (full.value) load_dy(then, full);
-            {
-                bf16x8 y[2][NK], a[RT][3], au[2][3];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) operand<NK>(W[2 * f], W[2 * f + 1], y[f]);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) mt.cols(1, rt, a[rt]);
-                multiply_rows<3>(U, a, y[1]);
-                f32x4 upper[2] = {U[0], U[1]};
-                mt.cols(0, 0, au[0]);
-                mt.cols(0, 1, au[1]);
-                multiply_rows<3>(upper, au, y[0]);
-                U[0] = upper[0];
-                U[1] = upper[1];
-            }
+        // exp(G_C) Z + Q^T (i dy); what Z was goes to memory
+        auto fade = [&]() __attribute__((always_inline)) {
             const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) Z[d] *= whole;
+            for (int o = 0; o < KO; ++o) {
+                const int dk = 32 * (half + 2 * o);
+                if (has) put_rows(Z[o], p.ds + (chunk * p.Dk + dk) * Dv + c, p.Dk - dk, Dv, in);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) W[rt] *= scalar(IN_Q, rt);
-            into_state(qt, W);
-
-            f32x4 X[RT];
-            {
-                bf16x8 u[2][3], a[RT][3], au[2][3];
+                for (int k = 0; k < 2; ++k) Z[o][k] *= whole;
+            }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    X[rt] = U[rt];
-                    U[rt] *= scalar(BETA, rt);
-                    tt.cols(1, rt, a[rt]);
+            for (int f = 0; f < 2; ++f) {
+                f32x4 d[2];
+                bf16x8 w[3];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f32x4 in_q = scalar(IN_Q, f, k);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) d[k][r] = in_q[r] * dy.value(2 * f + k, r);
                 }
-#pragma unroll
-                for (int f = 0; f < 2; ++f) operand<3>(U[2 * f], U[2 * f + 1], u[f]);
-                multiply_rows<3>(X, a, u[1]);
-                f32x4 upper[2] = {X[0], X[1]};
-                tt.cols(0, 0, au[0]);
-                tt.cols(0, 1, au[1]);
-                multiply_rows<3>(upper, au, u[0]);
-                X[0] = upper[0];
-                X[1] = upper[1];
+                operand<3>(d[0], d[1], w);
+                into_state(qt, f, w);
             }
-            put_state<RT>(X, p.dx + chunk * C * Dv + c, C, Dv, in);
+            if constexpr (full.value) load_dy(then, full);
+        };
+        bf16x8 y[2][NK];
+        if (busy)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                X[rt] *= scalar(BETA, rt);
-                W[rt] = -scalar(IN_K, rt) * X[rt];
+            for (int f = 1 - half; f >= 0; --f) {       // (the second half's tokens, and for the first half its own)
+                f32x4 d[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) d[k][r] = dy.value(2 * (1 - f) + k, r);
+                operand<NK>(d[0], d[1], y[1 - f]);
             }
-            put_column<full.value, T>(X, p.dv, b, t0, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
-            into_state(kt, W);
+        if constexpr (L::shared) {
+            if (busy) fade();
+            __syncthreads();
+        }
+        if (busy) {
+            to_other[0] = Y[2];
+            to_other[64] = Y[3];
+        }
+        __syncthreads();
+
+        // x = y - W^T (b y): the second half's tokens at once, the first's part of their own
+        f32x4 X[2], U[2];
+        bf16x8 u[3], w[3];
+        auto outer = [&]() __attribute__((always_inline)) {
+            const f32x4 in_k[2] = {scalar(IN_K, half, 0), scalar(IN_K, half, 1)};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) U[k] = -in_k[k] * (beta[k] * X[k]);
+            operand<3>(U[0], U[1], w);
+        };
+        auto results = [&]() __attribute__((always_inline)) {
+            put_rows(X, p.dx + (chunk * C + 32 * half) * Dv + c, 32, Dv, in);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) X[k] *= beta[k];
+            put_column<full.value, T>(X, p.dv, b, t0, half, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
+        };
+        if (busy) {
+            bf16x8 a[2][3];
+            mt.cols(half, 0, 1, a[0]);
+            mt.cols(half, 1, 1, a[1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) X[k] = (Y[k] + to_me[64 * k]) * out_k[k];
+            multiply_rows<3>(X, a, y[1]);
+            if constexpr (half == 0) {
+                mt.cols(0, 0, 0, a[0]);
+                mt.cols(0, 1, 0, a[1]);
+                multiply_rows<3>(X, a, y[0]);
+            }
+            wt.cols(half, 0, half, a[0]);
+            wt.cols(half, 1, half, a[1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) U[k] = beta[k] * X[k];
+            operand<3>(U[0], U[1], u);
+            multiply_rows<3>(X, a, u);
+            if constexpr (half == 1) {
+                outer();
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    one[64 * k] = u[k];
+                    two[64 * k] = w[k];
+                }
+            } else if constexpr (!L::shared) {
+                fade();
+            }
+        }
+        __syncthreads();
+        if constexpr (half == 1) {
+            if constexpr (full.value) load(then, full);
+            if (busy) {
+                if constexpr (!L::shared) fade();
+                into_state(kt, 1, w);
+                results();
+            }
+        } else if (busy) {
+            bf16x8 u1[3], a[2][3];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) u1[k] = one[64 * k];
+            wt.cols(0, 0, 1, a[0]);
+            wt.cols(0, 1, 1, a[1]);
+            multiply_rows<3>(X, a, u1);
+            outer();
+#pragma unroll
+            for (int k = 0; k < 3; ++k) one[64 * k] = w[k];
+        }
+        __syncthreads();
+        if (busy) {
+            if constexpr (half == 1) {
+#pragma unroll
+                for (int k = 0; k < 3; ++k) w[k] = one[64 * k];
+                into_state(kt, 0, w);
+            } else {
+                bf16x8 w1[3];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) w1[k] = two[64 * k];
+                into_state(kt, 0, w);
+                into_state(kt, 1, w1);
+                results();
+            }
         }
         __syncthreads();
     };
     const int whole_chunks = len / C;
     if (whole_chunks < n) {
-        load(n - 1, std::false_type());
+        if constexpr (half == 1) load(n - 1, std::false_type());
         load_dy(n - 1, std::false_type());
         step(n - 1, n - 1, std::false_type());
     }
     if (whole_chunks > 0) {
-        load(whole_chunks - 1, std::true_type());
+        if constexpr (half == 1) load(whole_chunks - 1, std::true_type());
         load_dy(whole_chunks - 1, std::true_type());
         for (int i = whole_chunks - 1; i >= 0; --i) step(i, max(i - 1, 0), std::true_type());     // (the first one's again: no branch)
     }
-    if (p.dh0) put_state<DT>(Z, p.dh0 + head * p.Dk * Dv + c, p.Dk, Dv, in);
-    const int cols = min(64, (int)Dv - c0);
-    for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += NT) {
+    if (p.dh0 && has)
+#pragma unroll
+        for (int o = 0; o < KO; ++o) {
+            const int dk = 32 * (half + 2 * o);
+            put_rows(Z[o], p.dh0 + (head * p.Dk + dk) * Dv + c, p.Dk - dk, Dv, in);
+        }
+    const int cols = min(p.width, (int)Dv - c0);
+    for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += CHUNK_THREADS) {
         const int64_t t = (int64_t)n * C + u / cols;
         static_cast<T *>(p.dv.data)[b * p.dv.s0 + t * p.dv.s1 + h * Dv + c0 + u % cols] = (T)0.0f;
     }
+}
+template <typename T, int KF, bool WIDE>
+__global__ __launch_bounds__(CHUNK_THREADS, 2) void merit_delta_back_chunks(DeltaParams p)
+{
+    extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) backward_half<T, KF, WIDE, 0>(p, smem);
+    else backward_half<T, KF, WIDE, 1>(p, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -271,17 +359,19 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
     const float bt = scal[BETA * C + tr];
     const int row = 16 * wave + l16;
     const bool keys = wave < 2 * KF;                           // (the wavefront has a tile of keys)
-    Eight<T> dy;
-    Eight<float> x, d, s, z;
-    auto load = [&](int c0) __attribute__((always_inline)) {
+    struct In {
+        Eight<T> dy;
+        Eight<float> x, d, s, z;
+    };
+    In in;
+    auto load = [&](In &to, int c0) __attribute__((always_inline)) {
         const int left = (int)Dv - c0;
-        dy = take8<WIDE, T>(dyrow + c0, tc, tr < m ? left : 0);
-        x = take8<WIDE, float>(xs + tr * Dv + c0, tc, left);
-        d = take8<WIDE, float>(kept + tr * Dv + c0, tc, left);
+        to.dy = take8<WIDE, T>(dyrow + c0, tc, left);
+        to.x = take8<WIDE, float>(xs + tr * Dv + c0, tc, left);
+        to.d = take8<WIDE, float>(kept + tr * Dv + c0, tc, left);
         const int64_t at = (int64_t)min(row, p.Dk - 1) * Dv + c0;
-        const int there = row < p.Dk ? left : 0;
-        s = take8<WIDE, float>(state + at, 8 * quad, there);
-        z = take8<WIDE, float>(zs + at, 8 * quad, there);
+        to.s = take8<WIDE, float>(state + at, 8 * quad, left);
+        to.z = take8<WIDE, float>(zs + at, 8 * quad, left);
     };
 
     f32x4 dq[RT], rows[RT], cols[RT], dP[RT], dM[RT];
@@ -292,11 +382,16 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
     const bool has_p = wave < 4, has_m = WAVES == 4 || wave >= 4;
     float db = 0.0f;
     double sz = 0.0;
-    load(0);
-    for (int c0 = 0; c0 < Dv; c0 += 32) {
+    const int end = ((int)Dv - 1) / 32 * 32;            // (the last turn's again behind it: no branch)
+    auto turn = [&](In &now, int c0) __attribute__((always_inline)) {
         __syncthreads();
         bf16x8 st[3], zt[3];
         {
+            const int left = (int)Dv - c0;
+            const Eight<T> dy = keep8<WIDE, T>(now.dy, tc, tr < m ? left : 0);
+            const Eight<float> x = keep8<WIDE, float>(now.x, tc, left), s = keep8<WIDE, float>(now.s, 8 * quad, row < p.Dk ? left : 0),
+                               z = keep8<WIDE, float>(now.z, 8 * quad, row < p.Dk ? left : 0);
+            Eight<float> d = keep8<WIDE, float>(now.d, tc, left);
             bf16x8 o[NK], o3[3];
             if (first) {
                 terms8<T>(dy, o);
@@ -318,7 +413,7 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
             terms8<float>(s, st);
             terms8<float>(z, zt);
         }
-        load(c0 + 32 < Dv ? c0 + 32 : c0);              // (the last ones again: no branch)
+        load(now, min(c0 + 32, end));
         __syncthreads();
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -342,6 +437,25 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
                 }
             }
         }
+    };
+    load(in, 0);
+    for (int c0 = 0; c0 <= end; c0 += 32) turn(in, c0);
+    // K and Q: a unit of eight values a thread and turn
+    constexpr int key_units = C * KF * 4 / THREADS;
+    static_assert(key_units >= 1, "");
+    Eight<T> ke[key_units], qe[key_units];
+#pragma unroll
+    for (int n = 0; n < key_units; ++n) {
+        const int u = tid + n * THREADS, r = u / (KF * 4), c = u % (KF * 4) * 8, D = p.Dk;
+        const T *krow = static_cast<const T *>(p.k.data) + b * p.k.s0 + (t0 + min(r, m - 1)) * p.k.s1 + (int64_t)kh * D;
+        const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + min(r, m - 1)) * p.q.s1 + (int64_t)kh * D;
+        if (p.wide_qk) {
+            ke[n] = take8<true, T>(krow, c, D);
+            qe[n] = take8<true, T>(qrow, c, D);
+        } else {
+            ke[n] = take8<false, T>(krow, c, D);
+            qe[n] = take8<false, T>(qrow, c, D);
+        }
     }
     db += lane_xor<0>(db);
     db += lane_xor<1>(db);
@@ -350,23 +464,14 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
     for (int k = 1; k < 64; k *= 2) sz += __shfl_xor(sz, k);
     if (lane == 0) sums[0][wave] = sz;
     __syncthreads();            // (the first part's LDS is free)
-    {
-        // a unit of eight values of K and Q a thread and turn
-        constexpr int units = C * KF * 4 / THREADS;
-        static_assert(units >= 1, "");
 #pragma unroll
-        for (int n = 0; n < units; ++n) {
-            const int u = tid + n * THREADS, r = u / (KF * 4), c = u % (KF * 4) * 8, there = r < m ? p.Dk : 0;
-            const T *krow = static_cast<const T *>(p.k.data) + b * p.k.s0 + (t0 + min(r, m - 1)) * p.k.s1 + (int64_t)kh * p.Dk;
-            const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + min(r, m - 1)) * p.q.s1 + (int64_t)kh * p.Dk;
-            const Eight<T> e = p.wide_qk ? take8<true, T>(krow, c, there) : take8<false, T>(krow, c, there);
-            const Eight<T> g = p.wide_qk ? take8<true, T>(qrow, c, there) : take8<false, T>(qrow, c, there);
-            bf16x8 o[NK];
-            terms8<T>(e, o);
-            kt.put8(r, c, o);
-            terms8<T>(g, o);
-            qt.put8(r, c, o);
-        }
+    for (int n = 0; n < key_units; ++n) {
+        const int u = tid + n * THREADS, r = u / (KF * 4), c = u % (KF * 4) * 8, there = r < m ? p.Dk : 0;
+        bf16x8 o[NK];
+        terms8<T>(p.wide_qk ? keep8<true, T>(ke[n], c, there) : keep8<false, T>(ke[n], c, there), o);
+        kt.put8(r, c, o);
+        terms8<T>(p.wide_qk ? keep8<true, T>(qe[n], c, there) : keep8<false, T>(qe[n], c, there), o);
+        qt.put8(r, c, o);
     }
     // the matrices' rows of the wavefront
     {
@@ -573,12 +678,13 @@ template <typename T> __global__ __launch_bounds__(NT) void merit_delta_sum_head
 
 template <typename T, int KF> hipError_t backward_chunks(DeltaParams p, hipStream_t s)
 {
-    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + 2 * Mixed<3, C>::bytes + SCALAR_FLOATS * 4;
+    constexpr int lds = BackwardLds<T, KF>::bytes;
     static_assert(lds <= 160 * 1024, "");
-    p.slices = (p.Dv + 63) / 64;
+    p.width = chunk_width(p);
+    p.slices = (p.Dv + p.width - 1) / p.width;
     const unsigned grid = (unsigned)(p.B * p.H * p.slices);
-    if (p.wide_qk) merit_delta_back_chunks<T, KF, true><<<grid, NT, lds, s>>>(p);
-    else merit_delta_back_chunks<T, KF, false><<<grid, NT, lds, s>>>(p);
+    if (p.wide_qk) merit_delta_back_chunks<T, KF, true><<<grid, CHUNK_THREADS, lds, s>>>(p);
+    else merit_delta_back_chunks<T, KF, false><<<grid, CHUNK_THREADS, lds, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int KF> hipError_t grads_of(const DeltaParams &p, hipStream_t s)

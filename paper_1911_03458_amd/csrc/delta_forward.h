@@ -10,7 +10,7 @@ namespace delta {
 // ---------------------------------------------------------------------------
 // chunks side by side: a workgroup a chunk of a head
 // ---------------------------------------------------------------------------
-// It leaves -W and P in terms, their columns interleaved, and the tokens' factors.
+// It leaves -W and P in terms, and the tokens' factors.
 template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 {
@@ -35,13 +35,13 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
     float *const scal = to.scal;
 
     // Two rows' loads in a wavefront: keys to LDS, their squares' sums over the lanes of a row
-    ChunkRows<T, KF> kr;
+    ChunkRows<T, KF, NT> kr;
     kr.template load<false, WIDE>(p.k, b, t0, m, kh, p.Dk);
     const int own = 16 * wave + l16;
     const T *qrow = static_cast<const T *>(p.q.data) + b * p.q.s0 + (t0 + min(own, m - 1)) * p.q.s1 + (int64_t)kh * p.Dk;
     Eight<T> qe[KF];
 #pragma unroll
-    for (int f = 0; f < KF; ++f) qe[f] = take8<WIDE, T>(qrow, 32 * f + 8 * quad, own < m ? p.Dk : 0);
+    for (int f = 0; f < KF; ++f) qe[f] = take8<WIDE, T>(qrow, 32 * f + 8 * quad, p.Dk);
     if (wave == 0) {
         double g = 0.0;
         float bt = 0.0f;
@@ -60,12 +60,15 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         beta[lane] = bt;
         finite_beta[lane] = isfinite(bt) ? bt : 0.0f;     // (the rows that it reaches are lost anyway)
     }
+#pragma unroll
+    for (int f = 0; f < KF; ++f) qe[f] = keep8<WIDE, T>(qe[f], 32 * f + 8 * quad, own < m ? p.Dk : 0);
     if (p.unit) {
 #pragma unroll
-        for (int u = 0; u < ChunkRows<T, KF>::units; ++u) {
+        for (int u = 0; u < ChunkRows<T, KF, NT>::units; ++u) {
+            const Eight<T> x = kr.template value<false, WIDE>(u, m, p.Dk);
             float s = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = fmaf((float)kr.e[u].v[e], (float)kr.e[u].v[e], s);
+            for (int e = 0; e < 8; ++e) s = fmaf((float)x.v[e], (float)x.v[e], s);
             s = sum_lanes(s, KF * 4);
             if (tid % (KF * 4) == 0) invk[(tid + u * NT) / (KF * 4)] = 1.0f / sqrtf(s + MERIT_DELTA_EPS);
         }
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         invk[tid] = invq[tid] = 1.0f;
     }
     if (tid == 0) bad = C;
-    kr.store(kt);
+    kr.template store<false, WIDE>(kt, m, p.Dk);
     __syncthreads();
 
     if (tid < C) {
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         if (jb <= (wave | 1))
 #pragma unroll
             for (int k = 0; k < 3; ++k)
-                if (k < p.mix_terms) *reinterpret_cast<bf16x4 *>(to.mix + k * TRIANGLE + triangle_at(t, interleaved(j0))) = out[k];
+                if (k < p.mix_terms) *reinterpret_cast<bf16x4 *>(to.mix + k * TRIANGLE + triangle_at(t, j0)) = out[k];
     }
     __syncthreads();
 
@@ -199,247 +202,319 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         if (r < C / 2 && c0 >= C / 2) return;
         const bool lost = r >= bad, below = r >> 4 >= c0 >> 4;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(&x[r][c0 + 4 * k]);
-            bf16x4 o[3];
+        for (int k = 0; k < 2; ++k) {
+            float e[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                __bf16 s[3];
-                split<3>(lost ? __builtin_nanf("") : below ? -v[e] : 0.0f, s);
+            for (int j = 0; j < 8; ++j) e[j] = lost ? __builtin_nanf("") : below ? -x[r][c0 + 8 * k + j] : 0.0f;
+            bf16x8 o[3];
+            split8<3>(e, o);
 #pragma unroll
-                for (int n = 0; n < 3; ++n) o[n][e] = s[n];
-            }
-#pragma unroll
-            for (int n = 0; n < 3; ++n) *reinterpret_cast<bf16x4 *>(to.w + n * TRIANGLE + triangle_at(r, interleaved(c0 + 4 * k))) = o[n];
+            for (int n = 0; n < 3; ++n) *reinterpret_cast<bf16x8 *>(to.w + n * TRIANGLE + triangle_at(r, c0 + 8 * k)) = o[n];
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// one chunk after the other: a wavefront 16 columns of a head's state
+// one chunk after the other: two wavefronts 16 columns of a head's state
 // ---------------------------------------------------------------------------
-// The columns of a state do not depend on each other.  A wavefront has 16 of them, all of a chunk's tokens and all rows of the state,
-// in registers: results go from product to product as they lie (delta.h: Mixed).  LDS holds the other operands, K, Q and the two
-// triangular matrices, for the four wavefronts of a workgroup; the next chunk's are on their way in registers meanwhile.
-template <typename T, int KF, bool WIDE>
-__global__ __launch_bounds__(NT) void merit_delta_chunks(DeltaParams p)
+// The columns of a state do not depend on each other.  Two wavefronts of a SIMD have 16 of them: each one half of a chunk's tokens and
+// every other 32 rows of the state, in registers, so that one issues while the other waits (a wavefront alone issues an instruction
+// in four cycles, 1.4 thousand a chunk).  They meet four times a chunk: for the sums over the state's rows, for what the first
+// half's tokens leave for the second's, for what both leave for the state.  LDS holds the other operands, K, Q and the two triangular
+// matrices, for the eight wavefronts of a workgroup; the next chunk's are on their way in registers meanwhile.
+constexpr int CHUNK_THREADS = 512;
+template <typename T, int KF> struct ForwardLds {
+    static constexpr int NK = Terms<T>::n, NP = mix_terms<T>();
+    static constexpr int k = 0, w = k + Keys<NK, KF * 32>::bytes, mix = w + Triangle<3>::bytes, scal = mix + Triangle<NP>::bytes,
+                         q = scal + SCALAR_FLOATS * 4;
+    // what the wavefronts of a pair hand each other: 4 KB to each, w and u of the first; where LDS is full, in the place of Q
+    static constexpr bool shared = NK == 3 && KF == 4;
+    static constexpr int pair = (8 + 3 + NP) * 1024, hand = shared ? q : q + Keys<NK, KF * 32>::bytes;
+    static constexpr int bytes = hand + 4 * pair > q + Keys<NK, KF * 32>::bytes ? hand + 4 * pair : q + Keys<NK, KF * 32>::bytes;
+};
+// (a half at a time is compiled: every place in LDS is then a lane's base and a constant)
+template <typename T, int KF, bool WIDE, bool KEEP, int half>
+__device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem, int *lost)
 {
-    constexpr int NK = Terms<T>::n, NP = mix_terms<T>(), ORD = NP, RT = C / 16, DT = 2 * KF;
-    extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
-    typedef Mixed<NK, KF * 32> TK;
-    const TK kt{smem}, qt{kt.at + TK::bytes / 2};
-    const Mixed<3, C> tt{qt.at + TK::bytes / 2};
-    const Mixed<NP, C> mt{tt.at + Mixed<3, C>::bytes / 2};
-    float *const sc = reinterpret_cast<float *>(mt.at + Mixed<NP, C>::bytes / 2);
+    typedef ForwardLds<T, KF> L;
+    constexpr int NK = L::NK, NP = L::NP, ORD = NP, KO = KF < 2 ? 1 : KF / 2;
+    char *const lds = reinterpret_cast<char *>(smem);
+    const Keys<NK, KF * 32> kt{reinterpret_cast<__bf16 *>(lds + L::k)}, qt{reinterpret_cast<__bf16 *>(lds + L::q)};
+    const Triangle<3> wt{reinterpret_cast<__bf16 *>(lds + L::w)};
+    const Triangle<NP> mt{reinterpret_cast<__bf16 *>(lds + L::mix)};
+    float *const sc = reinterpret_cast<float *>(lds + L::scal);
 
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
     const int kh = (int)h / p.each, len = tokens_of(p, b), n = (len + C - 1) / C;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, tile = tid >> 6 & 3, l16 = lane & 15, quad = lane >> 4;
     const int64_t head = b * p.H + h, Dv = p.Dv;
-    const int c0 = (int)(id % (uint32_t)p.slices) * 64, c = c0 + 16 * wave + l16;
-    const bool busy = c0 + 16 * wave < Dv, in = c < Dv;            // (the wavefront, the lane has columns)
+    const int c0 = (int)(id % (uint32_t)p.slices) * p.width, c = c0 + 16 * tile + l16;
+    const bool busy = 16 * tile < p.width && c0 + 16 * tile < Dv, in = busy && c < Dv, has = half < KF;
+    f32x4 *const to_me = reinterpret_cast<f32x4 *>(lds + L::hand + tile * L::pair + half * 4096) + lane;
+    f32x4 *const to_other = reinterpret_cast<f32x4 *>(lds + L::hand + tile * L::pair + (1 - half) * 4096) + lane;
+    bf16x8 *const first = reinterpret_cast<bf16x8 *>(lds + L::hand + tile * L::pair) + lane;                  // b x of the first
+    bf16x8 *const second = reinterpret_cast<bf16x8 *>(lds + L::hand + tile * L::pair + 4096) + lane;          // w of the second
+    bf16x8 *const third = reinterpret_cast<bf16x8 *>(lds + L::hand + tile * L::pair + 8192) + lane;           // w and u of the first
 
-    f32x4 S[DT];
+    f32x4 S[KO][2];
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dk = 16 * d + 4 * quad + r;
-            S[d][r] = p.h0 && dk < p.Dk && in ? p.h0[(head * p.Dk + dk) * Dv + c] : 0.0f;
-        }
+    for (int o = 0; o < KO; ++o) {
+        const int dk = 32 * (half + 2 * o);
+        get_rows(S[o], p.h0 ? p.h0 + (head * p.Dk + dk) * Dv + c : nullptr, p.Dk - dk, Dv, in);
+    }
     const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);         // (a lane without a column: any that is there)
-    ChunkRows<T, KF> kr, qr;
-    Triangle<3> tr;
-    Triangle<NP> mr;
+    // (the first half's wavefronts, which wait for the others later, move what the next chunk needs)
+    ChunkRows<T, KF, NT> kr, qr;
+    TriangleRows<3, NT> wr;
+    TriangleRows<NP, NT> mr;
     f32x4 sr;
-    ChunkColumn<T> v;
+    ChunkColumn<T, 1> v;
     auto load = [&](int i, auto full) __attribute__((always_inline)) {
-        const int64_t chunk = (b * p.n + i) * p.H + h;
         const int m = min(C, len - i * C);
         kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
         qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
-        const Prepared from = prepared(p, chunk);
-        tr.load(from.w);
+        const Prepared from = prepared(p, (b * p.n + i) * p.H + h);
+        wr.load(from.w);
         mr.load(from.mix);
         sr = reinterpret_cast<const f32x4 *>(from.scal)[tid % (SCALAR_FLOATS / 4)];
     };
     auto load_v = [&](int i, auto full) __attribute__((always_inline)) {
-        v.template load<full.value>(p.v, b, (int64_t)i * C, min(C, len - i * C), mine);
+        v.template load<full.value>(p.v, b, (int64_t)i * C, half, min(C, len - i * C), mine);
     };
-    auto scalar = [&](int which, int rt) __attribute__((always_inline)) {
-        return *reinterpret_cast<const f32x4 *>(sc + which * C + 16 * rt + 4 * quad);
+    auto scalar = [&](int which, int sub) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4 *>(sc + which * C + 32 * half + 8 * quad + 4 * sub);
     };
-    // Values that are not finite go into products as zeros, because those of earlier tokens have them too, times 0; `bad` is the
-    // first token of the chunk from which the lane's column has some, and everything from there on becomes a NaN.
-    int bad = C;
-    auto finite = [&](f32x4 (&x)[RT]) __attribute__((always_inline)) {
-        bool all = true;
+    // Values that are not finite go into products as zeros, because those of earlier tokens have them too, times 0; lost[] has the
+    // first token of a chunk from which a column has some, and everything from there on becomes a NaN (the chunks behind it start
+    // from a state of NaNs).
+    auto finite = [&](f32x4 (&x)[2]) __attribute__((always_inline)) {
+        float f = 0.0f;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int k = 0; k < 8; ++k) f = fmaf(x[k >> 2][k & 3], 0.0f, f);
+        if (__ballot(f != 0.0f) == 0) return;                       // (a NaN is not 0)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) all = all && isfinite(x[rt][r]);
-        if (__ballot(!all) == 0) return;
+        for (int k = 0; k < 8; ++k)
+            if (!isfinite(x[k >> 2][k & 3])) {
+                atomicMin(&lost[16 * tile + l16], 32 * half + 8 * quad + k);
+                x[k >> 2][k & 3] = 0.0f;
+            }
+    };
+    auto lose = [&](f32x4 (&x)[2], int from) __attribute__((always_inline)) {
 #pragma unroll
-        for (int rt = RT - 1; rt >= 0; --rt)
+        for (int k = 0; k < 8; ++k)
+            if (32 * half + 8 * quad + k >= from) x[k >> 2][k & 3] = __builtin_nanf("");
+    };
+    // S += K^T w over the tokens of half `f`
+    auto into_state = [&](int f, const bf16x8 (&w)[3]) __attribute__((always_inline)) {
+        if (has)
 #pragma unroll
-            for (int r = 3; r >= 0; --r)
-                if (!isfinite(x[rt][r])) {
-                    bad = min(bad, 16 * rt + 4 * quad + r);
-                    x[rt][r] = 0.0f;
-                }
-        bad = min(bad, __shfl_xor(bad, 16));
-        bad = min(bad, __shfl_xor(bad, 32));
+            for (int o = 0; o < KO; ++o) {
+                bf16x8 a[2][NK];
+                kt.cols(half + 2 * o, 0, f, a[0]);
+                kt.cols(half + 2 * o, 1, f, a[1]);
+                multiply_rows<3>(S[o], a, w);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     };
 
-    // Chunk i; `full`: whole, and so is chunk `then`, whose operands go out here
+    // Chunk i; `full`: whole, and so is chunk `then`, whose operands go out on the way
     auto step = [&](int i, int then, auto full) __attribute__((always_inline)) {
         const int64_t t0 = (int64_t)i * C, chunk = (b * p.n + i) * p.H + h;
         const int m = min(C, len - i * C);
-        kr.store(kt);
-        qr.store(qt);
-        tr.store(tt);
-        mr.store(mt);
-        if (tid < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid] = sr;
+        if constexpr (half == 0) {
+            kr.template store<full.value, WIDE>(kt, m, p.Dk);
+            qr.template store<full.value, WIDE>(qt, m, p.Dk);
+            wr.store(wt);
+            mr.store(mt);
+            if (tid < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid] = sr;
+        }
         __syncthreads();
-        if constexpr (full.value) load(then, full);
-        if (busy) {
-            // K S and Q S
-            f32x4 X[RT], Y[RT];
+
+        // K S and Q S over the own rows of the state: X, Y[0], [1] for the own tokens, [2], [3] for the other's
+        const f32x4 in_k[2] = {scalar(IN_K, 0), scalar(IN_K, 1)}, beta[2] = {scalar(BETA, 0), scalar(BETA, 1)};
+        f32x4 X[4], Y[4];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) X[rt] = Y[rt] = f32x4{0, 0, 0, 0};
+        for (int k = 0; k < 4; ++k) X[k] = Y[k] = f32x4{0, 0, 0, 0};
+        if (busy && has)
 #pragma unroll
-            for (int f = 0; f < KF; ++f) {
-                bf16x8 s[3], a[RT][NK];
-                operand<3>(S[2 * f], S[2 * f + 1], s);
+            for (int o = 0; o < KO; ++o) {
+                bf16x8 s[3], a[4][NK];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) kt.rows(rt, f, a[rt]);
+                for (int k = 0; k < 4; ++k) kt.rows(half ^ (k >> 1), k & 1, half + 2 * o, a[k]);
+                operand<3>(S[o][0], S[o][1], s);
                 multiply_rows<3>(X, a, s);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) qt.rows(rt, f, a[rt]);
-                multiply_rows<ORD>(Y, a, s);
+                for (int k = 0; k < 4; ++k) qt.rows(half ^ (k >> 1), k & 1, half + 2 * o, a[k]);
+                multiply_rows<3>(Y, a, s);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (p.states) put_state<DT>(S, p.states + chunk * p.prep_stride + PREPARED_FLOATS + c, p.Dk, Dv, in);
+        if constexpr (L::shared) __syncthreads();
+        if (busy) {
+            to_other[0] = X[2];
+            to_other[64] = X[3];
+            to_other[128] = Y[2];
+            to_other[192] = Y[3];
+        }
+        __syncthreads();
+
+        // d = r - W (b r), u, w = what goes into the state: the first half's tokens at once, the second's part of their own
+        f32x4 D[2], U[2], O[2];
+        bf16x8 x[3], w[3], u[NP];
+        if (busy) {
+            bf16x8 a[2][3];
+            wt.rows(half, 0, half, a[0]);
+            wt.rows(half, 1, half, a[1]);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const f32x4 in_k = scalar(IN_K, rt);
+            for (int k = 0; k < 2; ++k) {
+                const f32x4 sum = X[k] + to_me[64 * k];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) X[rt][r] = fmaf(-in_k[r], X[rt][r], (float)v.v[rt][r]);
+                for (int r = 0; r < 4; ++r) D[k][r] = fmaf(-in_k[k][r], sum[r], v.value(k, r));
+                O[k] = beta[k] * D[k];
             }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) Y[k] += to_me[128 + 64 * k];
             if constexpr (full.value) load_v(then, full);
-
-            // d, u
-            f32x4 D[RT], U[RT];
-            bf16x8 x[2][3];
+            finite(O);
+            operand<3>(O[0], O[1], x);
+            multiply_rows<3>(D, a, x);
+        }
+        auto outer = [&]() __attribute__((always_inline)) {
+            const f32x4 out_k[2] = {scalar(OUT_K, 0), scalar(OUT_K, 1)};
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                D[rt] = X[rt];
-                X[rt] *= scalar(BETA, rt);
-            }
-            finite(X);
-#pragma unroll
-            for (int f = 0; f < 2; ++f) operand<3>(X[2 * f], X[2 * f + 1], x[f]);
-            {
-                bf16x8 a[RT][3];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) tt.rows(rt, 0, a[rt]);
-                multiply_rows<3>(D, a, x[0]);
-                f32x4 lower[2] = {D[2], D[3]};
-                bf16x8 al[2][3];
-                tt.rows(2, 1, al[0]);
-                tt.rows(3, 1, al[1]);
-                multiply_rows<3>(lower, al, x[1]);
-                D[2] = lower[0];
-                D[3] = lower[1];
-            }
-            if (__ballot(bad < C) != 0)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (16 * rt + 4 * quad + r >= bad) D[rt][r] = __builtin_nanf("");
-            if (p.states) {
-                put_state<RT>(D, p.states + chunk * p.prep_stride + PREPARED_FLOATS + p.Dk * Dv + c, C, Dv, in);
-            }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) U[rt] = D[rt] * scalar(BETA, rt);
+            for (int k = 0; k < 2; ++k) U[k] = beta[k] * D[k];
             finite(U);
-
-            // the state behind the chunk
-            const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
-            {
-                bf16x8 o[2][3];
-                f32x4 w[RT];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) w[rt] = U[rt] * scalar(OUT_K, rt);
+            for (int k = 0; k < 2; ++k) O[k] = out_k[k] * U[k];
+            operand<3>(O[0], O[1], w);
+            operand<NP>(U[0], U[1], u);
+        };
+        if (busy && half == 0) {
+            const int from = lost[16 * tile + l16];
+            if (__ballot(from < C) != 0) lose(D, from);
+            outer();
 #pragma unroll
-                for (int f = 0; f < 2; ++f) operand<3>(w[2 * f], w[2 * f + 1], o[f]);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) S[d] *= whole;
-#pragma unroll
-                for (int f = 0; f < 2; ++f)
-#pragma unroll
-                    for (int g = 0; g < DT / 2; ++g) {
-                        bf16x8 a[2][NK];
-                        f32x4 two[2] = {S[2 * g], S[2 * g + 1]};
-                        kt.cols(f, 2 * g, a[0]);
-                        kt.cols(f, 2 * g + 1, a[1]);
-                        multiply_rows<3>(two, a, o[f]);
-                        S[2 * g] = two[0];
-                        S[2 * g + 1] = two[1];
-                    }
+            for (int k = 0; k < 3; ++k) {
+                first[64 * k] = x[k];
+                third[64 * k] = w[k];
             }
-            // y
-            {
-                bf16x8 u[2][NP], a[RT][NP], al[2][NP];
 #pragma unroll
-                for (int f = 0; f < 2; ++f) operand<NP>(U[2 * f], U[2 * f + 1], u[f]);
+            for (int k = 0; k < NP; ++k) third[192 + 64 * k] = u[k];
+        }
+        __syncthreads();
+        // the state before the chunk is not needed any more, but by those who keep it
+        auto fade = [&]() __attribute__((always_inline)) {
+            if (KEEP && has)
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    Y[rt] *= scalar(IN_Q, rt);
-                    mt.rows(rt, 0, a[rt]);
+                for (int o = 0; o < KO; ++o) {
+                    const int dk = 32 * (half + 2 * o);
+                    put_rows(S[o], p.states + chunk * p.prep_stride + PREPARED_FLOATS + dk * Dv + c, p.Dk - dk, Dv, in);
                 }
-                multiply_rows<ORD>(Y, a, u[0]);
-                f32x4 lower[2] = {Y[2], Y[3]};
-                mt.rows(2, 1, al[0]);
-                mt.rows(3, 1, al[1]);
-                multiply_rows<ORD>(lower, al, u[1]);
-                Y[2] = lower[0];
-                Y[3] = lower[1];
+            const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
+#pragma unroll
+            for (int o = 0; o < KO; ++o)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) S[o][k] *= whole;
+        };
+        auto results = [&]() __attribute__((always_inline)) {
+            bf16x8 a[2][NP];
+            mt.rows(half, 0, half, a[0]);
+            mt.rows(half, 1, half, a[1]);
+            f32x4 y[2] = {Y[0], Y[1]};
+            multiply_rows<ORD>(y, a, u);
+            const int from = lost[16 * tile + l16];
+            if (__ballot(from < C) != 0) lose(y, from);
+            put_column<full.value, T>(y, p.y, b, t0, half, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
+            if (KEEP) put_rows(D, p.states + chunk * p.prep_stride + PREPARED_FLOATS + (p.Dk + 32 * half) * Dv + c, 32, Dv, in);
+        };
+        if constexpr (half == 0) {
+            if constexpr (full.value) load(then, full);
+            if (busy) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) Y[k] *= scalar(IN_Q, k);
+                fade();
+                into_state(0, w);
+                results();
             }
-            if (__ballot(bad < C) != 0 && bad < C) {
+        } else if (busy) {
+            bf16x8 x0[3], a[2][3];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
+            for (int k = 0; k < 3; ++k) x0[k] = first[64 * k];
+            wt.rows(1, 0, 0, a[0]);
+            wt.rows(1, 1, 0, a[1]);
+            const int from = lost[16 * tile + l16];
+            multiply_rows<3>(D, a, x0);
+            if (__ballot(from < C) != 0) lose(D, from);
+            outer();
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (16 * rt + 4 * quad + r >= bad) Y[rt][r] = __builtin_nanf("");
+            for (int k = 0; k < 3; ++k) second[64 * k] = w[k];
+        }
+        __syncthreads();
+        if (busy) {
+            if constexpr (half == 0) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+                for (int k = 0; k < 3; ++k) w[k] = second[64 * k];
+                into_state(1, w);
+            } else {
+                bf16x8 w0[3], u0[NP], a[2][NP];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[d][r] = __builtin_nanf("");
+                for (int k = 0; k < 3; ++k) w0[k] = third[64 * k];
+                fade();
+                into_state(1, w);
+                into_state(0, w0);
+#pragma unroll
+                for (int k = 0; k < NP; ++k) u0[k] = third[192 + 64 * k];
+                mt.rows(1, 0, 0, a[0]);
+                mt.rows(1, 1, 0, a[1]);
+                f32x4 y[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) y[k] = Y[k] * scalar(IN_Q, k);
+                multiply_rows<ORD>(y, a, u0);
+                Y[0] = y[0];
+                Y[1] = y[1];
+                results();
             }
-            put_column<full.value, T>(Y, p.y, b, t0, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
+            if (lost[16 * tile + l16] < C)
+#pragma unroll
+                for (int o = 0; o < KO; ++o)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) S[o][k >> 2][k & 3] = __builtin_nanf("");
         }
         __syncthreads();
     };
+    if (tid < 64) lost[tid] = C;
     const int whole_chunks = len / C;
     if (whole_chunks > 0) {
-        load(0, std::true_type());
+        if constexpr (half == 0) load(0, std::true_type());
         load_v(0, std::true_type());
         for (int i = 0; i < whole_chunks; ++i) step(i, min(i + 1, whole_chunks - 1), std::true_type());    // (the last one's again: no branch)
     }
     if (whole_chunks < n) {
-        load(n - 1, std::false_type());
+        if constexpr (half == 0) load(n - 1, std::false_type());
         load_v(n - 1, std::false_type());
         step(n - 1, n - 1, std::false_type());
     }
-    if (p.h_last) put_state<DT>(S, p.h_last + head * p.Dk * Dv + c, p.Dk, Dv, in);
+    if (p.h_last && has)
+#pragma unroll
+        for (int o = 0; o < KO; ++o) {
+            const int dk = 32 * (half + 2 * o);
+            put_rows(S[o], p.h_last + (head * p.Dk + dk) * Dv + c, p.Dk - dk, Dv, in);
+        }
     // zeros behind the sequence's last chunk
-    const int cols = min(64, (int)Dv - c0);
-    for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += NT) {
+    const int cols = min(p.width, (int)Dv - c0);
+    for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += CHUNK_THREADS) {
         const int64_t t = (int64_t)n * C + u / cols;
         static_cast<T *>(p.y.data)[b * p.y.s0 + t * p.y.s1 + h * Dv + c0 + u % cols] = (T)0.0f;
     }
+}
+template <typename T, int KF, bool WIDE, bool KEEP>
+__global__ __launch_bounds__(CHUNK_THREADS, 2) void merit_delta_chunks(DeltaParams p)
+{
+    extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
+    __shared__ int lost[64];
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) forward_half<T, KF, WIDE, KEEP, 0>(p, smem, lost);
+    else forward_half<T, KF, WIDE, KEEP, 1>(p, smem, lost);
 }
 
 // ---------------------------------------------------------------------------
@@ -542,16 +617,31 @@ template <typename T, int KF> hipError_t prepare_of(const DeltaParams &p, hipStr
     else merit_delta_prepare<T, KF, false><<<grid, NT, 0, s>>>(p);
     return hipGetLastError();
 }
+// Columns of a workgroup of merit_delta_chunks and merit_delta_back_chunks: 64, or less where a compute unit would go without one.  The
+// operands come into LDS once for a workgroup, and take their time whatever it does with them (bfloat16, 128 x 128, 64 / 32 / 16
+// columns, us: 128 heads of 2048 tokens 241 / 390 / 699, 16 heads of 8191 620 / 570 / 559).
+inline int chunk_width(const DeltaParams &p)
+{
+    for (int w : {64, 32})
+        if (p.B * p.H * ((p.Dv + w - 1) / w) >= 256) return w;
+    return 16;
+}
 template <typename T, int KF> hipError_t forward_of(DeltaParams p, hipStream_t s)
 {
-    constexpr int lds = 2 * Mixed<Terms<T>::n, KF * 32>::bytes + Mixed<3, C>::bytes + Mixed<mix_terms<T>(), C>::bytes + SCALAR_FLOATS * 4;
-    static_assert(lds <= 160 * 1024, "");
+    constexpr int lds = ForwardLds<T, KF>::bytes;
+    static_assert(lds + 256 <= 160 * 1024, "");
     p.mix_terms = p.states ? 3 : mix_terms<T>();
     if (hipError_t e = prepare_of<T, KF>(p, s)) return e;
-    p.slices = (p.Dv + 63) / 64;
+    p.width = chunk_width(p);
+    p.slices = (p.Dv + p.width - 1) / p.width;
     const unsigned grid = (unsigned)(p.B * p.H * p.slices);
-    if (p.wide_qk) merit_delta_chunks<T, KF, true><<<grid, NT, lds, s>>>(p);
-    else merit_delta_chunks<T, KF, false><<<grid, NT, lds, s>>>(p);
+    if (p.wide_qk) {
+        if (p.states) merit_delta_chunks<T, KF, true, true><<<grid, CHUNK_THREADS, lds, s>>>(p);
+        else merit_delta_chunks<T, KF, true, false><<<grid, CHUNK_THREADS, lds, s>>>(p);
+    } else {
+        if (p.states) merit_delta_chunks<T, KF, false, true><<<grid, CHUNK_THREADS, lds, s>>>(p);
+        else merit_delta_chunks<T, KF, false, false><<<grid, CHUNK_THREADS, lds, s>>>(p);
+    }
     return hipGetLastError();
 }
 template <typename T> hipError_t forward_typed(const DeltaParams &p, hipStream_t s)

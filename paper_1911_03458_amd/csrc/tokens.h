@@ -104,7 +104,7 @@ struct DeltaParams {
     int unit;              // q and k count by their direction
     int type;
     int n;                 // chunks of MERIT_DELTA_CHUNK tokens
-    int slices;            // workgroups along v's columns
+    int width, slices;     // columns of v of a workgroup, workgroups along them
     int wide_qk, wide_v, wide_out, wide_state;      // whether rows can be moved in 16-byte pieces (wide_out: dq, dk)
     Rows q, k, v, y, dy, dq, dk, dv;
     Rows g, beta, dg, dbeta;            // a number a head

@@ -8,11 +8,11 @@ direction on top, 90; for dg, a sum over a chunk of 64 differences of such produ
 for a row's norms and the sums over rows 4 sqrt(terms of a thread or a tree): at most 64.  Held against the root mean square
 of the result (and 8 times that for a single value, where one in a million exceeds five).
 
-y of the 16-bit types has besides what the operands of its two products lose that go in as two bfloat16 terms (S, and P and u): the
-second term, at most 2^-8 of the value, is rounded by at most 2^-8 of itself, so 2^-16 of the value is lost at most and, for
-mantissas and remainders spread evenly, 2^-17 / sqrt(3) on average (root mean square); the product of two second terms, left out,
-is as much again.  These are relative to each term of a sum, so a sum of terms of either sign has as much of its own root mean
-square: S alone in Q S, and P, u and the product left out in P u, together sqrt(4) 2^-17 / sqrt(3) = 148 x 2^-24 (`y_of`)."""
+y of the 16-bit types has besides what P and u lose, which go into their product as two bfloat16 terms: the second term, at most
+2^-8 of the value, is rounded by at most 2^-8 of itself, so 2^-16 of the value is lost at most and, for mantissas and remainders
+spread evenly, 2^-17 / sqrt(3) on average (root mean square); the product of two second terms, left out, is as much again.  These
+are relative to each term of a sum, so a sum of terms of either sign has as much of its own root mean square: together
+sqrt(3) 2^-17 / sqrt(3) = 128 x 2^-24 (`y_of`)."""
 import numpy as np
 
 from token_helpers import host
@@ -21,7 +21,7 @@ DELTA, GRAD, DECAY, NORM = 45, 90, 720, 64
 
 
 def y_of(dtype):
-    return DELTA if dtype in ("f32", "torch.float32") else DELTA + 148
+    return DELTA if dtype in ("f32", "torch.float32") else DELTA + 128
 
 
 UNITS = {"torch.float32": 2.0 ** -24, "torch.float16": 2.0 ** -11, "torch.bfloat16": 2.0 ** -8}
