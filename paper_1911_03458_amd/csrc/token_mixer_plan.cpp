@@ -53,14 +53,18 @@ void block_layout(BlockNormParams &p, int vec, bool backward)
     const int cu = p.C / vec;
     p.lanes = 0;
     p.units = 1;
-    p.threads = cu <= 256 ? 256 : cu <= 512 ? 512 : 1024;
+    p.threads = cu <= 256 ? 256 : p.C <= 512 * 16 ? 512 : 1024;     // (at most 16 values a thread)
     if (cu <= 64) {
         p.lanes = 1;
         while (p.lanes < cu) p.lanes *= 2;
     }
     while (p.threads * p.units < cu) p.units *= 2;
     const int64_t at_once = p.lanes ? 256 / p.lanes : 1;
-    const int64_t most = (backward ? 131072 : 524288) / p.threads;
+    // No more workgroups than run at once, by the registers that each takes: forward 1024 wavefronts of 4 against twice as many,
+    // 8 x 2048 rows of 2048, both norms, 49 against 51 us; backward 512 against 768, the same rows, 85 against 99 us, and 1024
+    // against 512 where there is an after-norm only, 262144 rows of 128, 73 against 81 us.
+    const int64_t fours = backward && p.before ? 512 : 1024;
+    const int64_t most = p.threads == 1024 ? 256 : fours * 256 / p.threads;
     p.blocks = cdiv(p.rows, at_once);
     if (p.blocks > most) p.blocks = most;
 }
