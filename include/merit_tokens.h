@@ -61,7 +61,7 @@ typedef struct merit_token_plan merit_token_plan;   /* opaque, host memory only 
 #define MERIT_DELTA_CHUNK     64     /* tokens between two kept states of a forward pass */
 #define MERIT_DELTA_KEPT      9728   /* values that the forward pass keeps of a chunk besides its state and tokens */
 #define MERIT_DELTA_EPS       1e-6f  /* beside the square of a length that divides */
-#define MERIT_BLOCK_NORM_MAX_CHANNELS 16384
+#define MERIT_BLOCK_NORM_MAX_CHANNELS 8192
 
 /* Group norm of x[N, S, C]: the S positions x C / groups channels of a group share mean and variance.
  * S = 1: every token by itself; S = H * W: an image, channels last.  eps >= 0. */

@@ -5,11 +5,12 @@
 //     do = dout + rstd (g - [mean g] - oh mean(g oh)),   dr = do,   ds = sum do t,   dt = s do
 //     dz = dt u act'(z),   du = dt act(z),   dx = rstd (du aw - [mean(du aw)] - xh mean(du aw xh)),   daw = sum du xh, dab = sum du, ..
 // Bound by memory, rows of one head by their instructions as well (30 a value forward with a SiLU gate).  A row is held in
-// registers by a run of lanes, or a workgroup of 256 to 1024 threads, so every tensor is read once; a thread keeps its columns
+// registers by a run of lanes, or a workgroup of 256 or 512 threads, so every tensor is read once; a thread keeps its columns
 // while it walks down the rows, which keeps parameters and the sums of their gradients in registers, and asks for the next row
 // before it works on this one (backward, 16384 rows of 2048: 85 us against 139 without).  bf16, the bytes at their rate: 16384
 // rows of 2048, both norms, forward 49 us (5.5 TB/s), with an fp32 stream 77 us (5.2), backward 85 us (4.7); 262144 rows of 128,
-// after-norm and gate, forward 45 us (4.5), backward 69 us (4.9).  Rows past 8192 spill: 2000 of 16384, backward, 0.6 ms.
+// after-norm and gate, forward 45 us (4.5), backward 69 us (4.9).
+// Rows of more than 8 values a thread that are not in pieces of 16 bytes spill: 2048 of 8191, fp32, backward, 0.34 ms.
 #pragma once
 
 #include "merit_internal.h"
@@ -255,9 +256,8 @@ __global__ __launch_bounds__(NT) void merit_block_norm_rows(BlockNormParams p)
         has[j] = u * V < p.C;
         c[j] = has[j] ? u * V : 0;
     }
-    constexpr bool HOLD = NT < 1024;
-    const Vector<T, V, U, HOLD> aw(p.aw, 1.0f, c, has), ab(FORM ? Param{} : p.ab, 0.0f, c, has), sc(p.scale, 1.0f, c, has);
-    const Vector<T, V, U, HOLD> bw(p.bw, 1.0f, c, has), bb(FORM ? Param{} : p.bb, 0.0f, c, has);
+    const Vector<T, V, U, true> aw(p.aw, 1.0f, c, has), ab(FORM ? Param{} : p.ab, 0.0f, c, has), sc(p.scale, 1.0f, c, has);
+    const Vector<T, V, U, true> bw(p.bw, 1.0f, c, has), bb(FORM ? Param{} : p.bb, 0.0f, c, has);
     Piece<T, V> xn[U], zn[U];
     Piece<R, V> rn[U];
     Walk in(p, q), to(p, q);
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(NT) void merit_block_norm_rows(BlockNormParams p)
 }
 
 template <typename T, typename R, int V, int U, int NT, int FORM>
-__global__ __launch_bounds__(NT, FORM == 1 && NT < 1024 && V * U <= 8 ? 4 : 1) void merit_block_norm_rows_backward(BlockNormParams p)
+__global__ __launch_bounds__(NT, FORM == 1 && V * U <= 8 ? 4 : 1) void merit_block_norm_rows_backward(BlockNormParams p)
 {
     __shared__ float slots[2][2][NT / 64];
     __shared__ float red[NT == 256 ? NT : 1][V];
@@ -546,7 +546,6 @@ template <bool BACKWARD, typename T, typename R, int V> hipError_t launch_vec(co
 {
     if (p.threads == 256) return launch_rows<BACKWARD, T, R, V, 1, 256>(p, s);
     // (rows of at most MERIT_BLOCK_NORM_MAX_CHANNELS: 16 values a thread)
-    if (p.threads == 1024) return launch_rows<BACKWARD, T, R, V, 16 / V, 1024>(p, s);
     if (p.units == 1) return launch_rows<BACKWARD, T, R, V, 1, 512>(p, s);
     if (p.units == 2) return launch_rows<BACKWARD, T, R, V, 2, 512>(p, s);
     if constexpr (V <= 4) if (p.units == 4) return launch_rows<BACKWARD, T, R, V, 4, 512>(p, s);

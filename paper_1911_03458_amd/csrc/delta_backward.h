@@ -40,7 +40,7 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
     const int kh = (int)h / p.each, len = tokens_of(p, b), n = (len + C - 1) / C;
-    const int tid = threadIdx.x, lane = tid & 63, tile = tid >> 6 & 3, l16 = lane & 15, quad = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, tile = __builtin_amdgcn_readfirstlane(tid >> 6 & 3), l16 = lane & 15, quad = lane >> 4;
     const int64_t head = b * p.H + h, Dv = p.Dv;
     const int c0 = (int)(id % (uint32_t)p.slices) * p.width, c = c0 + 16 * tile + l16;
     const bool busy = 16 * tile < p.width && c0 + 16 * tile < Dv, in = busy && c < Dv, has = half < KF;
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
     const uint32_t i = bi % (uint32_t)p.n;
     const int64_t b = bi / (uint32_t)p.n, t0 = (int64_t)i * C, Dv = p.Dv;
     const int kh = (int)h / p.each, m = min(C, tokens_of(p, b) - (int)t0), here = (int)min((int64_t)C, p.L - t0);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     // rows t of dq or dk, as they lie: the tensor's, or the value head's part in fp32
     auto put8 = [&](const Rows &out, int64_t which, int t, int c, const float (&v)[8]) __attribute__((always_inline)) {
         if (p.part) {

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
     const int64_t b = bi / (uint32_t)p.n, t0 = (int64_t)i * C;
     const int kh = (int)h / p.each, m = min(C, tokens_of(p, b) - (int)t0);
     if (m <= 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quad = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const Prepared to = prepared(p, id);
     float *const scal = to.scal;
 
@@ -247,7 +247,10 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
     const int64_t b = id / (uint32_t)p.slices / (uint32_t)p.H;
     const int kh = (int)h / p.each, len = tokens_of(p, b), n = (len + C - 1) / C;
-    const int tid = threadIdx.x, lane = tid & 63, tile = tid >> 6 & 3, l16 = lane & 15, quad = lane >> 4;
+    // (a wavefront's number is said to be the same for its lanes: branches on it skip, and leave the lanes' mask as it is.  Behind one
+    // that masks lanes, the compiler put a copy of a register in front of the mask's restoring, and wavefronts that skip kept an
+    // old value: in fp32 with rows off 16 bytes and states kept, rows moved by wavefronts without columns were wrong.)
+    const int tid = threadIdx.x, lane = tid & 63, tile = __builtin_amdgcn_readfirstlane(tid >> 6 & 3), l16 = lane & 15, quad = lane >> 4;
     const int64_t head = b * p.H + h, Dv = p.Dv;
     const int c0 = (int)(id % (uint32_t)p.slices) * p.width, c = c0 + 16 * tile + l16;
     const bool busy = 16 * tile < p.width && c0 + 16 * tile < Dv, in = busy && c < Dv, has = half < KF;

@@ -53,7 +53,7 @@ void block_layout(BlockNormParams &p, int vec, bool backward)
     const int cu = p.C / vec;
     p.lanes = 0;
     p.units = 1;
-    p.threads = cu <= 256 ? 256 : p.C <= 512 * 16 ? 512 : 1024;     // (at most 16 values a thread)
+    p.threads = cu <= 256 ? 256 : 512;
     if (cu <= 64) {
         p.lanes = 1;
         while (p.lanes < cu) p.lanes *= 2;
@@ -64,7 +64,7 @@ void block_layout(BlockNormParams &p, int vec, bool backward)
     // 8 x 2048 rows of 2048, both norms, 49 against 51 us; backward 512 against 768, the same rows, 85 against 99 us, and 1024
     // against 512 where there is an after-norm only, 262144 rows of 128, 73 against 81 us.
     const int64_t fours = backward && p.before ? 512 : 1024;
-    const int64_t most = p.threads == 1024 ? 256 : fours * 256 / p.threads;
+    const int64_t most = fours * 256 / p.threads;
     p.blocks = cdiv(p.rows, at_once);
     if (p.blocks > most) p.blocks = most;
 }

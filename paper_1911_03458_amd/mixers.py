@@ -11,7 +11,7 @@ MERIT_ACT_SIGMOID = 3                   # the gate of merit_block_norm only
 MERIT_DELTA_MAX_KEYS = 128
 MERIT_DELTA_CHUNK = 64
 MERIT_DELTA_KEPT = 9728
-MERIT_BLOCK_NORM_MAX_CHANNELS = 16384
+MERIT_BLOCK_NORM_MAX_CHANNELS = 8192
 
 _ENTRIES = ("merit_delta_rule", "merit_delta_rule_backward", "merit_delta_rule_step", "merit_block_norm", "merit_block_norm_backward")
 

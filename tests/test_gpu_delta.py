@@ -77,6 +77,28 @@ def test_backward(mb, shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 100, 1, 1, 29, 10), (1, 228, 1, 1, 31, 40), (2, 100, 2, 1, 100, 24), (1, 165, 2, 2, 33, 16),
+                                   (1, 165, 2, 1, 128, 70), (1, 130, 1, 1, 64, 200), (70, 66, 4, 4, 40, 48), (1, 100, 1, 1, 8, 8)])
+def test_columns_for_some_of_a_workgroup(mb, shape, dtype):
+    """Whole chunks and part of one, with fewer columns than a workgroup has wavefronts for: those without any move rows for the
+    others.  With the states kept, without, and backward."""
+    a, g = _inputs(shape, dtype, sum(shape) + 2)
+    B, L, H, K, Dk, Dv = shape
+    plan, dy = _plan(mb, shape, dtype), g.normal(B, L, H, Dv, dtype=TYPES[dtype][0])
+    wy, wh, _ = om.delta_rule(**_h(a), scale=Dk ** -0.5)
+    y, h = mb.merit_delta_rule(plan, *a.values(), final=True)
+    y2, h2, states = mb.merit_delta_rule(plan, *a.values(), final=True, states=True)
+    for got in (y, y2):
+        near(got, wy, y_of(str(y.dtype)), "y")
+    for got in (h, h2):
+        near(got, wh, DELTA, "state")
+    got = mb.merit_delta_rule_backward(plan, dy, a["q"], a["k"], a["g"], a["beta"], states)
+    want = om.delta_rule_backward(host(dy), **_h(a), scale=Dk ** -0.5)
+    for k in ("dq", "dk", "dv", "dg", "dbeta"):
+        near(got[k], want[k], DECAY if k == "dg" else GRAD, k, floor=float(np.sqrt(np.mean(want["dbeta"] ** 2))) if k == "dg" else 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("B, H, K, Dk, Dv", [(1, 1, 1, 1, 1), (2, 4, 2, 64, 64), (3, 2, 2, 128, 128), (5, 6, 2, 100, 50), (1, 3, 3, 17, 260), (2, 2, 1, 128, 33)])
 def test_one_token(mb, B, H, K, Dk, Dv, dtype):
     unit = Dk % 2 == 0
