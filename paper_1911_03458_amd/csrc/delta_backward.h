@@ -290,6 +290,7 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
     __shared__ double G[C], sums[2][WAVES], suffix[C];
     __shared__ float invk[C], invq[C], beta[C];
+    __shared__ int before[WAVES];
     typedef Tile<3, C, 32> TU;
     typedef Tile<NK, C, KF * 32> TK;
     const Tile<NK, C, 32> yt{smem};
@@ -382,6 +383,7 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
     const bool has_p = wave < 4, has_m = WAVES == 4 || wave >= 4;
     float db = 0.0f;
     double sz = 0.0;
+    uint32_t held = 0;                                  // (bits of the state before the sequence's first chunk)
     const int end = ((int)Dv - 1) / 32 * 32;            // (the last turn's again behind it: no branch)
     auto turn = [&](In &now, int c0) __attribute__((always_inline)) {
         __syncthreads();
@@ -410,6 +412,9 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
 #pragma unroll
             for (int e = 0; e < 8; ++e) f = fmaf(s.v[e], z.v[e], f);
             sz += (double)f;
+            if (i == 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) held |= __builtin_bit_cast(uint32_t, s.v[e]) << 1;
             terms8<float>(s, st);
             terms8<float>(z, zt);
         }
@@ -463,6 +468,8 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) sz += __shfl_xor(sz, k);
     if (lane == 0) sums[0][wave] = sz;
+    const bool any = __ballot(held != 0) != 0;
+    if (lane == 0) before[wave] = i > 0 || any;
     __syncthreads();            // (the first part's LDS is free)
 #pragma unroll
     for (int n = 0; n < key_units; ++n) {
@@ -651,6 +658,11 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
             const double o = __shfl_down(a, k);
             if (lane + k < C) a += o;
         }
+        // Before the first token of a state of zeros there is nothing to fade: no gradient, where the sums cancel to their roundings
+        int some = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) some |= before[w];
+        if (lane == 0 && !some && isfinite(a)) a = 0.0;
         if (lane < here && p.dg.data)
             static_cast<float *>(p.dg.data)[b * p.dg.s0 + (t0 + lane) * p.dg.s1 + h] = lane < m ? (float)a : 0.0f;
     }

@@ -219,6 +219,22 @@ def test_without_decay_and_with_total_decay(mb):
     near(y1, wy[:, 40], DELTA, "token")
 
 
+@pytest.mark.parametrize("L", [1, 3, 100])
+def test_nothing_fades_before_the_first_token(mb, L):
+    """The decay of the first token has a gradient where a state is passed in, and exactly none where it is zeros or absent."""
+    shape = (2, L, 2, 1, 40, 24)
+    a, g = _inputs(shape, "f32", 45)
+    dy, plan = g.normal(2, L, 2, 24), _plan(mb, shape, "f32")
+    h = g.normal(2, 2, 40, 24)
+    h[1] = 0.0
+    for h0 in (None, torch.zeros_like(h), h):
+        st = mb.merit_delta_rule(plan, *a.values(), h0=h0, states=True)[-1]
+        dg = mb.merit_delta_rule_backward(plan, dy, a["q"], a["k"], a["g"], a["beta"], st)["dg"]
+        want = om.delta_rule_backward(host(dy), **_h(a), h0=None if h0 is None else host(h0), scale=40 ** -0.5)
+        assert not dg[1, 0].any() and (h0 is h) == bool(dg[0, 0].all())
+        near(dg, want["dg"], DECAY, "dg", floor=float(np.sqrt(np.mean(want["dbeta"] ** 2))))
+
+
 @pytest.mark.parametrize("beta_value", [0.0, 1.0, 2.0])
 def test_strengths(mb, beta_value):
     shape = (1, 100, 1, 1, 32, 16)
