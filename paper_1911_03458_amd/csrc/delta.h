@@ -1,4 +1,4 @@
-// Device helpers of the gated delta rule's kernels (delta.hip, delta_backward.hip).
+// Device helpers of the gated delta rule's kernels (delta_forward.h, delta_backward.h).
 //
 //     S_t = a_t S_{t-1} + k_t u_t^T,   u_t = b_t d_t,   d_t = v_t - a_t S_{t-1}^T k_t,   y_t = scale S_t^T q_t,   a_t = exp(g_t)
 //
@@ -9,8 +9,8 @@
 // one matrix serves the forward pass, d = r - W (b r), and the backward pass, x = y - W^T (b y), whatever b is (0 too).
 // merit_delta_prepare finds it and P = scale f o Q K^T for all chunks side by side.
 //
-// Products run on v_mfma_f32_16x16x32_bf16.  An fp32 operand goes in as three bfloat16 terms of 8 bits each (x = x0 + x1 + x2 with
-// the rounding error of the one before in each), a binary16 one as two, a bfloat16 one as it is, and terms whose product is below
+// Products run on v_mfma_f32_16x16x32_bf16.  An fp32 operand goes in as three bfloat16 terms of 8 bits each (x = x0 + x1 + x2, each
+// what the ones before it leave), a binary16 one as two, a bfloat16 one as it is, and terms whose product is below
 // 2^-24 of the leading one are left out: 3 products for an exact operand with an fp32 one, 6 for two fp32 ones, at a sixteenth of
 // the time each that v_mfma_f32_16x16x4_f32 takes.  States, sums and what is kept of them are fp32.
 #pragma once
@@ -94,22 +94,7 @@ __device__ __forceinline__ void multiply(f32x4 &acc, const bf16x8 (&a)[NA], cons
         }
 }
 
-// The same for columns side by side, one after the other in turn: a product into an accumulator waits for the one before it
-template <int ORDER, int NA, int NB, int NC>
-__device__ __forceinline__ void multiply(f32x4 (&acc)[NC], const bf16x8 (&a)[NA], const bf16x8 (&b)[NC][NB])
-{
-#pragma unroll
-    for (int s = ORDER - 1; s >= 0; --s)
-#pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const int j = s - i;
-            if (j >= 0 && j < NB)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[c][j], acc[c], 0, 0, 0);
-        }
-}
-
-// And for rows
+// The same for rows side by side, one after the other in turn: a product into an accumulator waits for the one before it
 template <int ORDER, int NA, int NB, int NR>
 __device__ __forceinline__ void multiply_rows(f32x4 (&acc)[NR], const bf16x8 (&a)[NR][NA], const bf16x8 (&b)[NB])
 {
@@ -125,7 +110,7 @@ __device__ __forceinline__ void multiply_rows(f32x4 (&acc)[NR], const bf16x8 (&a
 }
 
 // ---- operands -----------------------------------------------------------------------------------------------
-// Eight values of a row from column c on, zeros from column n on.  wide: rows start on 16 bytes and n is a multiple of 8.
+// Eight values of a row
 template <typename T> struct Eight {
     typedef T vec __attribute__((ext_vector_type(8)));      // (16-bit values stay two in a register)
     vec v;
@@ -137,26 +122,6 @@ template <typename T> __device__ __forceinline__ Eight<T> zero8()
     Eight<T> r;
     if constexpr (sizeof(T) == 2) r.v = __builtin_bit_cast(typename Eight<T>::vec, u32x4{0, 0, 0, 0});
     else r.v = __builtin_bit_cast(typename Eight<T>::vec, u32x8{0, 0, 0, 0, 0, 0, 0, 0});
-    return r;
-}
-template <typename T> __device__ __forceinline__ Eight<T> load8(const T *row, int c, int n, bool wide)
-{
-    Eight<T> r = zero8<T>();
-    if (wide) {
-        if (c < n) {
-            const u32x4 *from = reinterpret_cast<const u32x4 *>(row + c);
-            if constexpr (sizeof(T) == 2) {
-                r.v = __builtin_bit_cast(typename Eight<T>::vec, from[0]);
-            } else {
-                const u32x4 a = from[0], b = from[1];
-                r.v = __builtin_bit_cast(typename Eight<T>::vec, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e < n) r.v[e] = row[c + e];
-    }
     return r;
 }
 template <typename T> __device__ __forceinline__ void terms8(const Eight<T> &x, bf16x8 (&o)[Terms<T>::n])
@@ -200,20 +165,6 @@ template <int PLANES, int ROWS, int COLS> struct Tile {
             const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + i * plane + 4 * pitch));
             o[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
-    }
-    // Four values side by side in a row
-    __device__ __forceinline__ void put4(int r, int c, const float (&x)[4]) const
-    {
-        bf16x4 o[PLANES];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            __bf16 t[PLANES];
-            split<PLANES>(x[e], t);
-#pragma unroll
-            for (int i = 0; i < PLANES; ++i) o[i][e] = t[i];
-        }
-#pragma unroll
-        for (int i = 0; i < PLANES; ++i) *reinterpret_cast<bf16x4 *>(at + i * plane + r * pitch + c) = o[i];
     }
     __device__ __forceinline__ void put1(int r, int c, float x) const
     {
