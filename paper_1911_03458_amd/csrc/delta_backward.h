@@ -695,8 +695,8 @@ template <typename T, int KF> hipError_t backward_chunks(DeltaParams p, hipStrea
 {
     constexpr int lds = BackwardLds<T, KF>::bytes;
     static_assert(lds <= 160 * 1024, "");
-    p.width = chunk_width(p);
-    p.slices = (p.Dv + p.width - 1) / p.width;
+    p.width = delta_width(p.B * p.H, p.Dv, 0);
+    p.slices = delta_slices(p.width, p.Dv, 0);
     const unsigned grid = (unsigned)(p.B * p.H * p.slices);
     if (p.wide_qk) merit_delta_back_chunks<T, KF, true><<<grid, CHUNK_THREADS, lds, s>>>(p);
     else merit_delta_back_chunks<T, KF, false><<<grid, CHUNK_THREADS, lds, s>>>(p);

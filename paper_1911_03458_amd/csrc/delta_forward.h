@@ -225,7 +225,9 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 // for what the first half's tokens leave for the second's, and for what both leave for the state.  LDS holds the other operands, K, Q and the two triangular
 // matrices, for the eight wavefronts of a workgroup; the next chunk's are on their way in registers meanwhile.
 // Bound by the chain of a chunk's products and barriers, 4.2 us whatever else a compute unit has to do: bfloat16, states of 128 x 128,
-// 16 heads of 8191 tokens 535 us, 128 heads of 2048 with the states kept 262 us (0.79 GB, 3.0 TB/s; matrix cores 18 % busy).
+// 16 heads of 8191 tokens 533 us, 128 heads of 2048 with the states kept 262 us (0.79 GB, 3.0 TB/s; matrix cores 18 % busy).  Few long
+// sequences go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from
+// their first states on).
 constexpr int CHUNK_THREADS = 512;
 template <typename T, int KF> struct ForwardLds {
     static constexpr int NK = Terms<T>::n, NP = mix_terms<T>();
@@ -236,12 +238,21 @@ template <typename T, int KF> struct ForwardLds {
     static constexpr int pair = (8 + 3 + NP) * 1024, hand = shared ? q : q + Keys<NK, KF * 32>::bytes;
     static constexpr int bytes = hand + 4 * pair > q + Keys<NK, KF * 32>::bytes ? hand + 4 * pair : q + Keys<NK, KF * 32>::bytes;
 };
+// Where a segment's first state is, and the transition of one that is neither the first nor the last
+__device__ __forceinline__ float *segment_state(const DeltaParams &p, int seg) { return p.seg_state + seg * p.B * p.H * p.Dk * p.Dv; }
+__device__ __forceinline__ float *segment_through(const DeltaParams &p, int seg)
+{
+    return p.seg_state + delta_segment_floats(p, p.segments, seg - 1);
+}
+// What a launch leaves: y and the last state, besides what the backward pass takes, or nothing but what a segment does to a state
+enum Leaves { RESULTS, KEPT, SEGMENT };
 // (a half at a time is compiled: every place in LDS is then a lane's base and a constant)
-template <typename T, int KF, bool WIDE, bool KEEP, int half>
+template <typename T, int KF, bool WIDE, Leaves LEAVES, int half>
 __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem, int *lost)
 {
     typedef ForwardLds<T, KF> L;
     constexpr int NK = L::NK, NP = L::NP, ORD = NP, KO = KF < 2 ? 1 : KF / 2;
+    constexpr bool KEEP = LEAVES == KEPT, PASS = LEAVES == SEGMENT;
     char *const lds = reinterpret_cast<char *>(smem);
     const Keys<NK, KF * 32> kt{reinterpret_cast<__bf16 *>(lds + L::k)}, qt{reinterpret_cast<__bf16 *>(lds + L::q)};
     const Triangle<3> wt{reinterpret_cast<__bf16 *>(lds + L::w)};
@@ -256,8 +267,14 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
     // old value: in fp32 with rows off 16 bytes and states kept, rows moved by wavefronts without columns were wrong.)
     const int tid = threadIdx.x, lane = tid & 63, tile = __builtin_amdgcn_readfirstlane(tid >> 6 & 3), l16 = lane & 15, quad = lane >> 4;
     const int64_t head = b * p.H + h, Dv = p.Dv;
-    const int c0 = (int)(id % (uint32_t)p.slices) * p.width, c = c0 + 16 * tile + l16;
-    const bool busy = 16 * tile < p.width && c0 + 16 * tile < Dv, in = busy && c < Dv, has = half < KF;
+    // a segment of the sequence's chunks; its transition, what comes of the unit matrix where v is zeros, has slices behind those of v
+    const int seg = (int)blockIdx.y, i0 = seg * p.seg_chunks, i1 = min(n, i0 + p.seg_chunks), last = n > 0 ? (n - 1) / p.seg_chunks : 0;
+    const int slice = (int)(id % (uint32_t)p.slices), of_v = (p.Dv + p.width - 1) / p.width;
+    const bool through = PASS && slice >= of_v;
+    const int64_t cols = through ? p.Dk : Dv;
+    const int c0 = (slice - (through ? of_v : 0)) * p.width, c = c0 + 16 * tile + l16;
+    const bool busy = 16 * tile < p.width && c0 + 16 * tile < cols, in = busy && c < cols, has = half < KF;
+    if (PASS ? through && (seg == 0 || seg >= last) : seg > last) return;
     f32x4 *const to_me = reinterpret_cast<f32x4 *>(lds + L::hand + tile * L::pair + half * 4096) + lane;
     f32x4 *const to_other = reinterpret_cast<f32x4 *>(lds + L::hand + tile * L::pair + (1 - half) * 4096) + lane;
     bf16x8 *const first = reinterpret_cast<bf16x8 *>(lds + L::hand + tile * L::pair) + lane;                  // b x of the first
@@ -268,8 +285,18 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
 #pragma unroll
     for (int o = 0; o < KO; ++o) {
         const int dk = 32 * (half + 2 * o);
-        get_rows(S[o], p.h0 ? p.h0 + (head * p.Dk + dk) * Dv + c : nullptr, p.Dk - dk, Dv, in);
+        // (later segments start from what merit_delta_join left, and the first from a copy: h_last may be h0)
+        const float *from = p.h0;
+        if (PASS && seg > 0) from = nullptr;
+        if (!PASS && (seg > 0 || (p.segments > 1 && p.h0))) from = segment_state(p, seg);
+        get_rows(S[o], from ? from + (head * p.Dk + dk) * Dv + c : nullptr, p.Dk - dk, Dv, in && !through);
+        if (PASS && seg == 0 && p.h0 && has)
+            put_rows(S[o], segment_state(p, 0) + (head * p.Dk + dk) * Dv + c, p.Dk - dk, Dv, in);
+        if (through)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) S[o][k >> 2][k & 3] = dk + 8 * quad + k == c ? 1.0f : 0.0f;
     }
+    if (PASS && seg >= last) return;
     const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);         // (a lane without a column: any that is there)
     // (the first half's wavefronts, which wait for the others later, move what the next chunk needs)
     ChunkRows<T, KF, NT> kr, qr;
@@ -280,10 +307,10 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
     auto load = [&](int i, auto full) __attribute__((always_inline)) {
         const int m = min(C, len - i * C);
         kr.template load<full.value, WIDE>(p.k, b, (int64_t)i * C, m, kh, p.Dk);
-        qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
+        if (!PASS) qr.template load<full.value, WIDE>(p.q, b, (int64_t)i * C, m, kh, p.Dk);
         const Prepared from = prepared(p, (b * p.n + i) * p.H + h);
         wr.load(from.w);
-        mr.load(from.mix);
+        if (!PASS) mr.load(from.mix);
         sr = reinterpret_cast<const f32x4 *>(from.scal)[tid % (SCALAR_FLOATS / 4)];
     };
     auto load_v = [&](int i, auto full) __attribute__((always_inline)) {
@@ -331,9 +358,11 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
         const int m = min(C, len - i * C);
         if constexpr (half == 0) {
             kr.template store<full.value, WIDE>(kt, m, p.Dk);
-            qr.template store<full.value, WIDE>(qt, m, p.Dk);
             wr.store(wt);
-            mr.store(mt);
+            if (!PASS) {
+                qr.template store<full.value, WIDE>(qt, m, p.Dk);
+                mr.store(mt);
+            }
             if (tid < SCALAR_FLOATS / 4) reinterpret_cast<f32x4 *>(sc)[tid] = sr;
         }
         __syncthreads();
@@ -352,6 +381,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 operand<3>(S[o][0], S[o][1], s);
                 multiply_rows<3>(X, a, s);
                 __builtin_amdgcn_sched_barrier(0);
+                if (PASS) continue;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) qt.rows(half ^ (k >> 1), k & 1, half + 2 * o, a[k]);
                 multiply_rows<3>(Y, a, s);
@@ -361,8 +391,10 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
         if (busy) {
             to_other[0] = X[2];
             to_other[64] = X[3];
-            to_other[128] = Y[2];
-            to_other[192] = Y[3];
+            if (!PASS) {
+                to_other[128] = Y[2];
+                to_other[192] = Y[3];
+            }
         }
         __syncthreads();
 
@@ -377,11 +409,12 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
             for (int k = 0; k < 2; ++k) {
                 const f32x4 sum = X[k] + to_me[64 * k];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) D[k][r] = fmaf(-in_k[k][r], sum[r], v.value(k, r));
+                for (int r = 0; r < 4; ++r) D[k][r] = fmaf(-in_k[k][r], sum[r], through ? 0.0f : v.value(k, r));
                 O[k] = beta[k] * D[k];
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) Y[k] += to_me[128 + 64 * k];
+            for (int k = 0; k < 2; ++k)
+                if (!PASS) Y[k] += to_me[128 + 64 * k];
             if constexpr (full.value) load_v(then, full);
             finite(O);
             operand<3>(O[0], O[1], x);
@@ -395,7 +428,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
 #pragma unroll
             for (int k = 0; k < 2; ++k) O[k] = out_k[k] * U[k];
             operand<3>(O[0], O[1], w);
-            operand<NP>(U[0], U[1], u);
+            if (!PASS) operand<NP>(U[0], U[1], u);
         };
         if (busy && half == 0) {
             const int from = lost[16 * tile + l16];
@@ -407,7 +440,8 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 third[64 * k] = w[k];
             }
 #pragma unroll
-            for (int k = 0; k < NP; ++k) third[192 + 64 * k] = u[k];
+            for (int k = 0; k < NP; ++k)
+                if (!PASS) third[192 + 64 * k] = u[k];
         }
         __syncthreads();
         // the state before the chunk is not needed any more, but by those who keep it
@@ -439,10 +473,11 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
             if constexpr (full.value) load(then, full);
             if (busy) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k) Y[k] *= scalar(IN_Q, k);
+                for (int k = 0; k < 2; ++k)
+                    if (!PASS) Y[k] *= scalar(IN_Q, k);
                 fade();
                 into_state(0, w);
-                results();
+                if (!PASS) results();
             }
         } else if (busy) {
             bf16x8 x0[3], a[2][3];
@@ -470,17 +505,19 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 fade();
                 into_state(1, w);
                 into_state(0, w0);
+                if constexpr (!PASS) {
 #pragma unroll
-                for (int k = 0; k < NP; ++k) u0[k] = third[192 + 64 * k];
-                mt.rows(1, 0, 0, a[0]);
-                mt.rows(1, 1, 0, a[1]);
-                f32x4 y[2];
+                    for (int k = 0; k < NP; ++k) u0[k] = third[192 + 64 * k];
+                    mt.rows(1, 0, 0, a[0]);
+                    mt.rows(1, 1, 0, a[1]);
+                    f32x4 y[2];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) y[k] = Y[k] * scalar(IN_Q, k);
-                multiply_rows<ORD>(y, a, u0);
-                Y[0] = y[0];
-                Y[1] = y[1];
-                results();
+                    for (int k = 0; k < 2; ++k) y[k] = Y[k] * scalar(IN_Q, k);
+                    multiply_rows<ORD>(y, a, u0);
+                    Y[0] = y[0];
+                    Y[1] = y[1];
+                    results();
+                }
             }
             if (lost[16 * tile + l16] < C)
 #pragma unroll
@@ -491,17 +528,29 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
         __syncthreads();
     };
     if (tid < 64) lost[tid] = C;
-    const int whole_chunks = len / C;
-    if (whole_chunks > 0) {
-        if constexpr (half == 0) load(0, std::true_type());
-        load_v(0, std::true_type());
-        for (int i = 0; i < whole_chunks; ++i) step(i, min(i + 1, whole_chunks - 1), std::true_type());    // (the last one's again: no branch)
+    const int whole = min(len / C, i1);                     // (the chunks from there on: at most one, the sequence's last)
+    if (whole > i0) {
+        if constexpr (half == 0) load(i0, std::true_type());
+        load_v(i0, std::true_type());
+        for (int i = i0; i < whole; ++i) step(i, min(i + 1, whole - 1), std::true_type());      // (the last one's again: no branch)
     }
-    if (whole_chunks < n) {
+    if constexpr (PASS) {
+        const int64_t line = through ? delta_pitch(p) : Dv;
+        float *const to = through ? segment_through(p, seg) + head * p.Dk * delta_pitch(p) : segment_state(p, seg + 1) + head * p.Dk * Dv;
+        if (has)
+#pragma unroll
+            for (int o = 0; o < KO; ++o) {
+                const int dk = 32 * (half + 2 * o);
+                put_rows(S[o], to + dk * line + c, p.Dk - dk, line, in);
+            }
+        return;
+    }
+    if (whole < i1) {
         if constexpr (half == 0) load(n - 1, std::false_type());
         load_v(n - 1, std::false_type());
         step(n - 1, n - 1, std::false_type());
     }
+    if (seg < last) return;
     if (p.h_last && has)
 #pragma unroll
         for (int o = 0; o < KO; ++o) {
@@ -509,19 +558,73 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
             put_rows(S[o], p.h_last + (head * p.Dk + dk) * Dv + c, p.Dk - dk, Dv, in);
         }
     // zeros behind the sequence's last chunk
-    const int cols = min(p.width, (int)Dv - c0);
-    for (int64_t u = tid; u < (p.L - (int64_t)n * C) * cols; u += CHUNK_THREADS) {
-        const int64_t t = (int64_t)n * C + u / cols;
-        static_cast<T *>(p.y.data)[b * p.y.s0 + t * p.y.s1 + h * Dv + c0 + u % cols] = (T)0.0f;
+    const int wide = min(p.width, (int)Dv - c0);
+    for (int64_t u = tid; u < (p.L - (int64_t)n * C) * wide; u += CHUNK_THREADS) {
+        const int64_t t = (int64_t)n * C + u / wide;
+        static_cast<T *>(p.y.data)[b * p.y.s0 + t * p.y.s1 + h * Dv + c0 + u % wide] = (T)0.0f;
     }
 }
-template <typename T, int KF, bool WIDE, bool KEEP>
+template <typename T, int KF, bool WIDE, Leaves LEAVES>
 __global__ __launch_bounds__(CHUNK_THREADS, 2) void merit_delta_chunks(DeltaParams p)
 {
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
     __shared__ int lost[64];
-    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) forward_half<T, KF, WIDE, KEEP, 0>(p, smem, lost);
-    else forward_half<T, KF, WIDE, KEEP, 1>(p, smem, lost);
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) forward_half<T, KF, WIDE, LEAVES, 0>(p, smem, lost);
+    else forward_half<T, KF, WIDE, LEAVES, 1>(p, smem, lost);
+}
+
+// The states that segments start from, one after the other: S <- A S + E, with the segment's transition A and what it makes of a state
+// of zeros, E, in whose place the result goes.  A workgroup 16 columns of a head, a wavefront 16 rows; fp32 products, and the next
+// segment's A and E are asked for before this one's are used.  Bound by the latency of those loads, 3 us a segment.
+template <typename T> __global__ __launch_bounds__(CHUNK_THREADS) void merit_delta_join(DeltaParams p)
+{
+    constexpr int KEYS = MERIT_DELTA_MAX_KEYS;
+    static_assert(CHUNK_THREADS / 64 * 16 == KEYS, "");
+    __shared__ float s[KEYS][16];
+    const int tiles = (p.Dv + 15) / 16, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15,
+              quad = lane >> 4;
+    const int64_t head = blockIdx.x / (uint32_t)tiles;
+    const int c = (int)(blockIdx.x % (uint32_t)tiles) * 16 + l16, n = (tokens_of(p, head / p.H) + C - 1) / C;
+    const int last = n > 0 ? (n - 1) / p.seg_chunks : 0, row = min(16 * wave + l16, p.Dk - 1), r0 = 16 * wave + 4 * quad;
+    if (last < 2) return;
+    const int64_t column = min(c, p.Dv - 1);                            // (what is not there is read somewhere, and not written)
+    f32x4 a[KEYS / 16];
+    float e[4];
+    const int pitch = delta_pitch(p);
+    auto load = [&](int j) __attribute__((always_inline)) {
+        const float *A = segment_through(p, j) + (head * p.Dk + row) * pitch, *E = segment_state(p, j + 1) + head * p.Dk * p.Dv + column;
+#pragma unroll
+        for (int i = 0; i < KEYS / 16; ++i) a[i] = *reinterpret_cast<const f32x4 *>(A + min(16 * i + 4 * quad, pitch - 4));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = E[(int64_t)min(r0 + i, p.Dk - 1) * p.Dv];
+    };
+    const float *first = segment_state(p, 1) + head * p.Dk * p.Dv + column;
+    for (int r = tid >> 4; r < KEYS; r += CHUNK_THREADS / 16) s[r][l16] = r < p.Dk ? first[(int64_t)r * p.Dv] : 0.0f;
+    load(1);
+    __syncthreads();
+    for (int j = 1; j < last; ++j) {
+        f32x4 acc = {e[0], e[1], e[2], e[3]};
+        f32x4 now[KEYS / 16];
+#pragma unroll
+        for (int i = 0; i < KEYS / 16; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) now[i][k] = 16 * i + 4 * quad + k < p.Dk ? a[i][k] : 0.0f;
+        if (j + 1 < last) load(j + 1);
+#pragma unroll
+        for (int i = 0; i < KEYS / 16; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(now[i][k], s[16 * i + 4 * quad + k][l16], acc, 0, 0, 0);
+        __syncthreads();
+        float *to = segment_state(p, j + 1) + head * p.Dk * p.Dv + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r0 + i < p.Dk) {
+                s[r0 + i][l16] = acc[i];
+                if (c < p.Dv) to[(int64_t)(r0 + i) * p.Dv] = acc[i];
+            }
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -624,32 +727,32 @@ template <typename T, int KF> hipError_t prepare_of(const DeltaParams &p, hipStr
     else merit_delta_prepare<T, KF, false><<<grid, NT, 0, s>>>(p);
     return hipGetLastError();
 }
-// Columns of a workgroup of merit_delta_chunks and merit_delta_back_chunks: 64, or less where a compute unit would go without one.  The
-// operands come into LDS once for a workgroup, and take their time whatever it does with them (bfloat16, 128 x 128, 64 / 32 / 16
-// columns, us: 128 heads of 2048 tokens 241 / 390 / 699, 16 heads of 8191 620 / 570 / 559).
-inline int chunk_width(const DeltaParams &p)
-{
-    for (int w : {64, 32})
-        if (p.B * p.H * ((p.Dv + w - 1) / w) >= 256) return w;
-    return 16;
-}
-template <typename T, int KF> hipError_t forward_of(DeltaParams p, hipStream_t s)
+template <typename T, int KF, Leaves LEAVES> hipError_t chunks_of(const DeltaParams &p, int segments, hipStream_t s)
 {
     constexpr int lds = ForwardLds<T, KF>::bytes;
     static_assert(lds + 256 <= 160 * 1024, "");
+    const dim3 grid((unsigned)(p.B * p.H * p.slices), (unsigned)segments);
+    if (p.wide_qk) merit_delta_chunks<T, KF, true, LEAVES><<<grid, CHUNK_THREADS, lds, s>>>(p);
+    else merit_delta_chunks<T, KF, false, LEAVES><<<grid, CHUNK_THREADS, lds, s>>>(p);
+    return hipGetLastError();
+}
+template <typename T, int KF> hipError_t forward_of(DeltaParams p, hipStream_t s)
+{
     p.mix_terms = p.states ? 3 : mix_terms<T>();
     if (hipError_t e = prepare_of<T, KF>(p, s)) return e;
-    p.width = chunk_width(p);
-    p.slices = (p.Dv + p.width - 1) / p.width;
-    const unsigned grid = (unsigned)(p.B * p.H * p.slices);
-    if (p.wide_qk) {
-        if (p.states) merit_delta_chunks<T, KF, true, true><<<grid, CHUNK_THREADS, lds, s>>>(p);
-        else merit_delta_chunks<T, KF, true, false><<<grid, CHUNK_THREADS, lds, s>>>(p);
-    } else {
-        if (p.states) merit_delta_chunks<T, KF, false, true><<<grid, CHUNK_THREADS, lds, s>>>(p);
-        else merit_delta_chunks<T, KF, false, false><<<grid, CHUNK_THREADS, lds, s>>>(p);
+    if (p.segments > 1) {
+        DeltaParams o = p;
+        o.width = delta_width(p.B * p.H * (p.segments - 1), p.Dv, p.Dk);
+        o.slices = delta_slices(o.width, p.Dv, p.Dk);
+        if (hipError_t e = chunks_of<T, KF, SEGMENT>(o, p.segments - 1, s)) return e;
+        if (p.segments > 2) {
+            merit_delta_join<T><<<(unsigned)(p.B * p.H * ((p.Dv + 15) / 16)), CHUNK_THREADS, 0, s>>>(p);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
     }
-    return hipGetLastError();
+    p.width = delta_width(p.B * p.H * p.segments, p.Dv, 0);
+    p.slices = delta_slices(p.width, p.Dv, 0);
+    return p.states ? chunks_of<T, KF, KEPT>(p, p.segments, s) : chunks_of<T, KF, RESULTS>(p, p.segments, s);
 }
 template <typename T> hipError_t forward_typed(const DeltaParams &p, hipStream_t s)
 {

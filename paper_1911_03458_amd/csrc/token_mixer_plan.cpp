@@ -16,19 +16,48 @@ Rows rows_of(Views &v, const merit_view &view, int type, bool required)
 }
 
 // ---- gated delta rule ------------------------------------------------------------------------
+// Segments of a sequence's chunks side by side, where heads and sequences leave compute units idle: what a segment does to a state is
+// found first (a launch for all but the last, and a product a segment), then each goes from its own first state.  An estimate, in us:
+// a chunk takes a workgroup of 16, 32 or 64 columns 4.2, 4.9 or 5.9, and without results 3.0, 3.6 or 3.7 (states of 128 x 128,
+// bfloat16, up to 256 workgroups); launches 10, products 3.  16 heads of 8191 tokens in 1, 2, 4, 5, 6 and 8 segments: 533, 450, 283,
+// 243, 283, 242.  Not for less than a fifth.
+void delta_segments(DeltaParams &p)
+{
+    const int64_t heads = p.B * p.H;
+    auto turn = [](int64_t groups, int Dv, int more) {
+        const int w = delta_width(groups, Dv, more);
+        const double us = more ? w == 16 ? 3.0 : w == 32 ? 3.6 : 3.7 : w == 16 ? 4.2 : w == 32 ? 4.9 : 5.9;
+        return us * (double)cdiv(groups * delta_slices(w, Dv, more), 256);
+    };
+    p.segments = 1;
+    p.seg_chunks = p.n > 0 ? p.n : 1;
+    if (heads < 1 || heads > 256) return;
+    double least = 0.8 * p.n * turn(heads, p.Dv, 0);
+    for (int s = 2; s <= 16; ++s) {
+        const int chunks = (int)cdiv(p.n, s);
+        if (chunks < 1 || cdiv(p.n, chunks) != s) continue;
+        const double us = chunks * (turn(heads * s, p.Dv, 0) + turn(heads * (s - 1), p.Dv, p.Dk)) + 10.0 + 3.0 * (s - 2);
+        if (us < least) {
+            least = us;
+            p.segments = s;
+            p.seg_chunks = chunks;
+        }
+    }
+}
 // Floats that the forward pass keeps of a chunk of a head
 int64_t delta_kept(const DeltaParams &p) { return cdiv(DELTA_PREPARED_FLOATS + (int64_t)(p.Dk + MERIT_DELTA_CHUNK) * p.Dv, 4) * 4; }
-// Scratch memory.  Forward: what the chunks' tokens do to each other (a call that keeps states has it there instead).  Backward: x, the
+// Scratch memory.  Forward: what the chunks' tokens do to each other (a call that keeps states has it there instead), segments' states.  Backward: x, the
 // gradients of the states, and the value heads' parts of dq and dk; each a multiple of 16 bytes but the last.
 struct DeltaScratch {
-    int64_t dx, ds, part, bytes;
+    int64_t seg, dx, ds, part, bytes;
 };
 DeltaScratch delta_scratch(const DeltaParams &p, bool backward)
 {
     const int64_t chunks = p.B * p.n * p.H;
     DeltaScratch s = {};
     if (!backward) {
-        s.bytes = chunks * DELTA_PREPARED_FLOATS * 4;
+        s.seg = chunks * DELTA_PREPARED_FLOATS * 4;
+        s.bytes = s.seg + (p.segments > 1 ? delta_segment_floats(p, p.segments, p.segments - 2) * 4 : 0);
         return s;
     }
     s.ds = s.dx + chunks * MERIT_DELTA_CHUNK * p.Dv * 4;
@@ -114,7 +143,9 @@ merit_status mixer_kernel(const merit_token_plan *plan, merit_pass pass, const c
         *name = backward ? "merit_block_norm_rows_backward+merit_reduce_rows" : "merit_block_norm_rows";
     else
         *name = pass == MERIT_PASS_STEP   ? "merit_delta_token"
-                : !backward               ? "merit_delta_prepare+merit_delta_chunks"
+                : !backward               ? plan->delta.segments < 2   ? "merit_delta_prepare+merit_delta_chunks"
+                                            : plan->delta.segments > 2 ? "merit_delta_prepare+merit_delta_chunks+merit_delta_join+merit_delta_chunks"
+                                                                       : "merit_delta_prepare+merit_delta_chunks+merit_delta_chunks"
                 : plan->delta.each > 1    ? "merit_delta_back_chunks+merit_delta_grads+merit_delta_sum_heads"
                                           : "merit_delta_back_chunks+merit_delta_grads";
     return MERIT_OK;
@@ -150,6 +181,7 @@ merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64
     p.unit = normalize != 0;
     p.type = type;
     p.n = (int)n;
+    delta_segments(p);
     *out = pl;
     return MERIT_OK;
 }
@@ -203,6 +235,7 @@ merit_status merit_delta_rule(const merit_token_plan *plan, const merit_delta_ru
     const merit_status st = scratch(delta_scratch(p, false).bytes, workspace, workspace_bytes);
     if (st != MERIT_OK) return st;
     p.prep = p.states ? p.states : static_cast<float *>(workspace);
+    p.seg_state = static_cast<float *>(workspace) + delta_scratch(p, false).seg / 4;
     p.prep_stride = p.states ? delta_kept(p) : DELTA_PREPARED_FLOATS;
     p.wide_qk = p.Dk % 8 == 0 && in_16_bytes(p.q, p.B, p.L, p.type) && in_16_bytes(p.k, p.B, p.L, p.type);
     return done(launch_delta(p, static_cast<hipStream_t>(stream)));

@@ -105,6 +105,8 @@ struct DeltaParams {
     int type;
     int n;                 // chunks of MERIT_DELTA_CHUNK tokens
     int width, slices;     // columns of v of a workgroup, workgroups along them
+    int segments, seg_chunks;           // forward: segments of a sequence side by side, chunks of one
+    float *seg_state;      // their first states, and the transitions of those between the first and the last
     int wide_qk, wide_v, wide_out, wide_state;      // whether rows can be moved in 16-byte pieces (wide_out: dq, dk)
     Rows q, k, v, y, dy, dq, dk, dv;
     Rows g, beta, dg, dbeta;            // a number a head
@@ -118,6 +120,23 @@ struct DeltaParams {
     float *dx, *ds;        // backward: x of its tokens, the gradient of the state behind it
     float *part;           // dq, dk of a value head, where value heads share keys
 };
+// Floats of a row of a transition (rows start on 16 bytes), and of segments' first states with `transitions` behind them
+__host__ __device__ inline int delta_pitch(const DeltaParams &p) { return (p.Dk + 3) / 4 * 4; }
+__host__ __device__ inline int64_t delta_segment_floats(const DeltaParams &p, int64_t segments, int64_t transitions)
+{
+    return (segments * p.B * p.H * p.Dk * p.Dv + 3) / 4 * 4 + transitions * p.B * p.H * p.Dk * delta_pitch(p);
+}
+// Columns of v (and of a transition) that a workgroup of merit_delta_chunks or merit_delta_back_chunks takes from chunk to chunk, and
+// workgroups along them.  LDS has room for one workgroup a compute unit: as few columns as leave none a second one
+// (bfloat16, 128 x 128, 64 / 32 / 16 columns, us: 128 heads of 2048 tokens 241 / 390 / 699, 16 heads of 8191 620 / 570 / 533, those in
+// three segments - / 197 / 353).
+inline int delta_slices(int width, int Dv, int more) { return (Dv + width - 1) / width + (more + width - 1) / width; }
+inline int delta_width(int64_t groups, int Dv, int more)
+{
+    for (int w : {16, 32})
+        if (groups * delta_slices(w, Dv, more) <= 256) return w;
+    return 64;
+}
 constexpr int DELTA_SCALAR_FLOATS = 8 * MERIT_DELTA_CHUNK;
 constexpr int DELTA_PREPARED_FLOATS = DELTA_SCALAR_FLOATS + 2 * 3 * (MERIT_DELTA_CHUNK * MERIT_DELTA_CHUNK * 3 / 4) / 2;
 static_assert(DELTA_PREPARED_FLOATS == MERIT_DELTA_KEPT, "");

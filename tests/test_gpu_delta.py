@@ -235,6 +235,60 @@ def test_nothing_fades_before_the_first_token(mb, L):
         near(dg, want["dg"], DECAY, "dg", floor=float(np.sqrt(np.mean(want["dbeta"] ** 2))))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape, lens", [((1, 1500, 1, 1, 32, 32), None), ((1, 700, 1, 1, 128, 70), None), ((1, 1025, 2, 2, 5, 9), None),
+                                         ((3, 1100, 2, 1, 42, 25), [1100, 512, 130]), ((4, 1100, 1, 1, 64, 48), [0, 1, 385, 1099])])
+def test_segments_of_few_sequences(mb, shape, lens, dtype):
+    """Long sequences of few heads go in segments side by side: sequences that end in any of them, the last state in the first one's
+    place, states kept for the backward pass, equal bits on a second call."""
+    B, L, H, K, Dk, Dv = shape
+    a, g = _inputs(shape, dtype, sum(shape))
+    plan, h0 = _plan(mb, shape, dtype), g.normal(B, H, Dk, Dv)
+    assert "merit_delta_join" in plan.kernel()
+    n = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    how = dict(lens=lens, scale=Dk ** -0.5)
+    for h in (None, h0):
+        wy, wh, _ = om.delta_rule(**_h(a), h0=None if h is None else host(h), **how)
+        y, end = mb.merit_delta_rule(plan, *a.values(), h0=h, lens=n, final=True)
+        near(y, wy, y_of(str(y.dtype)), "y")
+        near(end, wh, DELTA, "state")
+    again = h0.clone()
+    y2, end2 = mb.merit_delta_rule(plan, *a.values(), h0=again, lens=n, final=again)
+    assert end2 is again and torch.equal(y2, y) and torch.equal(end2, end)
+    y3, st = mb.merit_delta_rule(plan, *a.values(), h0=h0, lens=n, states=True)
+    near(y3, wy, y_of(str(y.dtype)), "y with states")
+    dy = g.normal(B, L, H, Dv, dtype=TYPES[dtype][0])
+    got = mb.merit_delta_rule_backward(plan, dy, a["q"], a["k"], a["g"], a["beta"], st, lens=n, dh0=True)
+    want = om.delta_rule_backward(host(dy), **_h(a), h0=host(h0), **how)
+    for k in ("dq", "dk", "dv", "dg", "dbeta", "dh0"):
+        near(got[k], want[k], DECAY if k == "dg" else GRAD, k, floor=float(np.sqrt(np.mean(want["dbeta"] ** 2))) if k == "dg" else 0.0)
+
+
+def test_segments_and_what_is_not_finite(mb):
+    """A value's NaN stays in its column through later segments, a key's in its head; a decay of zero in a segment empties the state."""
+    shape = (1, 1500, 2, 2, 32, 32)
+    a, _ = _inputs(shape, "f32", 61)
+    plan = _plan(mb, shape, "f32")
+    assert "merit_delta_join" in plan.kernel()
+    y, h = mb.merit_delta_rule(plan, *a.values(), final=True)
+    for name in ("v", "k", "beta"):
+        b = {k: t.clone() for k, t in a.items()}
+        (b[name][0, 300, 0, 7:8] if name != "beta" else b[name][0, 300, 0:1]).fill_(float("nan"))
+        y2, h2 = mb.merit_delta_rule(plan, *b.values(), final=True)
+        assert torch.equal(y2[:, :300], y[:, :300]) and torch.equal(y2[:, :, 1], y[:, :, 1]) and torch.equal(h2[:, 1], h[:, 1])
+        lost, kept = y2[0, 301:, 0], y[0, 301:, 0]
+        if name == "v":
+            others = [c for c in range(32) if c != 7]
+            assert lost[:, 7].isnan().all() and torch.equal(lost[:, others], kept[:, others]) and h2[0, 0, :, 7].isnan().all()
+        else:
+            assert lost.isnan().all() and h2[0, 0].isnan().all()
+    a["g"][0, 800] = float("-inf")
+    y2, h2 = mb.merit_delta_rule(plan, *a.values(), final=True)
+    wy, wh, _ = om.delta_rule(**_h(a), scale=32 ** -0.5)
+    near(y2, wy, y_of(str(y.dtype)), "y")
+    near(h2, wh, DELTA, "state")
+
+
 @pytest.mark.parametrize("beta_value", [0.0, 1.0, 2.0])
 def test_strengths(mb, beta_value):
     shape = (1, 100, 1, 1, 32, 16)

@@ -115,6 +115,12 @@ def test_scratch_and_kernels():
     plan = mb.merit_plan_delta_rule(mb.MERIT_BF16, 2, 130, 4, 2, 64, 64)
     assert plan.workspace(1) > plan.workspace(0) > 0 and plan.workspace(2) == 0
     assert plan.kernel() == "merit_delta_prepare+merit_delta_chunks"
+    few = mb.merit_plan_delta_rule(mb.MERIT_BF16, 1, 8191, 16, 16, 128, 128)
+    assert few.kernel() == "merit_delta_prepare+merit_delta_chunks+merit_delta_join+merit_delta_chunks"
+    chunks = 128 * 16 * 9728 * 4
+    assert 0 < few.workspace(0) - chunks <= 16 * 4 * 128 * 128 * 2 * 16 and (few.workspace(0) - chunks) % (16 * 128 * 128 * 4) == 0
+    for one in ((8, 2048, 16), (1, 64, 1), (1, 0, 1), (300, 4096, 1)):
+        assert mb.merit_plan_delta_rule(mb.MERIT_F32, one[0], one[1], one[2], one[2], 128, 128).kernel().count("chunks") == 1
     assert plan.kernel(mb.MERIT_PASS_STEP) == "merit_delta_token"
     assert plan.kernel(mb.MERIT_PASS_BACKWARD) == "merit_delta_back_chunks+merit_delta_grads+merit_delta_sum_heads"
     assert mb.merit_plan_delta_rule(mb.MERIT_BF16, 2, 0, 4, 2, 64, 64).workspace(1) == 0
