@@ -224,9 +224,9 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 // in four cycles, 1.4 thousand a chunk; one for all tokens took 1.25 times as long).  They meet for the sums over the state's rows,
 // for what the first half's tokens leave for the second's, and for what both leave for the state.  LDS holds the other operands, K, Q and the two triangular
 // matrices, for the eight wavefronts of a workgroup; the next chunk's are on their way in registers meanwhile.
-// Bound by the chain of a chunk's products and barriers, 4.2 us whatever else a compute unit has to do: bfloat16, states of 128 x 128,
-// 16 heads of 8191 tokens 533 us, 128 heads of 2048 with the states kept 262 us (0.79 GB, 3.0 TB/s; matrix cores 18 % busy).  Few long
-// sequences go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from
+// Bound by the chain of a chunk's products and barriers, bfloat16, states of 128 x 128: 4.2 us a chunk with one pair at work (16 heads
+// of 8191 tokens 533 us), 8 with four in every compute unit, LDS, vector and matrix instructions a quarter of the time each (128 heads
+// of 2048 with the states kept 262 us, 0.79 GB, 3.0 TB/s).  Few long sequences go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from
 // their first states on).
 constexpr int CHUNK_THREADS = 512;
 template <typename T, int KF> struct ForwardLds {
@@ -244,7 +244,7 @@ __device__ __forceinline__ float *segment_through(const DeltaParams &p, int seg)
 {
     return p.seg_state + delta_segment_floats(p, p.segments, seg - 1);
 }
-// What a launch leaves: y and the last state, besides what the backward pass takes, or nothing but what a segment does to a state
+// What a launch leaves: y and the last state; the same, and what the backward pass takes; what a segment does to a state
 enum Leaves { RESULTS, KEPT, SEGMENT };
 // (a half at a time is compiled: every place in LDS is then a lane's base and a constant)
 template <typename T, int KF, bool WIDE, Leaves LEAVES, int half>
