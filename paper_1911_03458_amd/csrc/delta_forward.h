@@ -219,15 +219,16 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 // ---------------------------------------------------------------------------
 // one chunk after the other: two wavefronts 16 columns of a head's state
 // ---------------------------------------------------------------------------
-// The columns of a state do not depend on each other.  Two wavefronts of a SIMD have 16 of them: each one half of a chunk's tokens and
-// every other 32 rows of the state, in registers, so that one issues while the other waits (a wavefront alone issues an instruction
-// in four cycles, 1.4 thousand a chunk; one for all tokens took 1.25 times as long).  They meet for the sums over the state's rows,
-// for what the first half's tokens leave for the second's, and for what both leave for the state.  LDS holds the other operands, K, Q and the two triangular
-// matrices, for the eight wavefronts of a workgroup; the next chunk's are on their way in registers meanwhile.
-// Bound by the chain of a chunk's products and barriers, bfloat16, states of 128 x 128: 4.2 us a chunk with one pair at work (16 heads
-// of 8191 tokens 533 us), 8 with four in every compute unit, LDS, vector and matrix instructions a quarter of the time each (128 heads
-// of 2048 with the states kept 262 us, 0.79 GB, 3.0 TB/s).  Few long sequences go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from
-// their first states on).
+// The columns of a state do not depend on each other.  Two wavefronts of a SIMD have 16 of them: each one half of a chunk's
+// tokens and every other 32 rows of the state, in registers, so that one issues while the other waits (a wavefront alone issues
+// an instruction in four cycles, 1.4 thousand a chunk; one for all tokens took 1.25 times as long).  They meet for the sums over
+// the state's rows, for what the first half's tokens leave for the second's, and for what both leave for the state.  LDS holds
+// the other operands, K, Q and the two triangular matrices, for the eight wavefronts of a workgroup; the next chunk's are on
+// their way in registers meanwhile. Bound by the chain of a chunk's products and barriers, bfloat16, states of 128 x 128: 4.2 us
+// a chunk with one pair at work (16 heads of 8191 tokens 533 us), 8 with four in every compute unit, LDS, vector and matrix
+// instructions a quarter of the time each (128 heads of 2048 with the states kept 262 us, 0.79 GB, 3.0 TB/s).  Few long sequences
+// go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from their
+// first states on).
 constexpr int CHUNK_THREADS = 512;
 template <typename T, int KF> struct ForwardLds {
     static constexpr int NK = Terms<T>::n, NP = mix_terms<T>();
@@ -631,7 +632,8 @@ template <typename T> __global__ __launch_bounds__(CHUNK_THREADS) void merit_del
 // one token
 // ---------------------------------------------------------------------------
 // Bound by memory: the state is read once and held in registers.  y = q.S_t = a q.S_{t-1} + (q.k) u, so both sums over the
-// state's rows come from the one pass (512 states of 128 x 128: 16.2 us, 4.1 TB/s; 4 of 64 x 64: 6.5, the launch).  A workgroup has `lanes` vectors of V columns, NT / lanes threads share a column's rows.
+// state's rows come from the one pass (512 states of 128 x 128: 16.2 us, 4.1 TB/s; 4 of 64 x 64: 6.5, the launch).  A workgroup
+// has `lanes` vectors of V columns, NT / lanes threads share a column's rows.
 template <typename T, int V, int ROWS>
 __global__ __launch_bounds__(NT) void merit_delta_token(DeltaParams p, int lanes, int tiles)
 {

@@ -128,6 +128,43 @@ def test_under_capture(mb):
             assert _same(out, want), i
 
 
+def test_segments_under_capture_and_on_two_streams(mb):
+    """A long sequence in segments, its last state in place of the first: two graphs and two streams, each with scratch memory of its
+    own, and every replay as the eager call."""
+    g, B, L, H, D = Gen(71), 1, 1500, 2, 48
+    plan = mb.merit_plan_delta_rule(mb.MERIT_F32, B, L, H, H, D, D)
+    assert "merit_delta_join" in plan.kernel()
+    inputs = [(g.normal(B, L, H, D), g.normal(B, L, H, D), g.normal(B, L, H, D), -g.uniform(B, L, H, lo=0.0, hi=0.1),
+               g.uniform(B, L, H, lo=0.1, hi=0.9)) for _ in range(2)]
+    first = g.normal(B, H, D, D)
+
+    def run(i, h):
+        return mb.merit_delta_rule(plan, *inputs[i], h0=h, final=h)
+
+    want = [run(i, first.clone()) for i in range(2)]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for i, side in enumerate(streams):
+            with torch.cuda.stream(side):
+                got.append((i, run(i, first.clone())))
+    torch.cuda.synchronize()
+    assert all(_same(out, want[i]) for i, out in got)
+    graphs = []
+    for i in range(2):
+        graph, h = torch.cuda.CUDAGraph(), first.clone()
+        with torch.cuda.graph(graph):
+            out = run(i, h)
+        graphs.append((graph, out, h))
+    for _ in range(3):
+        for i, (graph, out, h) in enumerate(graphs):
+            h.copy_(first)
+            torch.randn(1000, device=DEV).sum().item()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert _same(out, want[i])
+
+
 def test_scratch_memory_is_handed_back(mb):
     run = _block(mb)
     run()
