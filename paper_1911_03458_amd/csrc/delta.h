@@ -36,10 +36,6 @@ template <typename T> struct Terms { static constexpr int n = 3; };
 template <> struct Terms<f16_t> { static constexpr int n = 2; };
 template <> struct Terms<bf16_t> { static constexpr int n = 1; };
 
-// Terms of P and u where they give y, which is rounded to T: two leave 2^-17, next to the 2^-12 of a rounding to binary16 (the
-// gradients that P gives go on into sums in fp32: three)
-template <typename T> constexpr int mix_terms() { return Terms<T>::n == 3 ? 3 : 2; }
-
 template <int N> __device__ __forceinline__ void split(float x, __bf16 (&o)[N])
 {
     o[0] = (__bf16)x;
@@ -285,7 +281,7 @@ template <int PLANES, int THREADS> struct TriangleRows {
 };
 // What merit_delta_prepare leaves of a chunk of a head
 struct Prepared {
-    __bf16 *w, *mix;        // -W and P, three terms each (of P two, where nothing but y of a 16-bit type is made of it)
+    __bf16 *w, *mix;        // -W and P, three terms each
     float *scal;
 };
 constexpr int PREPARED_FLOATS = DELTA_PREPARED_FLOATS;

@@ -145,7 +145,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         if (jb <= (wave | 1))
 #pragma unroll
             for (int k = 0; k < 3; ++k)
-                if (k < p.mix_terms) *reinterpret_cast<bf16x4 *>(to.mix + k * TRIANGLE + triangle_at(t, j0)) = out[k];
+                *reinterpret_cast<bf16x4 *>(to.mix + k * TRIANGLE + triangle_at(t, j0)) = out[k];
     }
     __syncthreads();
 
@@ -228,16 +228,18 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 // a chunk with one pair at work (16 heads of 8191 tokens 533 us), 8 with four in every compute unit, LDS, vector and matrix
 // instructions a quarter of the time each (128 heads of 2048 with the states kept 262 us, 0.79 GB, 3.0 TB/s).  Few long sequences
 // go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from their
-// first states on).
+// first states on).  P and u go into y with three terms as everything else does: two, enough for the rounding of a 16-bit y itself, lost
+2^-17 of each of a sum's terms, which shows where they cancel (128 heads of 2048, no states kept: 246 against 259 us a call).
 constexpr int CHUNK_THREADS = 512;
 template <typename T, int KF> struct ForwardLds {
-    static constexpr int NK = Terms<T>::n, NP = mix_terms<T>();
-    static constexpr int k = 0, w = k + Keys<NK, KF * 32>::bytes, mix = w + Triangle<3>::bytes, scal = mix + Triangle<NP>::bytes,
-                         q = scal + SCALAR_FLOATS * 4;
+    static constexpr int NK = Terms<T>::n;
+    static constexpr int k = 0, w = k + Keys<NK, KF * 32>::bytes, mix = w + Triangle<3>::bytes, scal = mix + Triangle<3>::bytes,
+                         q = scal + SCALAR_FLOATS * 4, past_q = q + Keys<NK, KF * 32>::bytes;
     // what the wavefronts of a pair hand each other: 4 KB to each, w and u of the first; where LDS is full, in the place of Q
-    static constexpr bool shared = NK == 3 && KF == 4;
-    static constexpr int pair = (8 + 3 + NP) * 1024, hand = shared ? q : q + Keys<NK, KF * 32>::bytes;
-    static constexpr int bytes = hand + 4 * pair > q + Keys<NK, KF * 32>::bytes ? hand + 4 * pair : q + Keys<NK, KF * 32>::bytes;
+    static constexpr int pair = (8 + 3 + 3) * 1024;
+    static constexpr bool shared = past_q + 4 * pair + 256 > 160 * 1024;
+    static constexpr int hand = shared ? q : past_q;
+    static constexpr int bytes = hand + 4 * pair > past_q ? hand + 4 * pair : past_q;
 };
 // Where a segment's first state is, and the transition of one that is neither the first nor the last
 __device__ __forceinline__ float *segment_state(const DeltaParams &p, int seg) { return p.seg_state + seg * p.B * p.H * p.Dk * p.Dv; }
@@ -252,12 +254,11 @@ template <typename T, int KF, bool WIDE, Leaves LEAVES, int half>
 __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem, int *lost)
 {
     typedef ForwardLds<T, KF> L;
-    constexpr int NK = L::NK, NP = L::NP, ORD = NP, KO = KF < 2 ? 1 : KF / 2;
+    constexpr int NK = L::NK, KO = KF < 2 ? 1 : KF / 2;
     constexpr bool KEEP = LEAVES == KEPT, PASS = LEAVES == SEGMENT;
     char *const lds = reinterpret_cast<char *>(smem);
     const Keys<NK, KF * 32> kt{reinterpret_cast<__bf16 *>(lds + L::k)}, qt{reinterpret_cast<__bf16 *>(lds + L::q)};
-    const Triangle<3> wt{reinterpret_cast<__bf16 *>(lds + L::w)};
-    const Triangle<NP> mt{reinterpret_cast<__bf16 *>(lds + L::mix)};
+    const Triangle<3> wt{reinterpret_cast<__bf16 *>(lds + L::w)}, mt{reinterpret_cast<__bf16 *>(lds + L::mix)};
     float *const sc = reinterpret_cast<float *>(lds + L::scal);
 
     const uint32_t id = blockIdx.x, h = id / (uint32_t)p.slices % (uint32_t)p.H;
@@ -301,8 +302,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
     const int64_t mine = h * Dv + min((int64_t)c, Dv - 1);         // (a lane without a column: any that is there)
     // (the first half's wavefronts, which wait for the others later, move what the next chunk needs)
     ChunkRows<T, KF, NT> kr, qr;
-    TriangleRows<3, NT> wr;
-    TriangleRows<NP, NT> mr;
+    TriangleRows<3, NT> wr, mr;
     f32x4 sr;
     ChunkColumn<T, 1> v;
     auto load = [&](int i, auto full) __attribute__((always_inline)) {
@@ -401,7 +401,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
 
         // d = r - W (b r), u, w = what goes into the state: the first half's tokens at once, the second's part of their own
         f32x4 D[2], U[2], O[2];
-        bf16x8 x[3], w[3], u[NP];
+        bf16x8 x[3], w[3], u[3];
         if (busy) {
             bf16x8 a[2][3];
             wt.rows(half, 0, half, a[0]);
@@ -429,7 +429,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
 #pragma unroll
             for (int k = 0; k < 2; ++k) O[k] = out_k[k] * U[k];
             operand<3>(O[0], O[1], w);
-            if (!PASS) operand<NP>(U[0], U[1], u);
+            if (!PASS) operand<3>(U[0], U[1], u);
         };
         if (busy && half == 0) {
             const int from = lost[16 * tile + l16];
@@ -441,7 +441,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 third[64 * k] = w[k];
             }
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
+            for (int k = 0; k < 3; ++k)
                 if (!PASS) third[192 + 64 * k] = u[k];
         }
         __syncthreads();
@@ -460,11 +460,11 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 for (int k = 0; k < 2; ++k) S[o][k] *= whole;
         };
         auto results = [&]() __attribute__((always_inline)) {
-            bf16x8 a[2][NP];
+            bf16x8 a[2][3];
             mt.rows(half, 0, half, a[0]);
             mt.rows(half, 1, half, a[1]);
             f32x4 y[2] = {Y[0], Y[1]};
-            multiply_rows<ORD>(y, a, u);
+            multiply_rows<3>(y, a, u);
             const int from = lost[16 * tile + l16];
             if (__ballot(from < C) != 0) lose(y, from);
             put_column<full.value, T>(y, p.y, b, t0, half, m, (int)min((int64_t)C, p.L - t0), h * Dv + c, in);
@@ -500,7 +500,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 for (int k = 0; k < 3; ++k) w[k] = second[64 * k];
                 into_state(1, w);
             } else {
-                bf16x8 w0[3], u0[NP], a[2][NP];
+                bf16x8 w0[3], u0[3], a[2][3];
 #pragma unroll
                 for (int k = 0; k < 3; ++k) w0[k] = third[64 * k];
                 fade();
@@ -508,13 +508,13 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                 into_state(0, w0);
                 if constexpr (!PASS) {
 #pragma unroll
-                    for (int k = 0; k < NP; ++k) u0[k] = third[192 + 64 * k];
+                    for (int k = 0; k < 3; ++k) u0[k] = third[192 + 64 * k];
                     mt.rows(1, 0, 0, a[0]);
                     mt.rows(1, 1, 0, a[1]);
                     f32x4 y[2];
 #pragma unroll
                     for (int k = 0; k < 2; ++k) y[k] = Y[k] * scalar(IN_Q, k);
-                    multiply_rows<ORD>(y, a, u0);
+                    multiply_rows<3>(y, a, u0);
                     Y[0] = y[0];
                     Y[1] = y[1];
                     results();
@@ -740,7 +740,6 @@ template <typename T, int KF, Leaves LEAVES> hipError_t chunks_of(const DeltaPar
 }
 template <typename T, int KF> hipError_t forward_of(DeltaParams p, hipStream_t s)
 {
-    p.mix_terms = p.states ? 3 : mix_terms<T>();
     if (hipError_t e = prepare_of<T, KF>(p, s)) return e;
     if (p.segments > 1) {
         DeltaParams o = p;

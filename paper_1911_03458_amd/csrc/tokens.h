@@ -116,7 +116,6 @@ struct DeltaParams {
     const int32_t *lens;
     float *prep;           // what merit_delta_prepare leaves of a chunk of a head (in scratch memory, or kept with its state),
     int64_t prep_stride;   // floats from one to the next
-    int mix_terms;         // terms of P to leave
     float *dx, *ds;        // backward: x of its tokens, the gradient of the state behind it
     float *part;           // dq, dk of a value head, where value heads share keys
 };

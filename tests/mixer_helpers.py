@@ -8,7 +8,8 @@ direction on top, 90; for dg, a sum over a chunk of 64 differences of such produ
 for a row's norms and the sums over rows 4 sqrt(terms of a thread or a tree): at most 64.  Held against the root mean square
 of the result (and 8 times that for a single value, where one in a million exceeds five).
 
-y of the 16-bit types has besides what P and u lose, which go into their product as two bfloat16 terms: the second term, at most
+y of the 16-bit types is allowed besides what P and u would lose if they went into their product as two bfloat16 terms (the kernels
+keep three, and test_gpu_delta_digits holds sums that cancel to DELTA): the second term, at most
 2^-8 of the value, is rounded by at most 2^-8 of itself, so 2^-16 of the value is lost at most and, for mantissas and remainders
 spread evenly, 2^-17 / sqrt(3) on average (root mean square); the product of two second terms, left out, is as much again.  These
 are relative to each term of a sum, so a sum of terms of either sign has as much of its own root mean square: together
