@@ -229,7 +229,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 // instructions a quarter of the time each (128 heads of 2048 with the states kept 262 us, 0.79 GB, 3.0 TB/s).  Few long sequences
 // go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from their
 // first states on).  P and u go into y with three terms as everything else does: two, enough for the rounding of a 16-bit y itself, lost
-2^-17 of each of a sum's terms, which shows where they cancel (128 heads of 2048, no states kept: 246 against 259 us a call).
+// 2^-17 of each of a sum's terms, which shows where they cancel (128 heads of 2048, no states kept: 246 against 259 us a call).
 constexpr int CHUNK_THREADS = 512;
 template <typename T, int KF> struct ForwardLds {
     static constexpr int NK = Terms<T>::n;
