@@ -443,15 +443,22 @@ enum { IN_K = 0,        // exp(G) / |k|
        IN_Q = 3,        // scale exp(G) / |q|
        INV_K = 4, INV_Q = 5,                    // 1 / |k|, 1 / |q| (1 where they are taken as they are)
        SCALARS = 6 };
-constexpr int SCALAR_FLOATS = DELTA_SCALAR_FLOATS;      // and G in 64 bits behind them
+constexpr int SCALAR_FLOATS = DELTA_SCALAR_FLOATS;      // and G, to base 2 and in 64 bits, behind them
 static_assert(SCALAR_FLOATS == SCALARS * C + 2 * C, "");
 
 __device__ __forceinline__ int tokens_of(const DeltaParams &p, int64_t b)
 {
     return p.lens ? min(max((int)p.lens[b], 0), (int)p.L) : (int)p.L;
 }
-// exp(x) of a difference of two 64-bit sums
-__device__ __forceinline__ float exp_of(double x) { return __builtin_amdgcn_exp2f((float)(x * 1.44269504088896340736)); }
+// A decay's logarithm to base 2, in 64 bits.  (No decay of fp32 is below exp(-1000); -inf, which has no differences, included.)
+__device__ __forceinline__ double log2_decay(float g) { return 1.44269504088896340736 * (g < -1000.0f ? -1000.0 : (double)g); }
+// 2^x of a difference of sums of those.  The whole part goes into the exponent: rounded to fp32 with it, x would lose the digits that
+// make the fraction's (44 x 2^-24 of 2^-86).
+__device__ __forceinline__ float exp2_of(double x)
+{
+    const double whole = __builtin_rint(x);
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(x - whole)), (int)fmin(whole, 2000.0));
+}
 
 }  // namespace delta
 }  // namespace merit

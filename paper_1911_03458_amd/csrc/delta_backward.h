@@ -119,7 +119,7 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
             }
         // exp(G_C) Z + Q^T (i dy); what Z was goes to memory
         auto fade = [&]() __attribute__((always_inline)) {
-            const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
+            const float whole = exp2_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
 #pragma unroll
             for (int o = 0; o < KO; ++o) {
                 const int dk = 32 * (half + 2 * o);
@@ -504,7 +504,7 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = 16 * own + 4 * quad + r;
-                const float f = c <= t ? exp_of(gt[r] - gc) * ck : 0.0f;
+                const float f = c <= t ? exp2_of(gt[r] - gc) * ck : 0.0f;
                 dP[j][r] = c <= t ? f * tq[r] * dP[j][r] : 0.0f;
                 dM[j][r] = c < t ? f * tb[r] * dM[j][r] : 0.0f;
                 if (has_p) wt.put1(t, c, dP[j][r]);
@@ -654,7 +654,7 @@ __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(De
                 f += sums[0][w];
                 g += sums[1][w];
             }
-            a += (double)exp_of(G[C - 1]) * f + g;
+            a += (double)exp2_of(G[C - 1]) * f + g;
         }
 #pragma unroll
         for (int k = 1; k < C; k *= 2) {

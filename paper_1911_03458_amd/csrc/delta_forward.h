@@ -48,8 +48,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
         double g = 0.0;
         float bt = 0.0f;
         if (lane < m) {
-            if (p.g.data) g = (double)static_cast<const float *>(p.g.data)[b * p.g.s0 + (t0 + lane) * p.g.s1 + h];
-            if (g < -1000.0) g = -1000.0;       // (no decay of fp32 is that small: -inf, which has no differences, included)
+            if (p.g.data) g = log2_decay(static_cast<const float *>(p.g.data)[b * p.g.s0 + (t0 + lane) * p.g.s1 + h]);
             const int64_t at = b * p.beta.s0 + (t0 + lane) * p.beta.s1 + h;
             bt = p.beta_f32 ? static_cast<const float *>(p.beta.data)[at] : (float)static_cast<const T *>(p.beta.data)[at];
         }
@@ -91,10 +90,10 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 
     if (tid < C) {
         const double g = G[tid], last = G[C - 1];
-        const float in = exp_of(g);
+        const float in = exp2_of(g);
         scal[IN_K * C + tid] = in * invk[tid];
         scal[BETA * C + tid] = beta[tid];
-        scal[OUT_K * C + tid] = exp_of(last - g) * invk[tid];
+        scal[OUT_K * C + tid] = exp2_of(last - g) * invk[tid];
         scal[IN_Q * C + tid] = p.scale * in * invq[tid];
         scal[INV_K * C + tid] = invk[tid];
         scal[INV_Q * C + tid] = invq[tid];
@@ -129,7 +128,7 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int j = j0 + r;
-            const float f = j <= t ? exp_of(gt - G[j]) * lens[r] : 0.0f;
+            const float f = j <= t ? exp2_of(gt - G[j]) * lens[r] : 0.0f;
             float w = j < t ? f * kt_len * kk[r] : 0.0f;
             if (j < t && !isfinite(w * beta[j])) {      // (0 times it would reach the tokens before)
                 atomicMin(&bad, t);
@@ -453,7 +452,7 @@ __device__ __forceinline__ void forward_half(const DeltaParams &p, __bf16 *smem,
                     const int dk = 32 * (half + 2 * o);
                     put_rows(S[o], p.states + chunk * p.prep_stride + PREPARED_FLOATS + dk * Dv + c, p.Dk - dk, Dv, in);
                 }
-            const float whole = exp_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
+            const float whole = exp2_of(reinterpret_cast<const double *>(sc + SCALARS * C)[C - 1]);
 #pragma unroll
             for (int o = 0; o < KO; ++o)
 #pragma unroll
@@ -693,7 +692,7 @@ __global__ __launch_bounds__(NT) void merit_delta_token(DeltaParams p, int lanes
     }
     __syncthreads();
     if (!in) return;
-    const float decay = p.g.data ? exp_of((double)static_cast<const float *>(p.g.data)[b * p.g.s0 + h]) : 1.0f;
+    const float decay = p.g.data ? exp2_of(log2_decay(static_cast<const float *>(p.g.data)[b * p.g.s0 + h])) : 1.0f;
     const int64_t at_beta = b * p.beta.s0 + h;
     const float beta = p.beta_f32 ? static_cast<const float *>(p.beta.data)[at_beta] : (float)static_cast<const T *>(p.beta.data)[at_beta];
     float u[V];

@@ -1,4 +1,4 @@
-"""How many digits the delta rule's fp32 arithmetic keeps, where a result shows them: sums that cancel."""
+"""How many digits the delta rule's fp32 arithmetic keeps, where a result shows them: sums that cancel, decays by themselves."""
 import numpy as np
 import pytest
 
@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 
 from mixer_helpers import DELTA, UNITS          # noqa: E402
 from oracle import mixers as om                 # noqa: E402
-from token_helpers import TYPES, Gen, host      # noqa: E402
+from token_helpers import DEV, TYPES, Gen, host     # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -38,3 +38,39 @@ def test_sums_that_cancel(mb, dtype, Dk, states):
     assert small.sum() >= 100
     err = float(np.sqrt(np.mean((host(y)[:, 16:] - want)[small] ** 2)))
     assert err <= 1.01 * unit * float(np.sqrt(np.mean(want[small] ** 2))) + DELTA * 2.0 ** -24 * size, (err / size * 2 ** 24)
+
+
+def test_decays_by_themselves(mb):
+    """exp(g) to fp32: the exponential function's one step of 2^-23, a rounding of its argument below one, and one of the product.
+    What goes through a product of bfloat16 terms has besides what the third one loses, which lies at 2^-16 of the value: bfloat16 has
+    steps of 2^-133 below 2^-126, so of values below 2^-110 the term loses half such a step where it is rounded (P, in y), up to a
+    whole one where it is cut off (what a state takes up)."""
+    H = 512
+    g = -torch.linspace(0.001, 80.0, H, dtype=torch.float64).float().to(DEV)
+    want = np.exp(host(g))
+
+    def near(got, what, term=0.0):
+        err = np.abs(host(got).reshape(H, -1) - want[:, None]) / (4.0 * 2.0 ** -24 * want[:, None] + term)
+        assert err.max() <= 1.0, (what, float(err.max()))
+
+    zero, one = torch.zeros(1, H, 1, device=DEV), torch.ones(1, H, 1, device=DEV)
+    # a token more: nothing is written, the state fades
+    step = mb.merit_plan_delta_rule(mb.MERIT_F32, 1, 1, H, H, 1, 1, scale=1.0, normalize=False)
+    y, h = mb.merit_delta_rule_step(step, one[..., None], one, one, zero, g[None], zero[..., 0])
+    near(h, "a token's state")
+    near(y, "a token's result")
+    # two tokens of a prompt: the second reads what the first wrote, and what was there before; both fade on the way
+    plan = mb.merit_plan_delta_rule(mb.MERIT_F32, 1, 2, H, H, 2, 1, scale=1.0, normalize=False)
+    k = torch.zeros(1, 2, H, 2, device=DEV)
+    k[:, 0, :, 0] = 1.0
+    v, beta = torch.ones(1, 2, H, 1, device=DEV), torch.zeros(1, 2, H, device=DEV)
+    beta[:, 0] = 1.0
+    gates = torch.stack([torch.zeros_like(g), g])[None]
+    h0 = torch.zeros(1, H, 2, 1, device=DEV)
+    h0[:, :, 1] = 1.0
+    for axis, what, term in ((0, "written", 2.0 ** -134), (1, "from before", 0.0)):
+        q = torch.zeros(1, 2, H, 2, device=DEV)
+        q[..., axis] = 1.0
+        y, h = mb.merit_delta_rule(plan, q, k, v, gates, beta, h0=h0, final=True)
+        near(y[0, 1], what, term)
+        near(h[0, :, axis], what + ", state", 2.0 * term)
