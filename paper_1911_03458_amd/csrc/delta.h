@@ -10,9 +10,11 @@
 // merit_delta_prepare finds it and P = scale f o Q K^T for all chunks side by side.
 //
 // Products run on v_mfma_f32_16x16x32_bf16.  An fp32 operand goes in as three bfloat16 terms of 8 bits each (x = x0 + x1 + x2, each
-// what the ones before it leave), a binary16 one as two, a bfloat16 one as it is, and terms whose product is below
-// 2^-24 of the leading one are left out: 3 products for an exact operand with an fp32 one, 6 for two fp32 ones, at a sixteenth of
-// the time each that v_mfma_f32_16x16x4_f32 takes.  States, sums and what is kept of them are fp32.
+// what the ones before it leave), a binary16 one as two, a bfloat16 one as it is: 3 products for a bfloat16 operand with an fp32
+// one, 5 for a binary16 one, 6 for two fp32 ones, at a sixteenth of the time each that v_mfma_f32_16x16x4_f32 takes.  Of the others
+// each is at most 2^-23 of the whole and of either sign (`split8`), so that sums are off by as much as those of fp32 products
+// rounded one by one.  (Below 2^-110 a value's third term has fewer than 8 bits: bfloat16 ends at 2^-133.)  States, sums and what is
+// kept of them are fp32.
 #pragma once
 
 #include <type_traits>
@@ -45,8 +47,9 @@ template <int N> __device__ __forceinline__ void split(float x, __bf16 (&o)[N])
         o[i] = (__bf16)x;
     }
 }
-// Eight values side by side.  Three terms of 8 bits each, cut off instead of rounded, are the value itself (24 bits), and take no
-// conversions; of fewer the last is rounded.
+// Eight values side by side.  Three terms of 8 bits each are the value itself (24 bits).  The first is cut off, so that it is never
+// beyond the largest value, the second is rounded to the nearest: the third then has either sign, and so have the products that
+// `multiply` leaves out, each at most 2^-23 of the whole (with the second cut off too, 2^-22, all of the product's own sign).
 template <int N> __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&o)[N])
 {
     if constexpr (N == 3) {
@@ -56,8 +59,15 @@ template <int N> __device__ __forceinline__ void split8(const float (&x)[8], bf1
             float a = x[e], b = x[e + 1];
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
-                const unsigned ua = __builtin_bit_cast(unsigned, a), ub = __builtin_bit_cast(unsigned, b);
-                w[i][e / 2] = __builtin_amdgcn_perm(ub, ua, 0x07060302);       // the upper halves of both
+                unsigned ua = __builtin_bit_cast(unsigned, a), ub = __builtin_bit_cast(unsigned, b);
+                if (i == 1) {
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                    w[1][e / 2] = __builtin_bit_cast(unsigned, (bf16x2){(__bf16)a, (__bf16)b});
+                    ua = w[1][e / 2] << 16;
+                    ub = w[1][e / 2];
+                } else {
+                    w[i][e / 2] = __builtin_amdgcn_perm(ub, ua, 0x07060302);       // the upper halves of both
+                }
                 if (i < 2) {
                     a -= __builtin_bit_cast(float, ua & 0xFFFF0000u);
                     b -= __builtin_bit_cast(float, ub & 0xFFFF0000u);

@@ -1,4 +1,5 @@
-"""How many digits the delta rule's fp32 arithmetic keeps, where a result shows them: sums that cancel, decays by themselves."""
+"""How many digits the delta rule's fp32 arithmetic keeps, where a result shows them: sums that cancel, decays by themselves,
+products of values with all of their bits set."""
 import numpy as np
 import pytest
 
@@ -74,3 +75,28 @@ def test_decays_by_themselves(mb):
         y, h = mb.merit_delta_rule(plan, q, k, v, gates, beta, h0=h0, final=True)
         near(y[0, 1], what, term)
         near(h[0, :, axis], what + ", state", 2.0 * term)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_products_of_values_with_all_bits_set(mb, dtype):
+    """1 + a / 128 - 2^-23: cut after eight bits, and after eight more, such a value leaves as much as it can.  A product of two is
+    a handful of fp32 sums of one sign, so nothing but the last one's rounding, or its cut, is of any size: two of 2^-24; a binary16
+    factor (1 + a / 128 - 2^-10) is in two terms and leaves nothing."""
+    H = 64
+    T, last = (torch.float32, 2.0 ** -23) if dtype == "f32" else (torch.float16, 2.0 ** -10)
+    a = torch.arange(1, 9, dtype=torch.float64) / 128
+    s, q = (1 + a - 2.0 ** -23).repeat_interleave(8), (1 + a - last).repeat(8)
+    h0, qd = s.float().view(1, H, 1, 1).to(DEV), q.to(T).view(1, 1, H, 1).to(DEV)
+    plan = mb.merit_plan_delta_rule(TYPES[dtype][1], 1, 1, H, H, 1, 1, scale=1.0, normalize=False)
+    none, v = torch.zeros(1, 1, H, device=DEV), torch.zeros(1, 1, H, 1, dtype=T, device=DEV)
+    # read by q: y of fp32 shows it, and what a key of the same value takes away from v, which the state keeps
+    if dtype == "f32":
+        y = mb.merit_delta_rule(plan, qd, torch.zeros_like(qd), v, None, none, h0=h0)
+        err = np.abs(host(y).ravel() / (s * q).numpy() - 1.0).max() * 2 ** 24
+        assert err <= 4.0, float(err)
+    one = torch.ones_like(none)
+    h = mb.merit_delta_rule(plan, torch.zeros_like(qd), qd, v, None, one, h0=h0, final=True)[1]
+    # S - q (q S): the products' cuts and roundings, of q S and of q (q S), and the difference's
+    inner = (s * q).numpy()
+    err = np.abs(host(h).ravel() - (s.numpy() - q.numpy() * inner)) / (q.numpy() * inner) * 2 ** 24
+    assert err.max() <= 6.0, float(err.max())
