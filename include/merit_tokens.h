@@ -247,6 +247,9 @@ typedef struct {
 merit_status merit_delta_rule(const merit_token_plan *plan, const merit_delta_rule_args *args, void *workspace,
                               int64_t workspace_bytes, void *hip_stream);
 
+/* A value of dy that is not finite makes NaN of what depends on it: dq of its token, dk, dg and dbeta of the head and dv of the
+ * column up to its token; one of dh_last of dk, dg and dbeta of all its head's tokens and dv of its column.  Where q, k, v, g, beta
+ * or h0 were not finite, any gradient of the head may be a NaN. */
 typedef struct {
     merit_view dy;           /* T [B, L, heads, Dv]; not read behind lens     */
     merit_view q;            /* T [B, L, key_heads, Dk]                       */

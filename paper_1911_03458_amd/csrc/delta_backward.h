@@ -28,7 +28,7 @@ template <typename T, int KF> struct BackwardLds {
 };
 // (a half at a time is compiled: every place in LDS is then a lane's base and a constant)
 template <typename T, int KF, bool WIDE, int half>
-__device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem)
+__device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem, int *lost)
 {
     typedef BackwardLds<T, KF> L;
     constexpr int NK = L::NK, KO = KF < 2 ? 1 : KF / 2;
@@ -75,6 +75,44 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
     };
     auto scalar = [&](int which, int at, int sub) __attribute__((always_inline)) {
         return *reinterpret_cast<const f32x4 *>(sc + which * C + 32 * at + 8 * quad + 4 * sub);
+    };
+    // As forward, the other way round: what is not finite goes into products as zeros, because later tokens have it too, times 0;
+    // lost[] has the last token of a chunk from which a column has some, and everything up to it becomes a NaN (the chunks before it
+    // start from a Z of NaNs).
+    auto finite = [&](f32x4 (&x)[2]) __attribute__((always_inline)) {
+        float f = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f = fmaf(x[k >> 2][k & 3], 0.0f, f);
+        if (__ballot(f != 0.0f) == 0) return;                       // (a NaN is not 0)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (!isfinite(x[k >> 2][k & 3])) {
+                atomicMax(&lost[16 * tile + l16], 32 * half + 8 * quad + k);
+                x[k >> 2][k & 3] = 0.0f;
+            }
+    };
+    auto finite_dy = [&]() __attribute__((always_inline)) {          // (of the tokens that the own ones are summed over)
+        float f = 0.0f;
+#pragma unroll
+        for (int k = 2 * half; k < 4; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) f = fmaf(dy.value(k, r), 0.0f, f);
+        if (__ballot(f != 0.0f) == 0) return;
+#pragma unroll
+        for (int k = 2 * half; k < 4; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!isfinite(dy.value(k, r))) {
+                    atomicMax(&lost[16 * tile + l16], 32 * (k >> 1) + 8 * quad + 4 * (k & 1) + r);
+                    dy.v[k][r] = 0;
+                }
+    };
+    auto lose = [&](f32x4 (&x)[2]) __attribute__((always_inline)) {
+        const int upto = lost[16 * tile + l16];
+        if (__ballot(upto >= 0) == 0) return;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (32 * half + 8 * quad + k <= upto) x[k >> 2][k & 3] = __builtin_nanf("");
     };
     // Z += (rows of keys)^T w over the tokens of half `f`
     auto into_state = [&](const Keys<NK, KF * 32> &t, int f, const bf16x8 (&w)[3]) __attribute__((always_inline)) {
@@ -143,7 +181,8 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
             if constexpr (full.value) load_dy(then, full);
         };
         bf16x8 y[2][NK];
-        if (busy)
+        if (busy) {
+            finite_dy();
 #pragma unroll
             for (int f = 1 - half; f >= 0; --f) {       // (the second half's tokens, and for the first half its own)
                 f32x4 d[2];
@@ -153,6 +192,7 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
                     for (int r = 0; r < 4; ++r) d[k][r] = dy.value(2 * (1 - f) + k, r);
                 operand<NK>(d[0], d[1], y[1 - f]);
             }
+        }
         if constexpr (L::shared) {
             if (busy) fade();
             __syncthreads();
@@ -194,9 +234,11 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
             wt.cols(half, 1, half, a[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) U[k] = beta[k] * X[k];
+            finite(U);
             operand<3>(U[0], U[1], u);
             multiply_rows<3>(X, a, u);
             if constexpr (half == 1) {
+                lose(X);
                 outer();
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {
@@ -222,6 +264,7 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
             wt.cols(0, 0, 1, a[0]);
             wt.cols(0, 1, 1, a[1]);
             multiply_rows<3>(X, a, u1);
+            lose(X);
             outer();
 #pragma unroll
             for (int k = 0; k < 3; ++k) one[64 * k] = w[k];
@@ -240,9 +283,15 @@ __device__ __forceinline__ void backward_half(const DeltaParams &p, __bf16 *smem
                 into_state(kt, 1, w1);
                 results();
             }
+            if (lost[16 * tile + l16] >= 0)
+#pragma unroll
+                for (int o = 0; o < KO; ++o)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) Z[o][k >> 2][k & 3] = __builtin_nanf("");
         }
         __syncthreads();
     };
+    if (tid < 64) lost[tid] = -1;                           // (the first chunk's barrier is before the first use)
     const int whole_chunks = len / C;
     if (whole_chunks < n) {
         if constexpr (half == 1) load(n - 1, std::false_type());
@@ -270,8 +319,9 @@ template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(CHUNK_THREADS, 2) void merit_delta_back_chunks(DeltaParams p)
 {
     extern __shared__ __attribute__((aligned(16))) __bf16 smem[];
-    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) backward_half<T, KF, WIDE, 0>(p, smem);
-    else backward_half<T, KF, WIDE, 1>(p, smem);
+    __shared__ int lost[64];
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) backward_half<T, KF, WIDE, 0>(p, smem, lost);
+    else backward_half<T, KF, WIDE, 1>(p, smem, lost);
 }
 
 // ---------------------------------------------------------------------------
@@ -694,7 +744,7 @@ template <typename T> __global__ __launch_bounds__(NT) void merit_delta_sum_head
 template <typename T, int KF> hipError_t backward_chunks(DeltaParams p, hipStream_t s)
 {
     constexpr int lds = BackwardLds<T, KF>::bytes;
-    static_assert(lds <= 160 * 1024, "");
+    static_assert(lds + 256 <= 160 * 1024, "");
     p.width = delta_width(p.B * p.H, p.Dv, 0);
     p.slices = delta_slices(p.width, p.Dv, 0);
     const unsigned grid = (unsigned)(p.B * p.H * p.slices);

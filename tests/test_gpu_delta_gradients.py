@@ -1,0 +1,51 @@
+"""Gradients of the delta rule that are not finite: what depends on them and what does not."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from token_helpers import TYPES, Gen        # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def mb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1911_03458_amd import binding
+    binding.lib()
+    return binding
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("Dk", [24, 40, 128])
+@pytest.mark.parametrize("at", [0, 20, 31, 63, 70, 95, 100, 139])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_gradient_that_is_not_finite_stays_in_front(mb, value, at, Dk, dtype):
+    """dy of a token reaches the gradients of that token and of those before it in its head, of v in its column, and no others."""
+    B, L, H, K, Dv = 2, 140, 4, 4, 40
+    T, g = TYPES[dtype][0], Gen(at + Dk)
+    q, k, v = g.normal(B, L, K, Dk, dtype=T), g.normal(B, L, K, Dk, dtype=T), g.normal(B, L, H, Dv, dtype=T)
+    a, beta = -g.uniform(B, L, H, lo=0.01, hi=0.3), g.uniform(B, L, H, lo=0.1, hi=0.9)
+    h0, dh, dy = g.normal(B, H, Dk, Dv), g.normal(B, H, Dk, Dv), g.normal(B, L, H, Dv, dtype=T)
+    plan = mb.merit_plan_delta_rule(TYPES[dtype][1], B, L, H, K, Dk, Dv)
+    states = mb.merit_delta_rule(plan, q, k, v, a, beta, h0=h0, states=True)[1]
+    want = mb.merit_delta_rule_backward(plan, dy, q, k, a, beta, states, dh_last=dh, dh0=True)
+    dy = dy.clone()
+    dy[0, at, 1, 3] = value
+    got = mb.merit_delta_rule_backward(plan, dy, q, k, a, beta, states, dh_last=dh, dh0=True)
+    others = [i for i in range(H) if i != 1]
+    for name in ("dq", "dk", "dv", "dg", "dbeta"):
+        s, t = got[name], want[name]
+        assert torch.equal(s[1], t[1]) and torch.equal(s[0][:, others], t[0][:, others]), name
+        assert torch.equal(s[0, at + 1:], t[0, at + 1:]), name
+    keep = [c for c in range(Dv) if c != 3]
+    assert torch.equal(got["dv"][0][:, :, keep], want["dv"][0][:, :, keep])
+    assert not torch.isfinite(got["dv"][0, :at + 1, 1, 3]).any()
+    rest = [t for t in range(L) if t != at]
+    assert not torch.isfinite(got["dq"][0, at, 1]).any() and torch.equal(got["dq"][0, rest], want["dq"][0, rest])
+    for name in ("dk", "dg", "dbeta"):
+        assert not torch.isfinite(got[name][0, :at + 1, 1]).any(), name
+    s, t = got["dh0"], want["dh0"]
+    assert torch.equal(s[1], t[1]) and torch.equal(s[0, others], t[0, others]) and torch.equal(s[0, 1][:, keep], t[0, 1][:, keep])
+    assert not torch.isfinite(s[0, 1, :, 3]).any()
