@@ -2,6 +2,8 @@
 // accepted, how a pass is split into workgroups, how much scratch memory it takes.  Host code only.
 #include "token_plan.h"
 
+#include <algorithm>
+
 using namespace merit;
 
 namespace {
@@ -20,7 +22,8 @@ Rows rows_of(Views &v, const merit_view &view, int type, bool required)
 // found first (a launch for all but the last, and a product a segment), then each goes from its own first state.  An estimate, in us:
 // a chunk takes a workgroup of 16, 32 or 64 columns 4.2, 4.9 or 5.9, and without results 3.0, 3.6 or 3.7 (states of 128 x 128,
 // bfloat16, up to 256 workgroups); launches 10, products 3.  16 heads of 8191 tokens in 1, 2, 4, 5, 6 and 8 segments: 533, 450, 283,
-// 243, 283, 242.  Not for less than a fifth.
+// 243, 283, 242.  Not for less than a fifth, which leaves more than about 300 workgroups of 64 columns in one piece: the launch that joins
+// segments, 512 threads for 16 columns of a head, is a small one.
 void delta_segments(DeltaParams &p)
 {
     const int64_t heads = p.B * p.H;
@@ -167,8 +170,10 @@ merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64
         L > MAX_ROWS || too_large(B, L, heads * (Dk + Dv)))
         return MERIT_ERR_UNSUPPORTED;
     const int64_t n = cdiv(L, MERIT_DELTA_CHUNK);
-    // workgroups of every pass, at the narrowest tiles and up to 512 threads a chunk; the sum over heads, a thread a value; states of all chunks
-    if (B > MAX_BLOCKS / heads || B * heads * (2 * n > cdiv(Dv, 16) ? 2 * n : cdiv(Dv, 16)) >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + MERIT_DELTA_CHUNK) * Dv + MERIT_DELTA_KEPT) ||
+    // workgroups of every pass, in units of 256 threads: of 512 a chunk, of 512 for at most 64 columns (fewer columns only in launches of up
+    // to 256 workgroups), of 256 for 16 columns of a token; the sum over heads, a thread a value; states of all chunks
+    const int64_t most = std::max(2 * std::max(n, cdiv(Dv, 64)), cdiv(Dv, 16));
+    if (B > MAX_BLOCKS / heads || B * heads * most >= MAX_BLOCKS || too_large(B * heads, n + 1, (Dk + MERIT_DELTA_CHUNK) * Dv + MERIT_DELTA_KEPT) ||
         (L > 0 && B > MAX_BLOCKS / L * 256 / (key_heads * Dk)))
         return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(DELTA, type);

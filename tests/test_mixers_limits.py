@@ -1,0 +1,20 @@
+"""Where the plans of the gated delta rule and of the block's norms end: the last size taken, the first one refused.  No GPU."""
+import pytest
+
+from paper_1911_03458_amd import binding as mb
+
+
+def _refused(f, *args, **kw):
+    with pytest.raises(mb.MeritError) as e:
+        f(*args, **kw)
+    assert e.value.status == mb.MERIT_ERR_UNSUPPORTED, e.value
+
+
+@pytest.mark.parametrize("L, Dv, most", [(0, 1, (1 << 23) - 1), (0, 16, (1 << 23) - 1), (0, 17, (1 << 23) - 1), (1, 16, (1 << 23) - 1),
+                                         (0, 64, (1 << 22) - 1), (65, 16, (1 << 22) - 1)])
+def test_workgroups_of_512_threads_fit_a_launch(L, Dv, most):
+    """Passes from chunk to chunk take 512 threads for at most 64 columns, also where there are no tokens (a state goes through):
+    a launch holds less than 2^32."""
+    mb.merit_plan_delta_rule(mb.MERIT_F32, most, L, 1, 1, 1, Dv)
+    _refused(mb.merit_plan_delta_rule, mb.MERIT_F32, most + 1, L, 1, 1, 1, Dv)
+    assert (most + 1) * -(-Dv // 64) * 512 <= 1 << 32
