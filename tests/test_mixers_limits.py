@@ -18,3 +18,16 @@ def test_workgroups_of_512_threads_fit_a_launch(L, Dv, most):
     mb.merit_plan_delta_rule(mb.MERIT_F32, most, L, 1, 1, 1, Dv)
     _refused(mb.merit_plan_delta_rule, mb.MERIT_F32, most + 1, L, 1, 1, 1, Dv)
     assert (most + 1) * -(-Dv // 64) * 512 <= 1 << 32
+
+
+@pytest.mark.parametrize("dtype", [mb.MERIT_F16, mb.MERIT_F32, mb.MERIT_BF16])
+def test_the_longest_rows(dtype):
+    assert mb.MERIT_BLOCK_NORM_MAX_CHANNELS == 8192
+    mb.merit_plan_block_norm(dtype, 1, 8, 8192)
+    _refused(mb.merit_plan_block_norm, dtype, 1, 8, 8193)
+
+
+def test_the_longest_keys():
+    assert mb.MERIT_DELTA_MAX_KEYS == 128
+    mb.merit_plan_delta_rule(mb.MERIT_F32, 1, 8, 1, 1, 128, 16)
+    _refused(mb.merit_plan_delta_rule, mb.MERIT_F32, 1, 8, 1, 1, 129, 16)
