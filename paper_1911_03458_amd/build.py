@@ -44,15 +44,20 @@ def is_stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def compile_command() -> list:
+    """hipcc as every source of the library is compiled."""
+    return [hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+            # keep hipcc from forming packed-fp32 VALU ops
+            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+            "-Wall", "-Wno-unused-command-line-argument",
+            "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+
+
 def build_library(force: bool = True, extra_flags=()) -> str:
     """Compile every HIP source for gfx950 into one shared library."""
     if not force and not is_stale():
         return LIB_PATH
-    common = [hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
-              # keep hipcc from forming packed-fp32 VALU ops
-              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-              "-Wall", "-Wno-unused-command-line-argument",
-              "-I", os.path.join(ROOT, "include"), "-I", CSRC, *extra_flags]
+    common = compile_command() + list(extra_flags)
     # one object per source, compiled side by side (the convolution file dominates), then one link
     objdir = os.path.join(_HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
