@@ -163,7 +163,7 @@ merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64
 {
     if (!out) return MERIT_ERR_NULL;
     *out = nullptr;
-    if (!type_ok(type) || B < 0 || L < 0 || heads < 1 || key_heads < 1 || Dk < 1 || Dv < 1 || !std::isfinite(scale))
+    if (!type_ok(type) || B < 0 || L < 0 || heads < 1 || key_heads < 1 || Dk < 1 || Dv < 1 || !std::isfinite((float)scale))
         return MERIT_ERR_INVALID_ARG;
     if (heads % key_heads != 0) return MERIT_ERR_SHAPE;
     if (Dk > MERIT_DELTA_MAX_KEYS || Dv > MAX_CHANNELS || heads > MAX_CHANNELS / Dv || heads > MAX_CHANNELS / Dk || B > MAX_ROWS ||
@@ -197,7 +197,7 @@ merit_status merit_plan_block_norm(merit_dtype type, merit_dtype stream, int64_t
     if (!out) return MERIT_ERR_NULL;
     *out = nullptr;
     if (!type_ok(type) || (stream != type && stream != MERIT_F32) || (int)act < 0 || (int)act > 3 || B < 0 || L < 0 || C < 1 ||
-        !(eps >= 0.0) || !std::isfinite(eps) || !(after || before))
+        !(eps >= 0.0) || !std::isfinite((float)eps) || !(after || before))
         return MERIT_ERR_INVALID_ARG;
     if (C > MERIT_BLOCK_NORM_MAX_CHANNELS || B > MAX_ROWS || L > MAX_ROWS || (L > 0 && B > MAX_ROWS / L)) return MERIT_ERR_UNSUPPORTED;
     merit_token_plan *pl = new_plan(BLOCK, type);

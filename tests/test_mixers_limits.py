@@ -4,10 +4,10 @@ import pytest
 from paper_1911_03458_amd import binding as mb
 
 
-def _refused(f, *args, **kw):
+def _refused(f, *args, status=mb.MERIT_ERR_UNSUPPORTED, **kw):
     with pytest.raises(mb.MeritError) as e:
         f(*args, **kw)
-    assert e.value.status == mb.MERIT_ERR_UNSUPPORTED, e.value
+    assert e.value.status == status, e.value
 
 
 @pytest.mark.parametrize("L, Dv, most", [(0, 1, (1 << 23) - 1), (0, 16, (1 << 23) - 1), (0, 17, (1 << 23) - 1), (1, 16, (1 << 23) - 1),
@@ -31,3 +31,11 @@ def test_the_longest_keys():
     assert mb.MERIT_DELTA_MAX_KEYS == 128
     mb.merit_plan_delta_rule(mb.MERIT_F32, 1, 8, 1, 1, 128, 16)
     _refused(mb.merit_plan_delta_rule, mb.MERIT_F32, 1, 8, 1, 1, 129, 16)
+
+
+@pytest.mark.parametrize("value", [3.5e38, -3.5e38, 1e300])
+def test_numbers_beyond_fp32(value):
+    """The kernels take a scale and an eps as fp32, which these are not."""
+    _refused(mb.merit_plan_delta_rule, mb.MERIT_F32, 1, 8, 1, 1, 16, 16, scale=value, status=mb.MERIT_ERR_INVALID_ARG)
+    _refused(mb.merit_plan_block_norm, mb.MERIT_F32, 1, 8, 16, eps=value, status=mb.MERIT_ERR_INVALID_ARG)
+    mb.merit_plan_delta_rule(mb.MERIT_F32, 1, 8, 1, 1, 16, 16, scale=3.4e38)
