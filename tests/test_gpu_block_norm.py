@@ -21,7 +21,7 @@ def mb():
     return binding
 
 
-# B, L, C: rows by runs of lanes, by workgroups of 256 to 1024 threads, of 2 to 16 vectors a thread; vectors of 16 bytes, two values, one
+# B, L, C: rows by runs of lanes, by workgroups of 256 and 512 threads, of 1 to 16 vectors a thread; vectors of 16 bytes, two values, one
 SHAPES = [(1, 1, 1), (2, 3, 8), (3, 70, 64), (2, 33, 130), (1, 5, 96), (5, 7, 37), (2, 9, 512), (3, 11, 770), (2, 5, 1025), (1, 3, 2048),
           (2, 3, 2051), (1, 4, 4096), (1, 3, 5000), (2, 2, 8192), (1, 3, 8191), (2, 3, 8190), (3, 5, 7000), (1, 2, 4094), (700, 3, 24), (1, 1500, 256)]
 # which parts there are: norm after, gate, its function, scale, stream, norm before, layer norm, fp32 stream
