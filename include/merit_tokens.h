@@ -75,7 +75,8 @@ merit_status merit_plan_causal_conv(merit_dtype type, int64_t B, int64_t L, int6
 merit_status merit_plan_scan(merit_dtype type, int64_t B, int64_t L, int64_t D, int64_t N, int64_t groups, int softplus,
                              merit_token_plan **out);
 /* Gated delta rule of q, k[B, L, key_heads, Dk] and v[B, L, heads, Dv], Dk <= MERIT_DELTA_MAX_KEYS; heads / key_heads value
- * heads share a key head.  normalize != 0: q and k count by their direction, x / sqrt(|x|^2 + MERIT_DELTA_EPS). */
+ * heads share a key head.  normalize != 0: q and k count by their direction, x / sqrt(|x|^2 + MERIT_DELTA_EPS), the squares
+ * summed in fp32 (values up to 1e18). */
 merit_status merit_plan_delta_rule(merit_dtype type, int64_t B, int64_t L, int64_t heads, int64_t key_heads, int64_t Dk, int64_t Dv,
                                    double scale, int normalize, merit_token_plan **out);
 /* The end of a block over rows x[B, L, C], C <= MERIT_BLOCK_NORM_MAX_CHANNELS: norm, gate, scale, residual sum, norm (below).
@@ -229,7 +230,8 @@ merit_status merit_scan_step(const merit_token_plan *plan, const merit_scan_step
  * state stays.  states: what the backward pass takes of every MERIT_DELTA_CHUNK tokens of a head (a chunk), from a 16-byte boundary on:
  * MERIT_DELTA_KEPT values of how they act on each other, the state before them, and for each of them the row of Dv values that it
  * would add to the state along its key for beta = 1; in all M = MERIT_DELTA_KEPT + (Dk + MERIT_DELTA_CHUNK) Dv values, rounded up to
- * a multiple of 4.  Of chunks behind a sequence's end nothing is written.
+ * a multiple of 4.  Of chunks behind a sequence's end nothing is written.  The plan's scratch memory is that of a call without `states`
+ * (MERIT_DELTA_KEPT values a chunk of a head, which a call with them has there).
  * A value that is not finite (an infinity, a NaN) makes NaN of what depends on it: q of its token's y, v of its column from its
  * token on, k, g (but -inf, which is a decay of 0) and beta of the head from there on. */
 typedef struct {
@@ -255,7 +257,7 @@ typedef struct {
     merit_view q;            /* T [B, L, key_heads, Dk]                       */
     merit_view k;            /* T [B, L, key_heads, Dk]                       */
     merit_view g;            /* F32 [B, L, heads], optional                   */
-    merit_view beta;         /* P [B, L, heads]                               */
+    merit_view beta;         /* P [B, L, heads]; neither is read: `states` has what the forward pass made of them */
     merit_view states;       /* F32, as the forward pass left them            */
     merit_view lens;         /* int32 [B], optional                           */
     merit_view dh_last;      /* F32 [B, heads, Dk, Dv] dense, optional        */
@@ -285,7 +287,7 @@ merit_status merit_delta_rule_step(const merit_token_plan *plan, const merit_del
 
 /* u = norm(x) after_weight + after_bias (x where the plan has no norm after the block);  t = u act(z), or u;
  * out = r + scale t;  n = norm(out) before_weight + before_bias, from `out` before it is rounded.
- * norm(x) = x / sqrt(mean(x^2) + eps), or (x - mean) / sqrt(var + eps); weights, scale: 1, biases, r: 0 where absent, and absent
+ * norm(x) = x / sqrt(mean(x^2) + eps), or (x - mean) / sqrt(var + eps), the squares summed in fp32 (values up to 1e17); weights, scale: 1, biases, r: 0 where absent, and absent
  * where the plan has no such norm.  The strides of z may be 0: a gate for each sequence. */
 typedef struct {
     merit_view x;            /* T [B, L, C]                                   */
@@ -311,7 +313,8 @@ typedef struct {
     merit_view dn;           /* T [B, L, C], where the plan has that norm     */
     merit_view x;            /* T [B, L, C]                                   */
     merit_view z;            /* T [B, L, C], optional                         */
-    merit_view r;            /* stream [B, L, C], optional; not read where the plan has no norm before the next block */
+    merit_view r;            /* stream [B, L, C], optional, as the forward pass read it (where `out` took its place: a copy of it);
+                              * not read where the plan has no norm before the next block */
     merit_view after_weight; /* P [C], optional                               */
     merit_view after_bias;   /* P [C], optional                               */
     merit_view scale;        /* P [C], optional                               */

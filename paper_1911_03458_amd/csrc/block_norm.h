@@ -9,7 +9,7 @@
 // while it walks down the rows, which keeps parameters and the sums of their gradients in registers, and asks for the next row
 // before it works on this one (backward, 16384 rows of 2048: 85 us against 139 without).  bf16, the bytes at their rate: 16384
 // rows of 2048, both norms, forward 49 us (5.5 TB/s), with an fp32 stream 77 us (5.2), backward 85 us (4.7); 262144 rows of 128,
-// after-norm and gate, forward 45 us (4.5), backward 69 us (4.9).
+// after-norm and gate, forward 44 us (4.6), backward 68 us (5.0).
 // Rows of more than 8 values a thread that are not in pieces of 16 bytes spill: 2048 of 8191, fp32, backward, 0.34 ms.
 #pragma once
 

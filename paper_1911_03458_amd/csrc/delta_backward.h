@@ -16,7 +16,8 @@ namespace delta {
 // one chunk after the other, from the last: two wavefronts 16 columns of a head's Z
 // ---------------------------------------------------------------------------
 // Split and bound as merit_delta_chunks is; here the second half's tokens come first.  The triangular matrices' transposes come out
-// of transposing reads.  128 heads of 2048 tokens, states of 128 x 128, bfloat16: 277 us (0.79 GB, 2.8 TB/s).
+// of transposing reads.  128 heads of 2048 tokens, states of 128 x 128, bfloat16: 277 us (0.79 GB, 2.9 TB/s), of which about 15 are
+// for keeping values that are not finite away from later tokens.
 template <typename T, int KF> struct BackwardLds {
     static constexpr int NK = Terms<T>::n;
     static constexpr int k = 0, w = k + Keys<NK, KF * 32>::bytes, mix = w + Triangle<3>::bytes, scal = mix + Triangle<3>::bytes,
@@ -332,9 +333,9 @@ __global__ __launch_bounds__(CHUNK_THREADS, 2) void merit_delta_back_chunks(Delt
 // after the other.  Results are kept times what a row goes through at the end: dQ scale / |q|, rows / |k|, cols / |k|, for which the
 // matrices have the lengths of both of their tokens, and serve both ways round.  Through LDS they come into rows of eight values a
 // thread, for the sums along the keys and the stores.
-// 4096 chunks, 128 x 128, bfloat16: 448 us for 0.64 GB (1.4 TB/s).  A compute unit holds one workgroup of eight wavefronts, which pass
+// 4096 chunks, 128 x 128, bfloat16: 424 us for 0.64 GB (1.5 TB/s).  A compute unit holds one workgroup of eight wavefronts, which pass
 // its barriers together: LDS reads (each wavefront reads dy, x and u), vector instructions (about 120 us of them), products (76)
-// and loads follow each other more than they overlap.  Asking for columns two turns ahead did not help (453), and spilled for 64 keys.
+// and loads follow each other more than they overlap.  Asking for columns two turns ahead did not help, and spilled for 64 keys.
 template <int KF> constexpr int grad_waves() { return KF < 4 ? 4 : 8; }
 template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(64 * grad_waves<KF>(), 2) void merit_delta_grads(DeltaParams p)

@@ -11,8 +11,8 @@ namespace delta {
 // chunks side by side: a workgroup a chunk of a head
 // ---------------------------------------------------------------------------
 // It leaves -W and P in terms, and the tokens' factors.  W is found in blocks of 16 x 16 on v_mfma_f32_16x16x4_f32: those on the
-// diagonal by forward substitution, a thread a column, the rest from them.  Keys of 128, bfloat16, 4096 chunks: 76 us, 0.24 GB (3.1
-// TB/s); vector instructions are busy 56 % of that time, and what waits are the steps for each other.
+// diagonal by forward substitution, a thread a column, the rest from them.  Keys of 128, bfloat16, 4096 chunks: 73 us, 0.24 GB (3.3
+// TB/s); vector instructions are busy more than half of that time, and what waits are the steps for each other.
 template <typename T, int KF, bool WIDE>
 __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 {
@@ -223,12 +223,12 @@ __global__ __launch_bounds__(NT) void merit_delta_prepare(DeltaParams p)
 // an instruction in four cycles, 1.4 thousand a chunk; one for all tokens took 1.25 times as long).  They meet for the sums over
 // the state's rows, for what the first half's tokens leave for the second's, and for what both leave for the state.  LDS holds
 // the other operands, K, Q and the two triangular matrices, for the eight wavefronts of a workgroup; the next chunk's are on
-// their way in registers meanwhile. Bound by the chain of a chunk's products and barriers, bfloat16, states of 128 x 128: 4.2 us
-// a chunk with one pair at work (16 heads of 8191 tokens 533 us), 8 with four in every compute unit, LDS, vector and matrix
-// instructions a quarter of the time each (128 heads of 2048 with the states kept 262 us, 0.79 GB, 3.0 TB/s).  Few long sequences
-// go in segments side by side (16 heads of 8191: 121 us for what eight segments do to a state, 23 to join them, 98 from their
-// first states on).  P and u go into y with three terms as everything else does: two, enough for the rounding of a 16-bit y itself, lost
-// 2^-17 of each of a sum's terms, which shows where they cancel (128 heads of 2048, no states kept: 246 against 259 us a call).
+// their way in registers meanwhile. Bound by the chain of a chunk's products and barriers, bfloat16, states of 128 x 128: 4.3 us
+// a chunk with one pair at work (16 heads of 8191 tokens 551 us), 8.6 with four in every compute unit, LDS, vector and matrix
+// instructions a quarter of the time each (128 heads of 2048 with the states kept 274 us, 0.79 GB, 2.9 TB/s; without 188).  Few long
+// sequences go in segments side by side (16 heads of 8191: 108 us for what eight segments do to a state, 22 to join them, 92 from their
+// first states on).  P and u go into y with three terms as everything else does: two, enough for the rounding of a 16-bit y itself,
+// lost 2^-17 of each of a sum's terms, which shows where they cancel (128 heads of 2048, no states kept, 246 against 259 us a call).
 constexpr int CHUNK_THREADS = 512;
 template <typename T, int KF> struct ForwardLds {
     static constexpr int NK = Terms<T>::n;

@@ -20,10 +20,13 @@ Rows rows_of(Views &v, const merit_view &view, int type, bool required)
 // ---- gated delta rule ------------------------------------------------------------------------
 // Segments of a sequence's chunks side by side, where heads and sequences leave compute units idle: what a segment does to a state is
 // found first (a launch for all but the last, and a product a segment), then each goes from its own first state.  An estimate, in us:
-// a chunk takes a workgroup of 16, 32 or 64 columns 4.2, 4.9 or 5.9, and without results 3.0, 3.6 or 3.7 (states of 128 x 128,
-// bfloat16, up to 256 workgroups); launches 10, products 3.  16 heads of 8191 tokens in 1, 2, 4, 5, 6 and 8 segments: 533, 450, 283,
-// 243, 283, 242.  Not for less than a fifth, which leaves more than about 300 workgroups of 64 columns in one piece: the launch that joins
-// segments, 512 threads for 16 columns of a head, is a small one.
+// a chunk takes a workgroup of 16, 32 or 64 columns 4.2, 4.9 or 5.9, and without results 3.0, 3.6 or 3.7; launches 10, products 3.
+// Those are times of states of 128 x 128, bfloat16, up to 256 workgroups, and stand for the others too: it is their ratios that
+// decide.  16 heads of 8191 tokens in 1, 2, 3, 4, 5, 6, 8 and 12 segments take 551, 460, 331, 273, 228, 268, 222 and 261 us
+// (merit_delta_prepare, 41, not included).  Whole calls in one piece against what this chooses: 16 heads of 8191, 128 x 128, fp32 1043 against
+// 434, binary16 826 against 338; 8 heads of 8192, 64 x 64, fp32 632 against 144; 16 heads of 1024, 32 x 32, 73 against 51; 64
+// heads of 16384, 64 x 64, 1607 against 1113.  Not for less than a fifth, which leaves more than about 300 workgroups of 64 columns
+// in one piece: the launch that joins segments, 512 threads for 16 columns of a head, is a small one.
 void delta_segments(DeltaParams &p)
 {
     const int64_t heads = p.B * p.H;

@@ -127,8 +127,8 @@ __host__ __device__ inline int64_t delta_segment_floats(const DeltaParams &p, in
 }
 // Columns of v (and of a transition) that a workgroup of merit_delta_chunks or merit_delta_back_chunks takes from chunk to chunk, and
 // workgroups along them.  LDS has room for one workgroup a compute unit: as few columns as leave none a second one
-// (bfloat16, 128 x 128, 64 / 32 / 16 columns, us: 128 heads of 2048 tokens 241 / 390 / 699, 16 heads of 8191 620 / 570 / 533, those in
-// three segments - / 197 / 353).
+// (merit_delta_chunks, bfloat16, 128 x 128, 64 / 32 / 16 columns, us: 128 heads of 2048 tokens 188 / 332 / 635, 16 heads of 8191 617 /
+// 569 / 553, those in three segments 208 / 198 / 363).
 inline int delta_slices(int width, int Dv, int more) { return (Dv + width - 1) / width + (more + width - 1) / width; }
 inline int delta_width(int64_t groups, int Dv, int more)
 {
