@@ -49,3 +49,57 @@ def test_a_gradient_that_is_not_finite_stays_in_front(mb, value, at, Dk, dtype):
     s, t = got["dh0"], want["dh0"]
     assert torch.equal(s[1], t[1]) and torch.equal(s[0, others], t[0, others]) and torch.equal(s[0, 1][:, keep], t[0, 1][:, keep])
     assert not torch.isfinite(s[0, 1, :, 3]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_last_state_whose_gradient_is_not_finite(mb, value, dtype):
+    """dh_last reaches k, g, beta of its head and v of its column, and nothing of q."""
+    B, L, H, D = 2, 140, 3, 40
+    T, g = TYPES[dtype][0], Gen(7)
+    q, k, v, dy = (g.normal(B, L, H, D, dtype=T) for _ in range(4))
+    a, beta, dh = -g.uniform(B, L, H, lo=0.01, hi=0.3), g.uniform(B, L, H, lo=0.1, hi=0.9), g.normal(B, H, D, D)
+    plan = mb.merit_plan_delta_rule(TYPES[dtype][1], B, L, H, H, D, D)
+    states = mb.merit_delta_rule(plan, q, k, v, a, beta, states=True)[1]
+    want = mb.merit_delta_rule_backward(plan, dy, q, k, a, beta, states, dh_last=dh, dh0=True)
+    dh = dh.clone()
+    dh[0, 1, 5, 3] = value
+    got = mb.merit_delta_rule_backward(plan, dy, q, k, a, beta, states, dh_last=dh, dh0=True)
+    keep = [c for c in range(D) if c != 3]
+    for name, t in want.items():
+        s = got[name]
+        assert torch.equal(s[1], t[1]), name
+        if name == "dh0":
+            assert torch.equal(s[0, ::2], t[0, ::2]) and torch.equal(s[0, 1][:, keep], t[0, 1][:, keep]) and not torch.isfinite(s[0, 1, :, 3]).any()
+            continue
+        assert torch.equal(s[0][:, ::2], t[0][:, ::2]), name
+        if name == "dq":
+            assert torch.equal(s, t)
+        elif name == "dv":
+            assert torch.equal(s[0, :, 1][:, keep], t[0, :, 1][:, keep]) and not torch.isfinite(s[0, :, 1, 3]).any()
+        else:
+            assert not torch.isfinite(s[0, :, 1]).any(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_that_are_not_finite_in_several_places(mb, dtype):
+    """Two columns with a token each: each column's v up to its own token, the head's others up to the later one."""
+    B, L, H, D = 1, 200, 2, 64
+    T, g = TYPES[dtype][0], Gen(8)
+    q, k, v, dy = (g.normal(B, L, H, D, dtype=T) for _ in range(4))
+    a, beta = -g.uniform(B, L, H, lo=0.01, hi=0.3), g.uniform(B, L, H, lo=0.1, hi=0.9)
+    plan = mb.merit_plan_delta_rule(TYPES[dtype][1], B, L, H, H, D, D)
+    states = mb.merit_delta_rule(plan, q, k, v, a, beta, states=True)[1]
+    want = mb.merit_delta_rule_backward(plan, dy, q, k, a, beta, states)
+    dy = dy.clone()
+    dy[0, 130, 0, 2], dy[0, 150, 0, 37], dy[0, 70, 0, 37] = float("nan"), float("-inf"), float("nan")
+    got = mb.merit_delta_rule_backward(plan, dy, q, k, a, beta, states)
+    for c, upto in ((2, 130), (37, 150)):
+        assert not torch.isfinite(got["dv"][0, :upto + 1, 0, c]).any() and torch.equal(got["dv"][0, upto + 1:, 0, c], want["dv"][0, upto + 1:, 0, c])
+    keep = [c for c in range(D) if c not in (2, 37)]
+    assert torch.equal(got["dv"][0, :, 0][:, keep], want["dv"][0, :, 0][:, keep])
+    for name in ("dk", "dg", "dbeta"):
+        assert not torch.isfinite(got[name][0, :151, 0]).any() and torch.equal(got[name][0, 151:], want[name][0, 151:]), name
+        assert torch.equal(got[name][:, :, 1], want[name][:, :, 1]), name
+    rest = [t for t in range(L) if t not in (70, 130, 150)]
+    assert torch.equal(got["dq"][0, rest], want["dq"][0, rest])
